@@ -40,7 +40,7 @@ extern "C" {
 
 typedef enum {
     MLIP_OK = 0,
-    MLIP_EINVAL = -1,      /* null pointer, N <= 0, r_cut <= 0, n_slabs outside [1,64], bad model dims */
+    MLIP_EINVAL = -1,      /* null pointer, N <= 0, r_cut <= 0, n_slabs outside [1,64], bad model dims, types or strides */
     MLIP_ECELL = -2,       /* singular cell, or cell/positions outside the supported image range */
     MLIP_ECOINCIDENT = -3, /* two atoms (or an atom and an image) at distance 0 */
     MLIP_ENOMEM = -4,      /* device allocation failed */
@@ -386,6 +386,74 @@ int mlip_profile_read(mlip_graph_t *graph, float *ms /*HOST [MLIP_PROF_COUNT]*/,
 
 /* Plain device -> host copy of `bytes` bytes after synchronising the graph's stream. */
 int mlip_copy_to_host(const mlip_graph_t *graph, void *dst_host, const void *src_device, size_t bytes);
+
+/*
+ * Per-species parameter tables, for programs that fit a potential's parameters (appendix "Training": gradient steps on batches of
+ * structures).  A potential keeps one row of parameters for each species (its embedding, reference energies and scales of the
+ * atoms' energies) or for each pair of species; a step of a fit looks rows up, sums the atoms' gradients by species and bounds
+ * the norm of all gradients before the update.
+ *
+ * These calls use no handle: they work on the caller's arrays, on the HIP stream given (hipStream_t as void*, NULL = default
+ * stream), and take scratch memory from the caller, so they can be captured in a HIP graph and run on any stream or thread.  Results
+ * are the same bits on every call with the same arguments.  Element pointers must be aligned to their elements; outputs must not
+ * overlap inputs (a clipped tensor may be its own output).
+ */
+enum { MLIP_DTYPE_F32 = 0, MLIP_DTYPE_BF16 = 1, MLIP_DTYPE_F16 = 2 };
+
+/*
+ * Lookup: out[i][f] = scale * table[ids[i]][f], the product in fp32, rounded once to the output's type.
+ *   table   DEVICE [n_rows][width] of table_dtype, element (r, f) at r * table_row_stride + f * table_col_stride (in elements, >= 0)
+ *   ids     DEVICE [n] int32 (id_bits = 32) or int64 (id_bits = 64).  A negative id stands for a place that pads a batch: its row
+ *           is zeros.  An id >= n_rows has no row: nothing is read for it and its row is NaN, so that it does not pass unnoticed.
+ *   out     DEVICE [n][width] of out_dtype, element (i, f) at i * out_row_stride + f, out_row_stride >= width
+ * n may be 0; 1 <= n_rows < 2^31, 1 <= width < 2^31, n < 2^31.
+ */
+int mlip_embed(const void *table, int32_t table_dtype, int64_t n_rows, int64_t width, int64_t table_row_stride,
+               int64_t table_col_stride, const void *ids, int32_t id_bits, int64_t n, float scale, void *out,
+               int32_t out_dtype, int64_t out_row_stride, void *stream);
+
+/*
+ * Its gradient: out[r][f] = scale * sum over i with ids[i] == r of grad[i][f], rows that no id names are zero; with
+ * accumulate != 0 the old out[r][f] is added.  Ids outside [0, n_rows) contribute nothing, whatever grad holds there.
+ *   grad    DEVICE [n][width] of grad_dtype, element (i, f) at i * grad_row_stride + f * grad_col_stride (>= 0; 0 for a
+ *           gradient that is the same for all atoms)
+ *   out     DEVICE [n_rows][width] of out_dtype, element (r, f) at r * out_row_stride + f
+ *   workspace   DEVICE scratch of at least mlip_embed_grad_workspace(n, n_rows, width) bytes, aligned to 16 bytes; its
+ *           contents do not matter before and mean nothing after the call
+ * Sums run in the order of the atoms, over at most MLIP_EMBED_GRAD_RUN atoms at a time in fp32 and over those parts in fp64, and
+ * are rounded to the output's type once.
+ */
+enum { MLIP_EMBED_GRAD_RUN = 1024 };
+size_t mlip_embed_grad_workspace(int64_t n, int64_t n_rows, int64_t width);
+int mlip_embed_grad(const void *grad, int32_t grad_dtype, int64_t grad_row_stride, int64_t grad_col_stride, const void *ids,
+                    int32_t id_bits, int64_t n, int64_t n_rows, int64_t width, float scale, int32_t accumulate, void *out,
+                    int32_t out_dtype, int64_t out_row_stride, void *workspace, size_t workspace_bytes, void *stream);
+
+/* One gradient tensor: n elements of type dtype, one after another.  dst: where the clipped tensor goes (may be src). */
+typedef struct {
+    const void *src; /* DEVICE */
+    void *dst;       /* DEVICE; not used by mlip_grad_norm */
+    int64_t n;
+    int32_t dtype;
+} mlip_tensor_t;
+
+/*
+ * Global norm of a list of tensors, sqrt(sum of all elements' squares), summed in fp64 and rounded to fp32 once.
+ *   tensors   HOST [count], read before the call returns; count and any n may be 0 (norm 0)
+ *   norm      DEVICE [1] fp32
+ *   workspace DEVICE scratch of at least mlip_grad_workspace(count) bytes, aligned to 16 bytes
+ */
+size_t mlip_grad_workspace(int32_t count);
+int mlip_grad_norm(const mlip_tensor_t *tensors, int32_t count, float *norm, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Norm as above, and dst = src * c for every element, with c = max_norm / norm where norm > max_norm and norm is finite, else
+ * c = 1 (max_norm >= 0).  A norm that is infinite or NaN leaves the values as they are: the caller sees it in `norm` and drops
+ * the step.  c is rounded to fp32, products are fp32, rounded to the tensor's type.  A tensor that is its own output is not
+ * written where c = 1.
+ */
+int mlip_clip_grads(const mlip_tensor_t *tensors, int32_t count, float max_norm, float *norm, void *workspace,
+                    size_t workspace_bytes, void *stream);
 
 const char *mlip_last_error(void);
 const char *mlip_version(void);

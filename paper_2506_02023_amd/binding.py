@@ -54,6 +54,10 @@ class _Pairs(ctypes.Structure):
                                                "l_row_ptr", "l_senders", "l_slot")]
 
 
+class _Tensor(ctypes.Structure):
+    _fields_ = [("src", ctypes.c_void_p), ("dst", ctypes.c_void_p), ("n", ctypes.c_int64), ("dtype", ctypes.c_int32)]
+
+
 class _Alloc(ctypes.Structure):
     _fields_ = [("alloc", _ALLOC_FN), ("free", _FREE_FN), ("ctx", ctypes.c_void_p)]
 
@@ -125,6 +129,15 @@ def lib():
         L.mlip_profile_enable.argtypes = [vp, i32]
         L.mlip_profile_read.argtypes = [vp, ctypes.POINTER(ctypes.c_float), ctypes.POINTER(i64), i32]
         L.mlip_copy_to_host.argtypes = [vp, vp, vp, ctypes.c_size_t]
+        f32, size = ctypes.c_float, ctypes.c_size_t
+        L.mlip_embed.argtypes = [vp, i32, i64, i64, i64, i64, vp, i32, i64, f32, vp, i32, i64, vp]
+        L.mlip_embed_grad_workspace.argtypes = [i64, i64, i64]
+        L.mlip_embed_grad_workspace.restype = size
+        L.mlip_embed_grad.argtypes = [vp, i32, i64, i64, vp, i32, i64, i64, i64, f32, i32, vp, i32, i64, vp, size, vp]
+        L.mlip_grad_workspace.argtypes = [i32]
+        L.mlip_grad_workspace.restype = size
+        L.mlip_grad_norm.argtypes = [vp, i32, vp, vp, size, vp]
+        L.mlip_clip_grads.argtypes = [vp, i32, f32, vp, vp, size, vp]
         L.mlip_last_error.restype = ctypes.c_char_p
         L.mlip_version.restype = ctypes.c_char_p
         _lib = L
@@ -363,3 +376,135 @@ def mlip_forward(graph, weights, mode=MODE_WHOLE, out=None, want_atom_energy=Tru
                               ctypes.c_void_p(forces.data_ptr()),
                               ctypes.c_void_p(atom_e.data_ptr() if atom_e is not None else None)))
     return energy, forces, atom_e
+
+
+# ---- per-species parameter tables and gradient clipping (no handle; results on the current stream)
+
+_DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+_ID_BITS = {torch.int32: 32, torch.int64: 64}
+
+
+def _refuse(condition, msg):
+    if condition:
+        raise MlipError(-1, msg)
+
+
+def _on_device(*tensors):
+    here = torch.cuda.current_device()
+    for t in tensors:
+        _refuse(not t.is_cuda or t.device.index != here, "tensors must be on the current GPU")
+
+
+def _matrix(t, what):
+    """(rows, width, row stride, column stride) of a matrix, or of a vector as a matrix of one column."""
+    _refuse(t.dtype not in _DTYPES, f"{what} must be float32, bfloat16 or float16")
+    if t.dim() == 1:
+        return t.shape[0], 1, t.stride(0), 1
+    _refuse(t.dim() != 2, f"{what} must be a matrix or a vector")
+    return t.shape[0], t.shape[1], t.stride(0), t.stride(1)
+
+
+def _ids(species):
+    _refuse(species.dtype not in _ID_BITS or species.dim() != 1 or (species.numel() > 1 and species.stride(0) != 1),
+            "species must be a contiguous int32 or int64 vector")
+    return species.data_ptr(), _ID_BITS[species.dtype], species.numel()
+
+
+def _output(out, rows, like):
+    """Row stride of an output matrix of `rows` rows and of the width (and dimensions) of `like`."""
+    shape = (rows,) if like.dim() == 1 else (rows, like.shape[1])
+    _refuse(out.dtype not in _DTYPES or tuple(out.shape) != shape, f"out must be a float32, bfloat16 or float16 tensor of shape {shape}")
+    if out.dim() == 1:
+        return out.stride(0)
+    _refuse(out.stride(1) != 1 and out.shape[1] > 1, "the columns of out must lie one after another")
+    return max(out.stride(0), out.shape[1]) if rows < 2 else out.stride(0)
+
+
+def mlip_embed(table, species, scale=1.0, out=None):
+    """out[i] = scale * table[species[i]]: rows of a per-species table (zeros for a species < 0, NaN for one the table lacks).
+
+    table: cuda [S, F] or [S], float32, bfloat16 or float16, any strides; species: cuda int32 or int64 [n]; out: [n, F] or [n] of any
+    of the three types (default: the table's), its columns one after another."""
+    rows, width, rs, cs = _matrix(table, "table")
+    ids, bits, n = _ids(species)
+    if out is None:
+        out = table.new_empty((n,) if table.dim() == 1 else (n, width))
+    os = _output(out, n, table)
+    _on_device(table, species, out)
+    _check(lib().mlip_embed(table.data_ptr(), _DTYPES[table.dtype], rows, width, rs, cs, ids, bits, n, scale, out.data_ptr(),
+                            _DTYPES[out.dtype], os, _stream()))
+    return out
+
+
+def mlip_embed_grad(grad, species, n_species, scale=1.0, out=None, accumulate=False):
+    """out[s] = scale * sum of grad[i] over the atoms with species[i] == s: the gradient of mlip_embed for its table.
+
+    grad: cuda [n, F] or [n], any strides (0 for a broadcast gradient); out: [n_species, F] or [n_species] (default: of grad's
+    type); accumulate: add to what out holds."""
+    rows, width, rs, cs = _matrix(grad, "grad")
+    ids, bits, n = _ids(species)
+    _refuse(rows != n, "grad must have a row for each atom")
+    _refuse(accumulate and out is None, "accumulate needs out")
+    if out is None:
+        out = grad.new_empty((n_species,) if grad.dim() == 1 else (n_species, width))
+    os = _output(out, n_species, grad)
+    _on_device(grad, species, out)
+    L = lib()
+    need = L.mlip_embed_grad_workspace(n, n_species, width)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    _check(L.mlip_embed_grad(grad.data_ptr(), _DTYPES[grad.dtype], rs, cs, ids, bits, n, n_species, width, scale, bool(accumulate),
+                             out.data_ptr(), _DTYPES[out.dtype], os, ws.data_ptr(), need, _stream()))
+    return out
+
+
+def _dense(t):
+    """Whether a tensor's elements fill one piece of memory, in any order of its dimensions."""
+    if t.is_contiguous():
+        return True
+    at = 1
+    for stride, size in sorted((s, d) for s, d in zip(t.stride(), t.shape) if d != 1):
+        if stride != at:
+            return False
+        at *= size
+    return True
+
+
+def _tensor_list(grads, out):
+    count = len(grads)
+    a = (_Tensor * count)()
+    _refuse(out is not None and len(out) != count, "out must have a tensor for each gradient")
+    for k, t in enumerate(grads):
+        _refuse(t.dtype not in _DTYPES, "gradients must be float32, bfloat16 or float16")
+        _refuse(not _dense(t), "gradients must be dense")
+        d = t if out is None else out[k]
+        _refuse(d is not t and (d.dtype != t.dtype or d.shape != t.shape or d.stride() != t.stride()),
+                "out must have the gradients' types, shapes and strides")
+        _on_device(t, d)
+        a[k] = (t.data_ptr(), d.data_ptr(), t.numel(), _DTYPES[t.dtype])
+    return a, count
+
+
+def _norm_scratch(count):
+    need = lib().mlip_grad_workspace(count)
+    return torch.empty((), dtype=torch.float32, device="cuda"), torch.empty(need, dtype=torch.uint8, device="cuda"), need
+
+
+def mlip_grad_norm(grads):
+    """Norm of all elements of the tensors together (cuda float32 scalar); asynchronous.
+
+    grads: dense cuda tensors, float32, bfloat16 or float16, mixed as they come."""
+    a, count = _tensor_list(grads, None)
+    norm, ws, need = _norm_scratch(count)
+    _check(lib().mlip_grad_norm(a, count, norm.data_ptr(), ws.data_ptr(), need, _stream()))
+    return norm
+
+
+def mlip_clip_grads(grads, max_norm, out=None):
+    """Scales the tensors so that the norm of all of them together is at most max_norm; returns the norm before.
+
+    In place, or into the tensors of `out` (of the same types, shapes and strides).  Where the norm is infinite or NaN the values stay as
+    they are: a caller that reads the norm skips the step."""
+    a, count = _tensor_list(grads, out)
+    norm, ws, need = _norm_scratch(count)
+    _check(lib().mlip_clip_grads(a, count, max_norm, norm.data_ptr(), ws.data_ptr(), need, _stream()))
+    return norm

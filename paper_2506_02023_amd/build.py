@@ -15,7 +15,7 @@ LIB = os.path.join(HERE, "libmlip.so")
 COMMON = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-I", INCLUDE, "-I", CSRC,
           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-Wno-unused-command-line-argument"]
 # graph.hip holds the fp64 edge predicate and slab rule, whose operation order is fixed: no FMA contraction
-SOURCES = {"api.hip": [], "graph.hip": ["-ffp-contract=off"], "model.hip": []}
+SOURCES = {"api.hip": [], "graph.hip": ["-ffp-contract=off"], "model.hip": [], "embed.hip": [], "clip.hip": []}
 
 
 def build(verbose=False, defines=(), lib=LIB, build_dir=BUILD):

@@ -1,5 +1,5 @@
 // C ABI of libmlip: argument checks, handle lifetime, error text, event profiler.
-#include "mlip_internal.h"
+#include "elem.h"
 
 #include <cstring>
 #include <mutex>
@@ -525,6 +525,106 @@ int mlip_profile_read(mlip_graph_t *g, float *ms, int64_t *launches, int32_t res
         if (reset) { g->prof.ms[k] = 0.f; g->prof.launches[k] = 0; }
     }
     return MLIP_OK;
+}
+
+// ---- per-species parameter tables and gradient clipping: no handle, the caller's scratch memory
+
+static bool aligned_to(const void *p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
+
+// of both table calls: `in_rows` rows of the input matrix, `out_rows` of the output
+static int check_embed_args(const EmbedArgs &a, int64_t in_rows, int64_t out_rows)
+{
+    constexpr int64_t kMost = 0x7fffffff;
+    if (a.n < 0 || a.n > kMost || a.n_rows < 1 || a.n_rows > kMost || a.width < 1 || a.width > kMost) {
+        set_error("sizes outside their ranges (need 0 <= n, 1 <= n_rows, 1 <= width, all below 2^31)");
+        return MLIP_EINVAL;
+    }
+    if (!elem_known(a.in_dtype) || !elem_known(a.out_dtype)) { set_error("unknown element type"); return MLIP_EINVAL; }
+    if (a.id_bits != 32 && a.id_bits != 64) { set_error("ids must have 32 or 64 bits"); return MLIP_EINVAL; }
+    if ((!a.in && in_rows > 0) || (!a.ids && a.n > 0) || (!a.out && out_rows > 0)) { set_error("null pointer argument"); return MLIP_EINVAL; }
+    if (!aligned_to(a.in, elem_size(a.in_dtype)) || !aligned_to(a.out, elem_size(a.out_dtype)) || !aligned_to(a.ids, a.id_bits / 8)) {
+        set_error("a pointer is not aligned to its elements");
+        return MLIP_EINVAL;
+    }
+    if (a.rs < 0 || a.cs < 0) { set_error("strides must not be negative"); return MLIP_EINVAL; }
+    if (a.os < a.width && out_rows > 1) { set_error("rows of the output overlap"); return MLIP_EINVAL; }
+    // byte offsets of the last elements, with room to spare
+    constexpr double kFar = 1e18;
+    if ((double)a.rs * (double)in_rows + (double)a.cs * (double)a.width > kFar || (double)a.os * (double)out_rows > kFar) {
+        set_error("strides too large");
+        return MLIP_EINVAL;
+    }
+    return MLIP_OK;
+}
+
+int mlip_embed(const void *table, int32_t table_dtype, int64_t n_rows, int64_t width, int64_t table_row_stride,
+               int64_t table_col_stride, const void *ids, int32_t id_bits, int64_t n, float scale, void *out,
+               int32_t out_dtype, int64_t out_row_stride, void *stream)
+{
+    const EmbedArgs a = {table, table_dtype, table_row_stride, table_col_stride, ids, id_bits, n, n_rows, width, scale, 0,
+                         out, out_dtype, out_row_stride, nullptr, static_cast<hipStream_t>(stream)};
+    MLIP_TRY(check_embed_args(a, n_rows, n));
+    return embed_impl(a);
+}
+
+size_t mlip_embed_grad_workspace(int64_t n, int64_t n_rows, int64_t width)
+{
+    return (n < 0 || n_rows < 1 || width < 1) ? 0 : embed_grad_workspace(n, n_rows, width);
+}
+
+// scratch memory that a call with `need` > 0 bytes was given
+static int check_workspace(const void *workspace, size_t bytes, size_t need)
+{
+    if (need && (!workspace || !aligned_to(workspace, 16) || bytes < need)) {
+        set_error("workspace of %zu bytes, aligned to 16, needed (%zu given)", need, workspace ? bytes : (size_t)0);
+        return MLIP_EINVAL;
+    }
+    return MLIP_OK;
+}
+
+int mlip_embed_grad(const void *grad, int32_t grad_dtype, int64_t grad_row_stride, int64_t grad_col_stride, const void *ids,
+                    int32_t id_bits, int64_t n, int64_t n_rows, int64_t width, float scale, int32_t accumulate, void *out,
+                    int32_t out_dtype, int64_t out_row_stride, void *workspace, size_t workspace_bytes, void *stream)
+{
+    const EmbedArgs a = {grad, grad_dtype, grad_row_stride, grad_col_stride, ids, id_bits, n, n_rows, width, scale, accumulate != 0,
+                         out, out_dtype, out_row_stride, workspace, static_cast<hipStream_t>(stream)};
+    MLIP_TRY(check_embed_args(a, n, n_rows));
+    MLIP_TRY(check_workspace(workspace, workspace_bytes, embed_grad_workspace(n, n_rows, width)));
+    return embed_grad_impl(a);
+}
+
+size_t mlip_grad_workspace(int32_t count) { return grad_workspace(count < 0 ? 0 : count); }
+
+static int norm_call(const mlip_tensor_t *tensors, int32_t count, bool clip, float max_norm, float *norm, void *workspace,
+                     size_t workspace_bytes, void *stream)
+{
+    if (count < 0) { set_error("count must not be negative"); return MLIP_EINVAL; }
+    if (!norm || (!tensors && count > 0)) { set_error("null pointer argument"); return MLIP_EINVAL; }
+    if (!aligned_to(norm, sizeof(float))) { set_error("a pointer is not aligned to its elements"); return MLIP_EINVAL; }
+    if (clip && !(max_norm >= 0.f)) { set_error("max_norm must be a number that is not negative"); return MLIP_EINVAL; }
+    for (int32_t t = 0; t < count; ++t) {
+        const mlip_tensor_t &x = tensors[t];
+        if (!elem_known(x.dtype)) { set_error("tensor %d: unknown element type", t); return MLIP_EINVAL; }
+        if (x.n < 0 || x.n > ((int64_t)1 << 40)) { set_error("tensor %d: size outside [0, 2^40]", t); return MLIP_EINVAL; }
+        if (x.n > 0 && (!x.src || (clip && !x.dst))) { set_error("tensor %d: null pointer", t); return MLIP_EINVAL; }
+        if (!aligned_to(x.src, elem_size(x.dtype)) || (clip && !aligned_to(x.dst, elem_size(x.dtype)))) {
+            set_error("tensor %d: a pointer is not aligned to its elements", t);
+            return MLIP_EINVAL;
+        }
+    }
+    MLIP_TRY(check_workspace(workspace, workspace_bytes, grad_workspace(count)));
+    return grad_norm_impl(tensors, count, clip, max_norm, norm, workspace, static_cast<hipStream_t>(stream));
+}
+
+int mlip_grad_norm(const mlip_tensor_t *tensors, int32_t count, float *norm, void *workspace, size_t workspace_bytes, void *stream)
+{
+    return norm_call(tensors, count, false, 0.f, norm, workspace, workspace_bytes, stream);
+}
+
+int mlip_clip_grads(const mlip_tensor_t *tensors, int32_t count, float max_norm, float *norm, void *workspace,
+                    size_t workspace_bytes, void *stream)
+{
+    return norm_call(tensors, count, true, max_norm, norm, workspace, workspace_bytes, stream);
 }
 
 int mlip_copy_to_host(const mlip_graph_t *g, void *dst_host, const void *src_device, size_t bytes)

@@ -277,4 +277,27 @@ int build_pairs_impl(mlip_graph *g, SlabView *views, int n_views, Carver *scratc
 int forward_bonds_impl(mlip_graph *g, const mlip_weights_t *w, const mlip_bond_weights_t *bw, int32_t mode,
                        double *energy, float *forces, float *atom_energy);
 
+// Arguments of the table lookup and of its gradient, checked (strides in elements).  in: the table [n_rows][width], or the incoming
+// gradient [n][width]; out: the rows [n][width], or the table's gradient [n_rows][width].
+struct EmbedArgs {
+    const void *in;
+    int32_t in_dtype;
+    int64_t rs, cs;
+    const void *ids;
+    int32_t id_bits;
+    int64_t n, n_rows, width;
+    float scale;
+    int32_t accumulate;
+    void *out;
+    int32_t out_dtype;
+    int64_t os;
+    void *workspace;
+    hipStream_t stream;
+};
+int embed_impl(const EmbedArgs &a);
+size_t embed_grad_workspace(int64_t n, int64_t n_rows, int64_t width);
+int embed_grad_impl(const EmbedArgs &a);
+size_t grad_workspace(int32_t count);
+int grad_norm_impl(const mlip_tensor_t *list, int32_t count, bool clip, float max_norm, float *norm, void *workspace, hipStream_t stream);
+
 }  // namespace mlip
