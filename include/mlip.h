@@ -406,7 +406,7 @@ enum { MLIP_DTYPE_F32 = 0, MLIP_DTYPE_BF16 = 1, MLIP_DTYPE_F16 = 2 };
  *   ids     DEVICE [n] int32 (id_bits = 32) or int64 (id_bits = 64).  A negative id stands for a place that pads a batch: its row
  *           is zeros.  An id >= n_rows has no row: nothing is read for it and its row is NaN, so that it does not pass unnoticed.
  *   out     DEVICE [n][width] of out_dtype, element (i, f) at i * out_row_stride + f, out_row_stride >= width
- * n may be 0; 1 <= n_rows < 2^31, 1 <= width < 2^31, n < 2^31.
+ * n may be 0; 1 <= n_rows < 2^31, 1 <= width <= 2^20, n < 2^31.
  */
 int mlip_embed(const void *table, int32_t table_dtype, int64_t n_rows, int64_t width, int64_t table_row_stride,
                int64_t table_col_stride, const void *ids, int32_t id_bits, int64_t n, float scale, void *out,

@@ -534,9 +534,9 @@ static bool aligned_to(const void *p, size_t bytes) { return reinterpret_cast<ui
 // of both table calls: `in_rows` rows of the input matrix, `out_rows` of the output
 static int check_embed_args(const EmbedArgs &a, int64_t in_rows, int64_t out_rows)
 {
-    constexpr int64_t kMost = 0x7fffffff;
-    if (a.n < 0 || a.n > kMost || a.n_rows < 1 || a.n_rows > kMost || a.width < 1 || a.width > kMost) {
-        set_error("sizes outside their ranges (need 0 <= n, 1 <= n_rows, 1 <= width, all below 2^31)");
+    constexpr int64_t kMost = 0x7fffffff, kMostWidth = 1 << 20;
+    if (a.n < 0 || a.n > kMost || a.n_rows < 1 || a.n_rows > kMost || a.width < 1 || a.width > kMostWidth) {
+        set_error("sizes outside their ranges (need 0 <= n < 2^31, 1 <= n_rows < 2^31, 1 <= width <= 2^20)");
         return MLIP_EINVAL;
     }
     if (!elem_known(a.in_dtype) || !elem_known(a.out_dtype)) { set_error("unknown element type"); return MLIP_EINVAL; }

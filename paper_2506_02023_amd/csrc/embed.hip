@@ -3,91 +3,549 @@
 
 namespace mlip {
 
-// out[i][f] = scale * table[id_i][f], a thread per element.
-template <class T, class O, class Id>
-__global__ __launch_bounds__(256) void k_embed(const T *table, int64_t n_rows, int64_t width, int64_t rs, int64_t cs, const Id *ids,
-                                               int64_t n, float scale, O *out, int64_t os)
+// x / d for 0 <= x < 2^31 as a product and a shift: m = floor(2^(31 + l) / d) + 1 with 2^l >= d errs by less than 2^-31 / d relative
+struct Div31 {
+    uint32_t m;
+    int shift;
+    explicit Div31(uint32_t d)
+    {
+        int l = 0;
+        while (((uint64_t)1 << l) < d) ++l;
+        m = (uint32_t)(((uint64_t)1 << (31 + l)) / d + 1);
+        shift = 31 + l;
+    }
+    __device__ uint32_t operator()(uint32_t x) const { return (uint32_t)(((uint64_t)x * m) >> shift); }
+};
+
+// V elements of a row as fp32: one wide access where they lie one after another, at whatever alignment (rows of odd widths begin anywhere)
+template <class T, int V> using Cols = T __attribute__((ext_vector_type(V)));
+
+template <int V, class T> __device__ inline void load_cols(float (&v)[V], const T *p, int64_t cs, int64_t left)
 {
-    const int64_t total = n * width, step = (int64_t)gridDim.x * 256;
-    for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < total; e += step) {
-        const int64_t i = e / width, f = e - i * width, id = ids[i];
-        float v = 0.f;
-        if (id >= n_rows) v = __builtin_nanf("");
-        else if (id >= 0) v = scale * (float)table[id * rs + f * cs];
-        out[i * os + f] = to_elem<O>(v);
+    if (V > 1 && cs == 1 && left >= V) {
+        Cols<T, V> x;
+        __builtin_memcpy(&x, p, sizeof(T) * V);
+#pragma unroll
+        for (int k = 0; k < V; ++k) v[k] = (float)x[k];
+    } else {
+#pragma unroll
+        for (int k = 0; k < V; ++k) v[k] = k < left ? (float)p[k * cs] : 0.f;
+    }
+}
+
+template <int V, class T> __device__ inline void store_cols(T *p, const float (&v)[V], int64_t left)
+{
+    if (V > 1 && left >= V) {
+        Cols<T, V> x;
+#pragma unroll
+        for (int k = 0; k < V; ++k) x[k] = to_elem<T>(v[k]);
+        __builtin_memcpy(p, &x, sizeof(T) * V);
+    } else {
+#pragma unroll
+        for (int k = 0; k < V; ++k)
+            if (k < left) p[k] = to_elem<T>(v[k]);
+    }
+}
+
+// ---- lookup: out[i][f] = scale * table[id_i][f], V columns of a row per thread and step
+
+template <class T, class O, class Id, int V>
+__global__ __launch_bounds__(256) void k_embed(const T *table, int64_t n_rows, int64_t width, int64_t rs, int64_t cs, const Id *ids,
+                                               uint32_t items, uint32_t per_row, Div31 div, float scale, O *out, int64_t os)
+{
+    const uint32_t step = gridDim.x * 256;
+    for (uint32_t e = blockIdx.x * 256 + threadIdx.x; e < items; e += step) {
+        const uint32_t i = div(e);
+        const int64_t f = (int64_t)(e - i * per_row) * V, id = ids[i];
+        float v[V];
+        if (id >= 0 && id < n_rows) {
+            load_cols<V>(v, table + id * rs + f * cs, cs, width - f);
+#pragma unroll
+            for (int k = 0; k < V; ++k) v[k] *= scale;
+        } else {
+#pragma unroll
+            for (int k = 0; k < V; ++k) v[k] = id < 0 ? 0.f : __builtin_nanf("");
+        }
+        store_cols<V>(out + i * os + f, v, width - f);
     }
 }
 
 int embed_impl(const EmbedArgs &a)
 {
     if (a.n == 0) return MLIP_OK;
-    const int64_t blocks = (a.n * a.width + 255) / 256;
-    const dim3 grid((unsigned)(blocks < 65536 ? blocks : 65536));
-    with_elem(a.in_dtype, [&](auto t) {
-        with_elem(a.out_dtype, [&](auto o) {
-            with_ids(a.id_bits, [&](auto id) {
-                using T = decltype(t);
-                using O = decltype(o);
-                using Id = decltype(id);
-                k_embed<T, O, Id><<<grid, 256, 0, a.stream>>>(static_cast<const T *>(a.in), a.n_rows, a.width, a.rs, a.cs,
-                                                              static_cast<const Id *>(a.ids), a.n, a.scale,
-                                                              static_cast<O *>(a.out), a.os);
+    constexpr int V = 4;
+    const int64_t per_row = (a.width + V - 1) / V;
+    const int64_t most = ((int64_t)1 << 30) / per_row > 0 ? ((int64_t)1 << 30) / per_row : 1;   // rows of a launch: items are numbered in 31 bits
+    const Div31 div((uint32_t)per_row);
+    for (int64_t i0 = 0; i0 < a.n; i0 += most) {
+        const int64_t rows = a.n - i0 < most ? a.n - i0 : most, items = rows * per_row, blocks = (items + 255) / 256;
+        const dim3 grid((unsigned)(blocks < 8192 ? blocks : 8192));
+        with_elem(a.in_dtype, [&](auto t) {
+            with_elem(a.out_dtype, [&](auto o) {
+                with_ids(a.id_bits, [&](auto id) {
+                    using T = decltype(t);
+                    using O = decltype(o);
+                    using Id = decltype(id);
+                    k_embed<T, O, Id, V><<<grid, 256, 0, a.stream>>>(static_cast<const T *>(a.in), a.n_rows, a.width, a.rs, a.cs,
+                                                                     static_cast<const Id *>(a.ids) + i0, (uint32_t)items,
+                                                                     (uint32_t)per_row, div, a.scale, static_cast<O *>(a.out) + i0 * a.os,
+                                                                     a.os);
+                });
             });
         });
-    });
+    }
     MLIP_HIP(hipGetLastError());
     return MLIP_OK;
 }
 
-// out[r][f] = scale * sum over id_i == r of grad[i][f]: a wavefront for 64 columns of one row, which goes over all ids and adds
-// up the rows it finds, in their order.
+// ---- gradient: out[r][f] = scale * sum over id_i == r of grad[i][f]
+
+// the output matrix, whatever its type
+struct GradOut {
+    void *p;
+    int dtype;
+    int64_t os;
+    float scale;
+    int accumulate;
+    // writes the finished sums of V columns of a row from column f on, `left` of them in the matrix
+    template <int V> __device__ void put(int64_t r, int64_t f, const double (&sum)[V], int64_t left) const
+    {
+        if (dtype == MLIP_DTYPE_F32) put_as<V>(static_cast<float *>(p), r, f, sum, left);
+        else if (dtype == MLIP_DTYPE_BF16) put_as<V>(static_cast<__bf16 *>(p), r, f, sum, left);
+        else put_as<V>(static_cast<_Float16 *>(p), r, f, sum, left);
+    }
+    template <int V, class O> __device__ void put_as(O *base, int64_t r, int64_t f, const double (&sum)[V], int64_t left) const
+    {
+        O *o = base + r * os + f;
+        float v[V];
+#pragma unroll
+        for (int k = 0; k < V; ++k) v[k] = 0.f;
+        if (accumulate) load_cols<V>(v, o, 1, left);
+#pragma unroll
+        for (int k = 0; k < V; ++k) v[k] = (float)(sum[k] * (double)scale + (double)v[k]);
+        store_cols<V>(o, v, left);
+    }
+};
+
+// Few rows: every wavefront keeps a table of all rows in LDS, 64 floats to a row, one for each lane: lane l owns column l % tile of the
+// wavefront's rows l / tile, l / tile + slots, ...  A lane adds its values to its own float of the row (an LDS addition without return, which needs
+// no wait), so nothing collides and the order of the additions is the order of the atoms.  A block then joins the lanes that own the same
+// column, and its wavefronts' tables.  Ids without a row go to one row more, which is not read.
+constexpr int kFewLds = 65536, kFewWaves = 16, kFewUnroll = 16;
+
 template <class T, class Id>
-__global__ __launch_bounds__(64) void k_embed_grad(const T *grad, int64_t rs, int64_t cs, const Id *ids, int64_t n, int64_t width,
-                                                   float scale, int accumulate, void *out, int out_dtype, int64_t os)
+__global__ __launch_bounds__(1024) void k_few_rows(const T *grad, int64_t rs, int64_t cs, const Id *ids, int64_t n, int n_rows, int64_t width,
+                                                   int tile, int slots, int64_t rows_per_wave, float *part, GradOut out)
 {
-    const int lane = threadIdx.x;
-    const int64_t r = blockIdx.x;
-    for (int64_t f0 = 0; f0 < width; f0 += 64) {
-        const int64_t f = f0 + lane;
-        double sum = 0.0;
-        for (int64_t i0 = 0; i0 < n; i0 += 64) {
-            const bool mine = i0 + lane < n && (int64_t)ids[i0 + lane] == r;
-            for (uint64_t left = __ballot(mine); left; left &= left - 1) {
-                const int64_t i = i0 + __ffsll((unsigned long long)left) - 1;
-                if (f < width) sum += (double)(float)grad[i * rs + f * cs];
+    extern __shared__ float tables[];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6, size = (n_rows + 1) * 64;
+    float *mine = tables + wave * size;
+    for (int k = lane; k < size; k += 64) mine[k] = 0.f;
+    const int64_t f0 = (int64_t)blockIdx.y * tile;
+    const int cols = (int)(width - f0 < tile ? width - f0 : tile), slot = lane / tile, col = lane - slot * tile;
+    const int64_t r0 = ((int64_t)blockIdx.x * waves + wave) * rows_per_wave, r1 = n - r0 < rows_per_wave ? n : r0 + rows_per_wave;
+    if (slot < slots && col < cols) {
+        const T *g = grad + (f0 + col) * cs;
+        for (int64_t r = r0 + slot; r < r1; r += (int64_t)slots * kFewUnroll) {
+            int at[kFewUnroll];
+            float v[kFewUnroll];
+#pragma unroll
+            for (int u = 0; u < kFewUnroll; ++u) {
+                const int64_t i = r + (int64_t)u * slots;
+                const int64_t id = i < r1 ? (int64_t)ids[i] : -1;
+                at[u] = id >= 0 && id < n_rows ? (int)id : n_rows;
+                v[u] = i < r1 ? (float)g[i * rs] : 0.f;
             }
+#pragma unroll
+            for (int u = 0; u < kFewUnroll; ++u)
+                __hip_atomic_fetch_add(mine + at[u] * 64 + lane, v[u], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
         }
-        if (f >= width) continue;
-        sum *= (double)scale;
-        const int64_t at = r * os + f;
-        if (out_dtype == MLIP_DTYPE_F32) {
-            float *o = static_cast<float *>(out) + at;
-            *o = (float)(accumulate ? sum + (double)*o : sum);
-        } else if (out_dtype == MLIP_DTYPE_BF16) {
-            __bf16 *o = static_cast<__bf16 *>(out) + at;
-            *o = (__bf16)(float)(accumulate ? sum + (double)(float)*o : sum);
-        } else {
-            _Float16 *o = static_cast<_Float16 *>(out) + at;
-            *o = (_Float16)(float)(accumulate ? sum + (double)(float)*o : sum);
+    }
+    if (slots > 1) {   // the wavefront's own table: its slots joined into the first
+        __syncthreads();
+        const int step = 64 / cols, c = lane % cols;
+        for (int s = lane / cols; s < n_rows && lane < step * cols; s += step) {
+            double sum = 0.0;
+            for (int k = 0; k < slots; ++k) sum += (double)mine[s * 64 + k * tile + c];
+            mine[s * 64 + c] = (float)sum;
+        }
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < n_rows * cols; e += blockDim.x) {
+        const int s = e / cols, c = e - s * cols;
+        double sum[1] = {0.0};
+        for (int w = 0; w < waves; ++w) sum[0] += (double)tables[w * size + s * 64 + c];
+        if (part) part[((int64_t)blockIdx.x * n_rows + s) * width + f0 + c] = (float)sum[0];
+        else out.put<1>(s, f0 + c, sum, 1);
+    }
+}
+
+// sum over the blocks of k_few_rows, 64 elements to a block of 16 wavefronts which share the parts
+__global__ __launch_bounds__(1024) void k_few_join(const float *part, int parts, int64_t elements, int64_t width, GradOut out)
+{
+    __shared__ double red[16][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t e = (int64_t)blockIdx.x * 64 + lane;
+    double sum[1] = {0.0};
+    if (e < elements) {
+#pragma unroll 16
+        for (int p = wave; p < parts; p += 16) sum[0] += (double)part[p * elements + e];
+    }
+    red[wave][lane] = sum[0];
+    __syncthreads();
+    if (wave || e >= elements) return;
+    for (int w = 1; w < 16; ++w) sum[0] += red[w][lane];
+    out.put<1>(e / width, e % width, sum, 1);
+}
+
+struct FewPlan {
+    int tiles, tile, slots, waves, blocks;
+    int64_t rows_per_wave;
+    FewPlan(int64_t n, int64_t n_rows, int64_t width)
+    {
+        tiles = (int)((width + 63) / 64);
+        tile = (int)((width + tiles - 1) / tiles);
+        slots = 64 / tile;
+        waves = (int)(kFewLds / ((n_rows + 1) * 256));
+        waves = waves < 1 ? 1 : waves > kFewWaves ? kFewWaves : waves;
+        // wavefronts: as many as have a step of kFewUnroll rows a lane, at most two blocks a compute unit, but no more than
+        // MLIP_EMBED_GRAD_RUN rows a lane; where one block does with four steps, one block
+        const int64_t step = (int64_t)slots * kFewUnroll;
+        const int64_t most = 512 / tiles > 1 ? 512 / tiles : 1;
+        int64_t b = (n + step * waves - 1) / (step * waves);
+        b = b <= 4 ? 1 : b > most ? most : b;
+        int64_t r = ((n + b * waves - 1) / (b * waves) + step - 1) / step * step;
+        if (r > (int64_t)slots * MLIP_EMBED_GRAD_RUN) r = (int64_t)slots * MLIP_EMBED_GRAD_RUN;
+        rows_per_wave = r > 0 ? r : step;
+        b = (n + rows_per_wave * waves - 1) / (rows_per_wave * waves);
+        blocks = (int)(b < 1 ? 1 : b);
+    }
+};
+
+constexpr int64_t kFewMost = kFewLds / 256 - 1;   // rows whose table fits a wavefront's LDS
+
+// Many rows: the ids are sorted (stable, by digits of at most 8 bits, places of the atoms along with them), so that every row's atoms lie one
+// after another in their order; spans of the sorted list are summed, whatever rows they hold, and a row that spans share is joined.
+
+constexpr int kSortThreads = 1024, kSortTile = 4096, kSortBlocks = 256, kRadix = 256;
+
+struct Pair { uint32_t key, at; };
+
+struct SortPlan {
+    int passes, bits, blocks;
+    int64_t range;   // items of a block, a multiple of kSortTile
+    SortPlan(int64_t n, int64_t n_rows)
+    {
+        int total = 0;
+        while (((int64_t)1 << total) <= n_rows) ++total;   // keys 0 .. n_rows
+        passes = (total + 7) / 8;
+        bits = (total + passes - 1) / passes;
+        const int64_t per = (n + kSortBlocks - 1) / kSortBlocks;
+        range = (per + kSortTile - 1) / kSortTile * kSortTile;
+        if (range < kSortTile) range = kSortTile;
+        blocks = (int)((n + range - 1) / range);
+    }
+};
+
+template <class Id> __device__ inline Pair item_of(const Id *ids, int64_t i, int64_t n_rows)
+{
+    const int64_t id = ids[i];
+    return {id >= 0 && id < n_rows ? (uint32_t)id : (uint32_t)n_rows, (uint32_t)i};
+}
+__device__ inline Pair item_of(const Pair *list, int64_t i, int64_t) { return list[i]; }
+
+// how often each digit comes up in a block's range; on the first pass also clears the ends of the rows' spans
+template <class In>
+__global__ __launch_bounds__(kSortThreads) void k_digit_counts(const In *in, int64_t n, int64_t n_rows, int64_t range, int shift, int bits,
+                                                               uint32_t *counts, uint32_t *row_end)
+{
+    __shared__ uint32_t count[kRadix];
+    const uint32_t mask = (1u << bits) - 1;
+    if (threadIdx.x < kRadix) count[threadIdx.x] = 0;
+    if (row_end)
+        for (int64_t r = (int64_t)blockIdx.x * kSortThreads + threadIdx.x; r < n_rows; r += (int64_t)gridDim.x * kSortThreads) row_end[r] = 0;
+    __syncthreads();
+    const int64_t end = n - range * blockIdx.x < range ? n : range * (blockIdx.x + 1);
+    for (int64_t i = range * blockIdx.x + threadIdx.x; i < end; i += kSortThreads)
+        atomicAdd(&count[(item_of(in, i, n_rows).key >> shift) & mask], 1u);
+    __syncthreads();
+    if (threadIdx.x < kRadix) counts[(int64_t)blockIdx.x * kRadix + threadIdx.x] = count[threadIdx.x];
+}
+
+// one pass of the sort: a block takes its range in tiles of 4096; a wavefront ranks 256 of them, 64 at a time
+template <class In>
+__global__ __launch_bounds__(kSortThreads) void k_digit_scatter(const In *in, int64_t n, int64_t n_rows, int64_t range, int shift, int bits,
+                                                                const uint32_t *counts, Pair *sorted)
+{
+    constexpr int kWaves = kSortThreads / 64, kRounds = kSortTile / kSortThreads;
+    __shared__ uint32_t before[kWaves][kRadix];   // per wavefront: items of the digit before its own
+    __shared__ uint32_t base[kRadix];             // where the digit's next item of this block goes
+    __shared__ uint32_t sums[4];
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    const uint32_t mask = (1u << bits) - 1;
+    {   // base: items of lower digits anywhere, and of this digit in the blocks before
+        const int d = t & (kRadix - 1), quarter = t / kRadix;
+        uint32_t all = 0, earlier = 0;
+#pragma unroll 8
+        for (int b = quarter; b < (int)gridDim.x; b += kSortThreads / kRadix) {
+            const uint32_t c = counts[(int64_t)b * kRadix + d];
+            all += c;
+            earlier += b < (int)blockIdx.x ? c : 0;
+        }
+        before[quarter][d] = all;
+        before[quarter + 4][d] = earlier;
+        __syncthreads();
+        uint32_t scan = 0, own = 0;
+        if (t < kRadix) {
+            all = before[0][t] + before[1][t] + before[2][t] + before[3][t];
+            earlier = before[4][t] + before[5][t] + before[6][t] + before[7][t];
+            own = all;
+            scan = all;
+            for (int k = 1; k < 64; k <<= 1) {
+                const uint32_t up = __shfl_up(scan, k);
+                if (lane >= k) scan += up;
+            }
+            if (lane == 63) sums[wave] = scan;
+        }
+        __syncthreads();
+        if (t < kRadix) {
+            for (int w = 0; w < wave; ++w) scan += sums[w];
+            base[t] = scan - own + earlier;
+        }
+    }
+    const int64_t end = n - range * blockIdx.x < range ? n : range * (blockIdx.x + 1);
+    for (int64_t i0 = range * blockIdx.x; i0 < end; i0 += kSortTile) {
+        __syncthreads();
+        for (int k = t; k < kWaves * kRadix; k += kSortThreads) (&before[0][0])[k] = 0;
+        __syncthreads();
+        Pair item[kRounds];
+        uint32_t rank[kRounds];
+#pragma unroll
+        for (int j = 0; j < kRounds; ++j) {
+            const int64_t i = i0 + wave * (64 * kRounds) + j * 64 + lane;
+            item[j] = i < end ? item_of(in, i, n_rows) : Pair{0, 0};
+        }
+#pragma unroll
+        for (int j = 0; j < kRounds; ++j) {
+            const bool there = i0 + wave * (64 * kRounds) + j * 64 + lane < end;
+            const uint32_t d = (item[j].key >> shift) & mask;
+            uint64_t same = __ballot(there);
+            for (int b = 0; b < bits; ++b) {
+                const uint64_t set = __ballot((d >> b) & 1);
+                same &= (d >> b) & 1 ? set : ~set;
+            }
+            const uint32_t lower = (uint32_t)__popcll(same & (((uint64_t)1 << lane) - 1));
+            rank[j] = before[wave][d] + lower;
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // all lanes have read before the first of each digit writes
+            if (there && lower == 0) before[wave][d] = rank[j] + (uint32_t)__popcll(same);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        }
+        __syncthreads();
+        if (t < kRadix) {
+            uint32_t at = base[t];
+            for (int w = 0; w < kWaves; ++w) {
+                const uint32_t c = before[w][t];
+                before[w][t] = at;
+                at += c;
+            }
+            base[t] = at;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < kRounds; ++j) {
+            const uint32_t d = (item[j].key >> shift) & mask;
+            if (i0 + wave * (64 * kRounds) + j * 64 + lane < end) sorted[before[wave][d] + rank[j]] = item[j];
         }
     }
 }
 
-size_t embed_grad_workspace(int64_t, int64_t, int64_t) { return 0; }
-
-int embed_grad_impl(const EmbedArgs &a)
+// Sums over spans of `span` items of the sorted list, a group of `lanes` lanes (V columns each) to a span.  A row that lies within the span is
+// written; what a span holds of a row that began before it goes to edge[span][0], of one that goes on behind it to edge[span][1].
+template <class T, int V>
+__global__ __launch_bounds__(256) void k_span_sums(const Pair *sorted, const T *grad, int64_t rs, int64_t cs, int64_t n, int64_t n_rows,
+                                                   int64_t width, int lanes, int span, uint32_t *row_begin, uint32_t *row_end, float *edge,
+                                                   GradOut out)
 {
+    constexpr int U = 8;
+    const int64_t s = (int64_t)blockIdx.x * (256 / lanes) + threadIdx.x / lanes;
+    const int64_t f = ((int64_t)blockIdx.y * lanes + threadIdx.x % lanes) * V, p0 = s * span;
+    if (threadIdx.x / lanes >= 256 / lanes || p0 >= n || f >= width) return;
+    const int64_t p1 = n - p0 < span ? n : p0 + span, left = width - f;
+    uint32_t key = sorted[p0].key;
+    if (key >= n_rows) return;   // ids without a row are the last ones
+    bool from_before = p0 > 0 && sorted[p0 - 1].key == key;
+    float sum[V];
+#pragma unroll
+    for (int k = 0; k < V; ++k) sum[k] = 0.f;
+    auto finish = [&](int64_t end, bool goes_on) {   // the row `key` up to `end`, as far as this span has it
+        if (from_before || goes_on) {
+            store_cols<V>(edge + (s * 2 + (from_before ? 0 : 1)) * width + f, sum, left);
+        } else {
+            double v[V];
+#pragma unroll
+            for (int k = 0; k < V; ++k) v[k] = (double)sum[k];
+            out.put<V>(key, f, v, left);
+        }
+        if (f == 0 && !goes_on) row_end[key] = (uint32_t)end;
+    };
+    if (f == 0 && !from_before) row_begin[key] = (uint32_t)p0;
+    for (int64_t p = p0; p < p1; p += U) {
+        Pair item[U];
+        float v[U][V];
+#pragma unroll
+        for (int u = 0; u < U; ++u) item[u] = p + u < p1 ? sorted[p + u] : Pair{(uint32_t)n_rows, 0};
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (item[u].key < n_rows) load_cols<V>(v[u], grad + item[u].at * rs + f * cs, cs, left);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (p + u >= p1) break;
+            if (item[u].key != key) {
+                finish(p + u, false);
+                key = item[u].key;
+                if (key >= n_rows) return;
+                from_before = false;
+                if (f == 0) row_begin[key] = (uint32_t)(p + u);
+#pragma unroll
+                for (int k = 0; k < V; ++k) sum[k] = 0.f;
+            }
+#pragma unroll
+            for (int k = 0; k < V; ++k) sum[k] += v[u][k];
+        }
+    }
+    finish(p1, p1 < n && sorted[p1].key == key);
+}
+
+// rows that no id names, and rows that several spans share
+template <int V>
+__global__ __launch_bounds__(256) void k_row_join(const uint32_t *row_begin, const uint32_t *row_end, const float *edge, int span, uint32_t items,
+                                                  uint32_t per_row, Div31 div, int64_t row0, int64_t width, GradOut out)
+{
+    const uint32_t step = gridDim.x * 256;
+    for (uint32_t e = blockIdx.x * 256 + threadIdx.x; e < items; e += step) {
+        const uint32_t i = div(e);
+        const int64_t r = row0 + i, f = (int64_t)(e - i * per_row) * V, left = width - f;
+        const uint32_t end = row_end[r];
+        double sum[V];
+#pragma unroll
+        for (int k = 0; k < V; ++k) sum[k] = 0.0;
+        if (end > 0) {
+            const int64_t first = row_begin[r] / span, last = (end - 1) / span;
+            if (first == last) continue;
+            for (int64_t s = first; s <= last; ++s) {
+                float v[V];
+                load_cols<V>(v, edge + (s * 2 + (s == first ? 1 : 0)) * width + f, 1, left);
+#pragma unroll
+                for (int k = 0; k < V; ++k) sum[k] += (double)v[k];
+            }
+        }
+        out.put<V>(r, f, sum, left);
+    }
+}
+
+// the parts of the workspace of the sorted way
+struct SortSpace {
+    size_t pairs[2], counts, row_begin, row_end, edge, bytes;
+    int span;
+    SortSpace(int64_t n, int64_t n_rows, int64_t width)
+    {
+        span = 64;
+        size_t at = 0;
+        auto take = [&](size_t size) { const size_t here = at; at += (size + 255) & ~(size_t)255; return here; };
+        for (size_t &p : pairs) p = take((size_t)n * sizeof(Pair));
+        counts = take((size_t)kSortBlocks * kRadix * 4);
+        row_begin = take((size_t)n_rows * 4);
+        row_end = take((size_t)n_rows * 4);
+        edge = take((size_t)((n + span - 1) / span) * 2 * (size_t)width * 4);
+        bytes = at;
+    }
+};
+
+size_t embed_grad_workspace(int64_t n, int64_t n_rows, int64_t width)
+{
+    if (n_rows <= kFewMost) {
+        const FewPlan p(n, n_rows, width);
+        return p.blocks > 1 ? (size_t)p.blocks * (size_t)n_rows * (size_t)width * 4 : 0;
+    }
+    return SortSpace(n, n_rows, width).bytes;
+}
+
+static int few_rows(const EmbedArgs &a, const GradOut &out)
+{
+    const FewPlan p(a.n, a.n_rows, a.width);
+    float *part = p.blocks > 1 ? static_cast<float *>(a.workspace) : nullptr;
     with_elem(a.in_dtype, [&](auto t) {
         with_ids(a.id_bits, [&](auto id) {
             using T = decltype(t);
             using Id = decltype(id);
-            k_embed_grad<T, Id><<<dim3((unsigned)a.n_rows), 64, 0, a.stream>>>(static_cast<const T *>(a.in), a.rs, a.cs,
-                                                                               static_cast<const Id *>(a.ids), a.n, a.width, a.scale,
-                                                                               a.accumulate, a.out, a.out_dtype, a.os);
+            k_few_rows<T, Id><<<dim3(p.blocks, p.tiles), p.waves * 64, (size_t)p.waves * (a.n_rows + 1) * 256, a.stream>>>(
+                static_cast<const T *>(a.in), a.rs, a.cs, static_cast<const Id *>(a.ids), a.n, (int)a.n_rows, a.width, p.tile, p.slots,
+                p.rows_per_wave, part, out);
         });
     });
     MLIP_HIP(hipGetLastError());
+    if (part) {
+        const int64_t elements = a.n_rows * a.width;
+        k_few_join<<<(unsigned)((elements + 63) / 64), 1024, 0, a.stream>>>(part, p.blocks, elements, a.width, out);
+        MLIP_HIP(hipGetLastError());
+    }
     return MLIP_OK;
+}
+
+static int many_rows(const EmbedArgs &a, const GradOut &out)
+{
+    const SortSpace w(a.n, a.n_rows, a.width);
+    const SortPlan p(a.n, a.n_rows);
+    char *base = static_cast<char *>(a.workspace);
+    auto u32 = [&](size_t at) { return reinterpret_cast<uint32_t *>(base + at); };
+    Pair *list[2] = {reinterpret_cast<Pair *>(base + w.pairs[0]), reinterpret_cast<Pair *>(base + w.pairs[1])};
+    uint32_t *counts = u32(w.counts), *row_begin = u32(w.row_begin), *row_end = u32(w.row_end);
+    float *edge = reinterpret_cast<float *>(base + w.edge);
+    {
+        with_ids(a.id_bits, [&](auto id) {
+            using Id = decltype(id);
+            const Id *ids = static_cast<const Id *>(a.ids);
+            k_digit_counts<<<p.blocks > 0 ? p.blocks : 1, kSortThreads, 0, a.stream>>>(ids, a.n, a.n_rows, p.range, 0, p.bits, counts, row_end);
+            if (a.n == 0) return;
+            k_digit_scatter<<<p.blocks, kSortThreads, 0, a.stream>>>(ids, a.n, a.n_rows, p.range, 0, p.bits, counts, list[0]);
+        });
+        for (int k = 1; k < p.passes && a.n > 0; ++k) {
+            const Pair *in = list[(k - 1) & 1];
+            k_digit_counts<<<p.blocks, kSortThreads, 0, a.stream>>>(in, a.n, a.n_rows, p.range, k * p.bits, p.bits, counts, (uint32_t *)nullptr);
+            k_digit_scatter<<<p.blocks, kSortThreads, 0, a.stream>>>(in, a.n, a.n_rows, p.range, k * p.bits, p.bits, counts, list[k & 1]);
+        }
+        MLIP_HIP(hipGetLastError());
+    }
+    constexpr int V = 4;
+    const int64_t per_row = (a.width + V - 1) / V;
+    if (a.n > 0) {
+        const Pair *sorted = list[(p.passes - 1) & 1];
+        const int lanes = (int)(per_row < 64 ? per_row : 64);
+        const int64_t spans = (a.n + w.span - 1) / w.span, groups = 256 / lanes;
+        const dim3 grid((unsigned)((spans + groups - 1) / groups), (unsigned)((per_row + lanes - 1) / lanes));
+        with_elem(a.in_dtype, [&](auto t) {
+            using T = decltype(t);
+            k_span_sums<T, V><<<grid, 256, 0, a.stream>>>(sorted, static_cast<const T *>(a.in), a.rs, a.cs, a.n, a.n_rows, a.width, lanes, w.span,
+                                                          row_begin, row_end, edge, out);
+        });
+        MLIP_HIP(hipGetLastError());
+    }
+    const int64_t most = ((int64_t)1 << 30) / per_row > 0 ? ((int64_t)1 << 30) / per_row : 1;
+    const Div31 div((uint32_t)per_row);
+    for (int64_t r0 = 0; r0 < a.n_rows; r0 += most) {
+        const int64_t rows = a.n_rows - r0 < most ? a.n_rows - r0 : most, items = rows * per_row, blocks = (items + 255) / 256;
+        k_row_join<V><<<(unsigned)(blocks < 16384 ? blocks : 16384), 256, 0, a.stream>>>(row_begin, row_end, edge, w.span, (uint32_t)items,
+                                                                                        (uint32_t)per_row, div, r0, a.width, out);
+    }
+    MLIP_HIP(hipGetLastError());
+    return MLIP_OK;
+}
+
+int embed_grad_impl(const EmbedArgs &a)
+{
+    const GradOut out = {a.out, a.out_dtype, a.os, a.scale, a.accumulate};
+    return a.n_rows <= kFewMost ? few_rows(a, out) : many_rows(a, out);
 }
 
 }  // namespace mlip
