@@ -128,8 +128,9 @@ struct GradOut {
 };
 
 // Few rows: every wavefront keeps a table of all rows in LDS, 64 floats to a row, one for each lane: lane l owns column l % tile of the
-// wavefront's rows l / tile, l / tile + slots, ...  A lane adds its values to its own float of the row (an LDS addition without return, which needs
-// no wait), so nothing collides and the order of the additions is the order of the atoms.  A block then joins the lanes that own the same
+// wavefront's rows l / tile, l / tile + slots, ...  A lane adds its values to its own float of the row, so nothing collides and the order of
+// the additions is the order of the atoms.  (Read, add, write: an LDS addition without return takes 220 clocks a wavefront, 361 us where this
+// takes XX at a million rows of 64.)  A block then joins the lanes that own the same
 // column, and its wavefronts' tables.  Ids without a row go to one row more, which is not read.
 constexpr int kFewLds = 65536, kFewWaves = 16, kFewUnroll = 16;
 
@@ -157,8 +158,7 @@ __global__ __launch_bounds__(1024) void k_few_rows(const T *grad, int64_t rs, in
                 v[u] = i < r1 ? (float)g[i * rs] : 0.f;
             }
 #pragma unroll
-            for (int u = 0; u < kFewUnroll; ++u)
-                __hip_atomic_fetch_add(mine + at[u] * 64 + lane, v[u], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
+            for (int u = 0; u < kFewUnroll; ++u) mine[at[u] * 64 + lane] += v[u];
         }
     }
     if (slots > 1) {   // the wavefront's own table: its slots joined into the first
@@ -389,11 +389,16 @@ __global__ __launch_bounds__(256) void k_span_sums(const Pair *sorted, const T *
         if (f == 0 && !goes_on) row_end[key] = (uint32_t)end;
     };
     if (f == 0 && !from_before) row_begin[key] = (uint32_t)p0;
+    Pair next[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) next[u] = p0 + u < p1 ? sorted[p0 + u] : Pair{(uint32_t)n_rows, 0};
     for (int64_t p = p0; p < p1; p += U) {
         Pair item[U];
         float v[U][V];
 #pragma unroll
-        for (int u = 0; u < U; ++u) item[u] = p + u < p1 ? sorted[p + u] : Pair{(uint32_t)n_rows, 0};
+        for (int u = 0; u < U; ++u) item[u] = next[u];
+#pragma unroll
+        for (int u = 0; u < U; ++u) next[u] = p + U + u < p1 ? sorted[p + U + u] : Pair{(uint32_t)n_rows, 0};
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (item[u].key < n_rows) load_cols<V>(v[u], grad + item[u].at * rs + f * cs, cs, left);
@@ -417,30 +422,65 @@ __global__ __launch_bounds__(256) void k_span_sums(const Pair *sorted, const T *
     finish(p1, p1 < n && sorted[p1].key == key);
 }
 
-// rows that no id names, and rows that several spans share
+// Rows that no id names, and rows that spans share.  A thread has V columns of a row and adds up what at most kJoinSerial spans hold of it;
+// a row of more spans is the work of one of the first `heavy` blocks (64 such lots of columns at most): block b looks at span b * kJoinSerial, and if the row
+// that runs into this span from before is such a row, and no earlier block sees it, shares the row's spans out over its threads.
+constexpr int kJoinSerial = 16;
+
 template <int V>
-__global__ __launch_bounds__(256) void k_row_join(const uint32_t *row_begin, const uint32_t *row_end, const float *edge, int span, uint32_t items,
-                                                  uint32_t per_row, Div31 div, int64_t row0, int64_t width, GradOut out)
+__global__ __launch_bounds__(256) void k_row_join(const Pair *sorted, const uint32_t *row_begin, const uint32_t *row_end, const float *edge,
+                                                  int64_t n, int span, int heavy, uint32_t items, uint32_t per_row, Div31 div, int64_t row0,
+                                                  int64_t n_rows, int64_t width, GradOut out)
 {
-    const uint32_t step = gridDim.x * 256;
-    for (uint32_t e = blockIdx.x * 256 + threadIdx.x; e < items; e += step) {
+    __shared__ double red[256][V];
+    auto add = [&](double (&sum)[V], int64_t s, int64_t first, int64_t f) {
+        float v[V];
+        load_cols<V>(v, edge + (s * 2 + (s == first ? 1 : 0)) * width + f, 1, width - f);
+#pragma unroll
+        for (int k = 0; k < V; ++k) sum[k] += (double)v[k];
+    };
+    if ((int)blockIdx.x < heavy) {
+        const int tiles = (per_row + 63) / 64, lanes = per_row < 64 ? per_row : 64, groups = 256 / lanes;
+        const int64_t at = ((int64_t)blockIdx.x / tiles + 1) * kJoinSerial;
+        const uint32_t r = sorted[at * span].key;
+        if (r >= n_rows) return;
+        const int64_t first = row_begin[r] / span, last = ((int64_t)row_end[r] - 1) / span;
+        if (last - first < kJoinSerial || first >= at || first < at - kJoinSerial) return;
+        const int group = threadIdx.x / lanes;
+        const int64_t f = ((int64_t)(blockIdx.x % tiles) * lanes + threadIdx.x % lanes) * V;
+        double sum[V];
+#pragma unroll
+        for (int k = 0; k < V; ++k) sum[k] = 0.0;
+        if (group < groups && f < width) {
+#pragma unroll 4
+            for (int64_t s = first + group; s <= last; s += groups) add(sum, s, first, f);
+        }
+#pragma unroll
+        for (int k = 0; k < V; ++k) red[threadIdx.x][k] = sum[k];
+        __syncthreads();
+        if (group > 0 || f >= width) return;
+        for (int g = 1; g < groups; ++g) {
+#pragma unroll
+            for (int k = 0; k < V; ++k) sum[k] += red[g * lanes + threadIdx.x][k];
+        }
+        out.put<V>(r, f, sum, width - f);
+        return;
+    }
+    const uint32_t step = (gridDim.x - heavy) * 256;
+    for (uint32_t e = (blockIdx.x - heavy) * 256 + threadIdx.x; e < items; e += step) {
         const uint32_t i = div(e);
-        const int64_t r = row0 + i, f = (int64_t)(e - i * per_row) * V, left = width - f;
+        const int64_t r = row0 + i, f = (int64_t)(e - i * per_row) * V;
         const uint32_t end = row_end[r];
         double sum[V];
 #pragma unroll
         for (int k = 0; k < V; ++k) sum[k] = 0.0;
         if (end > 0) {
             const int64_t first = row_begin[r] / span, last = (end - 1) / span;
-            if (first == last) continue;
-            for (int64_t s = first; s <= last; ++s) {
-                float v[V];
-                load_cols<V>(v, edge + (s * 2 + (s == first ? 1 : 0)) * width + f, 1, left);
-#pragma unroll
-                for (int k = 0; k < V; ++k) sum[k] += (double)v[k];
-            }
+            if (first == last || last - first >= kJoinSerial) continue;
+#pragma unroll 4
+            for (int64_t s = first; s <= last; ++s) add(sum, s, first, f);
         }
-        out.put<V>(r, f, sum, left);
+        out.put<V>(r, f, sum, width - f);
     }
 }
 
@@ -450,7 +490,10 @@ struct SortSpace {
     int span;
     SortSpace(int64_t n, int64_t n_rows, int64_t width)
     {
+        // spans as long as 4096 wavefronts still come of them, up to 64 items
+        const int64_t lots = (width + 3) / 4;
         span = 64;
+        while (span > 8 && n / span * lots < 4096 * 64) span /= 2;
         size_t at = 0;
         auto take = [&](size_t size) { const size_t here = at; at += (size + 255) & ~(size_t)255; return here; };
         for (size_t &p : pairs) p = take((size_t)n * sizeof(Pair));
@@ -519,8 +562,8 @@ static int many_rows(const EmbedArgs &a, const GradOut &out)
     }
     constexpr int V = 4;
     const int64_t per_row = (a.width + V - 1) / V;
+    const Pair *sorted = list[(p.passes - 1) & 1];
     if (a.n > 0) {
-        const Pair *sorted = list[(p.passes - 1) & 1];
         const int lanes = (int)(per_row < 64 ? per_row : 64);
         const int64_t spans = (a.n + w.span - 1) / w.span, groups = 256 / lanes;
         const dim3 grid((unsigned)((spans + groups - 1) / groups), (unsigned)((per_row + lanes - 1) / lanes));
@@ -535,8 +578,10 @@ static int many_rows(const EmbedArgs &a, const GradOut &out)
     const Div31 div((uint32_t)per_row);
     for (int64_t r0 = 0; r0 < a.n_rows; r0 += most) {
         const int64_t rows = a.n_rows - r0 < most ? a.n_rows - r0 : most, items = rows * per_row, blocks = (items + 255) / 256;
-        k_row_join<V><<<(unsigned)(blocks < 16384 ? blocks : 16384), 256, 0, a.stream>>>(row_begin, row_end, edge, w.span, (uint32_t)items,
-                                                                                        (uint32_t)per_row, div, r0, a.width, out);
+        // spans kJoinSerial, 2 kJoinSerial, ... that there are, each for every 64 lots of columns; once
+        const int64_t heavy = r0 == 0 && a.n > 0 ? ((a.n + w.span - 1) / w.span - 1) / kJoinSerial * ((per_row + 63) / 64) : 0;
+        k_row_join<V><<<(unsigned)((blocks < 16384 ? blocks : 16384) + heavy), 256, 0, a.stream>>>(
+            sorted, row_begin, row_end, edge, a.n, w.span, (int)heavy, (uint32_t)items, (uint32_t)per_row, div, r0, a.n_rows, a.width, out);
     }
     MLIP_HIP(hipGetLastError());
     return MLIP_OK;
