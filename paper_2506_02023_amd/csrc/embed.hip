@@ -1,4 +1,6 @@
 // Per-species parameter tables: row lookup with scaling, and its gradient.
+#include <type_traits>
+
 #include "elem.h"
 
 namespace mlip {
@@ -130,36 +132,54 @@ struct GradOut {
 // Few rows: every wavefront keeps a table of all rows in LDS, 64 floats to a row, one for each lane: lane l owns column l % tile of the
 // wavefront's rows l / tile, l / tile + slots, ...  A lane adds its values to its own float of the row, so nothing collides and the order of
 // the additions is the order of the atoms.  (Read, add, write: an LDS addition without return takes 220 clocks a wavefront, 361 us where this
-// takes XX at a million rows of 64.)  A block then joins the lanes that own the same
+// took 134 with the same loads, at a million rows of 64.)  A block then joins the lanes that own the same
 // column, and its wavefronts' tables.  Ids without a row go to one row more, which is not read.
-constexpr int kFewLds = 65536, kFewWaves = 16, kFewUnroll = 16;
+constexpr int kFewLds = 65536, kFewWaves = 16;
+constexpr int few_unroll(bool one) { return one ? 16 : 8; }   // rows of a lane in flight, as the registers of 8 wavefronts a SIMD hold
 
-template <class T, class Id>
-__global__ __launch_bounds__(1024) void k_few_rows(const T *grad, int64_t rs, int64_t cs, const Id *ids, int64_t n, int n_rows, int64_t width,
-                                                   int tile, int slots, int64_t rows_per_wave, float *part, GradOut out)
+// One: one row a step (wider than 32 columns), whose id is the same for the wavefront's lanes; Near: the lanes' elements of a step lie within 4 GB.
+template <class T, class Id, bool One, bool Near>
+__global__ __launch_bounds__(1024, 8) void k_few_rows(const T *grad, int64_t rs, int64_t cs, const Id *ids, int64_t n, int n_rows, int64_t width,
+                                                      int tile, int slots, int64_t rows_per_wave, float *part, GradOut out)
 {
     extern __shared__ float tables[];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6, size = (n_rows + 1) * 64;
+    constexpr int U = few_unroll(One);
+    if (One) slots = 1;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6, size = (n_rows + 1) * 64;
     float *mine = tables + wave * size;
     for (int k = lane; k < size; k += 64) mine[k] = 0.f;
     const int64_t f0 = (int64_t)blockIdx.y * tile;
-    const int cols = (int)(width - f0 < tile ? width - f0 : tile), slot = lane / tile, col = lane - slot * tile;
+    const int cols = (int)(width - f0 < tile ? width - f0 : tile), slot = One ? 0 : lane / tile, col = lane - slot * tile;
     const int64_t r0 = ((int64_t)blockIdx.x * waves + wave) * rows_per_wave, r1 = n - r0 < rows_per_wave ? n : r0 + rows_per_wave;
     if (slot < slots && col < cols) {
-        const T *g = grad + (f0 + col) * cs;
-        for (int64_t r = r0 + slot; r < r1; r += (int64_t)slots * kFewUnroll) {
-            int at[kFewUnroll];
-            float v[kFewUnroll];
+        using Offset = std::conditional_t<Near, uint32_t, int64_t>;
+        const Offset mine_at = (Offset)(slot * rs + col * cs);
+        // a step: U rows of the lane, all loaded before the first is added; past the end the last row stands in, and goes nowhere
+        auto step = [&](int64_t r, auto whole) {
+            Id id[U];
+            float v[U];
+            const T *g = grad + r * rs + f0 * cs;
+            const Id *p = ids + r;
+            const int left = (int)(r1 - r);   // rows, of all slots together
+            if (!decltype(whole)::value && slot >= left) return;
 #pragma unroll
-            for (int u = 0; u < kFewUnroll; ++u) {
-                const int64_t i = r + (int64_t)u * slots;
-                const int64_t id = i < r1 ? (int64_t)ids[i] : -1;
-                at[u] = id >= 0 && id < n_rows ? (int)id : n_rows;
-                v[u] = i < r1 ? (float)g[i * rs] : 0.f;
+            for (int u = 0; u < U; ++u) {
+                int k = u * slots;
+                if (!decltype(whole)::value && k + slot >= left) k = 0;
+                id[u] = p[(uint32_t)(k + slot)];
+                v[u] = (float)(g + k * rs)[mine_at];
             }
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int u = 0; u < kFewUnroll; ++u) mine[at[u] * 64 + lane] += v[u];
-        }
+            for (int u = 0; u < U; ++u) {
+                const bool there = decltype(whole)::value || u * slots + slot < left;
+                const int at = id[u] >= 0 && id[u] < n_rows && there ? (int)id[u] : n_rows;
+                mine[at * 64 + lane] += v[u];
+            }
+        };
+        int64_t r = r0;
+        for (; r + slots * U <= r1; r += slots * U) step(r, std::true_type{});
+        if (r < r1) step(r, std::false_type{});
     }
     if (slots > 1) {   // the wavefront's own table: its slots joined into the first
         __syncthreads();
@@ -208,9 +228,9 @@ struct FewPlan {
         slots = 64 / tile;
         waves = (int)(kFewLds / ((n_rows + 1) * 256));
         waves = waves < 1 ? 1 : waves > kFewWaves ? kFewWaves : waves;
-        // wavefronts: as many as have a step of kFewUnroll rows a lane, at most two blocks a compute unit, but no more than
+        // wavefronts: as many as have a step of rows in flight, at most two blocks a compute unit, but no more than
         // MLIP_EMBED_GRAD_RUN rows a lane; where one block does with four steps, one block
-        const int64_t step = (int64_t)slots * kFewUnroll;
+        const int64_t step = (int64_t)slots * few_unroll(slots == 1);
         const int64_t most = 512 / tiles > 1 ? 512 / tiles : 1;
         int64_t b = (n + step * waves - 1) / (step * waves);
         b = b <= 4 ? 1 : b > most ? most : b;
@@ -518,13 +538,18 @@ static int few_rows(const EmbedArgs &a, const GradOut &out)
 {
     const FewPlan p(a.n, a.n_rows, a.width);
     float *part = p.blocks > 1 ? static_cast<float *>(a.workspace) : nullptr;
+    const bool near = ((double)p.slots * (double)a.rs + (double)p.tile * (double)a.cs) * 4.0 < 4e9;
     with_elem(a.in_dtype, [&](auto t) {
         with_ids(a.id_bits, [&](auto id) {
             using T = decltype(t);
             using Id = decltype(id);
-            k_few_rows<T, Id><<<dim3(p.blocks, p.tiles), p.waves * 64, (size_t)p.waves * (a.n_rows + 1) * 256, a.stream>>>(
-                static_cast<const T *>(a.in), a.rs, a.cs, static_cast<const Id *>(a.ids), a.n, (int)a.n_rows, a.width, p.tile, p.slots,
-                p.rows_per_wave, part, out);
+            auto launch = [&](auto kernel) {
+                kernel<<<dim3(p.blocks, p.tiles), p.waves * 64, (size_t)p.waves * (a.n_rows + 1) * 256, a.stream>>>(
+                    static_cast<const T *>(a.in), a.rs, a.cs, static_cast<const Id *>(a.ids), a.n, (int)a.n_rows, a.width, p.tile, p.slots,
+                    p.rows_per_wave, part, out);
+            };
+            if (p.slots == 1) near ? launch(k_few_rows<T, Id, true, true>) : launch(k_few_rows<T, Id, true, false>);
+            else near ? launch(k_few_rows<T, Id, false, true>) : launch(k_few_rows<T, Id, false, false>);
         });
     });
     MLIP_HIP(hipGetLastError());
