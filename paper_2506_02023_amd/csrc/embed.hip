@@ -19,83 +19,106 @@ struct Div31 {
     __device__ uint32_t operator()(uint32_t x) const { return (uint32_t)(((uint64_t)x * m) >> shift); }
 };
 
-// V elements of a row as fp32: one wide access where they lie one after another, at whatever alignment (rows of odd widths begin anywhere)
+// A row is worked on in lots of V columns, one wide access each at whatever alignment (rows of odd widths begin anywhere).  The last lot of a row ends
+// with the row: it begins up to V - 1 columns inside the one before it, whose columns it computes too but does not store.  V = 1 where the
+// columns of the input do not lie one after another or where there are fewer than a wide access has.
 template <class T, int V> using Cols = T __attribute__((ext_vector_type(V)));
 
-template <int V, class T> __device__ inline void load_cols(float (&v)[V], const T *p, int64_t cs, int64_t left)
-{
-    if (V > 1 && cs == 1 && left >= V) {
-        Cols<T, V> x;
-        __builtin_memcpy(&x, p, sizeof(T) * V);
-#pragma unroll
-        for (int k = 0; k < V; ++k) v[k] = (float)x[k];
-    } else {
-#pragma unroll
-        for (int k = 0; k < V; ++k) v[k] = k < left ? (float)p[k * cs] : 0.f;
+template <int V> struct Lot {
+    int64_t f;   // first column
+    int skip;    // columns that the lot before has
+    __device__ Lot(int64_t number, int64_t width)
+    {
+        const int64_t want = number * V, most = width - V;
+        f = want < most ? want : most;
+        skip = (int)(want - f);
     }
+};
+inline int64_t lots_of(int64_t width, int V) { return (width + V - 1) / V; }
+
+template <int V, class T> __device__ inline void load_cols(float (&v)[V], const T *p)
+{
+    Cols<T, V> x;
+    __builtin_memcpy(&x, p, sizeof(T) * V);
+#pragma unroll
+    for (int k = 0; k < V; ++k) v[k] = (float)x[k];
 }
 
-template <int V, class T> __device__ inline void store_cols(T *p, const float (&v)[V], int64_t left)
+template <int V, class T> __device__ inline void store_cols(T *p, const float (&v)[V], int skip)
 {
-    if (V > 1 && left >= V) {
-        Cols<T, V> x;
+    Cols<T, V> x;
 #pragma unroll
-        for (int k = 0; k < V; ++k) x[k] = to_elem<T>(v[k]);
+    for (int k = 0; k < V; ++k) x[k] = to_elem<T>(v[k]);
+    if (skip == 0) {
         __builtin_memcpy(p, &x, sizeof(T) * V);
     } else {
 #pragma unroll
-        for (int k = 0; k < V; ++k)
-            if (k < left) p[k] = to_elem<T>(v[k]);
+        for (int k = 1; k < V; ++k)
+            if (k >= skip) p[k] = x[k];
     }
 }
 
-// ---- lookup: out[i][f] = scale * table[id_i][f], V columns of a row per thread and step
+// ---- lookup: out[i][f] = scale * table[id_i][f].  A thread has a lot of columns of a row and takes U of them at a time, a grid's size apart.
 
 template <class T, class O, class Id, int V>
 __global__ __launch_bounds__(256) void k_embed(const T *table, int64_t n_rows, int64_t width, int64_t rs, int64_t cs, const Id *ids,
                                                uint32_t items, uint32_t per_row, Div31 div, float scale, O *out, int64_t os)
 {
+    constexpr int U = 4;
     const uint32_t step = gridDim.x * 256;
-    for (uint32_t e = blockIdx.x * 256 + threadIdx.x; e < items; e += step) {
-        const uint32_t i = div(e);
-        const int64_t f = (int64_t)(e - i * per_row) * V, id = ids[i];
-        float v[V];
-        if (id >= 0 && id < n_rows) {
-            load_cols<V>(v, table + id * rs + f * cs, cs, width - f);
+    for (uint32_t e0 = blockIdx.x * 256 + threadIdx.x; e0 < items; e0 += step * U) {
+        uint32_t row[U], lot[U];
+        int64_t id[U];
+        float v[U][V];
 #pragma unroll
-            for (int k = 0; k < V; ++k) v[k] *= scale;
-        } else {
-#pragma unroll
-            for (int k = 0; k < V; ++k) v[k] = id < 0 ? 0.f : __builtin_nanf("");
+        for (int u = 0; u < U; ++u) {
+            const uint32_t e = e0 + u * step < items ? e0 + u * step : e0;   // past the end: the first once more, not stored
+            row[u] = div(e);
+            lot[u] = e - row[u] * per_row;
+            id[u] = ids[row[u]];
         }
-        store_cols<V>(out + i * os + f, v, width - f);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const Lot<V> l(lot[u], width);
+            load_cols<V>(v[u], table + (id[u] >= 0 && id[u] < n_rows ? id[u] : 0) * rs + (V == 1 ? l.f * cs : l.f));
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (u > 0 && e0 + u * step >= items) break;
+            const Lot<V> l(lot[u], width);
+#pragma unroll
+            for (int k = 0; k < V; ++k) v[u][k] = id[u] < 0 ? 0.f : id[u] < n_rows ? v[u][k] * scale : __builtin_nanf("");
+            store_cols<V>(out + row[u] * os + l.f, v[u], l.skip);
+        }
     }
 }
 
 int embed_impl(const EmbedArgs &a)
 {
     if (a.n == 0) return MLIP_OK;
-    constexpr int V = 4;
-    const int64_t per_row = (a.width + V - 1) / V;
-    const int64_t most = ((int64_t)1 << 30) / per_row > 0 ? ((int64_t)1 << 30) / per_row : 1;   // rows of a launch: items are numbered in 31 bits
-    const Div31 div((uint32_t)per_row);
-    for (int64_t i0 = 0; i0 < a.n; i0 += most) {
-        const int64_t rows = a.n - i0 < most ? a.n - i0 : most, items = rows * per_row, blocks = (items + 255) / 256;
-        const dim3 grid((unsigned)(blocks < 8192 ? blocks : 8192));
-        with_elem(a.in_dtype, [&](auto t) {
-            with_elem(a.out_dtype, [&](auto o) {
-                with_ids(a.id_bits, [&](auto id) {
-                    using T = decltype(t);
-                    using O = decltype(o);
-                    using Id = decltype(id);
-                    k_embed<T, O, Id, V><<<grid, 256, 0, a.stream>>>(static_cast<const T *>(a.in), a.n_rows, a.width, a.rs, a.cs,
-                                                                     static_cast<const Id *>(a.ids) + i0, (uint32_t)items,
-                                                                     (uint32_t)per_row, div, a.scale, static_cast<O *>(a.out) + i0 * a.os,
-                                                                     a.os);
-                });
+    with_elem(a.in_dtype, [&](auto t) {
+        with_elem(a.out_dtype, [&](auto o) {
+            with_ids(a.id_bits, [&](auto id) {
+                using T = decltype(t);
+                using O = decltype(o);
+                using Id = decltype(id);
+                constexpr int V = sizeof(T) == 2 || sizeof(O) == 2 ? 8 : 4;   // 16 bytes of the smaller type
+                const bool wide = (a.cs == 1 || a.width == 1) && a.width >= V;
+                const int64_t per_row = wide ? lots_of(a.width, V) : a.width;
+                const int64_t most = ((int64_t)1 << 30) / per_row;   // rows of a launch: items are numbered in 31 bits
+                const Div31 div((uint32_t)per_row);
+                for (int64_t i0 = 0; i0 < a.n; i0 += most) {
+                    const int64_t rows = a.n - i0 < most ? a.n - i0 : most, items = rows * per_row, blocks = (items + 255) / 256;
+                    auto launch = [&](auto kernel) {
+                        kernel<<<(unsigned)(blocks < 4096 ? blocks : 4096), 256, 0, a.stream>>>(
+                            static_cast<const T *>(a.in), a.n_rows, a.width, a.rs, a.cs, static_cast<const Id *>(a.ids) + i0, (uint32_t)items,
+                            (uint32_t)per_row, div, a.scale, static_cast<O *>(a.out) + i0 * a.os, a.os);
+                    };
+                    wide ? launch(k_embed<T, O, Id, V>) : launch(k_embed<T, O, Id, 1>);
+                }
             });
         });
-    }
+    });
     MLIP_HIP(hipGetLastError());
     return MLIP_OK;
 }
@@ -109,23 +132,27 @@ struct GradOut {
     int64_t os;
     float scale;
     int accumulate;
-    // writes the finished sums of V columns of a row from column f on, `left` of them in the matrix
-    template <int V> __device__ void put(int64_t r, int64_t f, const double (&sum)[V], int64_t left) const
+    // writes the finished sums of a lot of columns of a row
+    template <int V> __device__ void put(int64_t r, int64_t f, int skip, const double (&sum)[V]) const
     {
-        if (dtype == MLIP_DTYPE_F32) put_as<V>(static_cast<float *>(p), r, f, sum, left);
-        else if (dtype == MLIP_DTYPE_BF16) put_as<V>(static_cast<__bf16 *>(p), r, f, sum, left);
-        else put_as<V>(static_cast<_Float16 *>(p), r, f, sum, left);
+        if (dtype == MLIP_DTYPE_F32) put_as<float>(r, f, skip, sum);
+        else if (dtype == MLIP_DTYPE_BF16) put_as<__bf16>(r, f, skip, sum);
+        else put_as<_Float16>(r, f, skip, sum);
     }
-    template <int V, class O> __device__ void put_as(O *base, int64_t r, int64_t f, const double (&sum)[V], int64_t left) const
+    template <class O, int V> __device__ void put_as(int64_t r, int64_t f, int skip, const double (&sum)[V]) const
     {
-        O *o = base + r * os + f;
+        O *o = static_cast<O *>(p) + r * os + f;
         float v[V];
 #pragma unroll
         for (int k = 0; k < V; ++k) v[k] = 0.f;
-        if (accumulate) load_cols<V>(v, o, 1, left);
+        if (accumulate) {
+#pragma unroll
+            for (int k = 0; k < V; ++k)
+                if (k >= skip) v[k] = (float)o[k];
+        }
 #pragma unroll
         for (int k = 0; k < V; ++k) v[k] = (float)(sum[k] * (double)scale + (double)v[k]);
-        store_cols<V>(o, v, left);
+        store_cols<V>(o, v, skip);
     }
 };
 
@@ -196,7 +223,7 @@ __global__ __launch_bounds__(1024, 8) void k_few_rows(const T *grad, int64_t rs,
         double sum[1] = {0.0};
         for (int w = 0; w < waves; ++w) sum[0] += (double)tables[w * size + s * 64 + c];
         if (part) part[((int64_t)blockIdx.x * n_rows + s) * width + f0 + c] = (float)sum[0];
-        else out.put<1>(s, f0 + c, sum, 1);
+        else out.put<1>(s, f0 + c, 0, sum);
     }
 }
 
@@ -215,7 +242,7 @@ __global__ __launch_bounds__(1024) void k_few_join(const float *part, int parts,
     __syncthreads();
     if (wave || e >= elements) return;
     for (int w = 1; w < 16; ++w) sum[0] += red[w][lane];
-    out.put<1>(e / width, e % width, sum, 1);
+    out.put<1>(e / width, e % width, 0, sum);
 }
 
 struct FewPlan {
@@ -381,48 +408,52 @@ __global__ __launch_bounds__(kSortThreads) void k_digit_scatter(const In *in, in
 
 // Sums over spans of `span` items of the sorted list, a group of `lanes` lanes (V columns each) to a span.  A row that lies within the span is
 // written; what a span holds of a row that began before it goes to edge[span][0], of one that goes on behind it to edge[span][1].
-template <class T, int V>
+template <class T, class O, int V>
 __global__ __launch_bounds__(256) void k_span_sums(const Pair *sorted, const T *grad, int64_t rs, int64_t cs, int64_t n, int64_t n_rows,
                                                    int64_t width, int lanes, int span, uint32_t *row_begin, uint32_t *row_end, float *edge,
                                                    GradOut out)
 {
     constexpr int U = 8;
     const int64_t s = (int64_t)blockIdx.x * (256 / lanes) + threadIdx.x / lanes;
-    const int64_t f = ((int64_t)blockIdx.y * lanes + threadIdx.x % lanes) * V, p0 = s * span;
-    if (threadIdx.x / lanes >= 256 / lanes || p0 >= n || f >= width) return;
-    const int64_t p1 = n - p0 < span ? n : p0 + span, left = width - f;
+    const int64_t number = (int64_t)blockIdx.y * lanes + threadIdx.x % lanes, p0 = s * span;
+    if (threadIdx.x / lanes >= 256 / lanes || p0 >= n || number * V >= width) return;
+    const Lot<V> lot(number, width);
+    const int64_t p1 = n - p0 < span ? n : p0 + span;
     uint32_t key = sorted[p0].key;
     if (key >= n_rows) return;   // ids without a row are the last ones
     bool from_before = p0 > 0 && sorted[p0 - 1].key == key;
+    const T *mine = grad + (V == 1 ? lot.f * cs : lot.f);
     float sum[V];
 #pragma unroll
     for (int k = 0; k < V; ++k) sum[k] = 0.f;
     auto finish = [&](int64_t end, bool goes_on) {   // the row `key` up to `end`, as far as this span has it
         if (from_before || goes_on) {
-            store_cols<V>(edge + (s * 2 + (from_before ? 0 : 1)) * width + f, sum, left);
+            store_cols<V>(edge + (s * 2 + (from_before ? 0 : 1)) * width + lot.f, sum, lot.skip);
         } else {
             double v[V];
 #pragma unroll
             for (int k = 0; k < V; ++k) v[k] = (double)sum[k];
-            out.put<V>(key, f, v, left);
+            out.put_as<O>(key, lot.f, lot.skip, v);
         }
-        if (f == 0 && !goes_on) row_end[key] = (uint32_t)end;
+        if (number == 0 && !goes_on) row_end[key] = (uint32_t)end;
     };
-    if (f == 0 && !from_before) row_begin[key] = (uint32_t)p0;
+    if (number == 0 && !from_before) row_begin[key] = (uint32_t)p0;
+    // places past the span's end are its last one; the items of a step are loaded while the one before is under way
     Pair next[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) next[u] = p0 + u < p1 ? sorted[p0 + u] : Pair{(uint32_t)n_rows, 0};
+    for (int u = 0; u < U; ++u) next[u] = sorted[p0 + u < p1 ? p0 + u : p1 - 1];
     for (int64_t p = p0; p < p1; p += U) {
         Pair item[U];
         float v[U][V];
 #pragma unroll
         for (int u = 0; u < U; ++u) item[u] = next[u];
 #pragma unroll
-        for (int u = 0; u < U; ++u) next[u] = p + U + u < p1 ? sorted[p + U + u] : Pair{(uint32_t)n_rows, 0};
+        for (int u = 0; u < U; ++u) load_cols<V>(v[u], mine + item[u].at * rs);   // of ids without a row too: their atoms are there
+        if (p + U < p1) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (item[u].key < n_rows) load_cols<V>(v[u], grad + item[u].at * rs + f * cs, cs, left);
+            for (int u = 0; u < U; ++u) next[u] = sorted[p + U + u < p1 ? p + U + u : p1 - 1];
         }
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (p + u >= p1) break;
@@ -431,7 +462,7 @@ __global__ __launch_bounds__(256) void k_span_sums(const Pair *sorted, const T *
                 key = item[u].key;
                 if (key >= n_rows) return;
                 from_before = false;
-                if (f == 0) row_begin[key] = (uint32_t)(p + u);
+                if (number == 0) row_begin[key] = (uint32_t)(p + u);
 #pragma unroll
                 for (int k = 0; k < V; ++k) sum[k] = 0.f;
             }
@@ -447,15 +478,15 @@ __global__ __launch_bounds__(256) void k_span_sums(const Pair *sorted, const T *
 // that runs into this span from before is such a row, and no earlier block sees it, shares the row's spans out over its threads.
 constexpr int kJoinSerial = 16;
 
-template <int V>
+template <class O, int V>
 __global__ __launch_bounds__(256) void k_row_join(const Pair *sorted, const uint32_t *row_begin, const uint32_t *row_end, const float *edge,
-                                                  int64_t n, int span, int heavy, uint32_t items, uint32_t per_row, Div31 div, int64_t row0,
+                                                  int span, int heavy, uint32_t items, uint32_t per_row, Div31 div, int64_t row0,
                                                   int64_t n_rows, int64_t width, GradOut out)
 {
     __shared__ double red[256][V];
     auto add = [&](double (&sum)[V], int64_t s, int64_t first, int64_t f) {
         float v[V];
-        load_cols<V>(v, edge + (s * 2 + (s == first ? 1 : 0)) * width + f, 1, width - f);
+        load_cols<V>(v, edge + (s * 2 + (s == first ? 1 : 0)) * width + f);
 #pragma unroll
         for (int k = 0; k < V; ++k) sum[k] += (double)v[k];
     };
@@ -467,29 +498,32 @@ __global__ __launch_bounds__(256) void k_row_join(const Pair *sorted, const uint
         const int64_t first = row_begin[r] / span, last = ((int64_t)row_end[r] - 1) / span;
         if (last - first < kJoinSerial || first >= at || first < at - kJoinSerial) return;
         const int group = threadIdx.x / lanes;
-        const int64_t f = ((int64_t)(blockIdx.x % tiles) * lanes + threadIdx.x % lanes) * V;
+        const int64_t number = (int64_t)(blockIdx.x % tiles) * lanes + threadIdx.x % lanes;
+        const bool mine = group < groups && number < per_row;
+        const Lot<V> lot(number, width);
         double sum[V];
 #pragma unroll
         for (int k = 0; k < V; ++k) sum[k] = 0.0;
-        if (group < groups && f < width) {
-#pragma unroll 4
-            for (int64_t s = first + group; s <= last; s += groups) add(sum, s, first, f);
+        if (mine) {
+#pragma unroll 8
+            for (int64_t s = first + group; s <= last; s += groups) add(sum, s, first, lot.f);
         }
 #pragma unroll
         for (int k = 0; k < V; ++k) red[threadIdx.x][k] = sum[k];
         __syncthreads();
-        if (group > 0 || f >= width) return;
+        if (!mine || group > 0) return;
         for (int g = 1; g < groups; ++g) {
 #pragma unroll
             for (int k = 0; k < V; ++k) sum[k] += red[g * lanes + threadIdx.x][k];
         }
-        out.put<V>(r, f, sum, width - f);
+        out.put_as<O>(r, lot.f, lot.skip, sum);
         return;
     }
     const uint32_t step = (gridDim.x - heavy) * 256;
     for (uint32_t e = (blockIdx.x - heavy) * 256 + threadIdx.x; e < items; e += step) {
         const uint32_t i = div(e);
-        const int64_t r = row0 + i, f = (int64_t)(e - i * per_row) * V;
+        const int64_t r = row0 + i;
+        const Lot<V> lot(e - i * per_row, width);
         const uint32_t end = row_end[r];
         double sum[V];
 #pragma unroll
@@ -498,9 +532,9 @@ __global__ __launch_bounds__(256) void k_row_join(const Pair *sorted, const uint
             const int64_t first = row_begin[r] / span, last = (end - 1) / span;
             if (first == last || last - first >= kJoinSerial) continue;
 #pragma unroll 4
-            for (int64_t s = first; s <= last; ++s) add(sum, s, first, f);
+            for (int64_t s = first; s <= last; ++s) add(sum, s, first, lot.f);
         }
-        out.put<V>(r, f, sum, width - f);
+        out.put_as<O>(r, lot.f, lot.skip, sum);
     }
 }
 
@@ -585,28 +619,42 @@ static int many_rows(const EmbedArgs &a, const GradOut &out)
         }
         MLIP_HIP(hipGetLastError());
     }
-    constexpr int V = 4;
-    const int64_t per_row = (a.width + V - 1) / V;
     const Pair *sorted = list[(p.passes - 1) & 1];
     if (a.n > 0) {
-        const int lanes = (int)(per_row < 64 ? per_row : 64);
-        const int64_t spans = (a.n + w.span - 1) / w.span, groups = 256 / lanes;
-        const dim3 grid((unsigned)((spans + groups - 1) / groups), (unsigned)((per_row + lanes - 1) / lanes));
         with_elem(a.in_dtype, [&](auto t) {
             using T = decltype(t);
-            k_span_sums<T, V><<<grid, 256, 0, a.stream>>>(sorted, static_cast<const T *>(a.in), a.rs, a.cs, a.n, a.n_rows, a.width, lanes, w.span,
-                                                          row_begin, row_end, edge, out);
+            constexpr int V = 16 / sizeof(T);
+            const bool wide = (a.cs == 1 || a.width == 1) && a.width >= V;
+            const int64_t per_row = wide ? lots_of(a.width, V) : a.width;
+            const int lanes = (int)(per_row < 64 ? per_row : 64);
+            const int64_t spans = (a.n + w.span - 1) / w.span, groups = 256 / lanes;
+            const dim3 grid((unsigned)((spans + groups - 1) / groups), (unsigned)((per_row + lanes - 1) / lanes));
+            auto launch = [&](auto kernel) {
+                kernel<<<grid, 256, 0, a.stream>>>(sorted, static_cast<const T *>(a.in), a.rs, a.cs, a.n, a.n_rows, a.width, lanes, w.span,
+                                                   row_begin, row_end, edge, out);
+            };
+            with_elem(a.out_dtype, [&](auto o) {
+                using O = decltype(o);
+                wide ? launch(k_span_sums<T, O, V>) : launch(k_span_sums<T, O, 1>);
+            });
         });
         MLIP_HIP(hipGetLastError());
     }
-    const int64_t most = ((int64_t)1 << 30) / per_row > 0 ? ((int64_t)1 << 30) / per_row : 1;
+    const bool wide = a.width >= 4;
+    const int64_t per_row = wide ? lots_of(a.width, 4) : a.width, most = ((int64_t)1 << 30) / per_row;
     const Div31 div((uint32_t)per_row);
     for (int64_t r0 = 0; r0 < a.n_rows; r0 += most) {
         const int64_t rows = a.n_rows - r0 < most ? a.n_rows - r0 : most, items = rows * per_row, blocks = (items + 255) / 256;
         // spans kJoinSerial, 2 kJoinSerial, ... that there are, each for every 64 lots of columns; once
         const int64_t heavy = r0 == 0 && a.n > 0 ? ((a.n + w.span - 1) / w.span - 1) / kJoinSerial * ((per_row + 63) / 64) : 0;
-        k_row_join<V><<<(unsigned)((blocks < 16384 ? blocks : 16384) + heavy), 256, 0, a.stream>>>(
-            sorted, row_begin, row_end, edge, a.n, w.span, (int)heavy, (uint32_t)items, (uint32_t)per_row, div, r0, a.n_rows, a.width, out);
+        auto launch = [&](auto kernel) {
+            kernel<<<(unsigned)((blocks < 16384 ? blocks : 16384) + heavy), 256, 0, a.stream>>>(
+                sorted, row_begin, row_end, edge, w.span, (int)heavy, (uint32_t)items, (uint32_t)per_row, div, r0, a.n_rows, a.width, out);
+        };
+        with_elem(a.out_dtype, [&](auto o) {
+            using O = decltype(o);
+            wide ? launch(k_row_join<O, 4>) : launch(k_row_join<O, 1>);
+        });
     }
     MLIP_HIP(hipGetLastError());
     return MLIP_OK;
