@@ -149,7 +149,12 @@ def _check(rc):
         raise MlipError(rc, lib().mlip_last_error().decode())
 
 
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)   # the handle without a Stream object around it (0.1 us, not 3)
+
+
 def _stream():
+    if _raw_stream is not None:
+        return ctypes.c_void_p(_raw_stream(torch.cuda.current_device()))
     return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
 
 
@@ -384,40 +389,45 @@ _DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 _ID_BITS = {torch.int32: 32, torch.int64: 64}
 
 
-def _refuse(condition, msg):
-    if condition:
-        raise MlipError(-1, msg)
+def _refuse(msg):
+    raise MlipError(-1, msg)
 
 
 def _on_device(*tensors):
     here = torch.cuda.current_device()
     for t in tensors:
-        _refuse(not t.is_cuda or t.device.index != here, "tensors must be on the current GPU")
+        if t.get_device() != here:
+            _refuse("tensors must be on the current GPU")
 
 
 def _matrix(t, what):
-    """(rows, width, row stride, column stride) of a matrix, or of a vector as a matrix of one column."""
-    _refuse(t.dtype not in _DTYPES, f"{what} must be float32, bfloat16 or float16")
-    if t.dim() == 1:
-        return t.shape[0], 1, t.stride(0), 1
-    _refuse(t.dim() != 2, f"{what} must be a matrix or a vector")
-    return t.shape[0], t.shape[1], t.stride(0), t.stride(1)
+    """(type code, rows, width, row stride, column stride) of a matrix, or of a vector as a matrix of one column."""
+    dtype = _DTYPES.get(t.dtype)
+    if dtype is None:
+        _refuse(f"{what} must be float32, bfloat16 or float16")
+    if t.dim() == 2:
+        return dtype, *t.shape, *t.stride()
+    if t.dim() != 1:
+        _refuse(f"{what} must be a matrix or a vector")
+    return dtype, t.shape[0], 1, t.stride(0), 1
 
 
 def _ids(species):
-    _refuse(species.dtype not in _ID_BITS or species.dim() != 1 or (species.numel() > 1 and species.stride(0) != 1),
-            "species must be a contiguous int32 or int64 vector")
-    return species.data_ptr(), _ID_BITS[species.dtype], species.numel()
+    """(address, bits, number) of a vector of species."""
+    bits = _ID_BITS.get(species.dtype)
+    if bits is None or species.dim() != 1 or not species.is_contiguous():
+        _refuse("species must be a contiguous int32 or int64 vector")
+    return species.data_ptr(), bits, species.shape[0]
 
 
-def _output(out, rows, like):
-    """Row stride of an output matrix of `rows` rows and of the width (and dimensions) of `like`."""
-    shape = (rows,) if like.dim() == 1 else (rows, like.shape[1])
-    _refuse(out.dtype not in _DTYPES or tuple(out.shape) != shape, f"out must be a float32, bfloat16 or float16 tensor of shape {shape}")
-    if out.dim() == 1:
-        return out.stride(0)
-    _refuse(out.stride(1) != 1 and out.shape[1] > 1, "the columns of out must lie one after another")
-    return max(out.stride(0), out.shape[1]) if rows < 2 else out.stride(0)
+def _output(out, rows, width, vector):
+    """(type code, row stride) of an output of `rows` rows."""
+    dtype, have_rows, have_width, rs, cs = _matrix(out, "out")
+    if have_rows != rows or have_width != width or (out.dim() == 1) != vector:
+        _refuse(f"out must have {rows} rows of {width} columns, and the dimensions of the input")
+    if cs != 1 and width > 1:
+        _refuse("the columns of out must lie one after another")
+    return dtype, rs if rows > 1 else max(rs, width)
 
 
 def mlip_embed(table, species, scale=1.0, out=None):
@@ -425,14 +435,13 @@ def mlip_embed(table, species, scale=1.0, out=None):
 
     table: cuda [S, F] or [S], float32, bfloat16 or float16, any strides; species: cuda int32 or int64 [n]; out: [n, F] or [n] of any
     of the three types (default: the table's), its columns one after another."""
-    rows, width, rs, cs = _matrix(table, "table")
+    dtype, rows, width, rs, cs = _matrix(table, "table")
     ids, bits, n = _ids(species)
     if out is None:
         out = table.new_empty((n,) if table.dim() == 1 else (n, width))
-    os = _output(out, n, table)
+    out_dtype, out_rs = _output(out, n, width, table.dim() == 1)
     _on_device(table, species, out)
-    _check(lib().mlip_embed(table.data_ptr(), _DTYPES[table.dtype], rows, width, rs, cs, ids, bits, n, scale, out.data_ptr(),
-                            _DTYPES[out.dtype], os, _stream()))
+    _check(lib().mlip_embed(table.data_ptr(), dtype, rows, width, rs, cs, ids, bits, n, scale, out.data_ptr(), out_dtype, out_rs, _stream()))
     return out
 
 
@@ -441,19 +450,21 @@ def mlip_embed_grad(grad, species, n_species, scale=1.0, out=None, accumulate=Fa
 
     grad: cuda [n, F] or [n], any strides (0 for a broadcast gradient); out: [n_species, F] or [n_species] (default: of grad's
     type); accumulate: add to what out holds."""
-    rows, width, rs, cs = _matrix(grad, "grad")
+    dtype, rows, width, rs, cs = _matrix(grad, "grad")
     ids, bits, n = _ids(species)
-    _refuse(rows != n, "grad must have a row for each atom")
-    _refuse(accumulate and out is None, "accumulate needs out")
+    if rows != n:
+        _refuse("grad must have a row for each atom")
     if out is None:
+        if accumulate:
+            _refuse("accumulate needs out")
         out = grad.new_empty((n_species,) if grad.dim() == 1 else (n_species, width))
-    os = _output(out, n_species, grad)
+    out_dtype, out_rs = _output(out, n_species, width, grad.dim() == 1)
     _on_device(grad, species, out)
     L = lib()
     need = L.mlip_embed_grad_workspace(n, n_species, width)
-    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
-    _check(L.mlip_embed_grad(grad.data_ptr(), _DTYPES[grad.dtype], rs, cs, ids, bits, n, n_species, width, scale, bool(accumulate),
-                             out.data_ptr(), _DTYPES[out.dtype], os, ws.data_ptr(), need, _stream()))
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda") if need else None
+    _check(L.mlip_embed_grad(grad.data_ptr(), dtype, rs, cs, ids, bits, n, n_species, width, scale, bool(accumulate), out.data_ptr(),
+                             out_dtype, out_rs, ws.data_ptr() if need else None, need, _stream()))
     return out
 
 
@@ -470,30 +481,39 @@ def _dense(t):
 
 
 def _tensor_list(grads, out):
+    """The tensors as the library takes them (_Tensor's fields as four columns), checked."""
     count = len(grads)
-    a = (_Tensor * count)()
-    _refuse(out is not None and len(out) != count, "out must have a tensor for each gradient")
-    for k, t in enumerate(grads):
-        _refuse(t.dtype not in _DTYPES, "gradients must be float32, bfloat16 or float16")
-        _refuse(not _dense(t), "gradients must be dense")
-        d = t if out is None else out[k]
-        _refuse(d is not t and (d.dtype != t.dtype or d.shape != t.shape or d.stride() != t.stride()),
-                "out must have the gradients' types, shapes and strides")
-        _on_device(t, d)
-        a[k] = (t.data_ptr(), d.data_ptr(), t.numel(), _DTYPES[t.dtype])
-    return a, count
+    codes = [_DTYPES.get(t.dtype) for t in grads]
+    if None in codes:
+        _refuse("gradients must be float32, bfloat16 or float16")
+    if not all([t.is_contiguous() for t in grads]) and not all([_dense(t) for t in grads]):
+        _refuse("gradients must be dense")
+    if out is not None:
+        if len(out) != count:
+            _refuse("out must have a tensor for each gradient")
+        if not all([d.dtype == t.dtype and d.shape == t.shape and d.stride() == t.stride() for d, t in zip(out, grads)]):
+            _refuse("out must have the gradients' types, shapes and strides")
+        _on_device(*out)
+    _on_device(*grads)
+    a = np.empty((count, 4), np.int64)
+    a[:, 0] = src = [t.data_ptr() for t in grads]
+    a[:, 1] = src if out is None else [d.data_ptr() for d in out]
+    a[:, 2] = [t.numel() for t in grads]
+    a[:, 3] = codes
+    return a, a.ctypes.data, count
 
 
 def _norm_scratch(count):
     need = lib().mlip_grad_workspace(count)
-    return torch.empty((), dtype=torch.float32, device="cuda"), torch.empty(need, dtype=torch.uint8, device="cuda"), need
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    return torch.empty((), dtype=torch.float32, device="cuda"), ws, need
 
 
 def mlip_grad_norm(grads):
     """Norm of all elements of the tensors together (cuda float32 scalar); asynchronous.
 
     grads: dense cuda tensors, float32, bfloat16 or float16, mixed as they come."""
-    a, count = _tensor_list(grads, None)
+    held, a, count = _tensor_list(grads, None)
     norm, ws, need = _norm_scratch(count)
     _check(lib().mlip_grad_norm(a, count, norm.data_ptr(), ws.data_ptr(), need, _stream()))
     return norm
@@ -504,7 +524,7 @@ def mlip_clip_grads(grads, max_norm, out=None):
 
     In place, or into the tensors of `out` (of the same types, shapes and strides).  Where the norm is infinite or NaN the values stay as
     they are: a caller that reads the norm skips the step."""
-    a, count = _tensor_list(grads, out)
+    held, a, count = _tensor_list(grads, out)
     norm, ws, need = _norm_scratch(count)
     _check(lib().mlip_clip_grads(a, count, max_norm, norm.data_ptr(), ws.data_ptr(), need, _stream()))
     return norm

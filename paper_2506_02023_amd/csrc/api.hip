@@ -613,7 +613,7 @@ static int norm_call(const mlip_tensor_t *tensors, int32_t count, bool clip, flo
         }
     }
     MLIP_TRY(check_workspace(workspace, workspace_bytes, grad_workspace(count)));
-    return grad_norm_impl(tensors, count, clip, max_norm, norm, workspace, static_cast<hipStream_t>(stream));
+    return grad_norm_impl(tensors, count, clip, max_norm, norm, workspace, workspace_bytes, static_cast<hipStream_t>(stream));
 }
 
 int mlip_grad_norm(const mlip_tensor_t *tensors, int32_t count, float *norm, void *workspace, size_t workspace_bytes, void *stream)

@@ -1,124 +1,213 @@
 // Global norm of a list of tensors, and clipping by it.
+//
+// Both are bound by memory: the norm reads every element once (two operations each), clipping reads and writes each.  The sums of squares are fp64: the
+// square of an fp32 number would leave the range of fp32, and a conversion and an fp64 product-sum for each element are hidden behind the loads.
 #include <type_traits>
 
 #include "elem.h"
 
 namespace mlip {
 
-// Tensors of one launch, by value in its arguments (4 KB at most): a list of any length takes no upload and can be captured.
-constexpr int kListMax = 128, kBlocksMax = 1024, kTile = 4096;   // tensors of a launch, blocks of a launch, elements of a tile
-struct TensorChunk {
-    const void *src[kListMax];
-    void *dst[kListMax];
-    int64_t n[kListMax];
-    int32_t first[kListMax + 1];   // first tile of every tensor, tiles of all
-    uint8_t dtype[kListMax];
+// The tensors of a launch lie in its arguments (4 KB at most), so a list takes no upload and a captured call keeps it.  A tensor is cut into tiles
+// of 16 KB; a block takes a run of consecutive tiles of the whole list.
+constexpr int kThreads = 256, kTileBytes = 16384, kUnroll = 4;
+constexpr int kListNorm = 200, kListClip = 144;   // tensors of a launch: 20 and 28 bytes each
+constexpr int kBlocksMost = 2048;                 // blocks of a launch, and partial sums that every block of the next launch adds up for itself
+static_assert(kTileBytes == kThreads * kUnroll * 16, "a tile is one step of a block's wide loads");
+
+template <int Most, bool Dst> struct TensorChunk {
+    const void *src[Most];
+    void *dst[Dst ? Most : 1];
+    uint64_t n_type[Most];      // elements, type code in the top byte
+    uint32_t first[Most + 1];   // first tile of every tensor, tiles of all
     int32_t count;
 };
+using NormChunk = TensorChunk<kListNorm, false>;
+using ClipChunk = TensorChunk<kListClip, true>;
+static_assert(sizeof(NormChunk) <= 4060 && sizeof(ClipChunk) <= 4060, "arguments of a launch");
 
-struct NormOut { float norm, coef; };
-
-__device__ inline double block_sum(double v, double *red)
+__device__ inline double block_sum(double v)
 {
+    __shared__ double red[kThreads / 64];
     for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
     __syncthreads();
     v = 0.0;
-    for (unsigned w = 0; w < blockDim.x / 64; ++w) v += red[w];
-    __syncthreads();
+    for (int w = 0; w < kThreads / 64; ++w) v += red[w];
     return v;
 }
 
-// f(T *src, T *dst, elements) for every tile of the block
-template <class Fn> __device__ inline void for_tiles(const TensorChunk &c, Fn &&f)
+// f(src, dst, elements) for the block's run of tiles, tensor by tensor
+template <class Chunk, class Fn> __device__ inline void for_run(const Chunk &c, uint32_t block, Fn &&f)
 {
-    const int tiles = c.first[c.count];
-    for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-        int t = 0;
-        while (c.first[t + 1] <= tile) ++t;
-        const int64_t at = (int64_t)(tile - c.first[t]) * kTile;
-        const int len = (int)(c.n[t] - at < kTile ? c.n[t] - at : kTile);
-        if (c.dtype[t] == MLIP_DTYPE_F32) f(static_cast<const float *>(c.src[t]) + at, static_cast<float *>(c.dst[t]) + at, len);
-        else if (c.dtype[t] == MLIP_DTYPE_BF16) f(static_cast<const __bf16 *>(c.src[t]) + at, static_cast<__bf16 *>(c.dst[t]) + at, len);
-        else f(static_cast<const _Float16 *>(c.src[t]) + at, static_cast<_Float16 *>(c.dst[t]) + at, len);
+    const uint64_t tiles = c.first[c.count];
+    uint32_t tile = (uint32_t)(tiles * block / gridDim.x);
+    const uint32_t end = (uint32_t)(tiles * (block + 1) / gridDim.x);
+    int t = 0;   // the tensor of the first tile: tensors that begin at or before it, less one (64 looked at at a time)
+    for (int k = 0; k < c.count; k += 64) {
+        const int lane = k + (threadIdx.x & 63);
+        t += __popcll(__ballot(lane < c.count && c.first[lane < c.count ? lane : 0] <= tile));
+    }
+    for (t = __builtin_amdgcn_readfirstlane(t) - 1; tile < end; ++t) {
+        const uint32_t t0 = c.first[t], t1 = c.first[t + 1], stop = t1 < end ? t1 : end;
+        const int64_t n = (int64_t)(c.n_type[t] & (((uint64_t)1 << 56) - 1));
+        auto part = [&](auto tag) {
+            using T = decltype(tag);
+            constexpr int64_t per = kTileBytes / sizeof(T);
+            const int64_t lo = (int64_t)(tile - t0) * per, hi = (int64_t)(stop - t0) * per < n ? (int64_t)(stop - t0) * per : n;
+            T *dst = nullptr;
+            if constexpr (std::is_same_v<Chunk, ClipChunk>) dst = static_cast<T *>(c.dst[t]) + lo;
+            f(static_cast<const T *>(c.src[t]) + lo, dst, hi - lo);
+        };
+        const int type = (int)(c.n_type[t] >> 56);
+        if (type == MLIP_DTYPE_F32) part(float{});
+        else if (type == MLIP_DTYPE_BF16) part(__bf16{});
+        else part(_Float16{});
+        tile = stop;
     }
 }
 
-__global__ __launch_bounds__(256) void k_square_sums(TensorChunk c, double *part)
+// f(position, V, values) over n elements: steps of kUnroll wide loads a thread, single wide loads, single elements
+template <class T, class Fn> __device__ inline void for_elements(const T *p, int64_t n, Fn &&f)
 {
-    __shared__ double red[4];
-    double sum = 0.0;
-    for_tiles(c, [&](const auto *src, auto *, int len) {
-        for (int k = threadIdx.x; k < len; k += 256) {
-            const double x = (double)(float)src[k];
-            sum += x * x;
-        }
+    constexpr int V = 16 / sizeof(T);
+    const int64_t wide = n / V;
+    int64_t i = threadIdx.x;
+    for (; i + (kUnroll - 1) * kThreads < wide; i += kUnroll * kThreads) {
+        Cols<T, V> x[kUnroll];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) __builtin_memcpy(&x[u], p + (i + u * kThreads) * V, 16);
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) f((i + u * kThreads) * V, x[u]);
+    }
+    for (; i < wide; i += kThreads) {
+        Cols<T, V> x;
+        __builtin_memcpy(&x, p + i * V, 16);
+        f(i * V, x);
+    }
+    i = wide * V + threadIdx.x;
+    if (i < n) f(i, Cols<T, 1>{p[i]});
+}
+
+template <class Chunk> __device__ inline double run_squares(const Chunk &c, uint32_t block)
+{
+    double sum[2] = {0.0, 0.0};
+    for_run(c, block, [&](const auto *src, auto *, int64_t n) {
+        for_elements(src, n, [&](int64_t, auto x) {
+            constexpr int V = sizeof(x) / sizeof(*src);
+#pragma unroll
+            for (int k = 0; k < V; ++k) sum[k & 1] = fma((double)(float)x[k], (double)(float)x[k], sum[k & 1]);
+        });
     });
-    sum = block_sum(sum, red);
+    return block_sum(sum[0] + sum[1]);
+}
+
+struct Norm { double norm; float coef; };
+
+__device__ inline Norm norm_of(double squares, float max_norm)
+{
+    const double n = sqrt(squares);
+    return {n, n > (double)max_norm && n < (double)__builtin_inff() ? (float)((double)max_norm / n) : 1.f};
+}
+
+__device__ inline double sum_parts(const double *part, int count)
+{
+    double sum = 0.0;
+#pragma unroll 8
+    for (int k = threadIdx.x; k < count; k += kThreads) sum += part[k];
+    return block_sum(sum);
+}
+
+template <class Chunk> __device__ inline void run_clip(const Chunk &c, uint32_t block, float coef)
+{
+    for_run(c, block, [&](const auto *src, auto *dst, int64_t n) {
+        if (coef == 1.f && src == dst) return;
+        for_elements(src, n, [&](int64_t at, auto x) {
+            using T = std::remove_cv_t<std::remove_reference_t<decltype(*dst)>>;
+            constexpr int V = sizeof(x) / sizeof(T);
+            Cols<T, V> y;
+#pragma unroll
+            for (int k = 0; k < V; ++k) y[k] = to_elem<T>((float)x[k] * coef);
+            __builtin_memcpy(dst + at, &y, sizeof(T) * V);
+        });
+    });
+}
+
+template <class Chunk> __global__ __launch_bounds__(kThreads) void k_square_sums(Chunk c, double *part)
+{
+    const double sum = run_squares(c, blockIdx.x);
     if (threadIdx.x == 0) part[blockIdx.x] = sum;
 }
 
-__global__ __launch_bounds__(256) void k_norm_join(const double *part, int count, float max_norm, float *norm, float *coef)
+// the norm alone; or many partial sums made into one for the blocks of k_clip
+__global__ __launch_bounds__(kThreads) void k_norm(const double *part, int count, float *norm, double *joined)
 {
-    __shared__ double red[4];
-    double sum = 0.0;
-    for (int k = threadIdx.x; k < count; k += 256) sum += part[k];
-    sum = block_sum(sum, red);
+    const double sum = sum_parts(part, count);
     if (threadIdx.x) return;
-    const double n = sqrt(sum);
-    *norm = (float)n;
-    *coef = (n > (double)max_norm && n < (double)__builtin_inff()) ? (float)((double)max_norm / n) : 1.f;
+    if (norm) *norm = (float)sqrt(sum);
+    if (joined) *joined = sum;
 }
 
-__global__ __launch_bounds__(256) void k_clip(TensorChunk c, const float *coef)
+// Every block adds the partial sums up for itself, in the same order.  The runs are taken from the list's end: what the sums read last may still
+// be in the caches.
+__global__ __launch_bounds__(kThreads) void k_clip(ClipChunk c, const double *part, int count, float max_norm, float *norm)
 {
-    const float s = *coef;
-    for_tiles(c, [&](const auto *src, auto *dst, int len) {
-        if (s == 1.f && src == dst) return;
-        for (int k = threadIdx.x; k < len; k += 256) dst[k] = to_elem<std::remove_reference_t<decltype(*dst)>>((float)src[k] * s);
-    });
+    const Norm m = norm_of(sum_parts(part, count), max_norm);
+    if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)m.norm;
+    run_clip(c, gridDim.x - 1 - blockIdx.x, m.coef);
 }
 
-size_t grad_workspace(int32_t count) { return 256 + (size_t)(count / kListMax + 1) * kBlocksMax * sizeof(double); }
+constexpr size_t kHead = 256;   // bytes in front of the partial sums: the joined one
 
-// the next tensors of the list as a launch takes them, from tensor `at` on; tensors without elements are left out
-static int fill(TensorChunk &c, const mlip_tensor_t *list, int32_t count, int32_t at)
+size_t grad_workspace(int32_t count) { return kHead + ((size_t)count / kListClip + 1) * kBlocksMost * sizeof(double); }
+
+static int64_t tiles_of(const mlip_tensor_t &x) { const int64_t per = kTileBytes / (int64_t)elem_size(x.dtype); return (x.n + per - 1) / per; }
+
+// Takes the next tensors of the list for a launch, from tensor `at` on (backwards: up to `at`); those without elements are left out.  Returns where the
+// next launch goes on.
+template <class Chunk> static int32_t take(Chunk &c, const mlip_tensor_t *list, int32_t count, int32_t at)
 {
+    constexpr int most = std::is_same_v<Chunk, ClipChunk> ? kListClip : kListNorm;
     c.count = 0;
     int64_t tiles = 0;
-    for (; at < count && c.count < kListMax; ++at) {
-        const int64_t more = (list[at].n + kTile - 1) / kTile;
+    for (; at < count && c.count < most; ++at) {
+        const int64_t more = tiles_of(list[at]);
         if (!more) continue;
-        if (tiles + more > 0x7fffff00) break;
+        if (c.count && tiles + more > 0x7fffffff) break;
         c.src[c.count] = list[at].src;
-        c.dst[c.count] = list[at].dst;
-        c.n[c.count] = list[at].n;
-        c.dtype[c.count] = (uint8_t)list[at].dtype;
-        c.first[c.count++] = (int32_t)tiles;
+        if constexpr (std::is_same_v<Chunk, ClipChunk>) c.dst[c.count] = list[at].dst;
+        c.n_type[c.count] = (uint64_t)list[at].n | ((uint64_t)list[at].dtype << 56);
+        c.first[c.count++] = (uint32_t)tiles;
         tiles += more;
     }
-    c.first[c.count] = (int32_t)tiles;
+    c.first[c.count] = (uint32_t)tiles;
     return at;
 }
 
-static unsigned blocks_of(const TensorChunk &c) { return (unsigned)(c.first[c.count] < kBlocksMax ? c.first[c.count] : kBlocksMax); }
+template <class Chunk> static unsigned blocks_of(const Chunk &c) { return c.first[c.count] < kBlocksMost ? c.first[c.count] : kBlocksMost; }
 
-int grad_norm_impl(const mlip_tensor_t *list, int32_t count, bool clip, float max_norm, float *norm, void *workspace, hipStream_t stream)
+int grad_norm_impl(const mlip_tensor_t *list, int32_t count, bool clip, float max_norm, float *norm, void *workspace, size_t bytes, hipStream_t stream)
 {
-    TensorChunk c;
-    float *coef = static_cast<float *>(workspace);
-    double *part = reinterpret_cast<double *>(static_cast<char *>(workspace) + 256);
-    int parts = 0;
+    double *joined = static_cast<double *>(workspace), *part = reinterpret_cast<double *>(static_cast<char *>(workspace) + kHead);
+    const size_t room = (bytes - kHead) / sizeof(double);
+    size_t parts = 0;
+    NormChunk c;
     for (int32_t at = 0; at < count;) {
-        at = fill(c, list, count, at);
-        if (!c.count) continue;
-        k_square_sums<<<blocks_of(c), 256, 0, stream>>>(c, part + parts);
-        parts += (int)blocks_of(c);
+        at = take(c, list, count, at);
+        if (!c.count) break;
+        if (parts + blocks_of(c) > room) { set_error("tensors too large for the workspace"); return MLIP_EINVAL; }
+        k_square_sums<<<blocks_of(c), kThreads, 0, stream>>>(c, part + parts);
+        parts += blocks_of(c);
     }
-    k_norm_join<<<1, 256, 0, stream>>>(part, parts, max_norm, norm, coef);
-    for (int32_t at = 0; clip && at < count;) {
-        at = fill(c, list, count, at);
-        if (c.count) k_clip<<<blocks_of(c), 256, 0, stream>>>(c, coef);
+    const bool many = parts > kBlocksMost;
+    if (!clip || many || parts == 0) k_norm<<<1, kThreads, 0, stream>>>(part, (int)parts, norm, joined);
+    if (clip && parts > 0) {
+        ClipChunk d;
+        for (int32_t at = 0; at < count;) {
+            at = take(d, list, count, at);
+            if (!d.count) break;
+            k_clip<<<blocks_of(d), kThreads, 0, stream>>>(d, many ? joined : part, many ? 1 : (int)parts, max_norm, many ? nullptr : norm);
+        }
     }
     MLIP_HIP(hipGetLastError());
     return MLIP_OK;

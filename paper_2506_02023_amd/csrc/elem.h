@@ -28,6 +28,9 @@ template <class Fn> inline void with_ids(int32_t id_bits, Fn &&f)
     else f(int64_t{});
 }
 
+// V elements, as one access has them
+template <class T, int V> using Cols = T __attribute__((ext_vector_type(V)));
+
 #ifdef __HIPCC__
 // An fp32 value rounded to an element's type.  The value is made opaque on its way to fp16: the compiler would otherwise take the
 // product that it may be and this rounding as one mixed-precision instruction, which rounds once where two roundings are documented.

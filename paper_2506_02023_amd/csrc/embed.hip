@@ -22,8 +22,6 @@ struct Div31 {
 // A row is worked on in lots of V columns, one wide access each at whatever alignment (rows of odd widths begin anywhere).  The last lot of a row ends
 // with the row: it begins up to V - 1 columns inside the one before it, and computes those columns too.  V = 1 where the
 // columns of the input do not lie one after another or where there are fewer than a wide access has.
-template <class T, int V> using Cols = T __attribute__((ext_vector_type(V)));
-
 template <int V> struct Lot {
     int64_t f;   // first column
     int skip;    // columns that the lot before has

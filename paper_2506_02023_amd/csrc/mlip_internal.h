@@ -298,6 +298,7 @@ int embed_impl(const EmbedArgs &a);
 size_t embed_grad_workspace(int64_t n, int64_t n_rows, int64_t width);
 int embed_grad_impl(const EmbedArgs &a);
 size_t grad_workspace(int32_t count);
-int grad_norm_impl(const mlip_tensor_t *list, int32_t count, bool clip, float max_norm, float *norm, void *workspace, hipStream_t stream);
+int grad_norm_impl(const mlip_tensor_t *list, int32_t count, bool clip, float max_norm, float *norm, void *workspace, size_t bytes,
+                   hipStream_t stream);
 
 }  // namespace mlip
