@@ -5,8 +5,10 @@ The names mirror include/mlip.h.
 """
 from __future__ import annotations
 
+import array
 import ctypes
 import itertools
+import operator
 import os
 
 import numpy as np
@@ -480,27 +482,32 @@ def _dense(t):
     return True
 
 
+_Tensor_of, _dtype_of, _shape_of = torch.Tensor, operator.attrgetter("dtype"), operator.attrgetter("shape")
+
+
 def _tensor_list(grads, out):
-    """The tensors as the library takes them (_Tensor's fields as four columns), checked."""
-    count = len(grads)
-    codes = [_DTYPES.get(t.dtype) for t in grads]
+    """The tensors as the library takes them (an array of _Tensor, as 64-bit words), checked.  Lists run to hundreds of tensors, so
+    each property is taken of all of them in one map."""
+    codes = list(map(_DTYPES.get, map(_dtype_of, grads)))
     if None in codes:
         _refuse("gradients must be float32, bfloat16 or float16")
-    if not all([t.is_contiguous() for t in grads]) and not all([_dense(t) for t in grads]):
+    plain = all(map(_Tensor_of.is_contiguous, grads))
+    if not plain and not all(map(_dense, grads)):
         _refuse("gradients must be dense")
+    dst = src = list(map(_Tensor_of.data_ptr, grads))
     if out is not None:
-        if len(out) != count:
-            _refuse("out must have a tensor for each gradient")
-        if not all([d.dtype == t.dtype and d.shape == t.shape and d.stride() == t.stride() for d, t in zip(out, grads)]):
-            _refuse("out must have the gradients' types, shapes and strides")
-        _on_device(*out)
-    _on_device(*grads)
-    a = np.empty((count, 4), np.int64)
-    a[:, 0] = src = [t.data_ptr() for t in grads]
-    a[:, 1] = src if out is None else [d.data_ptr() for d in out]
-    a[:, 2] = [t.numel() for t in grads]
-    a[:, 3] = codes
-    return a, a.ctypes.data, count
+        same = len(out) == len(grads) and list(map(_dtype_of, out)) == list(map(_dtype_of, grads)) and \
+            all(map(operator.eq, map(_shape_of, out), map(_shape_of, grads))) and \
+            (plain and all(map(_Tensor_of.is_contiguous, out)) or all(d.stride() == t.stride() for d, t in zip(out, grads)))
+        if not same:
+            _refuse("out must have a tensor for each gradient, of its type, shape and strides")
+        dst = list(map(_Tensor_of.data_ptr, out))
+    if not {torch.cuda.current_device()}.issuperset(map(_Tensor_of.get_device, itertools.chain(grads, out or ()))):
+        _refuse("tensors must be on the current GPU")
+    words = [0] * (4 * len(src))
+    words[::4], words[1::4], words[2::4], words[3::4] = src, dst, map(_Tensor_of.numel, grads), codes
+    a = array.array("q", words)
+    return a, a.buffer_info()[0], len(src)
 
 
 def _norm_scratch(count):

@@ -12,7 +12,7 @@ namespace mlip {
 // of 16 KB; a block takes a run of consecutive tiles of the whole list.
 constexpr int kThreads = 256, kTileBytes = 16384, kUnroll = 4;
 constexpr int kListNorm = 200, kListClip = 144;   // tensors of a launch: 20 and 28 bytes each
-constexpr int kBlocksMost = 2048;                 // blocks of a launch, and partial sums that every block of the next launch adds up for itself
+constexpr int kBlocksMost = 4096;                 // blocks of a launch, and partial sums that every block of the next launch adds up for itself
 static_assert(kTileBytes == kThreads * kUnroll * 16, "a tile is one step of a block's wide loads");
 
 template <int Most, bool Dst> struct TensorChunk {
@@ -148,13 +148,21 @@ __global__ __launch_bounds__(kThreads) void k_norm(const double *part, int count
     if (joined) *joined = sum;
 }
 
-// Every block adds the partial sums up for itself, in the same order.  The runs are taken from the list's end: what the sums read last may still
-// be in the caches.
+// Every block adds the partial sums up for itself, in the same order: a launch less.
 __global__ __launch_bounds__(kThreads) void k_clip(ClipChunk c, const double *part, int count, float max_norm, float *norm)
 {
     const Norm m = norm_of(sum_parts(part, count), max_norm);
     if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)m.norm;
-    run_clip(c, gridDim.x - 1 - blockIdx.x, m.coef);
+    run_clip(c, blockIdx.x, m.coef);
+}
+
+// A list of few tiles: norm and clipping in one block
+constexpr uint32_t kFewTiles = 4;
+__global__ __launch_bounds__(kThreads) void k_few_tiles(ClipChunk c, bool clip, float max_norm, float *norm)
+{
+    const Norm m = norm_of(run_squares(c, 0), max_norm);
+    if (threadIdx.x == 0) *norm = (float)m.norm;
+    if (clip) run_clip(c, 0, m.coef);
 }
 
 constexpr size_t kHead = 256;   // bytes in front of the partial sums: the joined one
@@ -191,6 +199,12 @@ int grad_norm_impl(const mlip_tensor_t *list, int32_t count, bool clip, float ma
     double *joined = static_cast<double *>(workspace), *part = reinterpret_cast<double *>(static_cast<char *>(workspace) + kHead);
     const size_t room = (bytes - kHead) / sizeof(double);
     size_t parts = 0;
+    ClipChunk few;
+    if (take(few, list, count, 0) == count && few.first[few.count] <= kFewTiles) {
+        k_few_tiles<<<1, kThreads, 0, stream>>>(few, clip, max_norm, norm);
+        MLIP_HIP(hipGetLastError());
+        return MLIP_OK;
+    }
     NormChunk c;
     for (int32_t at = 0; at < count;) {
         at = take(c, list, count, at);
