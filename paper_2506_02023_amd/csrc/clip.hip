@@ -9,11 +9,11 @@
 namespace mlip {
 
 // The tensors of a launch lie in its arguments (4 KB at most), so a list takes no upload and a captured call keeps it.  A tensor is cut into tiles
-// of 16 KB; a block takes a run of consecutive tiles of the whole list.
-constexpr int kThreads = 256, kTileBytes = 16384, kUnroll = 4;
+// of 32 KB, one step of a block's wide loads; block b has tiles b, b + blocks, ...  Clipping 1 GB of fp32: 547 us; with runs of consecutive
+// tiles for a block 571 (both with steps of 128 bytes a thread; of 64 bytes 574 and 578), with half the blocks 564, with a quarter 582.
+constexpr int kThreads = 256, kUnroll = 8, kTileBytes = kThreads * kUnroll * 16;
 constexpr int kListNorm = 200, kListClip = 144;   // tensors of a launch: 20 and 28 bytes each
-constexpr int kBlocksMost = 4096;                 // blocks of a launch, and partial sums that every block of the next launch adds up for itself
-static_assert(kTileBytes == kThreads * kUnroll * 16, "a tile is one step of a block's wide loads");
+constexpr int kBlocksMost = 8192;                 // blocks of a launch, and partial sums that every block of the next launch adds up for itself
 
 template <int Most, bool Dst> struct TensorChunk {
     const void *src[Most];
@@ -37,63 +37,66 @@ __device__ inline double block_sum(double v)
     return v;
 }
 
-// f(src, dst, elements) for the block's run of tiles, tensor by tensor
-template <class Chunk, class Fn> __device__ inline void for_run(const Chunk &c, uint32_t block, Fn &&f)
+// f(src, dst, elements) for each tile of the block
+template <class Chunk, class Fn> __device__ inline void for_tiles(const Chunk &c, Fn &&f)
 {
-    const uint64_t tiles = c.first[c.count];
-    uint32_t tile = (uint32_t)(tiles * block / gridDim.x);
-    const uint32_t end = (uint32_t)(tiles * (block + 1) / gridDim.x);
-    int t = 0;   // the tensor of the first tile: tensors that begin at or before it, less one (64 looked at at a time)
-    for (int k = 0; k < c.count; k += 64) {
-        const int lane = k + (threadIdx.x & 63);
-        t += __popcll(__ballot(lane < c.count && c.first[lane < c.count ? lane : 0] <= tile));
+    constexpr int kWords = ((std::is_same_v<Chunk, ClipChunk> ? kListClip : kListNorm) + 63) / 64;
+    const uint32_t tiles = c.first[c.count];
+    uint32_t first[kWords];   // the tensors' first tiles, a few to a lane: a tile's tensor is the last that begins at or before it
+#pragma unroll
+    for (int k = 0; k < kWords; ++k) {
+        const int t = k * 64 + (threadIdx.x & 63);
+        first[k] = t < c.count ? c.first[t] : 0xffffffffu;
     }
-    for (t = __builtin_amdgcn_readfirstlane(t) - 1; tile < end; ++t) {
-        const uint32_t t0 = c.first[t], t1 = c.first[t + 1], stop = t1 < end ? t1 : end;
+    for (uint32_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+        int t = -1;
+#pragma unroll
+        for (int k = 0; k < kWords; ++k) t += __popcll(__ballot(first[k] <= tile));
+        t = __builtin_amdgcn_readfirstlane(t);
         const int64_t n = (int64_t)(c.n_type[t] & (((uint64_t)1 << 56) - 1));
         auto part = [&](auto tag) {
             using T = decltype(tag);
             constexpr int64_t per = kTileBytes / sizeof(T);
-            const int64_t lo = (int64_t)(tile - t0) * per, hi = (int64_t)(stop - t0) * per < n ? (int64_t)(stop - t0) * per : n;
+            const int64_t lo = (int64_t)(tile - c.first[t]) * per, hi = lo + per < n ? lo + per : n;
             T *dst = nullptr;
             if constexpr (std::is_same_v<Chunk, ClipChunk>) dst = static_cast<T *>(c.dst[t]) + lo;
-            f(static_cast<const T *>(c.src[t]) + lo, dst, hi - lo);
+            f(static_cast<const T *>(c.src[t]) + lo, dst, (int)(hi - lo));
         };
         const int type = (int)(c.n_type[t] >> 56);
         if (type == MLIP_DTYPE_F32) part(float{});
         else if (type == MLIP_DTYPE_BF16) part(__bf16{});
         else part(_Float16{});
-        tile = stop;
     }
 }
 
-// f(position, V, values) over n elements: steps of kUnroll wide loads a thread, single wide loads, single elements
-template <class T, class Fn> __device__ inline void for_elements(const T *p, int64_t n, Fn &&f)
+// f(position, values) over the n elements of a tile: a whole one in one step of kUnroll wide loads a thread, else by single wide loads, then single elements
+template <class T, class Fn> __device__ inline void for_elements(const T *p, int n, Fn &&f)
 {
     constexpr int V = 16 / sizeof(T);
-    const int64_t wide = n / V;
-    int64_t i = threadIdx.x;
-    for (; i + (kUnroll - 1) * kThreads < wide; i += kUnroll * kThreads) {
+    if (n == kTileBytes / (int)sizeof(T)) {
         Cols<T, V> x[kUnroll];
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) __builtin_memcpy(&x[u], p + (i + u * kThreads) * V, 16);
+        for (int u = 0; u < kUnroll; ++u) __builtin_memcpy(&x[u], p + (threadIdx.x + u * kThreads) * V, 16);
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) f((i + u * kThreads) * V, x[u]);
+        for (int u = 0; u < kUnroll; ++u) f((threadIdx.x + u * kThreads) * V, x[u]);
+        return;
     }
-    for (; i < wide; i += kThreads) {
+    const int wide = n / V;
+#pragma unroll 4
+    for (int i = threadIdx.x; i < wide; i += kThreads) {
         Cols<T, V> x;
         __builtin_memcpy(&x, p + i * V, 16);
         f(i * V, x);
     }
-    i = wide * V + threadIdx.x;
+    const int i = wide * V + threadIdx.x;
     if (i < n) f(i, Cols<T, 1>{p[i]});
 }
 
-template <class Chunk> __device__ inline double run_squares(const Chunk &c, uint32_t block)
+template <class Chunk> __device__ inline double squares(const Chunk &c)
 {
     double sum[2] = {0.0, 0.0};
-    for_run(c, block, [&](const auto *src, auto *, int64_t n) {
-        for_elements(src, n, [&](int64_t, auto x) {
+    for_tiles(c, [&](const auto *src, auto *, int n) {
+        for_elements(src, n, [&](int, auto x) {
             constexpr int V = sizeof(x) / sizeof(*src);
 #pragma unroll
             for (int k = 0; k < V; ++k) sum[k & 1] = fma((double)(float)x[k], (double)(float)x[k], sum[k & 1]);
@@ -118,11 +121,11 @@ __device__ inline double sum_parts(const double *part, int count)
     return block_sum(sum);
 }
 
-template <class Chunk> __device__ inline void run_clip(const Chunk &c, uint32_t block, float coef)
+template <class Chunk> __device__ inline void clip_tiles(const Chunk &c, float coef)
 {
-    for_run(c, block, [&](const auto *src, auto *dst, int64_t n) {
+    for_tiles(c, [&](const auto *src, auto *dst, int n) {
         if (coef == 1.f && src == dst) return;
-        for_elements(src, n, [&](int64_t at, auto x) {
+        for_elements(src, n, [&](int at, auto x) {
             using T = std::remove_cv_t<std::remove_reference_t<decltype(*dst)>>;
             constexpr int V = sizeof(x) / sizeof(T);
             Cols<T, V> y;
@@ -135,7 +138,7 @@ template <class Chunk> __device__ inline void run_clip(const Chunk &c, uint32_t 
 
 template <class Chunk> __global__ __launch_bounds__(kThreads) void k_square_sums(Chunk c, double *part)
 {
-    const double sum = run_squares(c, blockIdx.x);
+    const double sum = squares(c);
     if (threadIdx.x == 0) part[blockIdx.x] = sum;
 }
 
@@ -153,16 +156,16 @@ __global__ __launch_bounds__(kThreads) void k_clip(ClipChunk c, const double *pa
 {
     const Norm m = norm_of(sum_parts(part, count), max_norm);
     if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)m.norm;
-    run_clip(c, blockIdx.x, m.coef);
+    clip_tiles(c, m.coef);
 }
 
 // A list of few tiles: norm and clipping in one block
 constexpr uint32_t kFewTiles = 4;
 __global__ __launch_bounds__(kThreads) void k_few_tiles(ClipChunk c, bool clip, float max_norm, float *norm)
 {
-    const Norm m = norm_of(run_squares(c, 0), max_norm);
+    const Norm m = norm_of(squares(c), max_norm);
     if (threadIdx.x == 0) *norm = (float)m.norm;
-    if (clip) run_clip(c, 0, m.coef);
+    if (clip) clip_tiles(c, m.coef);
 }
 
 constexpr size_t kHead = 256;   // bytes in front of the partial sums: the joined one
@@ -213,7 +216,7 @@ int grad_norm_impl(const mlip_tensor_t *list, int32_t count, bool clip, float ma
         k_square_sums<<<blocks_of(c), kThreads, 0, stream>>>(c, part + parts);
         parts += blocks_of(c);
     }
-    const bool many = parts > kBlocksMost;
+        const bool many = parts > (size_t)kBlocksMost;
     if (!clip || many || parts == 0) k_norm<<<1, kThreads, 0, stream>>>(part, (int)parts, norm, joined);
     if (clip && parts > 0) {
         ClipChunk d;
