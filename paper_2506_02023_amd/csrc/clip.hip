@@ -70,13 +70,16 @@ template <class Chunk, class Fn> __device__ inline void for_tiles(const Chunk &c
 }
 
 // f(position, values) over the n elements of a tile: a whole one in one step of kUnroll wide loads a thread, else by single wide loads, then single elements
-template <class T, class Fn> __device__ inline void for_elements(const T *p, int n, Fn &&f)
+template <bool Stream, class T, class Fn> __device__ inline void for_elements(const T *p, int n, Fn &&f)
 {
     constexpr int V = 16 / sizeof(T);
     if (n == kTileBytes / (int)sizeof(T)) {
         Cols<T, V> x[kUnroll];
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) __builtin_memcpy(&x[u], p + (threadIdx.x + u * kThreads) * V, 16);
+        for (int u = 0; u < kUnroll; ++u) {
+            const Far<T, V> *at = reinterpret_cast<const Far<T, V> *>(p + (threadIdx.x + u * kThreads) * V);
+            x[u] = Stream ? __builtin_nontemporal_load(at) : *at;
+        }
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) f((threadIdx.x + u * kThreads) * V, x[u]);
         return;
@@ -85,18 +88,18 @@ template <class T, class Fn> __device__ inline void for_elements(const T *p, int
 #pragma unroll 4
     for (int i = threadIdx.x; i < wide; i += kThreads) {
         Cols<T, V> x;
-        __builtin_memcpy(&x, p + i * V, 16);
+        x = *reinterpret_cast<const Far<T, V> *>(p + i * V);
         f(i * V, x);
     }
     const int i = wide * V + threadIdx.x;
     if (i < n) f(i, Cols<T, 1>{p[i]});
 }
 
-template <class Chunk> __device__ inline double squares(const Chunk &c)
+template <bool Stream, class Chunk> __device__ inline double squares(const Chunk &c)
 {
     double sum[2] = {0.0, 0.0};
     for_tiles(c, [&](const auto *src, auto *, int n) {
-        for_elements(src, n, [&](int, auto x) {
+        for_elements<Stream>(src, n, [&](int, auto x) {
             constexpr int V = sizeof(x) / sizeof(*src);
 #pragma unroll
             for (int k = 0; k < V; ++k) sum[k & 1] = fma((double)(float)x[k], (double)(float)x[k], sum[k & 1]);
@@ -121,24 +124,26 @@ __device__ inline double sum_parts(const double *part, int count)
     return block_sum(sum);
 }
 
-template <class Chunk> __device__ inline void clip_tiles(const Chunk &c, float coef)
+template <bool Stream, class Chunk> __device__ inline void clip_tiles(const Chunk &c, float coef)
 {
     for_tiles(c, [&](const auto *src, auto *dst, int n) {
         if (coef == 1.f && src == dst) return;
-        for_elements(src, n, [&](int at, auto x) {
+        for_elements<Stream>(src, n, [&](int at, auto x) {
             using T = std::remove_cv_t<std::remove_reference_t<decltype(*dst)>>;
             constexpr int V = sizeof(x) / sizeof(T);
             Cols<T, V> y;
 #pragma unroll
             for (int k = 0; k < V; ++k) y[k] = to_elem<T>((float)x[k] * coef);
-            __builtin_memcpy(dst + at, &y, sizeof(T) * V);
+            Far<T, V> *to = reinterpret_cast<Far<T, V> *>(dst + at);
+            if (Stream) __builtin_nontemporal_store((Far<T, V>)y, to);
+            else *to = (Far<T, V>)y;
         });
     });
 }
 
-template <class Chunk> __global__ __launch_bounds__(kThreads) void k_square_sums(Chunk c, double *part)
+template <bool Stream> __global__ __launch_bounds__(kThreads) void k_square_sums(NormChunk c, double *part)
 {
-    const double sum = squares(c);
+    const double sum = squares<Stream>(c);
     if (threadIdx.x == 0) part[blockIdx.x] = sum;
 }
 
@@ -152,20 +157,20 @@ __global__ __launch_bounds__(kThreads) void k_norm(const double *part, int count
 }
 
 // Every block adds the partial sums up for itself, in the same order: a launch less.
-__global__ __launch_bounds__(kThreads) void k_clip(ClipChunk c, const double *part, int count, float max_norm, float *norm)
+template <bool Stream> __global__ __launch_bounds__(kThreads) void k_clip(ClipChunk c, const double *part, int count, float max_norm, float *norm)
 {
     const Norm m = norm_of(sum_parts(part, count), max_norm);
     if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)m.norm;
-    clip_tiles(c, m.coef);
+    clip_tiles<Stream>(c, m.coef);
 }
 
 // A list of few tiles: norm and clipping in one block
 constexpr uint32_t kFewTiles = 4;
 __global__ __launch_bounds__(kThreads) void k_few_tiles(ClipChunk c, bool clip, float max_norm, float *norm)
 {
-    const Norm m = norm_of(squares(c), max_norm);
+    const Norm m = norm_of(squares<false>(c), max_norm);
     if (threadIdx.x == 0) *norm = (float)m.norm;
-    if (clip) clip_tiles(c, m.coef);
+    if (clip) clip_tiles<false>(c, m.coef);
 }
 
 constexpr size_t kHead = 256;   // bytes in front of the partial sums: the joined one
@@ -208,12 +213,15 @@ int grad_norm_impl(const mlip_tensor_t *list, int32_t count, bool clip, float ma
         MLIP_HIP(hipGetLastError());
         return MLIP_OK;
     }
+    double total = 0.0;
+    for (int32_t t = 0; t < count; ++t) total += (double)list[t].n * (double)elem_size(list[t].dtype);
+    const bool far = total > kStreamBytes;
     NormChunk c;
     for (int32_t at = 0; at < count;) {
         at = take(c, list, count, at);
         if (!c.count) break;
         if (parts + blocks_of(c) > room) { set_error("tensors too large for the workspace"); return MLIP_EINVAL; }
-        k_square_sums<<<blocks_of(c), kThreads, 0, stream>>>(c, part + parts);
+        (far ? k_square_sums<true> : k_square_sums<false>)<<<blocks_of(c), kThreads, 0, stream>>>(c, part + parts);
         parts += blocks_of(c);
     }
         const bool many = parts > (size_t)kBlocksMost;
@@ -223,7 +231,7 @@ int grad_norm_impl(const mlip_tensor_t *list, int32_t count, bool clip, float ma
         for (int32_t at = 0; at < count;) {
             at = take(d, list, count, at);
             if (!d.count) break;
-            k_clip<<<blocks_of(d), kThreads, 0, stream>>>(d, many ? joined : part, many ? 1 : (int)parts, max_norm, many ? nullptr : norm);
+            (far ? k_clip<true> : k_clip<false>)<<<blocks_of(d), kThreads, 0, stream>>>(d, many ? joined : part, many ? 1 : (int)parts, max_norm, many ? nullptr : norm);
         }
     }
     MLIP_HIP(hipGetLastError());

@@ -28,8 +28,15 @@ template <class Fn> inline void with_ids(int32_t id_bits, Fn &&f)
     else f(int64_t{});
 }
 
+// What is larger than this is read or written past the caches where it is touched once: they could not keep it for anyone.  Measured, us past
+// the caches and through them: clipping 32 MB 21.7 and 18.8, 96 MB 52 and 56, 256 MB 128 and 148; lookup of 64 MB 11.9 and 12.5, 256 MB 44 and 46;
+// gradient into few rows of 32 MB 16.4 and 15.5, 96 MB 22.8 and 23.4, 256 MB 51 and 55, into many of 64 MB 53 and 50.5, 128 MB 69 and 71.
+constexpr double kStreamBytes = 100e6;
+
 // V elements, as one access has them
 template <class T, int V> using Cols = T __attribute__((ext_vector_type(V)));
+template <class T, int V> struct FarT { typedef T type __attribute__((ext_vector_type(V), aligned(sizeof(T)))); };
+template <class T, int V> using Far = typename FarT<T, V>::type;   // the same at the alignment of an element
 
 #ifdef __HIPCC__
 // An fp32 value rounded to an element's type.  The value is made opaque on its way to fp16: the compiler would otherwise take the

@@ -34,10 +34,11 @@ template <int V> struct Lot {
 };
 inline int64_t lots_of(int64_t width, int V) { return (width + V - 1) / V; }
 
-template <int V, class T> __device__ inline void load_cols(float (&v)[V], const T *p)
+// Stream: past the caches, for what is read once and is larger than they are
+template <int V, bool Stream = false, class T> __device__ inline void load_cols(float (&v)[V], const T *p)
 {
-    Cols<T, V> x;
-    __builtin_memcpy(&x, p, sizeof(T) * V);
+    const Far<T, V> *at = reinterpret_cast<const Far<T, V> *>(p);
+    const Cols<T, V> x = Stream ? __builtin_nontemporal_load(at) : *at;
 #pragma unroll
     for (int k = 0; k < V; ++k) v[k] = (float)x[k];
 }
@@ -53,23 +54,19 @@ template <class T, int V> __device__ inline Cols<T, V> to_cols(const float (&v)[
 // Stores a whole lot: where lots overlap, both write the same bits.
 template <int V, class T> __device__ inline void store_cols(T *p, const float (&v)[V])
 {
-    const Cols<T, V> x = to_cols<T>(v);
-    __builtin_memcpy(p, &x, sizeof(T) * V);
+    *reinterpret_cast<Far<T, V> *>(p) = to_cols<T>(v);
 }
 
 // The same past the caches, for what is larger than they are.
 template <int V, class T> __device__ inline void stream_cols(T *p, const float (&v)[V])
 {
-    typedef T Far __attribute__((ext_vector_type(V), aligned(sizeof(T))));
-    __builtin_nontemporal_store((Far)to_cols<T>(v), reinterpret_cast<Far *>(p));
+    __builtin_nontemporal_store((Far<T, V>)to_cols<T>(v), reinterpret_cast<Far<T, V> *>(p));
 }
 
 // ---- lookup: out[i][f] = scale * table[id_i][f].  A thread has a lot of columns of a row, and kEmbedUnroll of them at a time, a grid's size
-// apart.  Writing bounds it; results larger than kEmbedStream are stored past the caches, which could not keep them for the next reader (a million rows
-// of 64: 47 us, 59 through the caches; 31 MB: 14.1 us, 13.7 through the caches).
+// apart.  Writing bounds it: a million rows of 64 fp32 take 43 us, 6.0 TB/s.
 
 constexpr int kEmbedUnroll = 4;
-constexpr double kEmbedStream = 128e6;
 
 template <class T, class O, class Id, int V, bool Stream>
 __global__ __launch_bounds__(256) void k_embed(const T *table, int64_t n_rows, int64_t width, int64_t rs, int64_t cs, const Id *ids,
@@ -116,7 +113,7 @@ int embed_impl(const EmbedArgs &a)
                 using Id = decltype(id);
                 constexpr int V = sizeof(T) == 2 || sizeof(O) == 2 ? 8 : 4;   // 16 bytes of the smaller type
                 const bool wide = (a.cs == 1 || a.width == 1) && a.width >= V;
-                const bool stream = (double)a.n * (double)a.width * sizeof(O) > kEmbedStream;
+                const bool stream = (double)a.n * (double)a.width * sizeof(O) > kStreamBytes;
                 const int64_t per_row = wide ? lots_of(a.width, V) : a.width;
                 const int64_t most = ((int64_t)1 << 30) / per_row;   // rows of a launch: items are numbered in 31 bits
                 const Div31 div((uint32_t)per_row);
@@ -179,20 +176,21 @@ constexpr int kFewLds = 65536, kFewWaves = 16;
 constexpr int few_unroll(bool one) { return one ? 16 : 8; }   // rows of a lane in flight, as the registers of 8 wavefronts a SIMD hold
 
 // One: one row a step (wider than 32 columns), whose id is the same for the wavefront's lanes; Near: the lanes' elements of a step lie within 4 GB.
-template <class T, class Id, bool One, bool Near>
+template <class T, class Id, bool One, bool Near, bool Stream>
 __global__ __launch_bounds__(1024, 8) void k_few_rows(const T *grad, int64_t rs, int64_t cs, const Id *ids, int64_t n, int n_rows, int64_t width,
-                                                      int tile, int slots, int64_t rows_per_wave, float *part, GradOut out)
+                                                      int tile, int slots, int waves, int64_t rows_per_wave, float *part, GradOut out)
 {
     extern __shared__ float tables[];
     constexpr int U = few_unroll(One);
     if (One) slots = 1;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6, size = (n_rows + 1) * 64;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), size = (n_rows + 1) * 64;
     float *mine = tables + wave * size;
-    for (int k = lane; k < size; k += 64) mine[k] = 0.f;
+    for (int k = threadIdx.x; k < waves * size; k += blockDim.x) tables[k] = 0.f;
+    __syncthreads();
     const int64_t f0 = (int64_t)blockIdx.y * tile;
     const int cols = (int)(width - f0 < tile ? width - f0 : tile), slot = One ? 0 : lane / tile, col = lane - slot * tile;
     const int64_t r0 = ((int64_t)blockIdx.x * waves + wave) * rows_per_wave, r1 = n - r0 < rows_per_wave ? n : r0 + rows_per_wave;
-    if (slot < slots && col < cols) {
+    if (wave < waves && slot < slots && col < cols) {
         using Offset = std::conditional_t<Near, uint32_t, int64_t>;
         const Offset mine_at = (Offset)(slot * rs + col * cs);
         // a step: U rows of the lane, all loaded before the first is added; past the end the last row stands in, and goes nowhere
@@ -208,7 +206,7 @@ __global__ __launch_bounds__(1024, 8) void k_few_rows(const T *grad, int64_t rs,
                 int k = u * slots;
                 if (!decltype(whole)::value && k + slot >= left) k = 0;
                 id[u] = p[(uint32_t)(k + slot)];
-                v[u] = (float)(g + k * rs)[mine_at];
+                v[u] = (float)(Stream ? __builtin_nontemporal_load(g + k * rs + mine_at) : (g + k * rs)[mine_at]);
             }
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -222,45 +220,51 @@ __global__ __launch_bounds__(1024, 8) void k_few_rows(const T *grad, int64_t rs,
         for (; r + slots * U <= r1; r += slots * U) step(r, std::true_type{});
         if (r < r1) step(r, std::false_type{});
     }
-    if (slots > 1) {   // the wavefront's own table: its slots joined into the first
-        __syncthreads();
-        const int step = 64 / cols, c = lane % cols;
-        for (int s = lane / cols; s < n_rows && lane < step * cols; s += step) {
-            double sum = 0.0;
-            for (int k = 0; k < slots; ++k) sum += (double)mine[s * 64 + k * tile + c];
-            mine[s * 64 + c] = (float)sum;
-        }
-    }
     __syncthreads();
+    if (!One) {   // each table's slots into its first
+        for (int e = threadIdx.x; e < waves * n_rows * cols; e += blockDim.x) {
+            const int row = e / cols, w = row / n_rows;
+            float *at = tables + w * size + (row - w * n_rows) * 64 + (e - row * cols);
+            double sum = 0.0;
+#pragma unroll 8
+            for (int k = 0; k < slots; ++k) sum += (double)at[k * tile];
+            at[0] = (float)sum;
+        }
+        __syncthreads();
+    }
     for (int e = threadIdx.x; e < n_rows * cols; e += blockDim.x) {
-        const int s = e / cols, c = e - s * cols;
+        const int r = e / cols, c = e - r * cols;
         double sum[1] = {0.0};
-        for (int w = 0; w < waves; ++w) sum[0] += (double)tables[w * size + s * 64 + c];
-        if (part) part[((int64_t)blockIdx.x * n_rows + s) * width + f0 + c] = (float)sum[0];
-        else out.put<1>(s, f0 + c, 0, sum);
+#pragma unroll 4
+        for (int w = 0; w < waves; ++w) sum[0] += (double)tables[w * size + r * 64 + c];
+        if (part) part[((int64_t)blockIdx.x * n_rows + r) * width + f0 + c] = (float)sum[0];
+        else out.put<1>(r, f0 + c, 0, sum);
     }
 }
 
-// sum over the blocks of k_few_rows, 64 elements to a block of 16 wavefronts which share the parts
+// sum over the blocks of k_few_rows: a block has 16 elements, whose parts 64 groups of 16 lanes share
 __global__ __launch_bounds__(1024) void k_few_join(const float *part, int parts, int64_t elements, int64_t width, GradOut out)
 {
-    __shared__ double red[16][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t e = (int64_t)blockIdx.x * 64 + lane;
+    __shared__ double red[16][16];
+    const int lane = threadIdx.x & 15, group = threadIdx.x >> 4;
+    const int64_t e = (int64_t)blockIdx.x * 16 + lane;
     double sum[1] = {0.0};
     if (e < elements) {
-#pragma unroll 16
-        for (int p = wave; p < parts; p += 16) sum[0] += (double)part[p * elements + e];
+#pragma unroll 8
+        for (int p = group; p < parts; p += 64) sum[0] += (double)part[p * elements + e];
     }
-    red[wave][lane] = sum[0];
+    sum[0] += __shfl_xor(sum[0], 16);
+    sum[0] += __shfl_xor(sum[0], 32);
+    if ((group & 3) == 0) red[group >> 2][lane] = sum[0];
     __syncthreads();
-    if (wave || e >= elements) return;
-    for (int w = 1; w < 16; ++w) sum[0] += red[w][lane];
+    if (group || e >= elements) return;
+#pragma unroll
+    for (int g = 1; g < 16; ++g) sum[0] += red[g][lane];
     out.put<1>(e / width, e % width, 0, sum);
 }
 
 struct FewPlan {
-    int tiles, tile, slots, waves, blocks;
+    int tiles, tile, slots, waves, threads, blocks;   // waves: wavefronts with a table; all threads clear and join the tables
     int64_t rows_per_wave;
     FewPlan(int64_t n, int64_t n_rows, int64_t width)
     {
@@ -269,6 +273,7 @@ struct FewPlan {
         slots = 64 / tile;
         waves = (int)(kFewLds / ((n_rows + 1) * 256));
         waves = waves < 1 ? 1 : waves > kFewWaves ? kFewWaves : waves;
+        threads = 64 * (waves < 8 ? 8 : waves);
         // wavefronts: as many as have a step of rows in flight, at most two blocks a compute unit, but no more than
         // MLIP_EMBED_GRAD_RUN rows a lane; where one block does with four steps, one block
         const int64_t step = (int64_t)slots * few_unroll(slots == 1);
@@ -288,7 +293,7 @@ constexpr int64_t kFewMost = kFewLds / 256 - 1;   // rows whose table fits a wav
 // Many rows: the ids are sorted (stable, by digits of at most 8 bits, places of the atoms along with them), so that every row's atoms lie one
 // after another in their order; spans of the sorted list are summed, whatever rows they hold, and a row that spans share is joined.
 
-constexpr int kSortThreads = 1024, kSortTile = 4096, kSortBlocks = 256, kRadix = 256;
+constexpr int kSortThreads = 1024, kSortTile = 2048, kSortBlocks = 256, kRadix = 256;
 
 struct Pair { uint32_t key, at; };
 
@@ -333,7 +338,7 @@ __global__ __launch_bounds__(kSortThreads) void k_digit_counts(const In *in, int
     if (threadIdx.x < kRadix) counts[(int64_t)blockIdx.x * kRadix + threadIdx.x] = count[threadIdx.x];
 }
 
-// one pass of the sort: a block takes its range in tiles of 4096; a wavefront ranks 256 of them, 64 at a time
+// one pass of the sort: a block takes its range tile by tile; a wavefront ranks its part of a tile 64 items at a time
 template <class In>
 __global__ __launch_bounds__(kSortThreads) void k_digit_scatter(const In *in, int64_t n, int64_t n_rows, int64_t range, int shift, int bits,
                                                                 const uint32_t *counts, Pair *sorted)
@@ -344,10 +349,20 @@ __global__ __launch_bounds__(kSortThreads) void k_digit_scatter(const In *in, in
     __shared__ uint32_t sums[4];
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
     const uint32_t mask = (1u << bits) - 1;
+    const int64_t end = n - range * blockIdx.x < range ? n : range * (blockIdx.x + 1);
+    Pair item[kRounds];   // of the tile under way; the first one's are on their way while the counts are added up
+    auto load = [&](int64_t i0) {
+#pragma unroll
+        for (int j = 0; j < kRounds; ++j) {
+            const int64_t i = i0 + wave * (64 * kRounds) + j * 64 + lane;
+            item[j] = item_of(in, i < end ? i : end - 1, n_rows);
+        }
+    };
+    load(range * blockIdx.x);
     {   // base: items of lower digits anywhere, and of this digit in the blocks before
         const int d = t & (kRadix - 1), quarter = t / kRadix;
         uint32_t all = 0, earlier = 0;
-#pragma unroll 8
+#pragma unroll 16
         for (int b = quarter; b < (int)gridDim.x; b += kSortThreads / kRadix) {
             const uint32_t c = counts[(int64_t)b * kRadix + d];
             all += c;
@@ -374,18 +389,12 @@ __global__ __launch_bounds__(kSortThreads) void k_digit_scatter(const In *in, in
             base[t] = scan - own + earlier;
         }
     }
-    const int64_t end = n - range * blockIdx.x < range ? n : range * (blockIdx.x + 1);
     for (int64_t i0 = range * blockIdx.x; i0 < end; i0 += kSortTile) {
+        if (i0 > range * blockIdx.x) load(i0);
         __syncthreads();
         for (int k = t; k < kWaves * kRadix; k += kSortThreads) (&before[0][0])[k] = 0;
         __syncthreads();
-        Pair item[kRounds];
         uint32_t rank[kRounds];
-#pragma unroll
-        for (int j = 0; j < kRounds; ++j) {
-            const int64_t i = i0 + wave * (64 * kRounds) + j * 64 + lane;
-            item[j] = i < end ? item_of(in, i, n_rows) : Pair{0, 0};
-        }
 #pragma unroll
         for (int j = 0; j < kRounds; ++j) {
             const bool there = i0 + wave * (64 * kRounds) + j * 64 + lane < end;
@@ -422,7 +431,7 @@ __global__ __launch_bounds__(kSortThreads) void k_digit_scatter(const In *in, in
 
 // Sums over spans of `span` items of the sorted list, a group of `lanes` lanes (V columns each) to a span.  A row that lies within the span is
 // written; what a span holds of a row that began before it goes to edge[span][0], of one that goes on behind it to edge[span][1].
-template <class T, class O, int V>
+template <class T, class O, int V, bool Stream>
 __global__ __launch_bounds__(256) void k_span_sums(const Pair *sorted, const T *grad, int64_t rs, int64_t cs, int64_t n, int64_t n_rows,
                                                    int64_t width, int lanes, int span, uint32_t *row_begin, uint32_t *row_end, float *edge,
                                                    GradOut out)
@@ -462,7 +471,7 @@ __global__ __launch_bounds__(256) void k_span_sums(const Pair *sorted, const T *
 #pragma unroll
         for (int u = 0; u < U; ++u) item[u] = next[u];
 #pragma unroll
-        for (int u = 0; u < U; ++u) load_cols<V>(v[u], mine + item[u].at * rs);   // of ids without a row too: their atoms are there
+        for (int u = 0; u < U; ++u) load_cols<V, Stream>(v[u], mine + item[u].at * rs);   // of ids without a row too: their atoms are there
         if (p + U < p1) {
 #pragma unroll
             for (int u = 0; u < U; ++u) next[u] = sorted[p + U + u < p1 ? p + U + u : p1 - 1];
@@ -586,24 +595,28 @@ static int few_rows(const EmbedArgs &a, const GradOut &out)
 {
     const FewPlan p(a.n, a.n_rows, a.width);
     float *part = p.blocks > 1 ? static_cast<float *>(a.workspace) : nullptr;
+    const bool stream = (double)a.n * (double)a.width * (double)elem_size(a.in_dtype) > kStreamBytes;
     const bool near = ((double)p.slots * (double)a.rs + (double)p.tile * (double)a.cs) * 4.0 < 4e9;
     with_elem(a.in_dtype, [&](auto t) {
         with_ids(a.id_bits, [&](auto id) {
             using T = decltype(t);
             using Id = decltype(id);
             auto launch = [&](auto kernel) {
-                kernel<<<dim3(p.blocks, p.tiles), p.waves * 64, (size_t)p.waves * (a.n_rows + 1) * 256, a.stream>>>(
+                kernel<<<dim3(p.blocks, p.tiles), p.threads, (size_t)p.waves * (a.n_rows + 1) * 256, a.stream>>>(
                     static_cast<const T *>(a.in), a.rs, a.cs, static_cast<const Id *>(a.ids), a.n, (int)a.n_rows, a.width, p.tile, p.slots,
-                    p.rows_per_wave, part, out);
+                    p.waves, p.rows_per_wave, part, out);
             };
-            if (p.slots == 1) near ? launch(k_few_rows<T, Id, true, true>) : launch(k_few_rows<T, Id, true, false>);
-            else near ? launch(k_few_rows<T, Id, false, true>) : launch(k_few_rows<T, Id, false, false>);
+            auto pick = [&](auto one, auto close) {
+                stream ? launch(k_few_rows<T, Id, one.value, close.value, true>) : launch(k_few_rows<T, Id, one.value, close.value, false>);
+            };
+            if (p.slots == 1) near ? pick(std::true_type{}, std::true_type{}) : pick(std::true_type{}, std::false_type{});
+            else near ? pick(std::false_type{}, std::true_type{}) : pick(std::false_type{}, std::false_type{});
         });
     });
     MLIP_HIP(hipGetLastError());
     if (part) {
         const int64_t elements = a.n_rows * a.width;
-        k_few_join<<<(unsigned)((elements + 63) / 64), 1024, 0, a.stream>>>(part, p.blocks, elements, a.width, out);
+        k_few_join<<<(unsigned)((elements + 15) / 16), 1024, 0, a.stream>>>(part, p.blocks, elements, a.width, out);
         MLIP_HIP(hipGetLastError());
     }
     return MLIP_OK;
@@ -640,7 +653,8 @@ static int many_rows(const EmbedArgs &a, const GradOut &out)
             constexpr int V = 16 / sizeof(T);
             const bool wide = (a.cs == 1 || a.width == 1) && a.width >= V;
             const int64_t per_row = wide ? lots_of(a.width, V) : a.width;
-            const int lanes = (int)(per_row < 64 ? per_row : 64);
+                        const int lanes = (int)(per_row < 64 ? per_row : 64);
+            const bool stream = (double)a.n * (double)a.width * sizeof(T) > kStreamBytes;
             const int64_t spans = (a.n + w.span - 1) / w.span, groups = 256 / lanes;
             const dim3 grid((unsigned)((spans + groups - 1) / groups), (unsigned)((per_row + lanes - 1) / lanes));
             auto launch = [&](auto kernel) {
@@ -649,7 +663,8 @@ static int many_rows(const EmbedArgs &a, const GradOut &out)
             };
             with_elem(a.out_dtype, [&](auto o) {
                 using O = decltype(o);
-                wide ? launch(k_span_sums<T, O, V>) : launch(k_span_sums<T, O, 1>);
+                if (!wide) launch(k_span_sums<T, O, 1, false>);
+                else stream ? launch(k_span_sums<T, O, V, true>) : launch(k_span_sums<T, O, V, false>);
             });
         });
         MLIP_HIP(hipGetLastError());
@@ -676,7 +691,7 @@ static int many_rows(const EmbedArgs &a, const GradOut &out)
 
 int embed_grad_impl(const EmbedArgs &a)
 {
-    const GradOut out = {a.out, a.out_dtype, a.os, a.scale, a.accumulate};
+        const GradOut out = {a.out, a.out_dtype, a.os, a.scale, a.accumulate};
     return a.n_rows <= kFewMost ? few_rows(a, out) : many_rows(a, out);
 }
 
