@@ -338,82 +338,106 @@ __global__ __launch_bounds__(kSortThreads) void k_digit_counts(const In *in, int
     if (threadIdx.x < kRadix) counts[(int64_t)blockIdx.x * kRadix + threadIdx.x] = count[threadIdx.x];
 }
 
-// one pass of the sort: a block takes its range tile by tile; a wavefront ranks its part of a tile 64 items at a time
+constexpr int kSortWaves = kSortThreads / 64, kSortRounds = kSortTile / kSortThreads;
+
+// place of a thread's j-th item in a tile: a wavefront has consecutive items, 64 in a round
+__device__ inline int tile_place(int j) { return (threadIdx.x >> 6) * (64 * kSortRounds) + j * 64 + (threadIdx.x & 63); }
+
+// Ranks of a tile's `there` items among those of the same digit and wavefront; before[w][d] is left with the number of wavefront w's items of digit d.
+__device__ inline void tile_ranks(const Pair (&item)[kSortRounds], int there, int shift, int bits, uint32_t (&before)[kSortWaves][kRadix],
+                                  uint32_t (&rank)[kSortRounds])
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    __syncthreads();
+    for (int k = threadIdx.x; k < kSortWaves * kRadix; k += kSortThreads) (&before[0][0])[k] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kSortRounds; ++j) {
+        const uint32_t d = (item[j].key >> shift) & ((1u << bits) - 1);
+        const bool mine = tile_place(j) < there;
+        uint64_t same = __ballot(mine);
+        for (int b = 0; b < bits; ++b) {
+            const uint64_t set = __ballot((d >> b) & 1);
+            same &= (d >> b) & 1 ? set : ~set;
+        }
+        const uint32_t lower = (uint32_t)__popcll(same & (((uint64_t)1 << lane) - 1));
+        rank[j] = before[wave][d] + lower;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // all lanes have read before the first of each digit writes
+        if (mine && lower == 0) before[wave][d] = rank[j] + (uint32_t)__popcll(same);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
+    __syncthreads();
+}
+
+// sum over the digits below thread t's digit t (t < kRadix; all threads call)
+__device__ inline uint32_t digits_below(uint32_t own, uint32_t (&sums)[kRadix / 64])
+{
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    uint32_t scan = own;
+    if (t < kRadix) {
+        for (int k = 1; k < 64; k <<= 1) {
+            const uint32_t up = __shfl_up(scan, k);
+            if (lane >= k) scan += up;
+        }
+        if (lane == 63) sums[wave] = scan;
+    }
+    __syncthreads();
+    if (t < kRadix)
+        for (int w = 0; w < wave; ++w) scan += sums[w];
+    return scan - own;
+}
+
+// one pass of the sort: a block takes its range tile by tile
 template <class In>
 __global__ __launch_bounds__(kSortThreads) void k_digit_scatter(const In *in, int64_t n, int64_t n_rows, int64_t range, int shift, int bits,
                                                                 const uint32_t *counts, Pair *sorted)
 {
-    constexpr int kWaves = kSortThreads / 64, kRounds = kSortTile / kSortThreads;
-    __shared__ uint32_t before[kWaves][kRadix];   // per wavefront: items of the digit before its own
+    __shared__ uint32_t before[kSortWaves][kRadix];
     __shared__ uint32_t base[kRadix];             // where the digit's next item of this block goes
-    __shared__ uint32_t sums[4];
-    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    __shared__ uint32_t sums[kRadix / 64];
+    const int t = threadIdx.x, wave = t >> 6;
     const uint32_t mask = (1u << bits) - 1;
     const int64_t end = n - range * blockIdx.x < range ? n : range * (blockIdx.x + 1);
-    Pair item[kRounds];   // of the tile under way; the first one's are on their way while the counts are added up
+    Pair item[kSortRounds];   // of the tile under way; the first one's are on their way while the counts are added up
     auto load = [&](int64_t i0) {
 #pragma unroll
-        for (int j = 0; j < kRounds; ++j) {
-            const int64_t i = i0 + wave * (64 * kRounds) + j * 64 + lane;
+        for (int j = 0; j < kSortRounds; ++j) {
+            const int64_t i = i0 + tile_place(j);
             item[j] = item_of(in, i < end ? i : end - 1, n_rows);
         }
     };
     load(range * blockIdx.x);
     {   // base: items of lower digits anywhere, and of this digit in the blocks before
-        const int d = t & (kRadix - 1), quarter = t / kRadix;
+        constexpr int kShares = kSortThreads / kRadix;
+        const int d = t & (kRadix - 1), share = t / kRadix;
         uint32_t all = 0, earlier = 0;
 #pragma unroll 16
-        for (int b = quarter; b < (int)gridDim.x; b += kSortThreads / kRadix) {
+        for (int b = share; b < (int)gridDim.x; b += kShares) {
             const uint32_t c = counts[(int64_t)b * kRadix + d];
             all += c;
             earlier += b < (int)blockIdx.x ? c : 0;
         }
-        before[quarter][d] = all;
-        before[quarter + 4][d] = earlier;
+        before[share][d] = all;
+        before[share + kShares][d] = earlier;
         __syncthreads();
-        uint32_t scan = 0, own = 0;
+        all = earlier = 0;
         if (t < kRadix) {
-            all = before[0][t] + before[1][t] + before[2][t] + before[3][t];
-            earlier = before[4][t] + before[5][t] + before[6][t] + before[7][t];
-            own = all;
-            scan = all;
-            for (int k = 1; k < 64; k <<= 1) {
-                const uint32_t up = __shfl_up(scan, k);
-                if (lane >= k) scan += up;
+            for (int k = 0; k < kShares; ++k) {
+                all += before[k][t];
+                earlier += before[k + kShares][t];
             }
-            if (lane == 63) sums[wave] = scan;
         }
-        __syncthreads();
-        if (t < kRadix) {
-            for (int w = 0; w < wave; ++w) scan += sums[w];
-            base[t] = scan - own + earlier;
-        }
+        const uint32_t below = digits_below(all, sums);
+        if (t < kRadix) base[t] = below + earlier;
     }
     for (int64_t i0 = range * blockIdx.x; i0 < end; i0 += kSortTile) {
         if (i0 > range * blockIdx.x) load(i0);
-        __syncthreads();
-        for (int k = t; k < kWaves * kRadix; k += kSortThreads) (&before[0][0])[k] = 0;
-        __syncthreads();
-        uint32_t rank[kRounds];
-#pragma unroll
-        for (int j = 0; j < kRounds; ++j) {
-            const bool there = i0 + wave * (64 * kRounds) + j * 64 + lane < end;
-            const uint32_t d = (item[j].key >> shift) & mask;
-            uint64_t same = __ballot(there);
-            for (int b = 0; b < bits; ++b) {
-                const uint64_t set = __ballot((d >> b) & 1);
-                same &= (d >> b) & 1 ? set : ~set;
-            }
-            const uint32_t lower = (uint32_t)__popcll(same & (((uint64_t)1 << lane) - 1));
-            rank[j] = before[wave][d] + lower;
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // all lanes have read before the first of each digit writes
-            if (there && lower == 0) before[wave][d] = rank[j] + (uint32_t)__popcll(same);
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        }
-        __syncthreads();
+        const int there = end - i0 < kSortTile ? (int)(end - i0) : kSortTile;
+        uint32_t rank[kSortRounds];
+        tile_ranks(item, there, shift, bits, before, rank);
         if (t < kRadix) {
             uint32_t at = base[t];
-            for (int w = 0; w < kWaves; ++w) {
+            for (int w = 0; w < kSortWaves; ++w) {
                 const uint32_t c = before[w][t];
                 before[w][t] = at;
                 at += c;
@@ -422,10 +446,49 @@ __global__ __launch_bounds__(kSortThreads) void k_digit_scatter(const In *in, in
         }
         __syncthreads();
 #pragma unroll
-        for (int j = 0; j < kRounds; ++j) {
-            const uint32_t d = (item[j].key >> shift) & mask;
-            if (i0 + wave * (64 * kRounds) + j * 64 + lane < end) sorted[before[wave][d] + rank[j]] = item[j];
+        for (int j = 0; j < kSortRounds; ++j)
+            if (tile_place(j) < there) sorted[before[wave][(item[j].key >> shift) & mask] + rank[j]] = item[j];
+    }
+}
+
+// All passes over a list of one tile, in the first block's LDS; the others clear the ends of the rows' spans.
+template <class Id>
+__global__ __launch_bounds__(kSortThreads) void k_sort_tile(const Id *ids, int n, int64_t n_rows, int passes, int bits, Pair *sorted, uint32_t *row_end)
+{
+    __shared__ uint32_t before[kSortWaves][kRadix];
+    __shared__ uint32_t sums[kRadix / 64];
+    __shared__ Pair list[kSortTile];
+    const int t = threadIdx.x, wave = t >> 6;
+    if (blockIdx.x > 0) {
+        for (int64_t r = (int64_t)(blockIdx.x - 1) * kSortThreads + t; r < n_rows; r += (int64_t)(gridDim.x - 1) * kSortThreads) row_end[r] = 0;
+        return;
+    }
+    Pair item[kSortRounds];
+#pragma unroll
+    for (int j = 0; j < kSortRounds; ++j) item[j] = item_of(ids, tile_place(j) < n ? tile_place(j) : n - 1, n_rows);
+    for (int pass = 0; pass < passes; ++pass) {
+        const int shift = pass * bits;
+        uint32_t rank[kSortRounds], all = 0;
+        tile_ranks(item, n, shift, bits, before, rank);
+        if (t < kRadix)
+            for (int w = 0; w < kSortWaves; ++w) all += before[w][t];
+        uint32_t at = digits_below(all, sums);
+        if (t < kRadix) {
+            for (int w = 0; w < kSortWaves; ++w) {
+                const uint32_t c = before[w][t];
+                before[w][t] = at;
+                at += c;
+            }
         }
+        __syncthreads();
+        Pair *to = pass + 1 < passes ? list : sorted;
+#pragma unroll
+        for (int j = 0; j < kSortRounds; ++j)
+            if (tile_place(j) < n) to[before[wave][(item[j].key >> shift) & ((1u << bits) - 1)] + rank[j]] = item[j];
+        if (pass + 1 == passes) break;
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < kSortRounds; ++j) item[j] = list[tile_place(j) < n ? tile_place(j) : 0];
     }
 }
 
@@ -631,22 +694,26 @@ static int many_rows(const EmbedArgs &a, const GradOut &out)
     Pair *list[2] = {reinterpret_cast<Pair *>(base + w.pairs[0]), reinterpret_cast<Pair *>(base + w.pairs[1])};
     uint32_t *counts = u32(w.counts), *row_begin = u32(w.row_begin), *row_end = u32(w.row_end);
     float *edge = reinterpret_cast<float *>(base + w.edge);
-    {
-        with_ids(a.id_bits, [&](auto id) {
-            using Id = decltype(id);
-            const Id *ids = static_cast<const Id *>(a.ids);
-            k_digit_counts<<<p.blocks > 0 ? p.blocks : 1, kSortThreads, 0, a.stream>>>(ids, a.n, a.n_rows, p.range, 0, p.bits, counts, row_end);
-            if (a.n == 0) return;
-            k_digit_scatter<<<p.blocks, kSortThreads, 0, a.stream>>>(ids, a.n, a.n_rows, p.range, 0, p.bits, counts, list[0]);
-        });
-        for (int k = 1; k < p.passes && a.n > 0; ++k) {
-            const Pair *in = list[(k - 1) & 1];
-            k_digit_counts<<<p.blocks, kSortThreads, 0, a.stream>>>(in, a.n, a.n_rows, p.range, k * p.bits, p.bits, counts, (uint32_t *)nullptr);
-            k_digit_scatter<<<p.blocks, kSortThreads, 0, a.stream>>>(in, a.n, a.n_rows, p.range, k * p.bits, p.bits, counts, list[k & 1]);
+    const bool one_tile = a.n > 0 && a.n <= kSortTile;
+    const Pair *sorted = one_tile ? list[0] : list[(p.passes - 1) & 1];
+    with_ids(a.id_bits, [&](auto id) {
+        using Id = decltype(id);
+        const Id *ids = static_cast<const Id *>(a.ids);
+        if (one_tile) {
+            const int64_t clear = (a.n_rows + kSortThreads * 8 - 1) / (kSortThreads * 8);
+            k_sort_tile<<<(unsigned)(1 + (clear < 256 ? clear : 256)), kSortThreads, 0, a.stream>>>(ids, (int)a.n, a.n_rows, p.passes, p.bits, list[0],
+                                                                                               row_end);
+            return;
         }
-        MLIP_HIP(hipGetLastError());
+        k_digit_counts<<<p.blocks > 0 ? p.blocks : 1, kSortThreads, 0, a.stream>>>(ids, a.n, a.n_rows, p.range, 0, p.bits, counts, row_end);
+        if (a.n > 0) k_digit_scatter<<<p.blocks, kSortThreads, 0, a.stream>>>(ids, a.n, a.n_rows, p.range, 0, p.bits, counts, list[0]);
+    });
+    for (int k = 1; k < p.passes && a.n > kSortTile; ++k) {
+        const Pair *in = list[(k - 1) & 1];
+        k_digit_counts<<<p.blocks, kSortThreads, 0, a.stream>>>(in, a.n, a.n_rows, p.range, k * p.bits, p.bits, counts, (uint32_t *)nullptr);
+        k_digit_scatter<<<p.blocks, kSortThreads, 0, a.stream>>>(in, a.n, a.n_rows, p.range, k * p.bits, p.bits, counts, list[k & 1]);
     }
-    const Pair *sorted = list[(p.passes - 1) & 1];
+    MLIP_HIP(hipGetLastError());
     if (a.n > 0) {
         with_elem(a.in_dtype, [&](auto t) {
             using T = decltype(t);
