@@ -151,17 +151,17 @@ struct GradOut {
         else if (dtype == MLIP_DTYPE_BF16) put_as<__bf16>(r, f, skip, sum);
         else put_as<_Float16>(r, f, skip, sum);
     }
-    template <class O, int V> __device__ void put_as(int64_t r, int64_t f, int skip, const double (&sum)[V]) const
-    {
+    template <class O, int V, class S> __device__ void put_as(int64_t r, int64_t f, int skip, const S (&sum)[V]) const
+    {   // (fp32 sums: their fp32 product with the scale is what the fp64 product rounds to)
         O *o = static_cast<O *>(p) + r * os + f;
         float v[V];
         if (accumulate) {   // a column that another lot has too is that lot's to add to
 #pragma unroll
             for (int k = 0; k < V; ++k)
-                if (k >= skip) o[k] = to_elem<O>((float)(sum[k] * (double)scale + (double)(float)o[k]));
+                if (k >= skip) o[k] = to_elem<O>((float)((double)sum[k] * (double)scale + (double)(float)o[k]));
         } else {
 #pragma unroll
-            for (int k = 0; k < V; ++k) v[k] = (float)(sum[k] * (double)scale);
+            for (int k = 0; k < V; ++k) v[k] = (float)(sum[k] * (S)scale);
             store_cols<V>(o, v);
         }
     }
@@ -492,17 +492,20 @@ __global__ __launch_bounds__(kSortThreads) void k_sort_tile(const Id *ids, int n
     }
 }
 
-// Sums over spans of `span` items of the sorted list, a group of `lanes` lanes (V columns each) to a span.  A row that lies within the span is
+// Sums over spans of `span` items of the sorted list, a group of `lanes` lanes (V columns each) to a span; Wave: a whole wavefront, whose items are then
+// scalars to it, which leaves the vector unit the additions alone.  A row that lies within the span is
 // written; what a span holds of a row that began before it goes to edge[span][0], of one that goes on behind it to edge[span][1].
-template <class T, class O, int V, bool Stream>
+template <class T, class O, int V, bool Stream, bool Wave>
 __global__ __launch_bounds__(256) void k_span_sums(const Pair *sorted, const T *grad, int64_t rs, int64_t cs, int64_t n, int64_t n_rows,
                                                    int64_t width, int lanes, int span, uint32_t *row_begin, uint32_t *row_end, float *edge,
                                                    GradOut out)
 {
     constexpr int U = 8;
-    const int64_t s = (int64_t)blockIdx.x * (256 / lanes) + threadIdx.x / lanes;
-    const int64_t number = (int64_t)blockIdx.y * lanes + threadIdx.x % lanes, p0 = s * span;
-    if (threadIdx.x / lanes >= 256 / lanes || p0 >= n || number * V >= width) return;
+    if (Wave) lanes = 64;
+    const int group = Wave ? __builtin_amdgcn_readfirstlane(threadIdx.x / 64) : threadIdx.x / lanes;
+    const int64_t s = (int64_t)blockIdx.x * (256 / lanes) + group, p0 = s * span;
+    const int64_t number = (int64_t)blockIdx.y * lanes + threadIdx.x % lanes;
+    if (group >= 256 / lanes || p0 >= n || number * V >= width) return;
     const Lot<V> lot(number, width);
     const int64_t p1 = n - p0 < span ? n : p0 + span;
     uint32_t key = sorted[p0].key;
@@ -516,10 +519,7 @@ __global__ __launch_bounds__(256) void k_span_sums(const Pair *sorted, const T *
         if (from_before || goes_on) {
             store_cols<V>(edge + (s * 2 + (from_before ? 0 : 1)) * width + lot.f, sum);
         } else {
-            double v[V];
-#pragma unroll
-            for (int k = 0; k < V; ++k) v[k] = (double)sum[k];
-            out.put_as<O>(key, lot.f, lot.skip, v);
+            out.put_as<O>(key, lot.f, lot.skip, sum);
         }
         if (number == 0 && !goes_on) row_end[key] = (uint32_t)end;
     };
@@ -562,11 +562,11 @@ __global__ __launch_bounds__(256) void k_span_sums(const Pair *sorted, const T *
 // Rows that no id names, and rows that spans share.  A thread has V columns of a row and adds up what at most kJoinSerial spans hold of it;
 // a row of more spans is the work of one of the first `heavy` blocks (64 such lots of columns at most): block b looks at span b * kJoinSerial, and if the row
 // that runs into this span from before is such a row, and no earlier block sees it, shares the row's spans out over its threads.
-constexpr int kJoinSerial = 16;
+constexpr int kJoinSerial = 8, kJoinUnroll = 2;   // the second: rows looked up at a time
 
 template <class O, int V>
 __global__ __launch_bounds__(256) void k_row_join(const Pair *sorted, const uint32_t *row_begin, const uint32_t *row_end, const float *edge,
-                                                  int span, int heavy, uint32_t items, uint32_t per_row, Div31 div, int64_t row0,
+                                                  int shift, int heavy, uint32_t items, uint32_t per_row, Div31 div, int64_t row0,
                                                   int64_t n_rows, int64_t width, GradOut out)
 {
     __shared__ double red[256][V];
@@ -579,9 +579,9 @@ __global__ __launch_bounds__(256) void k_row_join(const Pair *sorted, const uint
     if ((int)blockIdx.x < heavy) {
         const int tiles = (per_row + 63) / 64, lanes = per_row < 64 ? per_row : 64, groups = 256 / lanes;
         const int64_t at = ((int64_t)blockIdx.x / tiles + 1) * kJoinSerial;
-        const uint32_t r = sorted[at * span].key;
+        const uint32_t r = sorted[at << shift].key;
         if (r >= n_rows) return;
-        const int64_t first = row_begin[r] / span, last = ((int64_t)row_end[r] - 1) / span;
+        const int64_t first = row_begin[r] >> shift, last = (row_end[r] - 1) >> shift;
         if (last - first < kJoinSerial || first >= at || first < at - kJoinSerial) return;
         const int group = threadIdx.x / lanes;
         const int64_t number = (int64_t)(blockIdx.x % tiles) * lanes + threadIdx.x % lanes;
@@ -605,22 +605,32 @@ __global__ __launch_bounds__(256) void k_row_join(const Pair *sorted, const uint
         out.put_as<O>(r, lot.f, lot.skip, sum);
         return;
     }
+    constexpr int U = kJoinUnroll;
     const uint32_t step = (gridDim.x - heavy) * 256;
-    for (uint32_t e = (blockIdx.x - heavy) * 256 + threadIdx.x; e < items; e += step) {
-        const uint32_t i = div(e);
-        const int64_t r = row0 + i;
-        const Lot<V> lot(e - i * per_row, width);
-        const uint32_t end = row_end[r];
-        double sum[V];
+    for (uint32_t e0 = (blockIdx.x - heavy) * 256 + threadIdx.x; e0 < items; e0 += step * U) {
+        uint32_t row[U], end[U], begin[U];
 #pragma unroll
-        for (int k = 0; k < V; ++k) sum[k] = 0.0;
-        if (end > 0) {
-            const int64_t first = row_begin[r] / span, last = (end - 1) / span;
-            if (first == last || last - first >= kJoinSerial) continue;
-#pragma unroll 4
-            for (int64_t s = first; s <= last; ++s) add(sum, s, first, lot.f);
+        for (int u = 0; u < U; ++u) {
+            row[u] = div(e0 + u * step < items ? e0 + u * step : e0);
+            end[u] = row_end[row0 + row[u]];
+            begin[u] = row_begin[row0 + row[u]];   // anything where the row has no end
         }
-        out.put_as<O>(r, lot.f, lot.skip, sum);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const uint32_t e = e0 + u * step;
+            if (u > 0 && e >= items) break;
+            const int64_t first = begin[u] >> shift, last = (end[u] - 1) >> shift;
+            if (end[u] > 0 && (first == last || last - first >= kJoinSerial)) continue;
+            const Lot<V> lot(e - row[u] * per_row, width);
+            double sum[V];
+#pragma unroll
+            for (int k = 0; k < V; ++k) sum[k] = 0.0;
+            if (end[u] > 0) {
+#pragma unroll 4
+                for (int64_t s = first; s <= last; ++s) add(sum, s, first, lot.f);
+            }
+            out.put_as<O>(row0 + row[u], lot.f, lot.skip, sum);
+        }
     }
 }
 
@@ -630,10 +640,10 @@ struct SortSpace {
     int span;
     SortSpace(int64_t n, int64_t n_rows, int64_t width)
     {
-        // spans as long as 4096 wavefronts still come of them, up to 64 items
+        // spans as long as 2048 wavefronts still come of them, up to 64 items
         const int64_t lots = (width + 3) / 4;
         span = 64;
-        while (span > 8 && n / span * lots < 4096 * 64) span /= 2;
+        while (span > 8 && n / span * lots < 2048 * 64) span /= 2;
         size_t at = 0;
         auto take = [&](size_t size) { const size_t here = at; at += (size + 255) & ~(size_t)255; return here; };
         for (size_t &p : pairs) p = take((size_t)n * sizeof(Pair));
@@ -717,21 +727,23 @@ static int many_rows(const EmbedArgs &a, const GradOut &out)
     if (a.n > 0) {
         with_elem(a.in_dtype, [&](auto t) {
             using T = decltype(t);
-            constexpr int V = 16 / sizeof(T);
-            const bool wide = (a.cs == 1 || a.width == 1) && a.width >= V;
-            const int64_t per_row = wide ? lots_of(a.width, V) : a.width;
-                        const int lanes = (int)(per_row < 64 ? per_row : 64);
+            const int64_t spans = (a.n + w.span - 1) / w.span;
             const bool stream = (double)a.n * (double)a.width * sizeof(T) > kStreamBytes;
-            const int64_t spans = (a.n + w.span - 1) / w.span, groups = 256 / lanes;
-            const dim3 grid((unsigned)((spans + groups - 1) / groups), (unsigned)((per_row + lanes - 1) / lanes));
-            auto launch = [&](auto kernel) {
-                kernel<<<grid, 256, 0, a.stream>>>(sorted, static_cast<const T *>(a.in), a.rs, a.cs, a.n, a.n_rows, a.width, lanes, w.span,
-                                                   row_begin, row_end, edge, out);
-            };
             with_elem(a.out_dtype, [&](auto o) {
                 using O = decltype(o);
-                if (!wide) launch(k_span_sums<T, O, 1, false>);
-                else stream ? launch(k_span_sums<T, O, V, true>) : launch(k_span_sums<T, O, V, false>);
+                constexpr int V = 16 / sizeof(T);
+                const bool wide = (a.cs == 1 || a.width == 1) && a.width >= V;
+                const int64_t per_row = wide ? lots_of(a.width, V) : a.width;
+                const int lanes = (int)(per_row < 64 ? per_row : 64);
+                const int64_t groups = 256 / lanes;
+                const dim3 grid((unsigned)((spans + groups - 1) / groups), (unsigned)((per_row + lanes - 1) / lanes));
+                auto launch = [&](auto kernel) {
+                    kernel<<<grid, 256, 0, a.stream>>>(sorted, static_cast<const T *>(a.in), a.rs, a.cs, a.n, a.n_rows, a.width, lanes, w.span,
+                                                       row_begin, row_end, edge, out);
+                };
+                if (!wide) launch(k_span_sums<T, O, 1, false, false>);
+                else if (lanes < 64) stream ? launch(k_span_sums<T, O, V, true, false>) : launch(k_span_sums<T, O, V, false, false>);
+                else stream ? launch(k_span_sums<T, O, V, true, true>) : launch(k_span_sums<T, O, V, false, true>);
             });
         });
         MLIP_HIP(hipGetLastError());
@@ -740,12 +752,12 @@ static int many_rows(const EmbedArgs &a, const GradOut &out)
     const int64_t per_row = wide ? lots_of(a.width, 4) : a.width, most = ((int64_t)1 << 30) / per_row;
     const Div31 div((uint32_t)per_row);
     for (int64_t r0 = 0; r0 < a.n_rows; r0 += most) {
-        const int64_t rows = a.n_rows - r0 < most ? a.n_rows - r0 : most, items = rows * per_row, blocks = (items + 255) / 256;
+        const int64_t rows = a.n_rows - r0 < most ? a.n_rows - r0 : most, items = rows * per_row, blocks = (items + 256 * kJoinUnroll - 1) / (256 * kJoinUnroll);
         // spans kJoinSerial, 2 kJoinSerial, ... that there are, each for every 64 lots of columns; once
         const int64_t heavy = r0 == 0 && a.n > 0 ? ((a.n + w.span - 1) / w.span - 1) / kJoinSerial * ((per_row + 63) / 64) : 0;
         auto launch = [&](auto kernel) {
             kernel<<<(unsigned)((blocks < 16384 ? blocks : 16384) + heavy), 256, 0, a.stream>>>(
-                sorted, row_begin, row_end, edge, w.span, (int)heavy, (uint32_t)items, (uint32_t)per_row, div, r0, a.n_rows, a.width, out);
+                sorted, row_begin, row_end, edge, __builtin_ctz((unsigned)w.span), (int)heavy, (uint32_t)items, (uint32_t)per_row, div, r0, a.n_rows, a.width, out);
         };
         with_elem(a.out_dtype, [&](auto o) {
             using O = decltype(o);
