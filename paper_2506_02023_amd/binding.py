@@ -395,11 +395,13 @@ def _refuse(msg):
     raise MlipError(-1, msg)
 
 
-def _on_device(*tensors):
+def _stream_of(*tensors):
+    """The current stream of the current GPU, on which all tensors must lie."""
     here = torch.cuda.current_device()
     for t in tensors:
         if t.get_device() != here:
             _refuse("tensors must be on the current GPU")
+    return _raw_stream(here) if _raw_stream is not None else torch.cuda.current_stream().cuda_stream
 
 
 def _matrix(t, what):
@@ -442,8 +444,8 @@ def mlip_embed(table, species, scale=1.0, out=None):
     if out is None:
         out = table.new_empty((n,) if table.dim() == 1 else (n, width))
     out_dtype, out_rs = _output(out, n, width, table.dim() == 1)
-    _on_device(table, species, out)
-    _check(lib().mlip_embed(table.data_ptr(), dtype, rows, width, rs, cs, ids, bits, n, scale, out.data_ptr(), out_dtype, out_rs, _stream()))
+    stream = _stream_of(table, species, out)
+    _check(lib().mlip_embed(table.data_ptr(), dtype, rows, width, rs, cs, ids, bits, n, scale, out.data_ptr(), out_dtype, out_rs, stream))
     return out
 
 
@@ -461,12 +463,12 @@ def mlip_embed_grad(grad, species, n_species, scale=1.0, out=None, accumulate=Fa
             _refuse("accumulate needs out")
         out = grad.new_empty((n_species,) if grad.dim() == 1 else (n_species, width))
     out_dtype, out_rs = _output(out, n_species, width, grad.dim() == 1)
-    _on_device(grad, species, out)
+    stream = _stream_of(grad, species, out)
     L = lib()
     need = L.mlip_embed_grad_workspace(n, n_species, width)
     ws = torch.empty(need, dtype=torch.uint8, device="cuda") if need else None
     _check(L.mlip_embed_grad(grad.data_ptr(), dtype, rs, cs, ids, bits, n, n_species, width, scale, bool(accumulate), out.data_ptr(),
-                             out_dtype, out_rs, ws.data_ptr() if need else None, need, _stream()))
+                             out_dtype, out_rs, ws.data_ptr() if need else None, need, stream))
     return out
 
 

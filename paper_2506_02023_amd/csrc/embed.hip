@@ -288,7 +288,15 @@ struct FewPlan {
     }
 };
 
-constexpr int64_t kFewMost = kFewLds / 256 - 1;   // rows whose table fits a wavefront's LDS
+// Which way a table takes.  The tables' LDS leaves the fewer wavefronts to load the more rows there are, so rows that fill a wavefront (64 columns) pass to
+// the sort near 100; of narrow ones several lie in one wavefront's load, and the sort's cost by atom is paid back later.  Measured, us by LDS tables and by
+// sorting: a million rows of 64 into 64 57 and 77, into 89 68 and 75, into 119 85 and 75; 20,000 rows of 64 into 64 15 and 19, into 119 21 and 19;
+// 300,000 rows of 16 into 119 23 and 29, into 200 28 and 29, into 255 32 and 29; a million rows of 2 into 255 21 and 49.
+static bool takes_few(int64_t n_rows, int64_t width)
+{
+    const int64_t slots = width < 64 ? 64 / width : 1, most = 64 + 48 * slots;
+    return n_rows <= (most < kFewLds / 256 - 1 ? most : kFewLds / 256 - 1);
+}
 
 // Many rows: the ids are sorted (stable, by digits of at most 8 bits, places of the atoms along with them), so that every row's atoms lie one
 // after another in their order; spans of the sorted list are summed, whatever rows they hold, and a row that spans share is joined.
@@ -657,7 +665,7 @@ struct SortSpace {
 
 size_t embed_grad_workspace(int64_t n, int64_t n_rows, int64_t width)
 {
-    if (n_rows <= kFewMost) {
+    if (takes_few(n_rows, width)) {
         const FewPlan p(n, n_rows, width);
         return p.blocks > 1 ? (size_t)p.blocks * (size_t)n_rows * (size_t)width * 4 : 0;
     }
@@ -771,7 +779,7 @@ static int many_rows(const EmbedArgs &a, const GradOut &out)
 int embed_grad_impl(const EmbedArgs &a)
 {
         const GradOut out = {a.out, a.out_dtype, a.os, a.scale, a.accumulate};
-    return a.n_rows <= kFewMost ? few_rows(a, out) : many_rows(a, out);
+    return takes_few(a.n_rows, a.width) ? few_rows(a, out) : many_rows(a, out);
 }
 
 }  // namespace mlip

@@ -308,3 +308,56 @@ def test_streams_and_graphs():
             g.mul_(2.0)
             table.mul_(2.0)
             want, want_rows = M.mlip_embed_grad(g, species, rows), M.mlip_embed(table, species, 3.0)
+
+
+# around the sizes at which another way is taken: rows whose tables still fit the wavefronts' LDS, lists of one sort tile, a block's few steps
+LIMITS = [(4097, 111, 64), (4097, 112, 64), (4097, 113, 64), (900, 160, 32), (5000, 161, 32), (6000, 254, 16), (6000, 255, 16), (6000, 256, 16),
+          (2047, 300, 20), (2048, 300, 20), (2049, 300, 20), (4096, 2000, 5), (1024, 4, 64), (1025, 4, 64), (65535, 255, 2), (65537, 256, 2),
+          (2100, 65535, 3), (2100, 65536, 3), (300, 70000, 4), (5000, 400, 512), (2500, 300, 257)]
+
+
+@pytest.mark.parametrize("n,rows,width", LIMITS)
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_gradient_at_the_limits_of_the_ways(n, rows, width, dtype):
+    import torch
+    for kind in ("uniform", "hot"):
+        rng = np.random.default_rng([n, rows, width, len(kind)])
+        species = torch.as_tensor(_species(rng, n, rows, kind), dtype=torch.int32, device="cuda")
+        _check_grad(_matrix(rng, n, width, dtype, "rows"), species, rows, dtype)
+        _check_grad(_matrix(rng, n, width, dtype, "gap"), species, rows, "f32", scale=3.0)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_arrays_larger_than_the_caches(dtype):
+    """Gradients and results beyond 100 MB are read and written past the caches"""
+    import torch
+    import paper_2506_02023_amd as M
+    rng = np.random.default_rng(4)
+    width = 72 if dtype == "f32" else 520
+    n = 110_000_000 // (width * (4 if dtype == "f32" else 2))
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    g = torch.randn((n, width), generator=gen, device="cuda").to(_types()[dtype][0])
+    for rows in (8, 9000):
+        species = torch.as_tensor(_species(rng, n, rows, "hot"), dtype=torch.int32, device="cuda")
+        out = M.mlip_embed_grad(g, species, rows, out=torch.empty((rows, width), device="cuda")).double()
+        z = torch.zeros((rows, width), dtype=torch.float64, device="cuda")
+        s, a = z.index_add(0, species.long(), g.double()), z.index_add(0, species.long(), g.double().abs())
+        assert ((out - s).abs() <= RUN * U * a + 2 * U * s.abs()).all()
+        table = g[:rows]
+        assert torch.equal(M.mlip_embed(table, species), table[species.long()])
+    del out, s, a, z
+
+
+@pytest.mark.parametrize("rows", [5, 700])
+def test_sums_of_subnormal_numbers(rows):
+    """fp32 numbers below the normal range are not flushed: whole multiples of the smallest one add up exactly"""
+    import torch
+    import paper_2506_02023_amd as M
+    rng = np.random.default_rng(rows)
+    k = rng.integers(-50, 50, (3000, 8))
+    species = rng.integers(0, rows, 3000)
+    g = torch.as_tensor((k * 2.0 ** -149).astype(np.float32), device="cuda")
+    out = M.mlip_embed_grad(g, torch.as_tensor(species, device="cuda"), rows).double().cpu().numpy()
+    want = np.zeros((rows, 8))
+    np.add.at(want, species, k)
+    assert np.array_equal(out * 2.0 ** 149, want)
