@@ -119,8 +119,7 @@ __device__ inline Norm norm_of(double squares, float max_norm)
 __device__ inline double sum_parts(const double *part, int count)
 {
     double sum = 0.0;
-#pragma unroll 8
-    for (int k = threadIdx.x; k < count; k += kThreads) sum += part[k];
+    in_steps<8>(threadIdx.x, count, kThreads, [&](int64_t k) { return part[k]; }, [&](double x) { sum += x; });
     return block_sum(sum);
 }
 

@@ -46,6 +46,19 @@ template <class T> __device__ inline T to_elem(float v)
     if constexpr (sizeof(T) == 2) asm("" : "+v"(v));
     return (T)v;
 }
+// add(load(k)) for k = from, from + step, ... below end, in this order, U loads at a time (the last ones too: past the end the first one of the step
+// stands in, which is not added)
+template <int U, class Load, class Add> __device__ inline void in_steps(int64_t from, int64_t end, int64_t step, Load &&load, Add &&add)
+{
+    for (int64_t k = from; k < end; k += step * U) {
+        decltype(load(k)) x[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) x[u] = load(k + u * step < end ? k + u * step : k);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (k + u * step < end) add(x[u]);
+    }
+}
 #endif
 
 }  // namespace mlip

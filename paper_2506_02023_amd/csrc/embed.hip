@@ -250,8 +250,7 @@ __global__ __launch_bounds__(1024) void k_few_join(const float *part, int parts,
     const int64_t e = (int64_t)blockIdx.x * 16 + lane;
     double sum[1] = {0.0};
     if (e < elements) {
-#pragma unroll 8
-        for (int p = group; p < parts; p += 64) sum[0] += (double)part[p * elements + e];
+        in_steps<8>(group, parts, 64, [&](int64_t p) { return part[p * elements + e]; }, [&](float x) { sum[0] += (double)x; });
     }
     sum[0] += __shfl_xor(sum[0], 16);
     sum[0] += __shfl_xor(sum[0], 32);
@@ -364,7 +363,8 @@ __device__ inline void tile_ranks(const Pair (&item)[kSortRounds], int there, in
         const uint32_t d = (item[j].key >> shift) & ((1u << bits) - 1);
         const bool mine = tile_place(j) < there;
         uint64_t same = __ballot(mine);
-        for (int b = 0; b < bits; ++b) {
+#pragma unroll
+        for (int b = 0; b < 8; ++b) {   // bits that a shorter digit lacks are zero in all
             const uint64_t set = __ballot((d >> b) & 1);
             same &= (d >> b) & 1 ? set : ~set;
         }
