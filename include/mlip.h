@@ -388,7 +388,7 @@ int mlip_profile_read(mlip_graph_t *graph, float *ms /*HOST [MLIP_PROF_COUNT]*/,
 int mlip_copy_to_host(const mlip_graph_t *graph, void *dst_host, const void *src_device, size_t bytes);
 
 /*
- * Per-species parameter tables, for programs that fit a potential's parameters (appendix "Training": gradient steps on batches of
+ * Per-species parameter tables, for programs that fit a potential's parameters (the paper's appendix demonstrates training on batches of
  * structures).  A potential keeps one row of parameters for each species (its embedding, reference energies and scales of the
  * atoms' energies) or for each pair of species; a step of a fit looks rows up, sums the atoms' gradients by species and bounds
  * the norm of all gradients before the update.
@@ -420,8 +420,9 @@ int mlip_embed(const void *table, int32_t table_dtype, int64_t n_rows, int64_t w
  *   out     DEVICE [n_rows][width] of out_dtype, element (r, f) at r * out_row_stride + f
  *   workspace   DEVICE scratch of at least mlip_embed_grad_workspace(n, n_rows, width) bytes, aligned to 16 bytes; its
  *           contents do not matter before and mean nothing after the call
- * Sums run in the order of the atoms, over at most MLIP_EMBED_GRAD_RUN atoms at a time in fp32 and over those parts in fp64, and
- * are rounded to the output's type once.
+ * Sums run in the order of the atoms, over fewer than MLIP_EMBED_GRAD_RUN atoms at a time in fp32 and over those parts in fp64 (rounded to
+ * fp32 up to twice on the way: fewer than MLIP_EMBED_GRAD_RUN fp32 roundings in all), and are rounded to the output's type once.
+ * mlip_embed_grad_workspace returns 0 for sizes that the call refuses.
  */
 enum { MLIP_EMBED_GRAD_RUN = 1024 };
 size_t mlip_embed_grad_workspace(int64_t n, int64_t n_rows, int64_t width);
@@ -448,7 +449,7 @@ int mlip_grad_norm(const mlip_tensor_t *tensors, int32_t count, float *norm, voi
 
 /*
  * Norm as above, and dst = src * c for every element, with c = max_norm / norm where norm > max_norm and norm is finite, else
- * c = 1 (max_norm >= 0).  A norm that is infinite or NaN leaves the values as they are: the caller sees it in `norm` and drops
+ * c = 1 (max_norm >= 0; finite: as an fp32 number).  A norm that is infinite or NaN leaves the values as they are: the caller sees it in `norm` and drops
  * the step.  c is rounded to fp32, products are fp32, rounded to the tensor's type.  A tensor that is its own output is not
  * written where c = 1.
  */

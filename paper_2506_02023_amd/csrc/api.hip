@@ -531,11 +531,16 @@ int mlip_profile_read(mlip_graph_t *g, float *ms, int64_t *launches, int32_t res
 
 static bool aligned_to(const void *p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
 
+constexpr int64_t kMostRows = 0x7fffffff, kMostWidth = 1 << 20;
+static bool embed_sizes(int64_t n, int64_t n_rows, int64_t width)
+{
+    return n >= 0 && n <= kMostRows && n_rows >= 1 && n_rows <= kMostRows && width >= 1 && width <= kMostWidth;
+}
+
 // of both table calls: `in_rows` rows of the input matrix, `out_rows` of the output
 static int check_embed_args(const EmbedArgs &a, int64_t in_rows, int64_t out_rows)
 {
-    constexpr int64_t kMost = 0x7fffffff, kMostWidth = 1 << 20;
-    if (a.n < 0 || a.n > kMost || a.n_rows < 1 || a.n_rows > kMost || a.width < 1 || a.width > kMostWidth) {
+    if (!embed_sizes(a.n, a.n_rows, a.width)) {
         set_error("sizes outside their ranges (need 0 <= n < 2^31, 1 <= n_rows < 2^31, 1 <= width <= 2^20)");
         return MLIP_EINVAL;
     }
@@ -569,7 +574,7 @@ int mlip_embed(const void *table, int32_t table_dtype, int64_t n_rows, int64_t w
 
 size_t mlip_embed_grad_workspace(int64_t n, int64_t n_rows, int64_t width)
 {
-    return (n < 0 || n_rows < 1 || width < 1) ? 0 : embed_grad_workspace(n, n_rows, width);
+    return embed_sizes(n, n_rows, width) ? embed_grad_workspace(n, n_rows, width) : 0;
 }
 
 // scratch memory that a call with `need` > 0 bytes was given

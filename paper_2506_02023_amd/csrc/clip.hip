@@ -113,7 +113,7 @@ struct Norm { double norm; float coef; };
 __device__ inline Norm norm_of(double squares, float max_norm)
 {
     const double n = sqrt(squares);
-    return {n, n > (double)max_norm && n < (double)__builtin_inff() ? (float)((double)max_norm / n) : 1.f};
+    return {n, n > (double)max_norm && (float)n < __builtin_inff() ? (float)((double)max_norm / n) : 1.f};
 }
 
 __device__ inline double sum_parts(const double *part, int count)

@@ -169,9 +169,10 @@ struct GradOut {
 
 // Few rows: every wavefront keeps a table of all rows in LDS, 64 floats to a row, one for each lane: lane l owns column l % tile of the
 // wavefront's rows l / tile, l / tile + slots, ...  A lane adds its values to its own float of the row, so nothing collides and the order of
-// the additions is the order of the atoms.  (Read, add, write: an LDS addition without return takes 220 clocks a wavefront, 361 us where this
-// took 134 with the same loads, at a million rows of 64.)  A block then joins the lanes that own the same
-// column, and its wavefronts' tables.  Ids without a row go to one row more, which is not read.
+// the additions is the order of the atoms.  A block then joins the lanes that own the same column (fp64, rounded to fp32: one more fp32 addition to
+// the bound) and its wavefronts' tables (the same), k_few_join the blocks.  Ids without a row go to one row more, which is not read.
+// Reading the gradients bounds it: a million rows of 64 into 8 take 47 us, 5.5 TB/s, and the join 4.5; with LDS additions without return in place of
+// read, add and write (220 clocks a wavefront each) 361 us against 134 at the time.  Small and narrow calls are bound by the latency of the few steps.
 constexpr int kFewLds = 65536, kFewWaves = 16;
 constexpr int few_unroll(bool one) { return one ? 16 : 8; }   // rows of a lane in flight, as the registers of 8 wavefronts a SIMD hold
 
@@ -274,13 +275,14 @@ struct FewPlan {
         waves = waves < 1 ? 1 : waves > kFewWaves ? kFewWaves : waves;
         threads = 64 * (waves < 8 ? 8 : waves);
         // wavefronts: as many as have a step of rows in flight, at most two blocks a compute unit, but no more than
-        // MLIP_EMBED_GRAD_RUN rows a lane; where one block does with four steps, one block
+        // MLIP_EMBED_GRAD_RUN rows a lane; where one block does with four steps, one block (and no second launch to join)
         const int64_t step = (int64_t)slots * few_unroll(slots == 1);
         const int64_t most = 512 / tiles > 1 ? 512 / tiles : 1;
         int64_t b = (n + step * waves - 1) / (step * waves);
         b = b <= 4 ? 1 : b > most ? most : b;
         int64_t r = ((n + b * waves - 1) / (b * waves) + step - 1) / step * step;
-        if (r > (int64_t)slots * MLIP_EMBED_GRAD_RUN) r = (int64_t)slots * MLIP_EMBED_GRAD_RUN;
+        const int64_t run = MLIP_EMBED_GRAD_RUN - 16;   // (room for the two roundings to fp32 on the way to the blocks' join)
+        if (r > slots * run) r = slots * run;
         rows_per_wave = r > 0 ? r : step;
         b = (n + rows_per_wave * waves - 1) / (rows_per_wave * waves);
         blocks = (int)(b < 1 ? 1 : b);
@@ -298,8 +300,9 @@ static bool takes_few(int64_t n_rows, int64_t width)
 }
 
 // Many rows: the ids are sorted (stable, by digits of at most 8 bits, places of the atoms along with them), so that every row's atoms lie one
-// after another in their order; spans of the sorted list are summed, whatever rows they hold, and a row that spans share is joined.
-
+// after another in their order; spans of the sorted list are summed, whatever rows they hold, and a row that spans share is joined.  An item is 8 bytes, so
+// the sort's kernels are bound by latency (4 and 6 to 9 us a pass at 131,072 to 300,000 items), the sums by memory: 131,072 bf16 rows of 1024 into
+// 50,021 are read in 83 us along with the writing of the rows that lie in one span, 4.5 TB/s (without those writes 5.0), the rest written in 24.
 constexpr int kSortThreads = 1024, kSortTile = 2048, kSortBlocks = 256, kRadix = 256;
 
 struct Pair { uint32_t key, at; };
@@ -723,7 +726,9 @@ static int many_rows(const EmbedArgs &a, const GradOut &out)
                                                                                                row_end);
             return;
         }
-        k_digit_counts<<<p.blocks > 0 ? p.blocks : 1, kSortThreads, 0, a.stream>>>(ids, a.n, a.n_rows, p.range, 0, p.bits, counts, row_end);
+        const int64_t clear = (a.n_rows + kSortThreads * 8 - 1) / (kSortThreads * 8);   // blocks past the list's only clear
+        const int blocks = clear > kSortBlocks ? kSortBlocks : clear > p.blocks ? (int)clear : p.blocks;
+        k_digit_counts<<<blocks, kSortThreads, 0, a.stream>>>(ids, a.n, a.n_rows, p.range, 0, p.bits, counts, row_end);
         if (a.n > 0) k_digit_scatter<<<p.blocks, kSortThreads, 0, a.stream>>>(ids, a.n, a.n_rows, p.range, 0, p.bits, counts, list[0]);
     });
     for (int k = 1; k < p.passes && a.n > kSortTile; ++k) {
@@ -778,7 +783,7 @@ static int many_rows(const EmbedArgs &a, const GradOut &out)
 
 int embed_grad_impl(const EmbedArgs &a)
 {
-        const GradOut out = {a.out, a.out_dtype, a.os, a.scale, a.accumulate};
+    const GradOut out = {a.out, a.out_dtype, a.os, a.scale, a.accumulate};
     return takes_few(a.n_rows, a.width) ? few_rows(a, out) : many_rows(a, out);
 }
 

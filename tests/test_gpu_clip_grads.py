@@ -179,3 +179,13 @@ def test_streams_graphs_and_same_bits():
             mine = [torch.empty_like(t) for t in ts]
             norm = M.mlip_clip_grads(ts, 0.5, out=mine)
             want = mine
+
+
+@pytest.mark.parametrize("n", [10, 400_000])
+def test_a_norm_beyond_fp32_leaves_the_values(n):
+    """Finite values whose norm is no fp32 number"""
+    import torch
+    import paper_2506_02023_amd as M
+    ts = [torch.full((n,), 3e38, device="cuda")]
+    norm = M.mlip_clip_grads(ts, 1.0)
+    assert float(norm) == float("inf") and (ts[0] == 3e38).all()

@@ -361,3 +361,17 @@ def test_sums_of_subnormal_numbers(rows):
     want = np.zeros((rows, 8))
     np.add.at(want, species, k)
     assert np.array_equal(out * 2.0 ** 149, want)
+
+
+@pytest.mark.parametrize("n", [0, 700, 3000])
+def test_a_table_of_many_more_rows_than_atoms(n):
+    import torch
+    import paper_2506_02023_amd as M
+    rng = np.random.default_rng(n)
+    rows = 3_000_000
+    g = _matrix(rng, n, 5, "f32", "rows")
+    ids = _species(rng, n, rows)
+    out = torch.full((rows, 5), 9.0, device="cuda")
+    M.mlip_embed_grad(g, torch.as_tensor(ids, dtype=torch.int64, device="cuda"), rows, out=out)
+    s, a = _sums(g.double().cpu().numpy(), ids, rows)
+    assert (np.abs(out.double().cpu().numpy() - s) <= RUN * U * a + 2 * U * np.abs(s)).all()

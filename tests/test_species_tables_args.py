@@ -52,6 +52,14 @@ def test_gradient_refuses_a_small_workspace():
     assert L.mlip_embed_grad_workspace(-1, 4, 8) == 0
 
 
+def test_workspace_of_sizes_that_are_refused():
+    L = B.lib()
+    for sizes in ((-1, 4, 8), (1 << 31, 4, 8), (5, 0, 8), (5, 1 << 31, 8), (5, 4, 0), (5, 4, (1 << 20) + 1), (5, 4, 1 << 62), (1 << 62, 1 << 62, 1 << 62)):
+        assert L.mlip_embed_grad_workspace(*sizes) == 0
+    assert L.mlip_embed_grad_workspace((1 << 31) - 1, (1 << 31) - 1, 1 << 20) > 0
+    assert L.mlip_grad_workspace(-5) > 0
+
+
 def test_lookup_of_nothing_is_no_error():
     assert _embed(n=0, ids=None, out=None) == 0
 
