@@ -484,7 +484,7 @@ def _dense(t):
     return True
 
 
-_Tensor_of, _dtype_of, _shape_of = torch.Tensor, operator.attrgetter("dtype"), operator.attrgetter("shape")
+_Tensor_of, _dtype_of = torch.Tensor, operator.attrgetter("dtype")
 
 
 def _tensor_list(grads, out):
@@ -497,17 +497,17 @@ def _tensor_list(grads, out):
     if not plain and not all(map(_dense, grads)):
         _refuse("gradients must be dense")
     dst = src = list(map(_Tensor_of.data_ptr, grads))
+    sizes = list(map(_Tensor_of.numel, grads))
     if out is not None:
-        same = len(out) == len(grads) and list(map(_dtype_of, out)) == list(map(_dtype_of, grads)) and \
-            all(map(operator.eq, map(_shape_of, out), map(_shape_of, grads))) and \
-            (plain and all(map(_Tensor_of.is_contiguous, out)) or all(d.stride() == t.stride() for d, t in zip(out, grads)))
+        same = list(map(_DTYPES.get, map(_dtype_of, out))) == codes and list(map(_Tensor_of.numel, out)) == sizes and \
+            (plain and all(map(_Tensor_of.is_contiguous, out)) or all(d.shape == t.shape and d.stride() == t.stride() for d, t in zip(out, grads)))
         if not same:
-            _refuse("out must have a tensor for each gradient, of its type, shape and strides")
+            _refuse("out must have a tensor for each gradient, of its type, size and layout")
         dst = list(map(_Tensor_of.data_ptr, out))
     if not {torch.cuda.current_device()}.issuperset(map(_Tensor_of.get_device, itertools.chain(grads, out or ()))):
         _refuse("tensors must be on the current GPU")
     words = [0] * (4 * len(src))
-    words[::4], words[1::4], words[2::4], words[3::4] = src, dst, map(_Tensor_of.numel, grads), codes
+    words[::4], words[1::4], words[2::4], words[3::4] = src, dst, sizes, codes
     a = array.array("q", words)
     return a, a.buffer_info()[0], len(src)
 
@@ -531,7 +531,7 @@ def mlip_grad_norm(grads):
 def mlip_clip_grads(grads, max_norm, out=None):
     """Scales the tensors so that the norm of all of them together is at most max_norm; returns the norm before.
 
-    In place, or into the tensors of `out` (of the same types, shapes and strides).  Where the norm is infinite or NaN the values stay as
+    In place, or into the tensors of `out` (of the same types, sizes and layouts).  Where the norm is infinite or NaN the values stay as
     they are: a caller that reads the norm skips the step."""
     held, a, count = _tensor_list(grads, out)
     norm, ws, need = _norm_scratch(count)

@@ -31,6 +31,13 @@ template <int V> struct Lot {
         f = want < most ? want : most;
         skip = (int)(want - f);
     }
+    // the lots of a row in memory that begin at multiples of V elements there, but for the row's first and last
+    template <class O> __device__ Lot(int64_t number, int64_t width, const O *row)
+    {
+        const int64_t want = number * V - (int64_t)(reinterpret_cast<uintptr_t>(row) / sizeof(O) % V), most = width - V;
+        f = want < 0 ? 0 : want < most ? want : most;
+        skip = 0;
+    }
 };
 inline int64_t lots_of(int64_t width, int V) { return (width + V - 1) / V; }
 
@@ -64,40 +71,40 @@ template <int V, class T> __device__ inline void stream_cols(T *p, const float (
 }
 
 // ---- lookup: out[i][f] = scale * table[id_i][f].  A thread has a lot of columns of a row, and kEmbedUnroll of them at a time, a grid's size
-// apart.  Writing bounds it: a million rows of 64 fp32 take 43 us, 6.0 TB/s.
+// apart.  Writing bounds it: a million rows of 64 fp32 take 43 us, 6.0 TB/s.  Results that the caches do not hold are stored past them if their rows begin at
+// whole lots (47 us, 59 through the caches, at a million rows of 64); stored so, lots that share a line of memory cost more than they save (a million bf16 rows
+// of 33 46 us and 32), and the lots are shifted to where memory has whole ones (1,546,331 fp32 rows of 59: 83 us, 95 from the row's beginning on).
 
+enum { kPlain, kStreamed, kShifted };
 constexpr int kEmbedUnroll = 4;
 
-template <class T, class O, class Id, int V, bool Stream>
+template <class T, class O, class Id, int V, int Way>
 __global__ __launch_bounds__(256) void k_embed(const T *table, int64_t n_rows, int64_t width, int64_t rs, int64_t cs, const Id *ids,
                                                uint32_t items, uint32_t per_row, Div31 div, float scale, O *out, int64_t os)
 {
     constexpr int U = kEmbedUnroll;
     const uint32_t step = gridDim.x * 256;
     for (uint32_t e0 = blockIdx.x * 256 + threadIdx.x; e0 < items; e0 += step * U) {
-        uint32_t row[U], lot[U];
+        O *to[U];
         int64_t id[U];
         float v[U][V];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const uint32_t e = e0 + u * step < items ? e0 + u * step : e0;   // past the end: the first once more, not stored
-            row[u] = div(e);
-            lot[u] = e - row[u] * per_row;
-            id[u] = ids[row[u]];
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const Lot<V> l(lot[u], width);
-            load_cols<V>(v[u], table + (id[u] >= 0 && id[u] < n_rows ? id[u] : 0) * rs + (V == 1 ? l.f * cs : l.f));
+            const uint32_t row = div(e);
+            id[u] = ids[row];
+            to[u] = out + row * os;
+            const int64_t f = Way == kShifted ? Lot<V>(e - row * per_row, width, to[u]).f : Lot<V>(e - row * per_row, width).f;
+            to[u] += f;
+            load_cols<V>(v[u], table + (id[u] >= 0 && id[u] < n_rows ? id[u] : 0) * rs + (V == 1 ? f * cs : f));
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (u > 0 && e0 + u * step >= items) break;
-            const Lot<V> l(lot[u], width);
 #pragma unroll
             for (int k = 0; k < V; ++k) v[u][k] = id[u] < 0 ? 0.f : id[u] < n_rows ? v[u][k] * scale : __builtin_nanf("");
-            if (Stream) stream_cols<V>(out + row[u] * os + l.f, v[u]);
-            else store_cols<V>(out + row[u] * os + l.f, v[u]);
+            if (Way == kStreamed) stream_cols<V>(to[u], v[u]);
+            else store_cols<V>(to[u], v[u]);
         }
     }
 }
@@ -113,8 +120,9 @@ int embed_impl(const EmbedArgs &a)
                 using Id = decltype(id);
                 constexpr int V = sizeof(T) == 2 || sizeof(O) == 2 ? 8 : 4;   // 16 bytes of the smaller type
                 const bool wide = (a.cs == 1 || a.width == 1) && a.width >= V;
-                const bool stream = (double)a.n * (double)a.width * sizeof(O) > kStreamBytes;
-                const int64_t per_row = wide ? lots_of(a.width, V) : a.width;
+                const bool large = (double)a.n * (double)a.width * sizeof(O) > kStreamBytes;
+                const bool even = reinterpret_cast<uintptr_t>(a.out) % (V * sizeof(O)) == 0 && a.os % V == 0;
+                const int64_t per_row = !wide ? a.width : lots_of(large && !even ? a.width + V - 1 : a.width, V);
                 const int64_t most = ((int64_t)1 << 30) / per_row;   // rows of a launch: items are numbered in 31 bits
                 const Div31 div((uint32_t)per_row);
                 for (int64_t i0 = 0; i0 < a.n; i0 += most) {
@@ -125,8 +133,9 @@ int embed_impl(const EmbedArgs &a)
                             static_cast<const T *>(a.in), a.n_rows, a.width, a.rs, a.cs, static_cast<const Id *>(a.ids) + i0, (uint32_t)items,
                             (uint32_t)per_row, div, a.scale, static_cast<O *>(a.out) + i0 * a.os, a.os);
                     };
-                    if (!wide) launch(k_embed<T, O, Id, 1, false>);
-                    else stream ? launch(k_embed<T, O, Id, V, true>) : launch(k_embed<T, O, Id, V, false>);
+                    if (!wide) launch(k_embed<T, O, Id, 1, kPlain>);
+                    else if (!large) launch(k_embed<T, O, Id, V, kPlain>);
+                    else even ? launch(k_embed<T, O, Id, V, kStreamed>) : launch(k_embed<T, O, Id, V, kShifted>);
                 }
             });
         });
@@ -292,10 +301,11 @@ struct FewPlan {
 // Which way a table takes.  The tables' LDS leaves the fewer wavefronts to load the more rows there are, so rows that fill a wavefront (64 columns) pass to
 // the sort near 100; of narrow ones several lie in one wavefront's load, and the sort's cost by atom is paid back later.  Measured, us by LDS tables and by
 // sorting: a million rows of 64 into 64 57 and 77, into 89 68 and 75, into 119 85 and 75; 20,000 rows of 64 into 64 15 and 19, into 119 21 and 19;
-// 300,000 rows of 16 into 119 23 and 29, into 200 28 and 29, into 255 32 and 29; a million rows of 2 into 255 21 and 49.
-static bool takes_few(int64_t n_rows, int64_t width)
+// 300,000 rows of 16 into 119 23 and 29, into 200 28 and 29, into 255 32 and 29; a million rows of 2 into 255 21 and 49; 4000 rows of 64 into 119 13 and 18,
+// into 160 19 and 18, 1000 into 200 15 and 16: the sort's launches count for more where there is little to load.
+static bool takes_few(int64_t n, int64_t n_rows, int64_t width)
 {
-    const int64_t slots = width < 64 ? 64 / width : 1, most = 64 + 48 * slots;
+    const int64_t slots = width < 64 ? 64 / width : 1, most = 64 + 48 * slots + (n <= 4096 ? 48 : 0);
     return n_rows <= (most < kFewLds / 256 - 1 ? most : kFewLds / 256 - 1);
 }
 
@@ -668,7 +678,7 @@ struct SortSpace {
 
 size_t embed_grad_workspace(int64_t n, int64_t n_rows, int64_t width)
 {
-    if (takes_few(n_rows, width)) {
+    if (takes_few(n, n_rows, width)) {
         const FewPlan p(n, n_rows, width);
         return p.blocks > 1 ? (size_t)p.blocks * (size_t)n_rows * (size_t)width * 4 : 0;
     }
@@ -784,7 +794,7 @@ static int many_rows(const EmbedArgs &a, const GradOut &out)
 int embed_grad_impl(const EmbedArgs &a)
 {
     const GradOut out = {a.out, a.out_dtype, a.os, a.scale, a.accumulate};
-    return takes_few(a.n_rows, a.width) ? few_rows(a, out) : many_rows(a, out);
+    return takes_few(a.n, a.n_rows, a.width) ? few_rows(a, out) : many_rows(a, out);
 }
 
 }  // namespace mlip

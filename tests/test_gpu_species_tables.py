@@ -375,3 +375,23 @@ def test_a_table_of_many_more_rows_than_atoms(n):
     M.mlip_embed_grad(g, torch.as_tensor(ids, dtype=torch.int64, device="cuda"), rows, out=out)
     s, a = _sums(g.double().cpu().numpy(), ids, rows)
     assert (np.abs(out.double().cpu().numpy() - s) <= RUN * U * a + 2 * U * np.abs(s)).all()
+
+
+@pytest.mark.parametrize("width", [33, 59, 64, 90])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_large_results_of_any_alignment(width, dtype):
+    """Results beyond 100 MB whose rows begin at any alignment, with and without gaps between them"""
+    import torch
+    import paper_2506_02023_amd as M
+    dt = _types()[dtype][0]
+    n = 104_000_000 // (width * (4 if dtype == "f32" else 2))
+    gen = torch.Generator(device="cuda").manual_seed(width)
+    table = torch.randn((300, width), generator=gen, device="cuda").to(dt)
+    species = torch.randint(-3, 300, (n,), generator=gen, device="cuda")
+    want = torch.where((species >= 0)[:, None], table[species.clamp(min=0)], 0.0)
+    assert torch.equal(M.mlip_embed(table, species), want)
+    for offset, gap in ((1, 0), (0, 3), (5, 7)):
+        whole = torch.full((offset + n * (width + gap),), 7.0, dtype=dt, device="cuda")
+        out = whole[offset:].view(n, width + gap)[:, :width]
+        M.mlip_embed(table, species, out=out)
+        assert torch.equal(out, want) and (whole[:offset] == 7).all() and (whole[offset:].view(n, width + gap)[:, width:] == 7).all()
