@@ -188,18 +188,24 @@ constexpr int few_unroll(bool one) { return one ? 16 : 8; }   // rows of a lane 
 // One: one row a step (wider than 32 columns), whose id is the same for the wavefront's lanes; Near: the lanes' elements of a step lie within 4 GB.
 template <class T, class Id, bool One, bool Near, bool Stream>
 __global__ __launch_bounds__(1024, 8) void k_few_rows(const T *grad, int64_t rs, int64_t cs, const Id *ids, int64_t n, int n_rows, int64_t width,
-                                                      int tile, int slots, int waves, int64_t rows_per_wave, float *part, GradOut out)
+                                                      int tile, int slots, int waves, int64_t rows_per_wave, int chunks, bool grouped, float *part,
+                                                      GradOut out)
 {
     extern __shared__ float tables[];
+    // Blocks go to the eight XCDs in turn.  Grouped: the tiles of a chunk of rows are consecutive on one of them, whose L2 has the lines that the tiles
+    // share (300,000 fp32 rows of 257 into 8: 66 us, 79 chunk by chunk).  Tiles of whole lines share none (100,000 rows of 512 into 64: 55 us either way).
+    const int tiles = (int)((width + tile - 1) / tile), b = (int)blockIdx.x;
+    const int chunk = grouped ? (b >> 3) / tiles * 8 + (b & 7) : b % chunks, tile_at = grouped ? (b >> 3) % tiles : b / chunks;
+    if (chunk >= chunks) return;
     constexpr int U = few_unroll(One);
     if (One) slots = 1;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), size = (n_rows + 1) * 64;
     float *mine = tables + wave * size;
     for (int k = threadIdx.x; k < waves * size; k += blockDim.x) tables[k] = 0.f;
     __syncthreads();
-    const int64_t f0 = (int64_t)blockIdx.y * tile;
+    const int64_t f0 = (int64_t)tile_at * tile;
     const int cols = (int)(width - f0 < tile ? width - f0 : tile), slot = One ? 0 : lane / tile, col = lane - slot * tile;
-    const int64_t r0 = ((int64_t)blockIdx.x * waves + wave) * rows_per_wave, r1 = n - r0 < rows_per_wave ? n : r0 + rows_per_wave;
+    const int64_t r0 = ((int64_t)chunk * waves + wave) * rows_per_wave, r1 = n - r0 < rows_per_wave ? n : r0 + rows_per_wave;
     if (wave < waves && slot < slots && col < cols) {
         using Offset = std::conditional_t<Near, uint32_t, int64_t>;
         const Offset mine_at = (Offset)(slot * rs + col * cs);
@@ -247,7 +253,7 @@ __global__ __launch_bounds__(1024, 8) void k_few_rows(const T *grad, int64_t rs,
         double sum[1] = {0.0};
 #pragma unroll 4
         for (int w = 0; w < waves; ++w) sum[0] += (double)tables[w * size + r * 64 + c];
-        if (part) part[((int64_t)blockIdx.x * n_rows + r) * width + f0 + c] = (float)sum[0];
+        if (part) part[((int64_t)chunk * n_rows + r) * width + f0 + c] = (float)sum[0];
         else out.put<1>(r, f0 + c, 0, sum);
     }
 }
@@ -283,10 +289,13 @@ struct FewPlan {
         waves = (int)(kFewLds / ((n_rows + 1) * 256));
         waves = waves < 1 ? 1 : waves > kFewWaves ? kFewWaves : waves;
         threads = 64 * (waves < 8 ? 8 : waves);
-        // wavefronts: as many as have a step of rows in flight, at most two blocks a compute unit, but no more than
+        // wavefronts: as many as have a step of rows in flight, at most the blocks that are resident together (two a compute unit where several rows lie
+        // in one load and more blocks only are more to join: a million rows of 2 into 89 15 us, 18; of 64 into 89 81, 68), but no more than
         // MLIP_EMBED_GRAD_RUN rows a lane; where one block does with four steps, one block (and no second launch to join)
         const int64_t step = (int64_t)slots * few_unroll(slots == 1);
-        const int64_t most = 512 / tiles > 1 ? 512 / tiles : 1;
+        const int lds = waves * (int)(n_rows + 1) * 256, fit = 163840 / lds < 2048 / threads ? 163840 / lds : 2048 / threads;
+        const int resident = 256 * (slots > 1 && fit > 2 ? 2 : fit);
+        const int64_t most = tiles * 8 <= resident ? resident / tiles / 8 * 8 : tiles <= resident ? resident / tiles : 1;   // (as many for each XCD)
         int64_t b = (n + step * waves - 1) / (step * waves);
         b = b <= 4 ? 1 : b > most ? most : b;
         int64_t r = ((n + b * waves - 1) / (b * waves) + step - 1) / step * step;
@@ -298,14 +307,14 @@ struct FewPlan {
     }
 };
 
-// Which way a table takes.  The tables' LDS leaves the fewer wavefronts to load the more rows there are, so rows that fill a wavefront (64 columns) pass to
-// the sort near 100; of narrow ones several lie in one wavefront's load, and the sort's cost by atom is paid back later.  Measured, us by LDS tables and by
-// sorting: a million rows of 64 into 64 57 and 77, into 89 68 and 75, into 119 85 and 75; 20,000 rows of 64 into 64 15 and 19, into 119 21 and 19;
-// 300,000 rows of 16 into 119 23 and 29, into 200 28 and 29, into 255 32 and 29; a million rows of 2 into 255 21 and 49; 4000 rows of 64 into 119 13 and 18,
-// into 160 19 and 18, 1000 into 200 15 and 16: the sort's launches count for more where there is little to load.
+// Which way a table takes.  The tables' LDS leaves the fewer wavefronts to load the more rows there are, so rows that fill a wavefront (33 columns and more) pass
+// to the sort at 80; of narrow ones several lie in one wavefront's load, and the sort's cost by atom is paid back later; where there is little to load the sort's
+// launches count for more.  Measured, us by LDS tables and by sorting: a million rows of 64 into 64 61 and 77, into 89 70 and 75, into 119 85 and 75; 20,000
+// rows of 64 into 64 16 and 19, into 89 24 and 19; 100,000 of 512 into 64 55 and 57, into 89 67 and 57; 300,000 rows of 16 into 119 22 and 29, into 200
+// 28 and 29, into 255 31 and 29; a million rows of 2 into 255 20 and 49; 4000 rows of 64 into 119 13 and 18, into 160 19 and 18.
 static bool takes_few(int64_t n, int64_t n_rows, int64_t width)
 {
-    const int64_t slots = width < 64 ? 64 / width : 1, most = 64 + 48 * slots + (n <= 4096 ? 48 : 0);
+    const int64_t slots = width < 64 ? 64 / width : 1, most = 32 + 48 * slots + (n <= 4096 ? 64 : 0);
     return n_rows <= (most < kFewLds / 256 - 1 ? most : kFewLds / 256 - 1);
 }
 
@@ -685,20 +694,33 @@ size_t embed_grad_workspace(int64_t n, int64_t n_rows, int64_t width)
     return SortSpace(n, n_rows, width).bytes;
 }
 
+// whether the gradients' rows begin at whole lines of memory
+static bool whole_lines(const EmbedArgs &a)
+{
+    return reinterpret_cast<uintptr_t>(a.in) % 128 == 0 && a.rs * (int64_t)elem_size(a.in_dtype) % 128 == 0;
+}
+
+// Whether they are read past the caches: where there are more than the caches hold and rows share no lines.  (Lines that rows or tiles of
+// columns share are better kept: a million bf16 rows of 77 into 8 60 us, 69 past the caches; of 800,000 fp32 rows of 64 42 and 37.)
+static bool streams(const EmbedArgs &a)
+{
+    return (double)a.n * (double)a.width * (double)elem_size(a.in_dtype) > kStreamBytes && whole_lines(a);
+}
+
 static int few_rows(const EmbedArgs &a, const GradOut &out)
 {
     const FewPlan p(a.n, a.n_rows, a.width);
     float *part = p.blocks > 1 ? static_cast<float *>(a.workspace) : nullptr;
-    const bool stream = (double)a.n * (double)a.width * (double)elem_size(a.in_dtype) > kStreamBytes;
+    const bool stream = streams(a), grouped = p.blocks >= 8 && p.tiles > 1 && !(whole_lines(a) && p.tile * elem_size(a.in_dtype) % 128 == 0);
     const bool near = ((double)p.slots * (double)a.rs + (double)p.tile * (double)a.cs) * 4.0 < 4e9;
     with_elem(a.in_dtype, [&](auto t) {
         with_ids(a.id_bits, [&](auto id) {
             using T = decltype(t);
             using Id = decltype(id);
             auto launch = [&](auto kernel) {
-                kernel<<<dim3(p.blocks, p.tiles), p.threads, (size_t)p.waves * (a.n_rows + 1) * 256, a.stream>>>(
+                kernel<<<(unsigned)((grouped ? (p.blocks + 7) / 8 * 8 : p.blocks) * p.tiles), p.threads, (size_t)p.waves * (a.n_rows + 1) * 256, a.stream>>>(
                     static_cast<const T *>(a.in), a.rs, a.cs, static_cast<const Id *>(a.ids), a.n, (int)a.n_rows, a.width, p.tile, p.slots,
-                    p.waves, p.rows_per_wave, part, out);
+                    p.waves, p.rows_per_wave, p.blocks, grouped, part, out);
             };
             auto pick = [&](auto one, auto close) {
                 stream ? launch(k_few_rows<T, Id, one.value, close.value, true>) : launch(k_few_rows<T, Id, one.value, close.value, false>);
@@ -751,7 +773,7 @@ static int many_rows(const EmbedArgs &a, const GradOut &out)
         with_elem(a.in_dtype, [&](auto t) {
             using T = decltype(t);
             const int64_t spans = (a.n + w.span - 1) / w.span;
-            const bool stream = (double)a.n * (double)a.width * sizeof(T) > kStreamBytes;
+            const bool stream = streams(a);
             with_elem(a.out_dtype, [&](auto o) {
                 using O = decltype(o);
                 constexpr int V = 16 / sizeof(T);

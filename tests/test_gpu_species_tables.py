@@ -395,3 +395,13 @@ def test_large_results_of_any_alignment(width, dtype):
         out = whole[offset:].view(n, width + gap)[:, :width]
         M.mlip_embed(table, species, out=out)
         assert torch.equal(out, want) and (whole[:offset] == 7).all() and (whole[offset:].view(n, width + gap)[:, width:] == 7).all()
+
+
+@pytest.mark.parametrize("n,rows,width", [(5000, 80, 64), (5000, 81, 64), (4096, 144, 64), (4096, 145, 64), (5000, 128, 32), (5000, 129, 32), (5000, 224, 16),
+                                          (5000, 225, 16), (30000, 8, 257), (30000, 8, 500), (40000, 60, 512), (2000, 3, 4200), (60, 5, 9000)])
+def test_gradient_of_few_rows_and_tiles_of_columns(n, rows, width):
+    import torch
+    rng = np.random.default_rng([n, rows, width])
+    species = torch.as_tensor(_species(rng, n, rows, "hot"), dtype=torch.int32, device="cuda")
+    for dtype, layout in (("f32", "rows"), ("bf16", "rows"), ("f32", "gap")):
+        _check_grad(_matrix(rng, n, width, dtype, layout), species, rows, "f32")
