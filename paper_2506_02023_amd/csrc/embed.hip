@@ -180,7 +180,7 @@ struct GradOut {
 // wavefront's rows l / tile, l / tile + slots, ...  A lane adds its values to its own float of the row, so nothing collides and the order of
 // the additions is the order of the atoms.  A block then joins the lanes that own the same column (fp64, rounded to fp32: one more fp32 addition to
 // the bound) and its wavefronts' tables (the same), k_few_join the blocks.  Ids without a row go to one row more, which is not read.
-// Reading the gradients bounds it: a million rows of 64 into 8 take 47 us, 5.5 TB/s, and the join 4.5; with LDS additions without return in place of
+// Reading the gradients bounds it: a million rows of 64 into 8 take 48 us, 5.4 TB/s, and the join 4.5; with LDS additions without return in place of
 // read, add and write (220 clocks a wavefront each) 361 us against 134 at the time.  Small and narrow calls are bound by the latency of the few steps.
 constexpr int kFewLds = 65536, kFewWaves = 16;
 constexpr int few_unroll(bool one) { return one ? 16 : 8; }   // rows of a lane in flight, as the registers of 8 wavefronts a SIMD hold
