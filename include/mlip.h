@@ -404,7 +404,8 @@ enum { MLIP_DTYPE_F32 = 0, MLIP_DTYPE_BF16 = 1, MLIP_DTYPE_F16 = 2 };
  * Lookup: out[i][f] = scale * table[ids[i]][f], the product in fp32, rounded once to the output's type.
  *   table   DEVICE [n_rows][width] of table_dtype, element (r, f) at r * table_row_stride + f * table_col_stride (in elements, >= 0)
  *   ids     DEVICE [n] int32 (id_bits = 32) or int64 (id_bits = 64).  A negative id stands for a place that pads a batch: its row
- *           is zeros.  An id >= n_rows has no row: nothing is read for it and its row is NaN, so that it does not pass unnoticed.
+ *           is zeros.  An id >= n_rows has no row in the table: its
+ *           row here is NaN, so that it does not pass unnoticed.
  *   out     DEVICE [n][width] of out_dtype, element (i, f) at i * out_row_stride + f, out_row_stride >= width
  * n may be 0; 1 <= n_rows < 2^31, 1 <= width <= 2^20, n < 2^31.
  */
