@@ -33,6 +33,17 @@ template <class Fn> inline void with_ids(int32_t id_bits, Fn &&f)
 // gradient into few rows of 32 MB 16.4 and 15.5, 96 MB 22.8 and 23.4, 256 MB 51 and 55, into many of 64 MB 53 and 50.5, 128 MB 69 and 71.
 constexpr double kStreamBytes = 100e6;
 
+// Blocks that a launch has at most, a multiple of eight so that the XCDs' turn goes on from launch to launch: HIP takes a grid's threads modulo 2^32, with
+// no error, and leaves the other blocks out.
+inline int64_t most_blocks(int threads) { return 0xffffffffll / threads / 8 * 8; }
+
+// launch(first block, blocks) for `blocks` blocks, in as many launches as that takes
+template <class Fn> inline void launch_blocks(int64_t blocks, int threads, Fn &&launch)
+{
+    const int64_t most = most_blocks(threads);
+    for (int64_t b = 0; b < blocks; b += most) launch(b, (unsigned)(blocks - b < most ? blocks - b : most));
+}
+
 // V elements, as one access has them
 template <class T, int V> using Cols = T __attribute__((ext_vector_type(V)));
 template <class T, int V> struct FarT { typedef T type __attribute__((ext_vector_type(V), aligned(sizeof(T)))); };

@@ -188,14 +188,15 @@ constexpr int few_unroll(bool one) { return one ? 16 : 8; }   // rows of a lane 
 // One: one row a step (wider than 32 columns), whose id is the same for the wavefront's lanes; Near: the lanes' elements of a step lie within 4 GB.
 template <class T, class Id, bool One, bool Near, bool Stream>
 __global__ __launch_bounds__(1024, 8) void k_few_rows(const T *grad, int64_t rs, int64_t cs, const Id *ids, int64_t n, int n_rows, int64_t width,
-                                                      int tile, int slots, int waves, int64_t rows_per_wave, int chunks, bool grouped, float *part,
-                                                      GradOut out)
+                                                      int tile, int slots, int waves, int64_t rows_per_wave, int chunks, bool grouped, int64_t block0,
+                                                      float *part, GradOut out)
 {
     extern __shared__ float tables[];
     // Blocks go to the eight XCDs in turn.  Grouped: the tiles of a chunk of rows are consecutive on one of them, whose L2 has the lines that the tiles
     // share (300,000 fp32 rows of 257 into 8: 66 us, 79 chunk by chunk).  Tiles of whole lines share none (100,000 rows of 512 into 64: 55 us either way).
-    const int tiles = (int)((width + tile - 1) / tile), b = (int)blockIdx.x;
-    const int chunk = grouped ? (b >> 3) / tiles * 8 + (b & 7) : b % chunks, tile_at = grouped ? (b >> 3) % tiles : b / chunks;
+    const int tiles = (int)((width + tile - 1) / tile);
+    const uint32_t b = (uint32_t)block0 + blockIdx.x;   // (2^32 blocks have more parts than memory holds)
+    const int chunk = (int)(grouped ? (b >> 3) / tiles * 8 + (b & 7) : b % chunks), tile_at = (int)(grouped ? (b >> 3) % tiles : b / chunks);
     if (chunk >= chunks) return;
     constexpr int U = few_unroll(One);
     if (One) slots = 1;
@@ -259,11 +260,11 @@ __global__ __launch_bounds__(1024, 8) void k_few_rows(const T *grad, int64_t rs,
 }
 
 // sum over the blocks of k_few_rows: a block has 16 elements, whose parts 64 groups of 16 lanes share
-__global__ __launch_bounds__(1024) void k_few_join(const float *part, int parts, int64_t elements, int64_t width, GradOut out)
+__global__ __launch_bounds__(1024) void k_few_join(const float *part, int parts, int64_t elements, int64_t width, int64_t block0, GradOut out)
 {
     __shared__ double red[16][16];
     const int lane = threadIdx.x & 15, group = threadIdx.x >> 4;
-    const int64_t e = (int64_t)blockIdx.x * 16 + lane;
+    const int64_t e = (block0 + blockIdx.x) * 16 + lane;
     double sum[1] = {0.0};
     if (e < elements) {
         in_steps<8>(group, parts, 64, [&](int64_t p) { return part[p * elements + e]; }, [&](float x) { sum[0] += (double)x; });
@@ -591,12 +592,13 @@ __global__ __launch_bounds__(256) void k_span_sums(const Pair *sorted, const T *
 
 // Rows that no id names, and rows that spans share.  A thread has V columns of a row and adds up what at most kJoinSerial spans hold of it;
 // a row of more spans is the work of one of the first `heavy` blocks (64 such lots of columns at most): block b looks at span b * kJoinSerial, and if the row
-// that runs into this span from before is such a row, and no earlier block sees it, shares the row's spans out over its threads.
+// that runs into this span from before is such a row, and no earlier block sees it, shares the row's spans out over its threads.  heavy0: of them, those
+// of the launches before.
 constexpr int kJoinSerial = 8, kJoinUnroll = 2;   // the second: rows looked up at a time
 
 template <class O, int V>
 __global__ __launch_bounds__(256) void k_row_join(const Pair *sorted, const uint32_t *row_begin, const uint32_t *row_end, const float *edge,
-                                                  int shift, int heavy, uint32_t items, uint32_t per_row, Div31 div, int64_t row0,
+                                                  int shift, uint32_t heavy0, uint32_t heavy, uint32_t items, uint32_t per_row, Div31 div, int64_t row0,
                                                   int64_t n_rows, int64_t width, GradOut out)
 {
     __shared__ double red[256][V];
@@ -606,15 +608,16 @@ __global__ __launch_bounds__(256) void k_row_join(const Pair *sorted, const uint
 #pragma unroll
         for (int k = 0; k < V; ++k) sum[k] += (double)v[k];
     };
-    if ((int)blockIdx.x < heavy) {
-        const int tiles = (per_row + 63) / 64, lanes = per_row < 64 ? per_row : 64, groups = 256 / lanes;
-        const int64_t at = ((int64_t)blockIdx.x / tiles + 1) * kJoinSerial;
+    if (blockIdx.x < heavy) {
+        const uint32_t tiles = (per_row + 63) / 64, heavy_at = heavy0 + blockIdx.x;   // (2^32 of them have more parts than memory holds)
+        const int lanes = per_row < 64 ? per_row : 64, groups = 256 / lanes;
+        const int64_t at = ((int64_t)(heavy_at / tiles) + 1) * kJoinSerial;
         const uint32_t r = sorted[at << shift].key;
         if (r >= n_rows) return;
         const int64_t first = row_begin[r] >> shift, last = (row_end[r] - 1) >> shift;
         if (last - first < kJoinSerial || first >= at || first < at - kJoinSerial) return;
         const int group = threadIdx.x / lanes;
-        const int64_t number = (int64_t)(blockIdx.x % tiles) * lanes + threadIdx.x % lanes;
+        const int64_t number = (int64_t)(heavy_at % tiles) * lanes + threadIdx.x % lanes;
         const bool mine = group < groups && number < per_row;
         const Lot<V> lot(number, width);
         double sum[V];
@@ -718,9 +721,11 @@ static int few_rows(const EmbedArgs &a, const GradOut &out)
             using T = decltype(t);
             using Id = decltype(id);
             auto launch = [&](auto kernel) {
-                kernel<<<(unsigned)((grouped ? (p.blocks + 7) / 8 * 8 : p.blocks) * p.tiles), p.threads, (size_t)p.waves * (a.n_rows + 1) * 256, a.stream>>>(
-                    static_cast<const T *>(a.in), a.rs, a.cs, static_cast<const Id *>(a.ids), a.n, (int)a.n_rows, a.width, p.tile, p.slots,
-                    p.waves, p.rows_per_wave, p.blocks, grouped, part, out);
+                launch_blocks((int64_t)(grouped ? (p.blocks + 7) / 8 * 8 : p.blocks) * p.tiles, p.threads, [&](int64_t block0, unsigned blocks) {
+                    kernel<<<blocks, p.threads, (size_t)p.waves * (a.n_rows + 1) * 256, a.stream>>>(
+                        static_cast<const T *>(a.in), a.rs, a.cs, static_cast<const Id *>(a.ids), a.n, (int)a.n_rows, a.width, p.tile, p.slots,
+                        p.waves, p.rows_per_wave, p.blocks, grouped, block0, part, out);
+                });
             };
             auto pick = [&](auto one, auto close) {
                 stream ? launch(k_few_rows<T, Id, one.value, close.value, true>) : launch(k_few_rows<T, Id, one.value, close.value, false>);
@@ -732,7 +737,9 @@ static int few_rows(const EmbedArgs &a, const GradOut &out)
     MLIP_HIP(hipGetLastError());
     if (part) {
         const int64_t elements = a.n_rows * a.width;
-        k_few_join<<<(unsigned)((elements + 15) / 16), 1024, 0, a.stream>>>(part, p.blocks, elements, a.width, out);
+        launch_blocks((elements + 15) / 16, 1024, [&](int64_t block0, unsigned blocks) {
+            k_few_join<<<blocks, 1024, 0, a.stream>>>(part, p.blocks, elements, a.width, block0, out);
+        });
         MLIP_HIP(hipGetLastError());
     }
     return MLIP_OK;
@@ -781,6 +788,7 @@ static int many_rows(const EmbedArgs &a, const GradOut &out)
                 const int64_t per_row = wide ? lots_of(a.width, V) : a.width;
                 const int lanes = (int)(per_row < 64 ? per_row : 64);
                 const int64_t groups = 256 / lanes;
+                // (2^31 items in spans of 64, four spans or more to a block of 256 threads: not half of what one launch has)
                 const dim3 grid((unsigned)((spans + groups - 1) / groups), (unsigned)((per_row + lanes - 1) / lanes));
                 auto launch = [&](auto kernel) {
                     kernel<<<grid, 256, 0, a.stream>>>(sorted, static_cast<const T *>(a.in), a.rs, a.cs, a.n, a.n_rows, a.width, lanes, w.span,
@@ -800,9 +808,15 @@ static int many_rows(const EmbedArgs &a, const GradOut &out)
         const int64_t rows = a.n_rows - r0 < most ? a.n_rows - r0 : most, items = rows * per_row, blocks = (items + 256 * kJoinUnroll - 1) / (256 * kJoinUnroll);
         // spans kJoinSerial, 2 kJoinSerial, ... that there are, each for every 64 lots of columns; once
         const int64_t heavy = r0 == 0 && a.n > 0 ? ((a.n + w.span - 1) / w.span - 1) / kJoinSerial * ((per_row + 63) / 64) : 0;
+        const int64_t light = blocks < 16384 ? blocks : 16384;
         auto launch = [&](auto kernel) {
-            kernel<<<(unsigned)((blocks < 16384 ? blocks : 16384) + heavy), 256, 0, a.stream>>>(
-                sorted, row_begin, row_end, edge, __builtin_ctz((unsigned)w.span), (int)heavy, (uint32_t)items, (uint32_t)per_row, div, r0, a.n_rows, a.width, out);
+            const int64_t most = most_blocks(256) - light;
+            for (int64_t h = 0; h == 0 || h < heavy; h += most) {
+                const int64_t some = heavy - h < most ? heavy - h : most;
+                kernel<<<(unsigned)(some + (h + some == heavy ? light : 0)), 256, 0, a.stream>>>(
+                    sorted, row_begin, row_end, edge, __builtin_ctz((unsigned)w.span), (uint32_t)h, (uint32_t)some, (uint32_t)items, (uint32_t)per_row, div, r0,
+                    a.n_rows, a.width, out);
+            }
         };
         with_elem(a.out_dtype, [&](auto o) {
             using O = decltype(o);
