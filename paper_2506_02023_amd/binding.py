@@ -490,6 +490,7 @@ _Tensor_of, _dtype_of = torch.Tensor, operator.attrgetter("dtype")
 def _tensor_list(grads, out):
     """The tensors as the library takes them (an array of _Tensor, as 64-bit words), checked.  Lists run to hundreds of tensors, so
     each property is taken of all of them in one map."""
+    grads, out = list(grads), None if out is None else list(out)   # (an iterator would be used up by the first of the maps)
     codes = list(map(_DTYPES.get, map(_dtype_of, grads)))
     if None in codes:
         _refuse("gradients must be float32, bfloat16 or float16")
@@ -521,7 +522,7 @@ def _norm_scratch(count):
 def mlip_grad_norm(grads):
     """Norm of all elements of the tensors together (cuda float32 scalar); asynchronous.
 
-    grads: dense cuda tensors, float32, bfloat16 or float16, mixed as they come."""
+    grads: an iterable of dense cuda tensors, float32, bfloat16 or float16, mixed as they come."""
     held, a, count = _tensor_list(grads, None)
     norm, ws, need = _norm_scratch(count)
     _check(lib().mlip_grad_norm(a, count, norm.data_ptr(), ws.data_ptr(), need, _stream()))
@@ -531,7 +532,7 @@ def mlip_grad_norm(grads):
 def mlip_clip_grads(grads, max_norm, out=None):
     """Scales the tensors so that the norm of all of them together is at most max_norm; returns the norm before.
 
-    In place, or into the tensors of `out` (of the same types, sizes and layouts).  Where the norm is infinite or NaN the values stay as
+    grads, out: iterables of tensors.  In place, or into the tensors of `out` (of the same types, sizes and layouts).  Where the norm is infinite or NaN the values stay as
     they are: a caller that reads the norm skips the step."""
     held, a, count = _tensor_list(grads, out)
     norm, ws, need = _norm_scratch(count)
