@@ -191,19 +191,21 @@ static int64_t tiles_of(const mlip_tensor_t &x, const void *at)
     return x.n > 0 ? (x.n + before_line(at, size) + per - 1) / per : 0;
 }
 
-// Takes the next tensors of the list for a launch, from tensor `at` on (backwards: up to `at`); those without elements are left out.  Returns where the
-// next launch goes on.
-template <class Chunk> static int32_t take(Chunk &c, const mlip_tensor_t *list, int32_t count, int32_t at)
+// Takes the next tensors of the list for a launch, from tensor `at` on; those without elements are left out.  Returns where the next launch goes on.
+// clip: whether the tensors have outputs; where they have none their `dst` is not read.
+template <class Chunk> static int32_t take(Chunk &c, const mlip_tensor_t *list, int32_t count, int32_t at, bool clip)
 {
-    constexpr int most = std::is_same_v<Chunk, ClipChunk> ? kListClip : kListNorm;
+    constexpr bool writes = std::is_same_v<Chunk, ClipChunk>;
+    constexpr int most = writes ? kListClip : kListNorm;
     c.count = 0;
     int64_t tiles = 0;
     for (; at < count && c.count < most; ++at) {
-        const int64_t more = tiles_of(list[at], std::is_same_v<Chunk, ClipChunk> ? list[at].dst : list[at].src);
+        const void *to = clip ? list[at].dst : list[at].src;
+        const int64_t more = tiles_of(list[at], to);
         if (!more) continue;
         if (c.count && tiles + more > 0x7fffffff) break;
         c.src[c.count] = list[at].src;
-        if constexpr (std::is_same_v<Chunk, ClipChunk>) c.dst[c.count] = list[at].dst;
+        if constexpr (writes) c.dst[c.count] = const_cast<void *>(to);
         c.n_type[c.count] = (uint64_t)list[at].n | ((uint64_t)list[at].dtype << 56);
         c.first[c.count++] = (uint32_t)tiles;
         tiles += more;
@@ -220,7 +222,7 @@ int grad_norm_impl(const mlip_tensor_t *list, int32_t count, bool clip, float ma
     const size_t room = (bytes - kHead) / sizeof(double);
     size_t parts = 0;
     ClipChunk few;
-    if (take(few, list, count, 0) == count && few.first[few.count] <= kFewTiles) {
+    if (take(few, list, count, 0, clip) == count && few.first[few.count] <= kFewTiles) {
         k_few_tiles<<<1, kThreads, 0, stream>>>(few, clip, max_norm, norm);
         MLIP_HIP(hipGetLastError());
         return MLIP_OK;
@@ -230,7 +232,7 @@ int grad_norm_impl(const mlip_tensor_t *list, int32_t count, bool clip, float ma
     const bool far = total > kStreamBytes;
     NormChunk c;
     for (int32_t at = 0; at < count;) {
-        at = take(c, list, count, at);
+        at = take(c, list, count, at, false);
         if (!c.count) break;
         if (parts + blocks_of(c) > room) { set_error("tensors too large for the workspace"); return MLIP_EINVAL; }
         (far ? k_square_sums<true> : k_square_sums<false>)<<<blocks_of(c), kThreads, 0, stream>>>(c, part + parts);
@@ -241,7 +243,7 @@ int grad_norm_impl(const mlip_tensor_t *list, int32_t count, bool clip, float ma
     if (clip && parts > 0) {
         ClipChunk d;
         for (int32_t at = 0; at < count;) {
-            at = take(d, list, count, at);
+            at = take(d, list, count, at, true);
             if (!d.count) break;
             (far ? k_clip<true> : k_clip<false>)<<<blocks_of(d), kThreads, 0, stream>>>(d, many ? joined : part, many ? 1 : (int)parts, max_norm, many ? nullptr : norm);
         }
