@@ -434,11 +434,56 @@ def _output(out, rows, width, vector):
     return dtype, rs if rows > 1 else max(rs, width)
 
 
+class _Embed(torch.autograd.Function):
+    """mlip_embed in an autograd graph.  `out` comes first: where it is a view, torch takes the first input for what is written."""
+
+    @staticmethod
+    def forward(ctx, out, table, species, scale):
+        ctx.save_for_backward(species)
+        ctx.shape, ctx.dtype, ctx.scale = table.shape, table.dtype, scale
+        if out is not None:
+            ctx.mark_dirty(out)
+        return mlip_embed(table, species, scale, out)
+
+    @staticmethod
+    def backward(ctx, bar):
+        out_bar = torch.zeros_like(bar) if ctx.needs_input_grad[0] else None      # what out held is overwritten
+        table_bar = None
+        if ctx.needs_input_grad[1]:
+            table_bar = mlip_embed_grad(bar, ctx.saved_tensors[0], ctx.shape[0], ctx.scale, bar.new_empty(ctx.shape, dtype=ctx.dtype))
+        return out_bar, table_bar, None, None
+
+
+class _EmbedGrad(torch.autograd.Function):
+    """mlip_embed_grad in an autograd graph, `out` first as above"""
+
+    @staticmethod
+    def forward(ctx, out, grad, species, n_species, scale, accumulate):
+        ctx.save_for_backward(species)
+        ctx.shape, ctx.dtype, ctx.n_species, ctx.scale, ctx.accumulate = grad.shape, grad.dtype, n_species, scale, accumulate
+        if out is not None:
+            ctx.mark_dirty(out)
+        return mlip_embed_grad(grad, species, n_species, scale, out, accumulate)
+
+    @staticmethod
+    def backward(ctx, bar):
+        out_bar = grad_bar = None
+        if ctx.needs_input_grad[0]:
+            out_bar = bar if ctx.accumulate else torch.zeros_like(bar)
+        if ctx.needs_input_grad[1]:
+            species, = ctx.saved_tensors
+            species = torch.where(species < ctx.n_species, species, -1)     # ids without a row brought nothing in: zeros, not NaN
+            grad_bar = mlip_embed(bar, species, ctx.scale, bar.new_empty(ctx.shape, dtype=ctx.dtype))
+        return out_bar, grad_bar, None, None, None, None
+
+
 def mlip_embed(table, species, scale=1.0, out=None):
     """out[i] = scale * table[species[i]]: rows of a per-species table (zeros for a species < 0, NaN for one the table lacks).
 
     table: cuda [S, F] or [S], float32, bfloat16 or float16, any strides; species: cuda int32 or int64 [n]; out: [n, F] or [n] of any
-    of the three types (default: the table's), its columns one after another."""
+    of the three types (default: the table's), its columns one after another.  Differentiable with respect to the table."""
+    if (table.requires_grad or (out is not None and out.requires_grad)) and torch.is_grad_enabled():
+        return _Embed.apply(out, table, species, scale)
     dtype, rows, width, rs, cs = _matrix(table, "table")
     ids, bits, n = _ids(species)
     if out is None:
@@ -453,7 +498,9 @@ def mlip_embed_grad(grad, species, n_species, scale=1.0, out=None, accumulate=Fa
     """out[s] = scale * sum of grad[i] over the atoms with species[i] == s: the gradient of mlip_embed for its table.
 
     grad: cuda [n, F] or [n], any strides (0 for a broadcast gradient); out: [n_species, F] or [n_species] (default: of grad's
-    type); accumulate: add to what out holds."""
+    type); accumulate: add to what out holds.  Differentiable with respect to grad and to what is added to."""
+    if (grad.requires_grad or (out is not None and out.requires_grad)) and torch.is_grad_enabled():
+        return _EmbedGrad.apply(out, grad, species, n_species, scale, accumulate)
     dtype, rows, width, rs, cs = _matrix(grad, "grad")
     ids, bits, n = _ids(species)
     if rows != n:
@@ -520,7 +567,7 @@ def _norm_scratch(count):
 
 
 def mlip_grad_norm(grads):
-    """Norm of all elements of the tensors together (cuda float32 scalar); asynchronous.
+    """Norm of all elements of the tensors together (cuda float32 scalar); asynchronous, not recorded by autograd.
 
     grads: an iterable of dense cuda tensors, float32, bfloat16 or float16, mixed as they come."""
     held, a, count = _tensor_list(grads, None)
