@@ -395,6 +395,11 @@ def _refuse(msg):
     raise MlipError(-1, msg)
 
 
+# Tells torch that the library has written tensors, so that autograd notices a value of its own that has changed (increment_version without
+# its look at the argument's type, in a third of its time)
+_written = getattr(torch._C, "_increment_version", None) or torch.autograd.graph.increment_version
+
+
 def _stream_of(*tensors):
     """The current stream of the current GPU, on which all tensors must lie."""
     here = torch.cuda.current_device()
@@ -486,11 +491,14 @@ def mlip_embed(table, species, scale=1.0, out=None):
         return _Embed.apply(out, table, species, scale)
     dtype, rows, width, rs, cs = _matrix(table, "table")
     ids, bits, n = _ids(species)
-    if out is None:
+    given = out is not None
+    if not given:
         out = table.new_empty((n,) if table.dim() == 1 else (n, width))
     out_dtype, out_rs = _output(out, n, width, table.dim() == 1)
     stream = _stream_of(table, species, out)
     _check(lib().mlip_embed(table.data_ptr(), dtype, rows, width, rs, cs, ids, bits, n, scale, out.data_ptr(), out_dtype, out_rs, stream))
+    if given:
+        _written((out,))
     return out
 
 
@@ -505,7 +513,8 @@ def mlip_embed_grad(grad, species, n_species, scale=1.0, out=None, accumulate=Fa
     ids, bits, n = _ids(species)
     if rows != n:
         _refuse("grad must have a row for each atom")
-    if out is None:
+    given = out is not None
+    if not given:
         if accumulate:
             _refuse("accumulate needs out")
         out = grad.new_empty((n_species,) if grad.dim() == 1 else (n_species, width))
@@ -516,6 +525,8 @@ def mlip_embed_grad(grad, species, n_species, scale=1.0, out=None, accumulate=Fa
     ws = torch.empty(need, dtype=torch.uint8, device="cuda") if need else None
     _check(L.mlip_embed_grad(grad.data_ptr(), dtype, rs, cs, ids, bits, n, n_species, width, scale, bool(accumulate), out.data_ptr(),
                              out_dtype, out_rs, ws.data_ptr() if need else None, need, stream))
+    if given:
+        _written((out,))
     return out
 
 
@@ -581,7 +592,9 @@ def mlip_clip_grads(grads, max_norm, out=None):
 
     grads, out: iterables of tensors.  In place, or into the tensors of `out` (of the same types, sizes and layouts).  Where the norm is infinite or NaN the values stay as
     they are: a caller that reads the norm skips the step."""
+    grads, out = list(grads), None if out is None else list(out)
     held, a, count = _tensor_list(grads, out)
     norm, ws, need = _norm_scratch(count)
     _check(lib().mlip_clip_grads(a, count, max_norm, norm.data_ptr(), ws.data_ptr(), need, _stream()))
+    _written(grads if out is None else out)
     return norm
