@@ -238,9 +238,9 @@ int grad_norm_impl(const mlip_tensor_t *list, int32_t count, bool clip, float ma
         (far ? k_square_sums<true> : k_square_sums<false>)<<<blocks_of(c), kThreads, 0, stream>>>(c, part + parts);
         parts += blocks_of(c);
     }
-        const bool many = parts > (size_t)kBlocksMost;
-    if (!clip || many || parts == 0) k_norm<<<1, kThreads, 0, stream>>>(part, (int)parts, norm, joined);
-    if (clip && parts > 0) {
+    const bool many = parts > (size_t)kBlocksMost;   // (not none: a list without elements is one of few tiles)
+    if (!clip || many) k_norm<<<1, kThreads, 0, stream>>>(part, (int)parts, norm, joined);
+    if (clip) {
         ClipChunk d;
         for (int32_t at = 0; at < count;) {
             at = take(d, list, count, at, true);

@@ -5,11 +5,6 @@
 
 namespace mlip {
 
-template <int DT> struct ElemT;
-template <> struct ElemT<MLIP_DTYPE_F32> { using type = float; };
-template <> struct ElemT<MLIP_DTYPE_BF16> { using type = __bf16; };
-template <> struct ElemT<MLIP_DTYPE_F16> { using type = _Float16; };
-
 inline size_t elem_size(int32_t dtype) { return dtype == MLIP_DTYPE_F32 ? 4 : 2; }
 inline bool elem_known(int32_t dtype) { return dtype >= MLIP_DTYPE_F32 && dtype <= MLIP_DTYPE_F16; }
 
