@@ -545,10 +545,15 @@ def _dense(t):
 _Tensor_of, _dtype_of = torch.Tensor, operator.attrgetter("dtype")
 
 
+def _listed(tensors):
+    """The tensors of an iterable, which the first of several looks at them may use up, as a list; None as it is."""
+    return tensors if tensors is None or type(tensors) is list else list(tensors)
+
+
 def _tensor_list(grads, out):
     """The tensors as the library takes them (an array of _Tensor, as 64-bit words), checked.  Lists run to hundreds of tensors, so
     each property is taken of all of them in one map."""
-    grads, out = list(grads), None if out is None else list(out)   # (an iterator would be used up by the first of the maps)
+    grads, out = _listed(grads), _listed(out)
     codes = list(map(_DTYPES.get, map(_dtype_of, grads)))
     if None in codes:
         _refuse("gradients must be float32, bfloat16 or float16")
@@ -592,7 +597,7 @@ def mlip_clip_grads(grads, max_norm, out=None):
 
     grads, out: iterables of tensors.  In place, or into the tensors of `out` (of the same types, sizes and layouts).  Where the norm is infinite or NaN the values stay as
     they are: a caller that reads the norm skips the step."""
-    grads, out = list(grads), None if out is None else list(out)
+    grads, out = _listed(grads), _listed(out)
     held, a, count = _tensor_list(grads, out)
     norm, ws, need = _norm_scratch(count)
     _check(lib().mlip_clip_grads(a, count, max_norm, norm.data_ptr(), ws.data_ptr(), need, _stream()))
