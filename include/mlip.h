@@ -396,7 +396,7 @@ int mlip_copy_to_host(const mlip_graph_t *graph, void *dst_host, const void *src
  * These calls use no handle: they work on the caller's arrays, on the HIP stream given (hipStream_t as void*, NULL = default
  * stream), and take scratch memory from the caller, so they can be captured in a HIP graph and run on any stream or thread.  Results
  * are the same bits on every call with the same arguments.  Element pointers must be aligned to their elements; outputs must not
- * overlap inputs (a clipped tensor may be its own output).
+ * overlap inputs (a clipped tensor may be its own output) or each other.
  */
 enum { MLIP_DTYPE_F32 = 0, MLIP_DTYPE_BF16 = 1, MLIP_DTYPE_F16 = 2 };
 
@@ -414,15 +414,15 @@ int mlip_embed(const void *table, int32_t table_dtype, int64_t n_rows, int64_t w
                int32_t out_dtype, int64_t out_row_stride, void *stream);
 
 /*
- * Its gradient: out[r][f] = scale * sum over i with ids[i] == r of grad[i][f], rows that no id names are zero; with
- * accumulate != 0 the old out[r][f] is added.  Ids outside [0, n_rows) contribute nothing, whatever grad holds there.
+ * Its gradient: out[r][f] = scale * sum over i with ids[i] == r of grad[i][f], rows that no id names are scale * 0; with
+ * accumulate != 0 the old out[r][f] is added, in fp64.  Ids outside [0, n_rows) contribute nothing, whatever grad holds there.
  *   grad    DEVICE [n][width] of grad_dtype, element (i, f) at i * grad_row_stride + f * grad_col_stride (>= 0; 0 for a
  *           gradient that is the same for all atoms)
  *   out     DEVICE [n_rows][width] of out_dtype, element (r, f) at r * out_row_stride + f
  *   workspace   DEVICE scratch of at least mlip_embed_grad_workspace(n, n_rows, width) bytes, aligned to 16 bytes; its
  *           contents do not matter before and mean nothing after the call
  * Sums run in the order of the atoms, over fewer than MLIP_EMBED_GRAD_RUN atoms at a time in fp32 and over those parts in fp64 (rounded to
- * fp32 up to twice on the way: fewer than MLIP_EMBED_GRAD_RUN fp32 roundings in all), and are rounded to the output's type once.
+ * fp32 up to twice on the way: fewer than MLIP_EMBED_GRAD_RUN fp32 roundings in all); the result is rounded to fp32 and then to the output's type.
  * mlip_embed_grad_workspace returns 0 for sizes that the call refuses.
  */
 enum { MLIP_EMBED_GRAD_RUN = 1024 };

@@ -23,9 +23,9 @@ template <class Fn> inline void with_ids(int32_t id_bits, Fn &&f)
     else f(int64_t{});
 }
 
-// What is larger than this is read or written past the caches where it is touched once: they could not keep it for anyone.  Measured, us past
-// the caches and through them: clipping 32 MB 21.7 and 18.8, 96 MB 52 and 56, 256 MB 128 and 148; lookup of 64 MB 11.9 and 12.5, 256 MB 44 and 46;
-// gradient into few rows of 32 MB 16.4 and 15.5, 96 MB 22.8 and 23.4, 256 MB 51 and 55, into many of 64 MB 53 and 50.5, 128 MB 69 and 71.
+// What is larger than this is read or written past the caches where it is touched once: they could not keep it for anyone.  Measured, us a call past
+// the caches and through them (fp32, rows of 64): clipping 32 MB 22 and 19, 96 MB 51 and 55, 256 MB 128 and 146; lookup of 32 MB 9.6 and 9.0, 64 MB 12.3 and
+// 12.5, 256 MB 43.6 and 45.4; gradient into few rows of 32 MB 16 and 15, 96 MB 21.6 and 22, 256 MB 50 and 54, into many of 64 MB 51 and 47, 128 MB 66.5 and 69.5.
 constexpr double kStreamBytes = 100e6;
 
 // Blocks that a launch has at most, a multiple of eight so that the XCDs' turn goes on from launch to launch: HIP takes a grid's threads modulo 2^32, with

@@ -72,8 +72,8 @@ template <int V, class T> __device__ inline void stream_cols(T *p, const float (
 
 // ---- lookup: out[i][f] = scale * table[id_i][f].  A thread has a lot of columns of a row, and kEmbedUnroll of them at a time, a grid's size
 // apart.  Writing bounds it: a million rows of 64 fp32 take 43 us, 6.0 TB/s.  Results that the caches do not hold are stored past them if their rows begin at
-// whole lots (47 us, 59 through the caches, at a million rows of 64); stored so, lots that share a line of memory cost more than they save (a million bf16 rows
-// of 33 46 us and 32), and the lots are shifted to where memory has whole ones (1,546,331 fp32 rows of 59: 83 us, 95 from the row's beginning on).
+// whole lots (a million rows of 64: 43.6 us a call, 45.4 through the caches); stored so, lots that share a line of memory cost more than they save, and the lots are
+// shifted to where memory has whole ones (1,546,331 fp32 rows of 59: 80 us shifted, 82 from the row's beginning on, 90 so and past the caches).
 
 enum { kPlain, kStreamed, kShifted };
 constexpr int kEmbedUnroll = 4;
@@ -310,9 +310,11 @@ struct FewPlan {
 
 // Which way a table takes.  The tables' LDS leaves the fewer wavefronts to load the more rows there are, so rows that fill a wavefront (33 columns and more) pass
 // to the sort at 80; of narrow ones several lie in one wavefront's load, and the sort's cost by atom is paid back later; where there is little to load the sort's
-// launches count for more.  Measured, us by LDS tables and by sorting: a million rows of 64 into 64 61 and 77, into 89 70 and 75, into 119 85 and 75; 20,000
-// rows of 64 into 64 16 and 19, into 89 24 and 19; 100,000 of 512 into 64 55 and 57, into 89 67 and 57; 300,000 rows of 16 into 119 22 and 29, into 200
-// 28 and 29, into 255 31 and 29; a million rows of 2 into 255 20 and 49; 4000 rows of 64 into 119 13 and 18, into 160 19 and 18.
+// launches count for more.  Measured, us a call by LDS tables and by sorting: a million rows of 64 into 64 58 and 76, into 119 83 and 74; 20,000
+// rows of 64 into 64 15 and 19, into 89 23 and 18; 100,000 of 512 into 64 53 and 57, into 89 64 and 56; 300,000 rows of 16 into 119 21 and 28, into 200
+// 27.5 and 28.5, into 255 31 and 28.5; a million rows of 2 into 255 20 and 48; 4000 rows of 64 into 119 14 and 19, into 160 19 and 18.  Between 4096 and some
+// 100,000 atoms sorting is the better way for 89 rows of 64, beyond it the LDS tables would be (100,000: 23.6 and 24.4; a million: 67 and 75): the rule has no such
+// second limit.
 static bool takes_few(int64_t n, int64_t n_rows, int64_t width)
 {
     const int64_t slots = width < 64 ? 64 / width : 1, most = 32 + 48 * slots + (n <= 4096 ? 64 : 0);
@@ -704,7 +706,7 @@ static bool whole_lines(const EmbedArgs &a)
 }
 
 // Whether they are read past the caches: where there are more than the caches hold and rows share no lines.  (Lines that rows or tiles of
-// columns share are better kept: a million bf16 rows of 77 into 8 60 us, 69 past the caches; of 800,000 fp32 rows of 64 42 and 37.)
+// columns share are better kept: a million bf16 rows of 77 into 8 58 us a call, 61 past the caches; of 800,000 fp32 rows of 64 43 and 38.)
 static bool streams(const EmbedArgs &a)
 {
     return (double)a.n * (double)a.width * (double)elem_size(a.in_dtype) > kStreamBytes && whole_lines(a);
