@@ -457,6 +457,137 @@ int mlip_grad_norm(const mlip_tensor_t *tensors, int32_t count, float *norm, voi
 int mlip_clip_grads(const mlip_tensor_t *tensors, int32_t count, float max_norm, float *norm, void *workspace,
                     size_t workspace_bytes, void *stream);
 
+/*
+ * Networks on the nodes of a potential and their training (the models of the paper's Methods, "Graph-Parallel Message Passing", update their node features
+ * by such networks): gated projections, the norms, gate and residual sum around a block, and orthogonal updates of weight matrices.
+ * As the table calls they use no handle, run on the stream given and take scratch memory from the caller (aligned to 16 bytes, its contents do not matter
+ * before and mean nothing after the call), so they can be captured in a HIP graph; calls that share scratch memory must not overlap in time.
+ * Element pointers must be aligned to their elements; strides are in elements and not negative; outputs must not overlap inputs or each other except where said.
+ * Results are the same bits on every call with the same arguments.  Sums, statistics and what lies between input and output are fp32 or more,
+ * rounded to the output's type once, except where said.
+ */
+
+/*
+ * Gated projections: h = phi(g, v) for every element of g = x Wg + bg, v = x Wv + bv, with phi =
+ *   MLIP_GATE_SILU          silu(g) v              (silu(t) = t sigmoid(t))
+ *   MLIP_GATE_GELU          g Phi(g) v             (Phi the normal distribution function)
+ *   MLIP_GATE_SIGMOID       sigmoid(g) v
+ *   MLIP_GATE_SILU_SIGMOID  sigmoid(g) silu(v)
+ * All arrays are of type dtype; products are exact, sums fp32 (fp32 arrays: products of three bf16 parts each, all terms down to 2^-24; a value that is
+ * infinite, or beyond the bf16 range of 3.39e38, makes its row of x, or its column of the weights, NaN).
+ *   x        DEVICE [n][d], any strides;  w_gate, w_value DEVICE [d][f], any strides (so that weights kept as [f][d] serve as well)
+ *   b_gate, b_value   DEVICE [f], one element after another, or NULL
+ *   out      DEVICE [n][f], element (i, k) at i * out_row_stride + k
+ * 0 <= n < 2^31, 1 <= d, f <= 65536.  mlip_gated_workspace returns 0 for calls that are refused.
+ */
+enum { MLIP_GATE_SILU = 0, MLIP_GATE_GELU = 1, MLIP_GATE_SIGMOID = 2, MLIP_GATE_SILU_SIGMOID = 3 };
+typedef struct {
+    int32_t dtype, act;
+    int64_t n, d, f;
+    const void *x;
+    int64_t x_row_stride, x_col_stride;
+    const void *w_gate;
+    int64_t w_gate_row_stride, w_gate_col_stride;
+    const void *w_value;
+    int64_t w_value_row_stride, w_value_col_stride;
+    const void *b_gate, *b_value;
+} mlip_gated_t;
+size_t mlip_gated_workspace(const mlip_gated_t *call, int32_t grad /* 0: of mlip_gated, 1: of mlip_gated_grad */);
+int mlip_gated(const mlip_gated_t *call, void *out, int64_t out_row_stride, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Its gradient, from the gradient of out.  The products are computed again: nothing is kept from the forward call.  The gradients of g and v are rounded
+ * to the arrays' type (fp32: not rounded) before the products with x and the weights take them up.
+ *   grad     DEVICE [n][f], any strides
+ *   x        DEVICE [n][d], element (i, k) at i * x_row_stride + k;  w_gate, w_value DEVICE [d][f], any strides that keep elements apart
+ *   b_gate, b_value   DEVICE [f]
+ * Every output may be NULL, and is then left out.
+ */
+typedef struct {
+    const void *grad;
+    int64_t grad_row_stride, grad_col_stride;
+    void *x;
+    int64_t x_row_stride;
+    void *w_gate;
+    int64_t w_gate_row_stride, w_gate_col_stride;
+    void *w_value;
+    int64_t w_value_row_stride, w_value_col_stride;
+    void *b_gate, *b_value;
+} mlip_gated_grad_t;
+int mlip_gated_grad(const mlip_gated_t *call, const mlip_gated_grad_t *grad, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Residual sum of a block with its norms and gate:  y = x + factor * gate * scale * post(z),  norm = pre(y) (of y before it is rounded), where the norm
+ * of a row t is  (t - m) / sqrt(mean of (t - m)^2 + eps) * w + b  with m the row's mean (MLIP_NORM_LAYER) or 0 (MLIP_NORM_RMS).
+ *   x, z     DEVICE [n][width] of dtype, any strides;  z NULL: y = x, and pre(x) is all there is to compute (y NULL, no gate, scale or post)
+ *   gate     DEVICE of dtype: one for each element [n][width], row [n] (column stride not used) or column [width] (row stride not used), by gate_kind
+ *   scale, post_w, post_b, pre_w, pre_b   DEVICE [width] of param_dtype (fp32 or dtype), one element after another, or NULL (1, and 0 for a bias)
+ *   post, pre   whether there is such a norm
+ *   y, norm  DEVICE [n][width] of dtype, element (i, k) at i * row stride + k;  y may be NULL (only the norm is wanted), norm is NULL if pre is 0.
+ *            y may be x itself or z itself, with the same strides.
+ * 0 <= n < 2^31, 1 <= width <= 8192.
+ */
+enum { MLIP_NORM_RMS = 0, MLIP_NORM_LAYER = 1 };
+enum { MLIP_RESIDUAL_GATE_NONE = 0, MLIP_RESIDUAL_GATE_FULL = 1, MLIP_RESIDUAL_GATE_ROW = 2, MLIP_RESIDUAL_GATE_COL = 3 };
+typedef struct {
+    int32_t dtype, param_dtype, kind, gate_kind, post, pre;
+    int64_t n, width;
+    float eps, factor;
+    const void *x;
+    int64_t x_row_stride, x_col_stride;
+    const void *z;
+    int64_t z_row_stride, z_col_stride;
+    const void *gate;
+    int64_t gate_row_stride, gate_col_stride;
+    const void *scale, *post_w, *post_b, *pre_w, *pre_b;
+} mlip_residual_t;
+int mlip_residual(const mlip_residual_t *call, void *y, int64_t y_row_stride, void *norm, int64_t norm_row_stride, void *stream);
+
+/*
+ * Its gradient, from the gradients of y and of norm (either may be NULL: zeros; not both) and the inputs; y and the norms are computed again.
+ *   y, norm   DEVICE [n][width] of dtype, any strides
+ *   x, z, gate   outputs of dtype, element (i, k) at i * row stride + k; the gate's as the gate is: [n][width], [n] (i * row stride) or [width]
+ *   scale, post_w, post_b, pre_w, pre_b   outputs [width] of param_dtype
+ * Every output may be NULL; outputs of what the call does not have must be.  x may be y or norm itself, z the other one, with the same strides.
+ * Sums over the rows: fp32, over fewer than n / 256 + 64 rows at a time, and those parts in fp32.
+ */
+typedef struct {
+    const void *y;
+    int64_t y_row_stride, y_col_stride;
+    const void *norm;
+    int64_t norm_row_stride, norm_col_stride;
+    void *x;
+    int64_t x_row_stride;
+    void *z;
+    int64_t z_row_stride;
+    void *gate;
+    int64_t gate_row_stride;
+    void *scale, *post_w, *post_b, *pre_w, *pre_b;
+} mlip_residual_grad_t;
+size_t mlip_residual_grad_workspace(int64_t n, int64_t width);
+int mlip_residual_grad(const mlip_residual_t *call, const mlip_residual_grad_t *grad, void *workspace, size_t workspace_bytes, void *stream);
+
+/* A matrix of a list: element (i, k) at i * row stride + k * col stride of src, and of dst, where its result goes (dst may be src, with the same strides). */
+typedef struct {
+    const void *src; /* DEVICE */
+    void *dst;       /* DEVICE */
+    int64_t rows, cols, src_row_stride, src_col_stride, dst_row_stride, dst_col_stride;
+    int32_t dtype;
+} mlip_matrix_t;
+
+/*
+ * Orthogonalises the matrices of a list (gradients or their running means, before an optimiser's update): X_0 = G / max(|G|, eps) with |G| the root of the sum of
+ * squares, then `steps` times X <- (a + b X X^T + c (X X^T)^2) X, of the transpose where a matrix has more rows than columns; dst = scale * X.
+ * |G| is summed in fp64.  X and the products X X^T are held in two fp16 parts (22 bits), sums are fp32: entries of X must stay below
+ * 2^11 / sqrt(columns) and those of the polynomials below 2^7, which coefficients hold that keep singular values in [0, 1] below 1.3 (larger ones become NaN).
+ * A matrix with values that are not finite gets none that is; one of zeros stays so.  The same matrix must not be in the list twice.
+ *   matrices      HOST [count], read before the call returns; count, rows and cols may be 0;  rows, cols <= 2^20, the smaller one of them <= 32768, elements < 2^31
+ *   coefficients  HOST [3] a, b, c
+ */
+size_t mlip_orthogonalise_workspace(const mlip_matrix_t *matrices, int32_t count);
+int mlip_orthogonalise(const mlip_matrix_t *matrices, int32_t count, int32_t steps, const double *coefficients, double eps, float scale, void *workspace,
+                       size_t workspace_bytes, void *stream);
+
 const char *mlip_last_error(void);
 const char *mlip_version(void);
 

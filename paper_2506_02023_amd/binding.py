@@ -60,6 +60,69 @@ class _Tensor(ctypes.Structure):
     _fields_ = [("src", ctypes.c_void_p), ("dst", ctypes.c_void_p), ("n", ctypes.c_int64), ("dtype", ctypes.c_int32)]
 
 
+def _fields(text):
+    """Fields of a structure from lines "type: names" """
+    kinds = {"i32": ctypes.c_int32, "i64": ctypes.c_int64, "f32": ctypes.c_float, "ptr": ctypes.c_void_p}
+    return [(name, kinds[line.split(":")[0].strip()]) for line in text.strip().splitlines() for name in line.split(":")[1].split()]
+
+
+class _Gated(ctypes.Structure):
+    _fields_ = _fields("""i32: dtype act
+                          i64: n d f
+                          ptr: x
+                          i64: x_rs x_cs
+                          ptr: wg
+                          i64: wg_rs wg_cs
+                          ptr: wv
+                          i64: wv_rs wv_cs
+                          ptr: bg bv""")
+
+
+class _GatedGrad(ctypes.Structure):
+    _fields_ = _fields("""ptr: grad
+                          i64: grad_rs grad_cs
+                          ptr: x
+                          i64: x_rs
+                          ptr: wg
+                          i64: wg_rs wg_cs
+                          ptr: wv
+                          i64: wv_rs wv_cs
+                          ptr: bg bv""")
+
+
+class _Residual(ctypes.Structure):
+    _fields_ = _fields("""i32: dtype param_dtype kind gate_kind post pre
+                          i64: n width
+                          f32: eps factor
+                          ptr: x
+                          i64: x_rs x_cs
+                          ptr: z
+                          i64: z_rs z_cs
+                          ptr: gate
+                          i64: gate_rs gate_cs
+                          ptr: scale post_w post_b pre_w pre_b""")
+
+
+class _ResidualGrad(ctypes.Structure):
+    _fields_ = _fields("""ptr: y
+                          i64: y_rs y_cs
+                          ptr: norm
+                          i64: norm_rs norm_cs
+                          ptr: x
+                          i64: x_rs
+                          ptr: z
+                          i64: z_rs
+                          ptr: gate
+                          i64: gate_rs
+                          ptr: scale post_w post_b pre_w pre_b""")
+
+
+class _Matrix(ctypes.Structure):
+    _fields_ = _fields("""ptr: src dst
+                          i64: rows cols src_rs src_cs dst_rs dst_cs
+                          i32: dtype""")
+
+
 class _Alloc(ctypes.Structure):
     _fields_ = [("alloc", _ALLOC_FN), ("free", _FREE_FN), ("ctx", ctypes.c_void_p)]
 
@@ -132,6 +195,15 @@ def lib():
         L.mlip_profile_read.argtypes = [vp, ctypes.POINTER(ctypes.c_float), ctypes.POINTER(i64), i32]
         L.mlip_copy_to_host.argtypes = [vp, vp, vp, ctypes.c_size_t]
         f32, size = ctypes.c_float, ctypes.c_size_t
+        ref = ctypes.POINTER
+        L.mlip_gated_workspace.argtypes, L.mlip_gated_workspace.restype = [ref(_Gated), i32], size
+        L.mlip_gated.argtypes = [ref(_Gated), vp, i64, vp, size, vp]
+        L.mlip_gated_grad.argtypes = [ref(_Gated), ref(_GatedGrad), vp, size, vp]
+        L.mlip_residual.argtypes = [ref(_Residual), vp, i64, vp, i64, vp]
+        L.mlip_residual_grad_workspace.argtypes, L.mlip_residual_grad_workspace.restype = [i64, i64], size
+        L.mlip_residual_grad.argtypes = [ref(_Residual), ref(_ResidualGrad), vp, size, vp]
+        L.mlip_orthogonalise_workspace.argtypes, L.mlip_orthogonalise_workspace.restype = [ref(_Matrix), i32], size
+        L.mlip_orthogonalise.argtypes = [ref(_Matrix), i32, i32, ref(ctypes.c_double), ctypes.c_double, f32, vp, size, vp]
         L.mlip_embed.argtypes = [vp, i32, i64, i64, i64, i64, vp, i32, i64, f32, vp, i32, i64, vp]
         L.mlip_embed_grad_workspace.argtypes = [i64, i64, i64]
         L.mlip_embed_grad_workspace.restype = size
@@ -603,3 +675,270 @@ def mlip_clip_grads(grads, max_norm, out=None):
     _check(lib().mlip_clip_grads(a, count, max_norm, norm.data_ptr(), ws.data_ptr(), need, _stream()))
     _written(grads if out is None else out)
     return norm
+
+
+# ---- networks on the nodes: gated projections, residual sums with norms, orthogonal updates (results on the current stream)
+
+_ACTS = {"silu": 0, "gelu": 1, "sigmoid": 2, "silu_sigmoid": 3}
+_KINDS = {"rms": 0, "layer": 1}
+
+
+def _scratch(need):
+    """(tensor, address) of scratch memory"""
+    if not need:
+        return None, None
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    return ws, ws.data_ptr()
+
+
+def _address(t):
+    return None if t is None else t.data_ptr()
+
+
+def _rows_of(t, what, shape, dtype):
+    """Checks a matrix of a given shape and type; its row and column strides."""
+    if t.dtype is not dtype or t.shape != shape:
+        _refuse(f"{what} must be a {dtype} tensor of {tuple(shape)}")
+    return t.stride()
+
+
+def _vector_of(t, what, width, dtype):
+    if t is not None and (t.dtype is not dtype or t.shape != (width,) or not t.is_contiguous()):
+        _refuse(f"{what} must be a contiguous {dtype} vector of {width}")
+    return t
+
+
+def _gated_call(x, w_gate, w_value, b_gate, b_value, act):
+    """(the call's structure, its tensors)"""
+    if x.dim() != 2 or x.dtype not in _DTYPES:
+        _refuse("x must be a matrix of float32, bfloat16 or float16")
+    if act not in _ACTS:
+        _refuse(f"act must be one of {', '.join(_ACTS)}")
+    n, d = x.shape
+    if w_gate.dim() != 2:
+        _refuse("w_gate must be a matrix")
+    f = w_gate.shape[1]
+    g, v = (_rows_of(w, what, (d, f), x.dtype) for w, what in ((w_gate, "w_gate"), (w_value, "w_value")))
+    for b, what in ((b_gate, "b_gate"), (b_value, "b_value")):
+        _vector_of(b, what, f, x.dtype)
+    call = _Gated(_DTYPES[x.dtype], _ACTS[act], n, d, f, x.data_ptr(), *x.stride(), w_gate.data_ptr(), *g, w_value.data_ptr(), *v, _address(b_gate), _address(b_value))
+    return call, [t for t in (x, w_gate, w_value, b_gate, b_value) if t is not None]
+
+
+def _wants_graph(*tensors):
+    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
+
+
+class _GatedFn(torch.autograd.Function):
+    """mlip_gated in an autograd graph"""
+
+    @staticmethod
+    def forward(ctx, act, *inputs):
+        ctx.save_for_backward(*inputs)
+        ctx.act = act
+        return mlip_gated(*inputs, act=act)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, bar):
+        return None, *_gated_grad(bar, ctx.saved_tensors, ctx.act, ctx.needs_input_grad[1:])
+
+
+def mlip_gated(x, w_gate, w_value, b_gate=None, b_value=None, act="silu"):
+    """phi(x @ w_gate + b_gate, x @ w_value + b_value), the gated projections of a node network.
+
+    act: "silu" silu(g) v, "gelu" gelu(g) v, "sigmoid" sigmoid(g) v, "silu_sigmoid" sigmoid(g) silu(v).  x: cuda [n, d], w_gate, w_value: [d, f], any strides (weights
+    kept as [f, d]: their .t()); b_gate, b_value: [f] or None; all float32, bfloat16 or float16 alike.  Differentiable once."""
+    if _wants_graph(x, w_gate, w_value, b_gate, b_value):
+        return _GatedFn.apply(act, x, w_gate, w_value, b_gate, b_value)
+    call, tensors = _gated_call(x, w_gate, w_value, b_gate, b_value, act)
+    stream = _stream_of(*tensors)
+    out = x.new_empty((call.n, call.f))
+    need = lib().mlip_gated_workspace(call, 0)
+    ws, at = _scratch(need)
+    _check(lib().mlip_gated(call, out.data_ptr(), call.f, at, need, stream))
+    return out
+
+
+def _gated_grad(grad, inputs, act, needs):
+    call, tensors = _gated_call(*inputs, act)
+    rs, cs = _rows_of(grad, "grad", (call.n, call.f), inputs[0].dtype)
+    stream = _stream_of(grad, *tensors)
+    outs = [torch.empty_like(t) if need and t is not None else None for t, need in zip(inputs, needs)]
+    if outs[0] is not None:
+        outs[0] = inputs[0].new_empty(inputs[0].shape)
+    for k in (1, 2):
+        if outs[k] is not None and not _dense(outs[k]):
+            outs[k] = inputs[k].new_empty(inputs[k].shape)
+    dx, dwg, dwv, dbg, dbv = outs
+    strides = [t.stride() if t is not None else (0, 0) for t in (dwg, dwv)]
+    g = _GatedGrad(grad.data_ptr(), rs, cs, _address(dx), call.d, _address(dwg), *strides[0], _address(dwv), *strides[1], _address(dbg), _address(dbv))
+    need = lib().mlip_gated_workspace(call, 1)
+    ws, at = _scratch(need)
+    _check(lib().mlip_gated_grad(call, g, at, need, stream))
+    return tuple(outs)
+
+
+def mlip_gated_grad(grad, x, w_gate, w_value, b_gate=None, b_value=None, act="silu"):
+    """Gradients of mlip_gated for x, w_gate, w_value, b_gate and b_value (None for a bias that is None) from grad, the gradient of its result."""
+    return _gated_grad(grad, (x, w_gate, w_value, b_gate, b_value), act, (True,) * 5)
+
+
+def _residual_call(x, z, gate, scale, post, pre, kind, eps, factor):
+    """(the call's structure, its tensors)"""
+    if x.dim() != 2 or x.dtype not in _DTYPES:
+        _refuse("x must be a matrix of float32, bfloat16 or float16")
+    if kind not in _KINDS:
+        _refuse(f"kind must be one of {', '.join(_KINDS)}")
+    n, width = x.shape
+    z_rs, z_cs = _rows_of(z, "z", (n, width), x.dtype) if z is not None else (0, 0)
+    gate_kind, g_rs, g_cs = 0, 0, 0
+    if gate is not None:
+        if gate.dtype is not x.dtype:
+            _refuse("gate must be of the type of x")
+        shape = tuple(gate.shape)
+        if shape == (n, width):
+            gate_kind, g_rs, g_cs = 1, *gate.stride()
+        elif shape == (n, 1):
+            gate_kind, g_rs = 2, gate.stride(0)
+        elif shape in ((width,), (1, width)) and gate.is_contiguous():
+            gate_kind = 3
+        else:
+            _refuse("gate must have a value for each element, row ([n, 1]) or column (contiguous [width] or [1, width])")
+    params = [scale, *(post or (None, None)), *(pre or (None, None))]
+    there = [p for p in params if p is not None]
+    param_dtype = there[0].dtype if there else x.dtype
+    if param_dtype is not torch.float32 and param_dtype is not x.dtype:
+        _refuse("scale and the norms' parameters must be float32 or of the type of x")
+    for p in there:
+        _vector_of(p, "scale and the norms' parameters", width, param_dtype)
+    call = _Residual(_DTYPES[x.dtype], _DTYPES[param_dtype], _KINDS[kind], gate_kind, post is not None, pre is not None, n, width, eps, factor, x.data_ptr(), *x.stride(),
+                     _address(z), z_rs, z_cs, _address(gate), g_rs, g_cs, *map(_address, params))
+    return call, [t for t in (x, z, gate, *there) if t is not None]
+
+
+def _residual_forward(x, z, gate, scale, post, pre, kind, eps, factor):
+    call, tensors = _residual_call(x, z, gate, scale, post, pre, kind, eps, factor)
+    stream = _stream_of(*tensors)
+    y = x.new_empty(x.shape) if z is not None else None
+    norm = x.new_empty(x.shape) if pre is not None else None
+    _check(lib().mlip_residual(call, _address(y), call.width, _address(norm), call.width, stream))
+    return y, norm
+
+
+def _residual_backward(dy, dn, x, z, gate, scale, post, pre, kind, eps, factor, needs):
+    """Gradients of (x, z, gate, scale, post_w, post_b, pre_w, pre_b) where `needs` says so, else None"""
+    call, tensors = _residual_call(x, z, gate, scale, post, pre, kind, eps, factor)
+    bars = [(*_rows_of(t, what, x.shape, x.dtype), t) if t is not None else (0, 0, None) for t, what in ((dy, "dy"), (dn, "dn"))]
+    stream = _stream_of(*[b[2] for b in bars if b[2] is not None], *tensors)
+    params = (scale, *(post or (None, None)), *(pre or (None, None)))
+    outs = [t.new_empty(t.shape) if need and t is not None else None for t, need in zip((x, z, gate, *params), needs)]
+    gate_rs = outs[2].stride(0) if outs[2] is not None else 0
+    g = _ResidualGrad(_address(dy), *bars[0][:2], _address(dn), *bars[1][:2], _address(outs[0]), call.width, _address(outs[1]), call.width, _address(outs[2]), gate_rs,
+                      *map(_address, outs[3:]))
+    need = lib().mlip_residual_grad_workspace(call.n, call.width)
+    ws, at = _scratch(need)
+    _check(lib().mlip_residual_grad(call, g, at, need, stream))
+    return outs
+
+
+class _ResidualFn(torch.autograd.Function):
+    """mlip_residual and mlip_norm in an autograd graph; gives the outputs that there are"""
+
+    @staticmethod
+    def forward(ctx, how, *inputs):
+        x, z, gate, scale, post_w, post_b, pre_w, pre_b = inputs
+        ctx.save_for_backward(*inputs)
+        ctx.how = how
+        ctx.set_materialize_grads(False)
+        post, pre, kind, eps, factor = how
+        y, norm = _residual_forward(x, z, gate, scale, (post_w, post_b) if post else None, (pre_w, pre_b) if pre else None, kind, eps, factor)
+        return tuple(t for t in (y, norm) if t is not None)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, *bars):
+        x, z, gate, scale, post_w, post_b, pre_w, pre_b = ctx.saved_tensors
+        post, pre, kind, eps, factor = ctx.how
+        if all(b is None for b in bars):
+            return (None,) * 9
+        dy = bars[0] if z is not None else None
+        dn = bars[-1] if pre else None
+        return None, *_residual_backward(dy, dn, x, z, gate, scale, (post_w, post_b) if post else None, (pre_w, pre_b) if pre else None, kind, eps, factor,
+                                         ctx.needs_input_grad[1:])
+
+
+def _residual_any(x, z, gate, scale, post, pre, kind, eps, factor):
+    """The outputs that there are"""
+    params = (*(post or (None, None)), *(pre or (None, None)))
+    if _wants_graph(x, z, gate, scale, *params):
+        return _ResidualFn.apply((post is not None, pre is not None, kind, eps, factor), x, z, gate, scale, *params)
+    return tuple(t for t in _residual_forward(x, z, gate, scale, post, pre, kind, eps, factor) if t is not None)
+
+
+def mlip_residual(x, z, gate=None, scale=None, post=None, pre=None, kind="rms", eps=1e-6, factor=1.0):
+    """x + factor * gate * scale * post(z), the residual sum of a block's result z with the norm after it; with `pre` also that sum's norm, before the next block.
+
+    x, z: cuda [n, width], float32, bfloat16 or float16, any strides; gate: [n, width], [n, 1] or [width], of x's type; scale: [width];
+    post, pre: None (no norm) or (weights, biases), each [width] or None; scale and these float32 or of x's type; kind: "rms" or "layer".
+    Returns the sum, or (sum, norm) with `pre`.  Differentiable once."""
+    if z is None:
+        _refuse("mlip_residual needs z (a norm alone: mlip_norm)")
+    outs = _residual_any(x, z, gate, scale, post, pre, kind, eps, factor)
+    return outs if pre is not None else outs[0]
+
+
+def mlip_residual_grad(dy, dn, x, z, gate=None, scale=None, post=None, pre=None, kind="rms", eps=1e-6, factor=1.0):
+    """Gradients of mlip_residual from those of its sum (dy) and of the norm (dn; either may be None, not both).
+
+    Returns (dx, dz, dgate, dscale, (d post weights, d post biases), (d pre weights, d pre biases)), None for what there is not."""
+    if z is None:
+        _refuse("mlip_residual_grad needs z (a norm alone: mlip_norm_grad)")
+    dx, dz, dgate, dscale, *d = _residual_backward(dy, dn, x, z, gate, scale, post, pre, kind, eps, factor, (True,) * 8)
+    return dx, dz, dgate, dscale, tuple(d[:2]) if post is not None else None, tuple(d[2:]) if pre is not None else None
+
+
+def mlip_norm(x, weight=None, bias=None, kind="rms", eps=1e-6):
+    """The norm of x's rows, (x - m) / sqrt(mean of (x - m)^2 + eps) * weight + bias with m their mean (kind "layer") or 0 ("rms").
+
+    x: cuda [n, width], any strides; weight, bias: [width] or None, float32 or of x's type.  Differentiable once."""
+    return _residual_any(x, None, None, None, None, (weight, bias), kind, eps, 1.0)[0]
+
+
+def mlip_norm_grad(grad, x, weight=None, bias=None, kind="rms", eps=1e-6):
+    """Gradients of mlip_norm for x, weight and bias (None for one that is None) from grad, the gradient of its result."""
+    d = _residual_backward(None, grad, x, None, None, None, None, (weight, bias), kind, eps, 1.0, (True,) * 8)
+    return d[0], d[6], d[7]
+
+
+def _matrices(tensors, what):
+    """The matrices of an iterable of matrices and stacks of matrices"""
+    out = []
+    for t in tensors:
+        if t.dim() not in (2, 3):
+            _refuse(f"{what} must be matrices, or stacks of matrices")
+        out += [t] if t.dim() == 2 else list(t.unbind(0))
+    return out
+
+
+def mlip_orthogonalise(updates, steps=5, coefficients=(3.4445, -4.7750, 2.0315), eps=1e-7, scale=1.0, out=None):
+    """Orthogonalises matrices (gradients or their running means, before an update): X = G / max(|G|, eps), then `steps` times
+    X <- (a + b X X^T + c (X X^T)^2) X, of the transpose where a matrix has more rows than columns; times `scale`.
+
+    updates, out: iterables of cuda matrices [rows, cols] or stacks of them [k, rows, cols], float32, bfloat16 or float16, any strides.  In place, or
+    into the tensors of `out` (of the same types and shapes).  Not recorded by autograd.  Returns the list of results."""
+    updates = _listed(updates)
+    out = updates if out is None else _listed(out)
+    if [(t.dtype, t.shape) for t in updates] != [(t.dtype, t.shape) for t in out]:
+        _refuse("out must have a tensor for each update, of its type and shape")
+    if any(t.dtype not in _DTYPES for t in updates):
+        _refuse("updates must be float32, bfloat16 or float16")
+    a, b, c = coefficients
+    src, dst = _matrices(updates, "updates"), _matrices(out, "out")
+    stream = _stream_of(*src, *dst)
+    list_ = (_Matrix * len(src))(*[_Matrix(s.data_ptr(), d.data_ptr(), *s.shape, *s.stride(), *d.stride(), _DTYPES[s.dtype]) for s, d in zip(src, dst)])
+    need = lib().mlip_orthogonalise_workspace(list_, len(src))
+    ws, at = _scratch(need)
+    _check(lib().mlip_orthogonalise(list_, len(src), steps, (ctypes.c_double * 3)(a, b, c), eps, scale, at, need, stream))
+    _written(out)
+    return out

@@ -632,6 +632,182 @@ int mlip_clip_grads(const mlip_tensor_t *tensors, int32_t count, float max_norm,
     return norm_call(tensors, count, true, max_norm, norm, workspace, workspace_bytes, stream);
 }
 
+// ---- networks on the nodes: gated projections, residual sums with norms, orthogonal updates; the caller's scratch memory
+
+// A matrix at `p` that a call has (rows or cols may be 0): why it cannot be used, or NULL.  out: its elements must lie apart.
+static const char *matrix_fault(const void *p, size_t size, int64_t rows, int64_t cols, int64_t rs, int64_t cs, bool out)
+{
+    constexpr double kFar = 1e18;   // byte offsets of the last elements, with room to spare
+    if (!aligned_to(p, size)) return "a pointer is not aligned to its elements";
+    if (rs < 0 || cs < 0) return "strides must not be negative";
+    if ((double)rs * (double)rows + (double)cs * (double)cols > kFar) return "strides too large";
+    if (rows == 0 || cols == 0) return nullptr;
+    if (!p) return "null pointer argument";
+    if (out && rows > 1 && cols > 1 && !(rs >= 1 && cs >= 1 && (rs >= (cols - 1) * cs + 1 || cs >= (rows - 1) * rs + 1))) return "elements of an output overlap";
+    if (out && ((rows > 1 && rs < 1) || (cols > 1 && cs < 1))) return "elements of an output overlap";
+    return nullptr;
+}
+#define MLIP_MATRIX(...)                                                                  \
+    do {                                                                                  \
+        if (const char *why_ = matrix_fault(__VA_ARGS__)) { set_error("%s", why_); return MLIP_EINVAL; } \
+    } while (0)
+
+static int check_gated(const mlip_gated_t *c)
+{
+    if (!c) { set_error("null pointer argument"); return MLIP_EINVAL; }
+    if (!elem_known(c->dtype)) { set_error("unknown element type"); return MLIP_EINVAL; }
+    if (c->act < MLIP_GATE_SILU || c->act > MLIP_GATE_SILU_SIGMOID) { set_error("unknown gate"); return MLIP_EINVAL; }
+    if (c->n < 0 || c->n > kMostRows || c->d < 1 || c->d > 65536 || c->f < 1 || c->f > 65536) {
+        set_error("sizes outside their ranges (need 0 <= n < 2^31, 1 <= d, f <= 65536)");
+        return MLIP_EINVAL;
+    }
+    const size_t size = elem_size(c->dtype);
+    MLIP_MATRIX(c->x, size, c->n, c->d, c->x_row_stride, c->x_col_stride, false);
+    MLIP_MATRIX(c->w_gate, size, c->d, c->f, c->w_gate_row_stride, c->w_gate_col_stride, false);
+    MLIP_MATRIX(c->w_value, size, c->d, c->f, c->w_value_row_stride, c->w_value_col_stride, false);
+    MLIP_MATRIX(c->b_gate, size, 0, 0, 0, 0, false);
+    MLIP_MATRIX(c->b_value, size, 0, 0, 0, 0, false);
+    return MLIP_OK;
+}
+
+static GatedArgs gated_args(const mlip_gated_t *c, void *out, int64_t out_rs, void *workspace, void *stream)
+{
+    return {c->dtype, c->act, c->n, c->d, c->f, c->x, c->x_row_stride, c->x_col_stride, c->w_gate, c->w_gate_row_stride, c->w_gate_col_stride,
+            c->w_value, c->w_value_row_stride, c->w_value_col_stride, c->b_gate, c->b_value, out, out_rs, workspace, static_cast<hipStream_t>(stream)};
+}
+
+size_t mlip_gated_workspace(const mlip_gated_t *call, int32_t grad)
+{
+    return check_gated(call) == MLIP_OK ? gated_workspace(gated_args(call, nullptr, 0, nullptr, nullptr), grad != 0) : 0;
+}
+
+int mlip_gated(const mlip_gated_t *call, void *out, int64_t out_row_stride, void *workspace, size_t workspace_bytes, void *stream)
+{
+    MLIP_TRY(check_gated(call));
+    MLIP_MATRIX(out, elem_size(call->dtype), call->n, call->f, out_row_stride, 1, true);
+    const GatedArgs a = gated_args(call, out, out_row_stride, workspace, stream);
+    MLIP_TRY(check_workspace(workspace, workspace_bytes, gated_workspace(a, false)));
+    return gated_impl(a);
+}
+
+int mlip_gated_grad(const mlip_gated_t *call, const mlip_gated_grad_t *g, void *workspace, size_t workspace_bytes, void *stream)
+{
+    MLIP_TRY(check_gated(call));
+    if (!g) { set_error("null pointer argument"); return MLIP_EINVAL; }
+    const size_t size = elem_size(call->dtype);
+    MLIP_MATRIX(g->grad, size, call->n, call->f, g->grad_row_stride, g->grad_col_stride, false);
+    if (g->x) MLIP_MATRIX(g->x, size, call->n, call->d, g->x_row_stride, 1, true);
+    if (g->w_gate) MLIP_MATRIX(g->w_gate, size, call->d, call->f, g->w_gate_row_stride, g->w_gate_col_stride, true);
+    if (g->w_value) MLIP_MATRIX(g->w_value, size, call->d, call->f, g->w_value_row_stride, g->w_value_col_stride, true);
+    MLIP_MATRIX(g->b_gate, size, 0, 0, 0, 0, false);
+    MLIP_MATRIX(g->b_value, size, 0, 0, 0, 0, false);
+    const GatedArgs a = gated_args(call, nullptr, 0, workspace, stream);
+    MLIP_TRY(check_workspace(workspace, workspace_bytes, gated_workspace(a, true)));
+    return gated_grad_impl(a, {g->grad, g->grad_row_stride, g->grad_col_stride, g->x, g->x_row_stride, g->w_gate, g->w_gate_row_stride, g->w_gate_col_stride,
+                               g->w_value, g->w_value_row_stride, g->w_value_col_stride, g->b_gate, g->b_value});
+}
+
+static bool residual_sizes(int64_t n, int64_t width) { return n >= 0 && n <= kMostRows && width >= 1 && width <= 8192; }
+
+static int check_residual(const mlip_residual_t *c)
+{
+    if (!c) { set_error("null pointer argument"); return MLIP_EINVAL; }
+    if (!elem_known(c->dtype) || (c->param_dtype != MLIP_DTYPE_F32 && c->param_dtype != c->dtype)) { set_error("unknown element type, or parameters of another type than fp32 and the arrays'"); return MLIP_EINVAL; }
+    if (c->kind != MLIP_NORM_RMS && c->kind != MLIP_NORM_LAYER) { set_error("unknown norm"); return MLIP_EINVAL; }
+    if (!residual_sizes(c->n, c->width)) { set_error("sizes outside their ranges (need 0 <= n < 2^31, 1 <= width <= 8192)"); return MLIP_EINVAL; }
+    if (c->gate_kind < MLIP_RESIDUAL_GATE_NONE || c->gate_kind > MLIP_RESIDUAL_GATE_COL) { set_error("unknown kind of gate"); return MLIP_EINVAL; }
+    if (!(c->eps >= 0.f)) { set_error("eps must be a number that is not negative"); return MLIP_EINVAL; }
+    if ((!c->post && (c->post_w || c->post_b)) || (!c->pre && (c->pre_w || c->pre_b))) { set_error("parameters of a norm that the call does not have"); return MLIP_EINVAL; }
+    if (c->n > 0 && !c->z && (c->gate_kind != MLIP_RESIDUAL_GATE_NONE || c->scale || c->post || !c->pre)) {
+        set_error("without z there is a norm of x alone");
+        return MLIP_EINVAL;
+    }
+    const size_t size = elem_size(c->dtype), param = elem_size(c->param_dtype);
+    MLIP_MATRIX(c->x, size, c->n, c->width, c->x_row_stride, c->x_col_stride, false);
+    if (c->z) MLIP_MATRIX(c->z, size, c->n, c->width, c->z_row_stride, c->z_col_stride, false);
+    if (c->gate_kind == MLIP_RESIDUAL_GATE_FULL) MLIP_MATRIX(c->gate, size, c->n, c->width, c->gate_row_stride, c->gate_col_stride, false);
+    if (c->gate_kind == MLIP_RESIDUAL_GATE_ROW) MLIP_MATRIX(c->gate, size, c->n, 1, c->gate_row_stride, 0, false);
+    if (c->gate_kind == MLIP_RESIDUAL_GATE_COL) MLIP_MATRIX(c->gate, size, 1, c->width, 0, 1, false);
+    for (const void *p : {c->scale, c->post_w, c->post_b, c->pre_w, c->pre_b}) MLIP_MATRIX(p, param, 0, 0, 0, 0, false);
+    return MLIP_OK;
+}
+
+static ResidualArgs residual_args(const mlip_residual_t *c, void *y, int64_t y_rs, void *norm, int64_t norm_rs, void *stream)
+{
+    return {c->dtype, c->param_dtype, c->kind, c->gate_kind, c->post != 0, c->pre != 0, c->n, c->width, c->eps, c->factor, c->x, c->x_row_stride, c->x_col_stride,
+            c->z, c->z_row_stride, c->z_col_stride, c->gate, c->gate_row_stride, c->gate_kind == MLIP_RESIDUAL_GATE_COL ? 1 : c->gate_col_stride,
+            c->scale, c->post_w, c->post_b, c->pre_w, c->pre_b, y, y_rs, norm, norm_rs, static_cast<hipStream_t>(stream)};
+}
+
+int mlip_residual(const mlip_residual_t *call, void *y, int64_t y_row_stride, void *norm, int64_t norm_row_stride, void *stream)
+{
+    MLIP_TRY(check_residual(call));
+    const size_t size = elem_size(call->dtype);
+    if ((y && !call->z && call->n > 0) || (norm && !call->pre)) { set_error("an output of what the call does not have"); return MLIP_EINVAL; }
+    if (y || !call->pre) MLIP_MATRIX(y, size, call->n, call->width, y_row_stride, 1, true);
+    if (call->pre) MLIP_MATRIX(norm, size, call->n, call->width, norm_row_stride, 1, true);
+    return residual_impl(residual_args(call, y, y_row_stride, norm, norm_row_stride, stream));
+}
+
+size_t mlip_residual_grad_workspace(int64_t n, int64_t width) { return residual_sizes(n, width) ? residual_grad_workspace(n, width) : 0; }
+
+int mlip_residual_grad(const mlip_residual_t *call, const mlip_residual_grad_t *g, void *workspace, size_t workspace_bytes, void *stream)
+{
+    MLIP_TRY(check_residual(call));
+    if (!g || (call->n > 0 && !g->y && !g->norm)) { set_error("null pointer argument"); return MLIP_EINVAL; }
+    if (g->norm && !call->pre) { set_error("a gradient of a norm that the call does not have"); return MLIP_EINVAL; }
+    if ((call->n > 0 && !call->z && g->z) || (call->gate_kind == MLIP_RESIDUAL_GATE_NONE && g->gate) || (!call->scale && g->scale) || (!call->post_w && g->post_w) ||
+        (!call->post_b && g->post_b) || (!call->pre_w && g->pre_w) || (!call->pre_b && g->pre_b)) {
+        set_error("an output of what the call does not have");
+        return MLIP_EINVAL;
+    }
+    const size_t size = elem_size(call->dtype), param = elem_size(call->param_dtype);
+    if (g->y) MLIP_MATRIX(g->y, size, call->n, call->width, g->y_row_stride, g->y_col_stride, false);
+    if (g->norm) MLIP_MATRIX(g->norm, size, call->n, call->width, g->norm_row_stride, g->norm_col_stride, false);
+    if (g->x) MLIP_MATRIX(g->x, size, call->n, call->width, g->x_row_stride, 1, true);
+    if (g->z) MLIP_MATRIX(g->z, size, call->n, call->width, g->z_row_stride, 1, true);
+    if (g->gate && call->gate_kind == MLIP_RESIDUAL_GATE_FULL) MLIP_MATRIX(g->gate, size, call->n, call->width, g->gate_row_stride, 1, true);
+    else if (g->gate) MLIP_MATRIX(g->gate, size, call->gate_kind == MLIP_RESIDUAL_GATE_ROW ? call->n : 1, 1, g->gate_row_stride, 1, true);
+    for (const void *p : {g->scale, g->post_w, g->post_b, g->pre_w, g->pre_b}) MLIP_MATRIX(p, param, 0, 0, 0, 0, false);
+    MLIP_TRY(check_workspace(workspace, workspace_bytes, residual_grad_workspace(call->n, call->width)));
+    return residual_grad_impl(residual_args(call, nullptr, 0, nullptr, 0, stream),
+                              {g->y, g->y_row_stride, g->y_col_stride, g->norm, g->norm_row_stride, g->norm_col_stride, g->x, g->x_row_stride, g->z, g->z_row_stride,
+                               g->gate, g->gate_row_stride, g->scale, g->post_w, g->post_b, g->pre_w, g->pre_b, workspace});
+}
+
+static int check_matrices(const mlip_matrix_t *list, int32_t count)
+{
+    if (count < 0) { set_error("count must not be negative"); return MLIP_EINVAL; }
+    if (!list && count > 0) { set_error("null pointer argument"); return MLIP_EINVAL; }
+    for (int32_t t = 0; t < count; ++t) {
+        const mlip_matrix_t &x = list[t];
+        const char *why = nullptr;
+        if (!elem_known(x.dtype)) why = "unknown element type";
+        else if (x.rows < 0 || x.rows > (1 << 20) || x.cols < 0 || x.cols > (1 << 20) || (x.rows > 32768 && x.cols > 32768) || x.rows * x.cols > kMostRows)
+            why = "sizes outside their ranges (need rows, cols <= 2^20, one of them <= 32768, elements < 2^31)";
+        else why = matrix_fault(x.src, elem_size(x.dtype), x.rows, x.cols, x.src_row_stride, x.src_col_stride, false);
+        if (!why) why = matrix_fault(x.dst, elem_size(x.dtype), x.rows, x.cols, x.dst_row_stride, x.dst_col_stride, true);
+        if (why) { set_error("matrix %d: %s", t, why); return MLIP_EINVAL; }
+    }
+    return MLIP_OK;
+}
+
+size_t mlip_orthogonalise_workspace(const mlip_matrix_t *matrices, int32_t count)
+{
+    return check_matrices(matrices, count) == MLIP_OK ? ortho_workspace(matrices, count) : 0;
+}
+
+int mlip_orthogonalise(const mlip_matrix_t *matrices, int32_t count, int32_t steps, const double *coefficients, double eps, float scale, void *workspace,
+                       size_t workspace_bytes, void *stream)
+{
+    MLIP_TRY(check_matrices(matrices, count));
+    if (!coefficients) { set_error("null pointer argument"); return MLIP_EINVAL; }
+    if (steps < 0 || steps > 1000) { set_error("steps outside [0, 1000]"); return MLIP_EINVAL; }
+    if (!(eps >= 0.0)) { set_error("eps must be a number that is not negative"); return MLIP_EINVAL; }
+    MLIP_TRY(check_workspace(workspace, workspace_bytes, ortho_workspace(matrices, count)));
+    return ortho_impl(matrices, count, steps, coefficients, eps, scale, workspace, static_cast<hipStream_t>(stream));
+}
+
 int mlip_copy_to_host(const mlip_graph_t *g, void *dst_host, const void *src_device, size_t bytes)
 {
     if (!g || !dst_host || (!src_device && bytes)) { set_error("null pointer argument"); return MLIP_EINVAL; }

@@ -301,4 +301,74 @@ size_t grad_workspace(int32_t count);
 int grad_norm_impl(const mlip_tensor_t *list, int32_t count, bool clip, float max_norm, float *norm, void *workspace, size_t bytes,
                    hipStream_t stream);
 
+// Arguments of the gated projections, of the residual sum and of their gradients, checked (strides in elements)
+struct GatedArgs {
+    int32_t dtype, act;
+    int64_t n, d, f;
+    const void *x;
+    int64_t x_rs, x_cs;
+    const void *wg;
+    int64_t wg_rs, wg_cs;
+    const void *wv;
+    int64_t wv_rs, wv_cs;
+    const void *bg, *bv;
+    void *out;
+    int64_t out_rs;
+    void *workspace;
+    hipStream_t stream;
+};
+struct GatedGrad {
+    const void *bar;
+    int64_t bar_rs, bar_cs;
+    void *dx;
+    int64_t dx_rs;
+    void *dwg;
+    int64_t dwg_rs, dwg_cs;
+    void *dwv;
+    int64_t dwv_rs, dwv_cs;
+    void *dbg, *dbv;
+};
+size_t gated_workspace(const GatedArgs &a, bool grad);
+int gated_impl(const GatedArgs &a);
+int gated_grad_impl(const GatedArgs &a, const GatedGrad &g);
+
+struct ResidualArgs {
+    int32_t dtype, param_dtype, kind, gate_kind;
+    bool post, pre;
+    int64_t n, width;
+    float eps, factor;
+    const void *x;
+    int64_t x_rs, x_cs;
+    const void *z;
+    int64_t z_rs, z_cs;
+    const void *gate;
+    int64_t gate_rs, gate_cs;
+    const void *scale, *post_w, *post_b, *pre_w, *pre_b;
+    void *y;
+    int64_t y_rs;
+    void *norm;
+    int64_t norm_rs;
+    hipStream_t stream;
+};
+struct ResidualGrad {
+    const void *dy;
+    int64_t dy_rs, dy_cs;
+    const void *dn;
+    int64_t dn_rs, dn_cs;
+    void *dx;
+    int64_t dx_rs;
+    void *dz;
+    int64_t dz_rs;
+    void *dgate;
+    int64_t dgate_rs;
+    void *dscale, *dpost_w, *dpost_b, *dpre_w, *dpre_b;
+    void *workspace;
+};
+size_t residual_grad_workspace(int64_t n, int64_t width);
+int residual_impl(const ResidualArgs &a);
+int residual_grad_impl(const ResidualArgs &a, const ResidualGrad &g);
+
+size_t ortho_workspace(const mlip_matrix_t *list, int32_t count);
+int ortho_impl(const mlip_matrix_t *list, int32_t count, int32_t steps, const double coef[3], double eps, float scale, void *workspace, hipStream_t stream);
+
 }  // namespace mlip
