@@ -131,43 +131,90 @@ template <class K> struct GateArgs {
     int64_t gv_ld, gv_part;
 };
 
-template <class K, bool BACK> using GateProduct = Product<typename K::T, K::kParts, true, true, 128, 128, 64, 64>;
+// Four elements from column c of a row on, zeros from `cols` on
+template <class E> __device__ inline void load4(float (&v)[4], const E *row, int64_t cs, int64_t c, int64_t cols)
+{
+    if (cs == 1 && c + 4 <= cols) {
+        const Cols<E, 4> w = *reinterpret_cast<const Far<E, 4> *>(row + c);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = (float)w[k];
+        return;
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = c + k < cols ? (float)row[(c + k) * cs] : 0.f;
+}
+template <class E> __device__ inline void store4(const float (&v)[4], E *row, int64_t c, int64_t cols)
+{
+    if (c + 4 <= cols) {
+        Cols<E, 4> w;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[k] = to_elem<E>(v[k]);
+        *reinterpret_cast<Far<E, 4> *>(row + c) = w;
+        return;
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+        if (c + k < cols) row[c + k] = to_elem<E>(v[k]);
+}
 
+// The weights are the products' first operand and the rows their second, so that a lane has four neighbouring features of one row in a row of
+// registers, and loads and stores them as one access.
 template <class K, bool BACK> __global__ __launch_bounds__(256) void k_gates(GateArgs<K> a)
 {
-    using P = GateProduct<K, BACK>;
+    using P = Product<typename K::T, K::kParts, true, true, 128, 128, 64, 64>;
     __shared__ typename P::Lds lds;
     const int64_t tile = xcd_order(blockIdx.x, gridDim.x), m0 = tile / a.n_tiles * 128, n0 = tile % a.n_tiles * 128;
     f32x16 acc[2][2] = {};
-    P::run(a.x, a.w, m0, n0, 0, a.d_p, lds, acc, NoEach{});
+    P::run(a.w, a.x, n0, m0, 0, a.d_p, lds, acc, NoEach{});
     const int wave = threadIdx.x >> 6;
-    const int64_t row0 = m0 + wave / 2 * 64, col0 = n0 + wave % 2 * 64, f = col0 / 2 + acc_col();
+    const int64_t col0 = n0 + wave / 2 * 64, f0 = col0 / 2 + acc_row(0);
     if (col0 >= a.w.rows) return;
-    const bool there = f < a.f;
-    const float bg = there && a.bg ? (float)a.bg[f] : 0.f, bv = there && a.bv ? (float)a.bv[f] : 0.f;
+    float bg[4][4] = {}, bv[4][4] = {};
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        if (a.bg) load4(bg[q], a.bg, 1, f0 + 8 * q, a.f);
+        if (a.bv) load4(bv[q], a.bv, 1, f0 + 8 * q, a.f);
+    }
     with_act(a.act, [&](auto act) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int j = 0; j < 2; ++j) {
+            const int64_t row = m0 + wave % 2 * 64 + 32 * j + acc_col();
+            if (row >= a.x.rows) continue;
+            float bar[4][4];
+            if constexpr (BACK)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int64_t row = row0 + 32 * i + acc_row(r);
-                if (row >= a.x.rows) continue;
-                const Phi y = phi<decltype(act)::value>(acc[i][0][r] + bg, acc[i][1][r] + bv);
-                if constexpr (!BACK) {
-                    if (there) a.out[row * a.out_rs + f] = to_elem<typename K::E>(y.h);
-                } else {
-                    const float bar = there ? (float)a.bar[row * a.bar_rs + f * a.bar_cs] : 0.f;
-                    typename K::T g[K::kParts], v[K::kParts];
-                    split(there ? bar * y.g : 0.f, g);
-                    split(there ? bar * y.v : 0.f, v);
-                    typename K::T *to = a.gv + row * a.gv_ld + col0 + acc_col();
+                for (int q = 0; q < 4; ++q) load4(bar[q], a.bar + row * a.bar_rs, a.bar_cs, f0 + 8 * q, a.f);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int64_t f = f0 + 8 * q;
+                float h[4];
+                Half4<typename K::T> g[K::kParts], v[K::kParts];
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    const Phi y = phi<decltype(act)::value>(acc[0][j][4 * q + t] + bg[q][t], acc[1][j][4 * q + t] + bv[q][t]);
+                    if constexpr (!BACK) h[t] = y.h;
+                    else {
+                        typename K::T gs[K::kParts], vs[K::kParts];
+                        split(f + t < a.f ? bar[q][t] * y.g : 0.f, gs);
+                        split(f + t < a.f ? bar[q][t] * y.v : 0.f, vs);
+#pragma unroll
+                        for (int p = 0; p < K::kParts; ++p) {
+                            g[p][t] = gs[p];
+                            v[p][t] = vs[p];
+                        }
+                    }
+                }
+                if constexpr (!BACK) store4(h, a.out + row * a.out_rs, f, a.f);
+                else {
+                    typename K::T *to = a.gv + row * a.gv_ld + col0 + acc_row(4 * q);
 #pragma unroll
                     for (int p = 0; p < K::kParts; ++p) {
-                        to[p * a.gv_part] = g[p];
-                        to[p * a.gv_part + 32] = v[p];
+                        *reinterpret_cast<Half4<typename K::T> *>(to + p * a.gv_part) = g[p];
+                        *reinterpret_cast<Half4<typename K::T> *>(to + p * a.gv_part + 32) = v[p];
                     }
                 }
             }
+        }
     });
 }
 
@@ -180,23 +227,24 @@ template <class K> struct RowBarArgs {
 };
 template <class K, int BM, int BN> __global__ __launch_bounds__(256) void k_row_bars(RowBarArgs<K> a)
 {
-    using P = Product<typename K::T, K::kParts, true, true, BM, BN, 64, 64>;
+    using P = Product<typename K::T, K::kParts, true, true, BN, BM, 64, 64>;   // (d first, rows second, as above)
     __shared__ typename P::Lds lds;
     const int64_t tile = xcd_order(blockIdx.x, gridDim.x), m0 = tile / a.n_tiles * BM, n0 = tile % a.n_tiles * BN;
     f32x16 acc[2][2] = {};
-    P::run(a.gv, a.w, m0, n0, 0, a.gv.cols, lds, acc, NoEach{});
+    P::run(a.w, a.gv, n0, m0, 0, a.gv.cols, lds, acc, NoEach{});
     const int wave = threadIdx.x >> 6;
-    const int64_t row0 = m0 + wave / (BN / 64) * 64, col0 = n0 + wave % (BN / 64) * 64 + acc_col();
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int j = 0; j < 2; ++j) {
+        const int64_t row = m0 + wave % (BM / 64) * 64 + 32 * j + acc_col();
+        if (row >= a.gv.rows) continue;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const int64_t row = row0 + 32 * i + acc_row(r);
-            if (row >= a.gv.rows) continue;
+        for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int j = 0; j < 2; ++j)
-                if (col0 + 32 * j < a.w.rows) a.out[row * a.out_rs + col0 + 32 * j] = to_elem<typename K::E>(acc[i][j][r]);
-        }
+            for (int q = 0; q < 4; ++q) {
+                const float v[4] = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+                store4(v, a.out + row * a.out_rs, n0 + wave / (BM / 64) * 64 + 32 * i + acc_row(4 * q), a.w.rows);
+            }
+    }
 }
 
 // The chunk's share of [dWg dWv]^T = [G V]^T x, [2 f][d], its rows in `splits` runs; and of the biases' gradients, the column sums of G and V

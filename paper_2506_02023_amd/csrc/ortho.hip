@@ -2,8 +2,12 @@
 // columns).  An odd polynomial of X acts on its singular values alone, and the usual coefficients bring them all near 1.
 //
 // A step is three products: A = X X^T and B = b A + c A A, which are symmetric (the tiles above the diagonal are computed and written twice), and
-// a X + B X.  The steps stretch small singular values by a each, up to a^5 = 485 times in all, and with them what a rounding of X put there: X, A and
-// B are therefore held in two fp16 parts each (22 bits) and the products taken as three, at the precision of fp32 and at 16/3 of its matrix rate.
+// a X + B X.  The steps stretch small singular values by a each, up to a^5 = 485 times in all, and with them what a rounding of X put there: X is
+// therefore held in two fp16 parts (22 bits).  The diagonals of A and B, which are large against the rest, are kept in fp32 beside them and enter the
+// next result element by element: X' = (a + diag B) X + (B - diag B) X.  Only what is left goes through the matrix units,
+//   fp32 and fp16 matrices: in two parts each, three products, at the precision of fp32;
+//   bf16 matrices: rounded to fp16, one product.  The result is then off by 0.4 to 1.2e-3 (norm of the difference by norm; gradients of shared directions
+//   and noise 5e-4, singular values down to 10^-5 1.2e-3) beside the 1.7e-3 of its own rounding; with the diagonals rounded too it would be 2e-3.
 // Powers of two bring the entries into the range of fp16: X holds at most |X| <= 1.3 (for coefficients that keep it there), entries of the size 1/sqrt(n).
 #include "products.h"
 
@@ -12,17 +16,16 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kList = 24;                  // matrices of a launch
-constexpr int kNormBlocks = 64;            // partial sums of a matrix
+constexpr int kNormBlocks = 256;           // partial sums of a matrix
 constexpr float kGramScale = 256.f;
 
 using P = _Float16;
-constexpr int kParts = 2;
 
 struct Item {
     const void *src;
     void *dst;
     int64_t src_rs, src_cs, dst_rs, dst_cs;   // of the matrix with m <= n
-    int64_t x[2], gram, poly;                 // places in scratch memory, in elements of 16 bits
+    int64_t x[2], low[2], gram, poly, diag;   // places in scratch memory, in elements of 16 bits: X's high and low parts, now and next; A, B, their diagonals
     int32_t m, n, m_p, n_p, dtype;
     float x_scale;
 };
@@ -34,12 +37,12 @@ struct List {
 static_assert(sizeof(List) <= 3800, "arguments of a launch");
 
 // The item of a block, and the block's number among the item's
-__device__ inline const Item &item_of(const List &l, uint32_t block, uint32_t &at)
+__device__ inline int item_of(const List &l, uint32_t block, uint32_t &at)
 {
     int i = 0;
     while (i + 1 < l.count && l.first[i + 1] <= block) ++i;
     at = block - l.first[i];
-    return l.item[i];
+    return i;
 }
 
 template <class Fn> __device__ inline void device_elem(int32_t dtype, Fn &&f)
@@ -62,51 +65,89 @@ __device__ inline double block_sum(double v)
     return v;
 }
 
-// squares of item i to part[i * kNormBlocks + block], in kNormBlocks blocks each
+// squares of item i to part[i * kNormBlocks + block], in kNormBlocks blocks each: rows (or columns, whichever lie close together) in pieces of eight elements
 __global__ __launch_bounds__(kThreads) void k_squares(List l, double *part)
 {
     const Item &it = l.item[blockIdx.y];
     double sum = 0.0;
     device_elem(it.dtype, [&](auto e) {
-        const decltype(e) *src = static_cast<const decltype(e) *>(it.src);
-        const bool by_row = it.src_cs <= it.src_rs;   // the inner loop along what lies close together
-        const int64_t in = by_row ? it.n : it.m, out = by_row ? it.m : it.n, is = by_row ? it.src_cs : it.src_rs, os = by_row ? it.src_rs : it.src_cs;
-        const int64_t total = in * out;
+        using E = decltype(e);
+        const E *src = static_cast<const E *>(it.src);
+        const bool by_row = it.src_cs <= it.src_rs;
+        const int64_t is = by_row ? it.src_cs : it.src_rs, os = by_row ? it.src_rs : it.src_cs;
+        const int in = by_row ? it.n : it.m, out = by_row ? it.m : it.n, pieces = (in + 7) / 8;
+        const int64_t total = (int64_t)pieces * out;
+#pragma unroll 4
         for (int64_t k = (int64_t)blockIdx.x * kThreads + threadIdx.x; k < total; k += (int64_t)kNormBlocks * kThreads) {
-            const double x = (double)(float)src[k / in * os + k % in * is];
-            sum = fma(x, x, sum);
+            const int o = (int)((uint32_t)k / (uint32_t)pieces), i = (int)((uint32_t)k % (uint32_t)pieces) * 8;
+            const E *p = src + o * os + i * is;
+            if (is == 1 && i + 8 <= in) {
+                const Cols<E, 8> w = *reinterpret_cast<const Far<E, 8> *>(p);
+#pragma unroll
+                for (int t = 0; t < 8; ++t) sum = fma((double)(float)w[t], (double)(float)w[t], sum);
+            } else
+                for (int t = 0; t < 8 && i + t < in; ++t) sum = fma((double)(float)p[t * is], (double)(float)p[t * is], sum);
         }
     });
     sum = block_sum(sum);
     if (threadIdx.x == 0) part[blockIdx.y * kNormBlocks + blockIdx.x] = sum;
 }
 
-// X_0 in parts: tiles of 64 rows and 64 columns, zeros up to n_p
+// What X_0 is G times, x_scale included
+__device__ inline double start_scale(double squares, double eps, float x_scale)
+{
+    const double norm = sqrt(squares);
+    return (double)x_scale / (norm > eps || norm != norm ? norm : eps);
+}
+
+// X_0 in parts: tiles of 64 rows and 64 columns, zeros up to n_p.  Loads and stores go along what lies close together, eight elements a thread.
 __global__ __launch_bounds__(kThreads) void k_start(List l, const double *part, double eps, P *ws)
 {
     __shared__ float tile[64][65];
     uint32_t at;
-    const Item &it = item_of(l, blockIdx.x, at);
-    const double squares = block_sum(threadIdx.x < kNormBlocks ? part[(&it - l.item) * kNormBlocks + threadIdx.x] : 0.0);
-    const double norm = sqrt(squares);
-    const double scale = (double)it.x_scale / (norm > eps || norm != norm ? norm : eps);
-    const int tiles = it.n_p / 64;
-    const int64_t r0 = at / tiles * 64, c0 = at % tiles * 64;
+    const int i = item_of(l, blockIdx.x, at);
+    const Item &it = l.item[i];
+    const double scale = start_scale(block_sum(threadIdx.x < kNormBlocks ? part[i * kNormBlocks + threadIdx.x] : 0.0), eps, it.x_scale);
+    const int tiles = it.n_p / 64, m = it.m, n = it.n, r0 = at / tiles * 64, c0 = at % tiles * 64;
     const bool by_row = it.src_cs <= it.src_rs;
-    const int p = threadIdx.x & 63, q = threadIdx.x >> 6;
+    const int64_t in = by_row ? it.src_cs : it.src_rs, out = by_row ? it.src_rs : it.src_cs;   // strides along the inner and the outer loop
     device_elem(it.dtype, [&](auto e) {
-        const decltype(e) *src = static_cast<const decltype(e) *>(it.src);
-        for (int i = q; i < 64; i += 4) {
-            const int r = by_row ? i : p, c = by_row ? p : i;
-            tile[r][c] = r0 + r < it.m && c0 + c < it.n ? (float)((double)(float)src[(r0 + r) * it.src_rs + (c0 + c) * it.src_cs] * scale) : 0.f;
+        using E = decltype(e);
+        const E *src = static_cast<const E *>(it.src) + r0 * it.src_rs + c0 * it.src_cs;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int piece = threadIdx.x + k * kThreads, o = piece / 8, i0 = piece % 8 * 8;
+            const int most = by_row ? n - c0 : m - r0;
+            float v[8] = {};
+            if (o < (by_row ? m - r0 : n - c0)) {
+                if (in == 1 && i0 + 8 <= most) {
+                    const Cols<E, 8> w = *reinterpret_cast<const Far<E, 8> *>(src + o * out + i0);
+#pragma unroll
+                    for (int t = 0; t < 8; ++t) v[t] = (float)w[t];
+                } else
+#pragma unroll
+                    for (int t = 0; t < 8; ++t) v[t] = i0 + t < most ? (float)src[o * out + (i0 + t) * in] : 0.f;
+            }
+#pragma unroll
+            for (int t = 0; t < 8; ++t) (by_row ? tile[o][i0 + t] : tile[i0 + t][o]) = (float)(v[t] * scale);
         }
     });
     __syncthreads();
-    for (int i = q; i < 64 && r0 + i < it.m; i += 4) {
-        P v[kParts];
-        split(tile[i][p], v);
-        P *to = ws + it.x[0] + (r0 + i) * it.n_p + c0 + p;
-        for (int k = 0; k < kParts; ++k) to[(int64_t)k * it.m * it.n_p] = v[k];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int piece = threadIdx.x + k * kThreads, r = piece / 8, c = piece % 8 * 8;
+        if (r0 + r >= m) continue;
+        Half8<P> hi, lo;
+#pragma unroll
+        for (int t = 0; t < 8; ++t) {
+            P v[2];
+            split(tile[r][c + t], v);
+            hi[t] = v[0];
+            lo[t] = v[1];
+        }
+        const int64_t to = (int64_t)(r0 + r) * it.n_p + c0 + c;
+        *reinterpret_cast<Half8<P> *>(ws + it.x[0] + to) = hi;
+        *reinterpret_cast<Half8<P> *>(ws + it.low[0] + to) = lo;
     }
 }
 
@@ -114,13 +155,23 @@ __global__ __launch_bounds__(kThreads) void k_start(List l, const double *part, 
 
 struct NoEach { template <class F> __device__ inline void operator()(F &) const {} };
 
-__device__ inline Panel x_panel(const Item &it, const P *ws, int which)
-{
-    return {ws + it.x[which], it.n_p, (int64_t)it.m * it.n_p, it.m, it.n_p};
-}
+// X, or A - diag A, or B - diag B
+__device__ inline Panel x_panel(const Item &it, const P *ws, int which) { return {ws + it.x[which], it.n_p, it.low[which] - it.x[which], it.m, it.n_p}; }
 __device__ inline Panel square_panel(const Item &it, const P *ws, int64_t at) { return {ws + at, it.m_p, (int64_t)it.m * it.m_p, it.m, it.m_p}; }
 
-__device__ inline float both(const P *p, int64_t part) { return (float)p[0] + (float)p[part]; }
+__device__ inline float both(P hi, P lo) { return (float)hi + (float)lo; }
+
+// Four values split in two
+__device__ inline void split4(const float (&v)[4], Half4<P> &hi, Half4<P> &lo)
+{
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+        P s[2];
+        split(v[t], s);
+        hi[t] = s[0];
+        lo[t] = s[1];
+    }
+}
 
 // Tile (i, j) with j >= i of number t: rows of the triangle of `tiles` tiles a side one after another
 __device__ inline void triangle(int t, int tiles, int &i, int &j)
@@ -130,76 +181,125 @@ __device__ inline void triangle(int t, int tiles, int &i, int &j)
     j = i + t;
 }
 
-// SQUARE: poly = b gram + c gram gram; else gram = X X^T
-template <bool SQUARE> __global__ __launch_bounds__(kThreads) void k_symmetric(List l, P *ws, int which, float b, float c)
+// SQUARE: B = b A + c A A; else A = X X^T.  Off the diagonal with D = diag A, R = A - D:  A A = R R + (D_i + D_j) R_ij, on it D_i^2 + (R R)_ii.
+// A lane has four neighbouring columns of one row (the row is the second operand's); the mirrored tile is stored by columns.
+template <int PARTS, bool SQUARE> __global__ __launch_bounds__(kThreads) void k_symmetric(List l, P *ws, int which, float b, float c)
 {
-    using M = Product<P, kParts, true, true, 128, 128, 64, 64>;
-    __shared__ M::Lds lds;
+    using M = Product<P, PARTS, true, true, 128, 128, 64, 64>;
+    __shared__ typename M::Lds lds;
     uint32_t at;
-    const Item &it = item_of(l, blockIdx.x, at);
+    const Item &it = l.item[item_of(l, blockIdx.x, at)];
     int ti, tj;
     triangle((int)at, (it.m + 127) / 128, ti, tj);
     const Panel from = SQUARE ? square_panel(it, ws, it.gram) : x_panel(it, ws, which);
     f32x16 acc[2][2] = {};
-    M::run(from, from, ti * 128, tj * 128, 0, SQUARE ? it.m_p : it.n_p, lds, acc, NoEach{});
-    const int wave = threadIdx.x >> 6, row0 = ti * 128 + wave / 2 * 64, col0 = tj * 128 + wave % 2 * 64 + acc_col();
+    M::run(from, from, tj * 128, ti * 128, 0, SQUARE ? it.m_p : it.n_p, lds, acc, NoEach{});
+    const int wave = threadIdx.x >> 6, m = it.m, m_p = it.m_p;
+    const int64_t part = (int64_t)m * m_p;
     P *to = ws + (SQUARE ? it.poly : it.gram);
-    const int64_t part = (int64_t)it.m * it.m_p;
+    const P *gram = ws + it.gram;
+    float *diag = reinterpret_cast<float *>(ws + it.diag);   // of A, then of B
     const float scale = SQUARE ? c / kGramScale : kGramScale / (it.x_scale * it.x_scale);
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int j = 0; j < 2; ++j) {
+        const int row = ti * 128 + wave % 2 * 64 + 32 * j + acc_col();
+        if (row >= m) continue;
+        const float dr = SQUARE ? diag[row] : 0.f;
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+        for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int row = row0 + 32 * i + acc_row(r), col = col0 + 32 * j;
-                if (row >= it.m || col >= it.m_p) continue;
-                float y = acc[i][j][r] * scale;
-                if (SQUARE && col < it.m) y = fmaf(b, both(ws + it.gram + (int64_t)row * it.m_p + col, part), y);
-                if (col >= it.m) y = 0.f;
-                P v[kParts];
-                split(y, v);
-                for (int p = 0; p < kParts; ++p) {
-                    to[p * part + (int64_t)row * it.m_p + col] = v[p];
-                    if (tj > ti && col < it.m) to[p * part + (int64_t)col * it.m_p + row] = v[p];
+            for (int q = 0; q < 4; ++q) {
+                const int col = tj * 128 + wave / 2 * 64 + 32 * i + acc_row(4 * q);
+                if (col >= m_p) continue;
+                const int64_t here = (int64_t)row * m_p + col;
+                float y[4];
+                Half4<P> gh = {}, gl = {};
+                if constexpr (SQUARE) {
+                    gh = *reinterpret_cast<const Half4<P> *>(gram + here);
+                    gl = *reinterpret_cast<const Half4<P> *>(gram + part + here);
+                }
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    y[t] = acc[i][j][4 * q + t] * scale;
+                    if (SQUARE && col + t < m) {
+                        const float dc = diag[col + t];
+                        y[t] = fmaf(fmaf(c, dr + dc, b), both(gh[t], gl[t]), y[t]);
+                    }
+                    if (col + t == row) {
+                        const float d = y[t] * (1.f / kGramScale);
+                        diag[SQUARE ? m + row : row] = SQUARE ? fmaf(dr, fmaf(c, dr, b), d) : d;
+                        y[t] = 0.f;
+                    }
+                    if (col + t >= m) y[t] = 0.f;
+                }
+                Half4<P> v[2];
+                split4(y, v[0], v[1]);
+#pragma unroll
+                for (int p = 0; p < (SQUARE ? PARTS : 2); ++p) {
+                    *reinterpret_cast<Half4<P> *>(to + p * part + here) = v[p];
+                    if (tj > ti)
+#pragma unroll
+                        for (int t = 0; t < 4; ++t)
+                            if (col + t < m) to[p * part + (int64_t)(col + t) * m_p + row] = v[p][t];
                 }
             }
+    }
 }
 
-// X' = a X + poly X; the last one to where it belongs, times `scale`
-template <bool LAST> __global__ __launch_bounds__(kThreads) void k_apply(List l, P *ws, int which, float a, float scale)
+// X' = (a + diag B) X + (B - diag B) X; the last one to where it belongs, times `scale`.  Columns of X are the first operand, its rows the second.
+template <int PARTS, bool LAST> __global__ __launch_bounds__(kThreads) void k_apply(List l, P *ws, int which, float a, float scale)
 {
-    using M = Product<P, kParts, true, false, 128, 128, 64, 64>;
-    __shared__ M::Lds lds;
+    using M = Product<P, PARTS, false, true, 128, 128, 64, 64>;
+    __shared__ typename M::Lds lds;
     uint32_t at;
-    const Item &it = item_of(l, blockIdx.x, at);
-    const int tiles = (it.n_p + 127) / 128, m0 = at / tiles * 128, n0 = at % tiles * 128;
+    const Item &it = l.item[item_of(l, blockIdx.x, at)];
+    const int tiles = (it.m + 127) / 128, m0 = at % tiles * 128, n0 = at / tiles * 128;   // (tiles of the same columns one after another)
     f32x16 acc[2][2] = {};
-    M::run(square_panel(it, ws, it.poly), x_panel(it, ws, which), m0, n0, 0, it.m_p, lds, acc, NoEach{});
-    const int wave = threadIdx.x >> 6, row0 = m0 + wave / 2 * 64, col0 = n0 + wave % 2 * 64 + acc_col();
-    const int64_t part = (int64_t)it.m * it.n_p;
+    M::run(x_panel(it, ws, which), square_panel(it, ws, it.poly), n0, m0, 0, it.m_p, lds, acc, NoEach{});
+    const int wave = threadIdx.x >> 6, n_p = it.n_p;
     const P *old = ws + it.x[which];
-    P *to = ws + it.x[which ^ 1];
+    const P *old_low = ws + it.low[which];
+    P *to = ws + it.x[which ^ 1], *to_low = ws + it.low[which ^ 1];   // (of one part the low ones stay where they are)
+    const float *diag = reinterpret_cast<const float *>(ws + it.diag) + it.m;
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int j = 0; j < 2; ++j) {
+        const int row = m0 + wave % 2 * 64 + 32 * j + acc_col();
+        if (row >= it.m) continue;
+        const float f = a + diag[row];
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+        for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int row = row0 + 32 * i + acc_row(r), col = col0 + 32 * j;
-                if (row >= it.m || col >= (LAST ? it.n : it.n_p)) continue;
-                const int64_t here = (int64_t)row * it.n_p + col;
-                const float y = fmaf(a, both(old + here, part), acc[i][j][r] * (1.f / kGramScale));
+            for (int q = 0; q < 4; ++q) {
+                const int col = n0 + wave / 2 * 64 + 32 * i + acc_row(4 * q);
+                if (col >= n_p) continue;
+                const int64_t here = (int64_t)row * n_p + col;
+                const Half4<P> hi = *reinterpret_cast<const Half4<P> *>(old + here), lo = *reinterpret_cast<const Half4<P> *>(old_low + here);
+                float y[4];
+#pragma unroll
+                for (int t = 0; t < 4; ++t) y[t] = fmaf(f, both(hi[t], lo[t]), acc[i][j][4 * q + t] * (1.f / kGramScale));
                 if constexpr (LAST) {
                     device_elem(it.dtype, [&](auto e) {
-                        static_cast<decltype(e) *>(it.dst)[row * it.dst_rs + col * it.dst_cs] = to_elem<decltype(e)>(y * (scale / it.x_scale));
+                        using E = decltype(e);
+                        E *dst = static_cast<E *>(it.dst) + row * it.dst_rs + col * it.dst_cs;
+                        const float s = scale / it.x_scale;
+                        if (it.dst_cs == 1 && col + 4 <= it.n) {
+                            Cols<E, 4> w;
+#pragma unroll
+                            for (int t = 0; t < 4; ++t) w[t] = to_elem<E>(y[t] * s);
+                            *reinterpret_cast<Far<E, 4> *>(dst) = w;
+                        } else
+#pragma unroll
+                            for (int t = 0; t < 4; ++t)
+                                if (col + t < it.n) dst[t * it.dst_cs] = to_elem<E>(y[t] * s);
                     });
                 } else {
-                    P v[kParts];
-                    split(y, v);
-                    for (int p = 0; p < kParts; ++p) to[p * part + here] = v[p];
+                    Half4<P> v[2];
+                    split4(y, v[0], v[1]);
+                    *reinterpret_cast<Half4<P> *>(to + here) = v[0];
+                    *reinterpret_cast<Half4<P> *>(to_low + here) = v[1];
                 }
             }
+    }
 }
 
 // no steps: the matrix divided by its norm
@@ -218,24 +318,210 @@ __global__ __launch_bounds__(kThreads) void k_normed(List l, const double *part,
     });
 }
 
+// ---------------------------------------------------------------- matrices that fit a compute unit
+
+// All steps of one matrix in one block of eight wavefronts, X and A (then B) in two parts each in LDS, rows 16 bytes longer than a multiple of 32 elements.  A
+// wavefront has up to two 32 x 32 squares of A or B and four of X.
+constexpr int kSmallThreads = 512, kSmallWaves = kSmallThreads / 64;
+constexpr int kSmallHalves = 36 << 10, kSmallMost = 76 << 10;   // elements in LDS: 72 KB, so that two blocks share a compute unit, or 152
+
+inline int64_t small_elems(int64_t m, int64_t n)
+{
+    const int64_t mp = pad_to(m, 32), np = pad_to(n, 32);
+    return mp <= 128 && mp / 32 * (np / 32) <= 32 ? 2 * mp * (np + 8 + mp + 8) : (int64_t)1 << 40;
+}
+
+__device__ inline Half8<P> along(const P *p, int ld, int row, int k) { const int lane = threadIdx.x & 63; return *reinterpret_cast<const Half8<P> *>(p + (row + (lane & 31)) * ld + k + (lane >> 5) * 8); }
+__device__ inline Half8<P> across(const P *p, int ld, int col, int k)
+{
+    const int lane = threadIdx.x & 63, g = lane >> 4, i = lane & 15;
+    const P *q = p + (k + (g >> 1) * 8 + (i >> 2)) * ld + col + (g & 1) * 16 + (i & 3) * 4;
+    return __builtin_shufflevector(read_turned(q), read_turned(q + 4 * ld), 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
+template <int ELEMS> __global__ __launch_bounds__(kSmallThreads) void k_small(List l, double eps, int steps, float a, float b, float c, float scale)
+{
+    __shared__ alignas(16) P lds[ELEMS];
+    __shared__ float diag[2][128];
+    __shared__ double red[kSmallWaves];
+    const Item &it = l.item[blockIdx.x];
+    const int m = it.m, n = it.n, mp = (m + 31) / 32 * 32, np = (n + 31) / 32 * 32, xs = np + 8, as = mp + 8, mb = mp / 32, nb = np / 32;
+    P *x[2] = {lds, lds + mp * xs}, *q[2] = {lds + 2 * mp * xs, lds + 2 * mp * xs + mp * as};
+    const int wave = threadIdx.x >> 6;
+    const bool by_row = it.src_cs <= it.src_rs;
+    const int in = by_row ? np : mp, all = mp * np;
+    device_elem(it.dtype, [&](auto e) {
+        using E = decltype(e);
+        const E *src = static_cast<const E *>(it.src);
+        auto value = [&](int k, int &r, int &col) {
+            r = by_row ? k / in : k % in;
+            col = by_row ? k % in : k / in;
+            return r < m && col < n ? (float)src[r * it.src_rs + col * it.src_cs] : 0.f;
+        };
+        double sum = 0.0;
+        int r, col;
+        in_steps<4>(threadIdx.x, all, kSmallThreads, [&](int64_t k) { return value((int)k, r, col); }, [&](float v) { sum = fma((double)v, (double)v, sum); });
+        for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
+        if ((threadIdx.x & 63) == 0) red[wave] = sum;
+        __syncthreads();
+        sum = 0.0;
+        for (int w = 0; w < kSmallWaves; ++w) sum += red[w];
+        const double f = start_scale(sum, eps, it.x_scale);
+#pragma unroll 4
+        for (int k = threadIdx.x; k < all; k += kSmallThreads) {
+            P v[2];
+            const float t = value(k, r, col);
+            split((float)(t * f), v);
+            x[0][r * xs + col] = v[0];
+            x[1][r * xs + col] = v[1];
+        }
+    });
+    const float from_gram = kGramScale / (it.x_scale * it.x_scale);
+    for (int step = 0; step < steps; ++step) {
+        __syncthreads();
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {   // A
+            const int sq = wave + s * kSmallWaves, i0 = sq / mb * 32, j0 = sq % mb * 32;
+            if (sq >= mb * mb) break;
+            f32x16 acc = {};
+            for (int k = 0; k < np; k += 16) {
+                const Half8<P> u0 = along(x[0], xs, i0, k), u1 = along(x[1], xs, i0, k), v0 = along(x[0], xs, j0, k), v1 = along(x[1], xs, j0, k);
+                acc = mfma<P>(u1, v0, acc);
+                acc = mfma<P>(u0, v1, acc);
+                acc = mfma<P>(u0, v0, acc);
+            }
+            const int row = j0 + acc_col();
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                float y[4];
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    y[t] = acc[4 * g + t] * from_gram;
+                    if (i0 + acc_row(4 * g + t) == row) {
+                        diag[0][row] = y[t] * (1.f / kGramScale);
+                        y[t] = 0.f;
+                    }
+                }
+                Half4<P> v[2];
+                split4(y, v[0], v[1]);
+#pragma unroll
+                for (int p = 0; p < 2; ++p) *reinterpret_cast<Half4<P> *>(q[p] + row * as + i0 + acc_row(4 * g)) = v[p];
+            }
+        }
+        __syncthreads();
+        f32x16 poly[2] = {};
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {   // B
+            const int sq = wave + s * kSmallWaves, i0 = sq / mb * 32, j0 = sq % mb * 32;
+            if (sq >= mb * mb) break;
+            for (int k = 0; k < mp; k += 16) {
+                const Half8<P> u0 = along(q[0], as, i0, k), u1 = along(q[1], as, i0, k), v0 = along(q[0], as, j0, k), v1 = along(q[1], as, j0, k);
+                poly[s] = mfma<P>(u1, v0, poly[s]);
+                poly[s] = mfma<P>(u0, v1, poly[s]);
+                poly[s] = mfma<P>(u0, v0, poly[s]);
+            }
+            const int row = j0 + acc_col();
+            const float dr = diag[0][row];
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int col = i0 + acc_row(r);
+                float y = fmaf(fmaf(c, dr + diag[0][col], b), both(q[0][row * as + col], q[1][row * as + col]), poly[s][r] * (c / kGramScale));
+                if (col == row) {
+                    diag[1][row] = fmaf(dr, fmaf(c, dr, b), y * (1.f / kGramScale));
+                    y = 0.f;
+                }
+                poly[s][r] = y;
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const int sq = wave + s * kSmallWaves, i0 = sq / mb * 32, j0 = sq % mb * 32;
+            if (sq >= mb * mb) break;
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const float y[4] = {poly[s][4 * g], poly[s][4 * g + 1], poly[s][4 * g + 2], poly[s][4 * g + 3]};
+                Half4<P> v[2];
+                split4(y, v[0], v[1]);
+#pragma unroll
+                for (int p = 0; p < 2; ++p) *reinterpret_cast<Half4<P> *>(q[p] + (j0 + acc_col()) * as + i0 + acc_row(4 * g)) = v[p];
+            }
+        }
+        __syncthreads();
+        f32x16 next[4] = {};
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {   // X: columns i0, rows j0
+            const int sq = wave + s * kSmallWaves, i0 = sq / mb * 32, j0 = sq % mb * 32;
+            if (sq >= mb * nb) break;
+            for (int k = 0; k < mp; k += 16) {
+                const Half8<P> u0 = across(x[0], xs, i0, k), u1 = across(x[1], xs, i0, k), v0 = along(q[0], as, j0, k), v1 = along(q[1], as, j0, k);
+                next[s] = mfma<P>(u1, v0, next[s]);
+                next[s] = mfma<P>(u0, v1, next[s]);
+                next[s] = mfma<P>(u0, v0, next[s]);
+            }
+            const int row = j0 + acc_col();
+            const float f = a + diag[1][row];
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int at = row * xs + i0 + acc_row(r);
+                next[s][r] = fmaf(f, both(x[0][at], x[1][at]), next[s][r] * (1.f / kGramScale));
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            const int sq = wave + s * kSmallWaves, i0 = sq / mb * 32, j0 = sq % mb * 32, row = j0 + acc_col();
+            if (sq >= mb * nb) break;
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const float y[4] = {next[s][4 * g], next[s][4 * g + 1], next[s][4 * g + 2], next[s][4 * g + 3]};
+                Half4<P> v[2];
+                split4(y, v[0], v[1]);
+#pragma unroll
+                for (int p = 0; p < 2; ++p) *reinterpret_cast<Half4<P> *>(x[p] + row * xs + i0 + acc_row(4 * g)) = v[p];
+            }
+        }
+    }
+    __syncthreads();
+    device_elem(it.dtype, [&](auto e) {   // (X has 22 bits: fp32 results too)
+        using E = decltype(e);
+        const bool rows = it.dst_cs <= it.dst_rs;
+        const int inner = rows ? n : m, total = m * n;
+        const float to = scale / it.x_scale;
+        for (int k = threadIdx.x; k < total; k += kSmallThreads) {
+            const int r = rows ? k / inner : k % inner, col = rows ? k % inner : k / inner, at = r * xs + col;
+            static_cast<E *>(it.dst)[r * it.dst_rs + col * it.dst_cs] = to_elem<E>(both(x[0][at], x[1][at]) * to);
+        }
+    });
+}
+
 // ---------------------------------------------------------------- a call's launches
 
 constexpr int64_t kHead = kList * kNormBlocks * 8;   // bytes of the norms' partial sums
+constexpr int64_t kMostBytes = (int64_t)1 << 31;    // of a group's scratch memory, where it has more than one matrix
+
+// How a matrix is taken: in one block (of the smaller or the larger amount of LDS), or by products of two parts or one
+enum { W_SMALL, W_MEDIUM, W_TWO, W_ONE, W_COUNT };
+int way_of(const mlip_matrix_t &x)
+{
+    const int64_t elems = x.rows < x.cols ? small_elems(x.rows, x.cols) : small_elems(x.cols, x.rows);
+    return elems <= kSmallHalves ? W_SMALL : elems <= kSmallMost ? W_MEDIUM : x.dtype == MLIP_DTYPE_BF16 ? W_ONE : W_TWO;
+}
 
 struct Group {
     List l;
     int64_t bytes;
     int32_t next;
 };
-constexpr int64_t kMostBytes = (int64_t)1 << 31;    // of a group's scratch memory, where it has more than one matrix
 
-Group group_of(const mlip_matrix_t *list, int32_t count, int32_t at)
+// The next matrices of the list, from `at` on, that go one way
+Group group_of(const mlip_matrix_t *list, int32_t count, int32_t at, int way, bool no_steps)
 {
     Group g{};
     int64_t used = kHead;
     for (; at < count && g.l.count < kList; ++at) {
         const mlip_matrix_t &x = list[at];
-        if (x.rows == 0 || x.cols == 0) continue;
+        if (x.rows == 0 || x.cols == 0 || way_of(x) != way) continue;
         Item it{};
         const bool tall = x.rows > x.cols;
         it.src = x.src;
@@ -253,11 +539,17 @@ Group group_of(const mlip_matrix_t *list, int32_t count, int32_t at)
         while ((int64_t)1 << (2 * (e - 4)) < it.n) ++e;
         it.x_scale = (float)(1 << e);
         int64_t place = used;
-        auto take = [&](int64_t elems) { const int64_t here = place / 2; place += pad_to(elems * kParts * 2, 256); return here; };
-        it.x[0] = take((int64_t)it.m * it.n_p);
-        it.x[1] = take((int64_t)it.m * it.n_p);
-        it.gram = take((int64_t)it.m * it.m_p);
-        it.poly = take((int64_t)it.m * it.m_p);
+        auto take = [&](int64_t bytes) { const int64_t here = place / 2; place += pad_to(bytes, 256); return here; };
+        if (way >= W_TWO && !no_steps) {
+            const int64_t all = (int64_t)it.m * it.n_p * 2, square = (int64_t)it.m * it.m_p * 2;
+            it.x[0] = take(all);
+            it.low[0] = take(all);
+            it.x[1] = take(all);
+            it.low[1] = way == W_TWO ? take(all) : it.low[0];
+            it.gram = take(2 * square);
+            it.poly = take((way == W_TWO ? 2 : 1) * square);
+            it.diag = take((int64_t)it.m * 8);
+        }
         if (g.l.count && place > kMostBytes) break;
         used = place;
         g.l.item[g.l.count++] = it;
@@ -278,16 +570,29 @@ template <class Fn> unsigned number_blocks(List &l, Fn &&blocks_of)
     return at;
 }
 
+template <int PARTS> void steps_of(List &l, P *ws, int32_t steps, float a, float b, float c, float scale, hipStream_t stream)
+{
+    for (int s = 0; s < steps; ++s) {
+        const int now = s & 1;
+        unsigned blocks = number_blocks(l, [](const Item &it) { const int64_t t = (it.m + 127) / 128; return t * (t + 1) / 2; });
+        k_symmetric<PARTS, false><<<blocks, kThreads, 0, stream>>>(l, ws, now, 0.f, 0.f);
+        k_symmetric<PARTS, true><<<blocks, kThreads, 0, stream>>>(l, ws, now, b, c);
+        blocks = number_blocks(l, [](const Item &it) { return (int64_t)((it.m + 127) / 128) * ((it.n_p + 127) / 128); });
+        (s + 1 == steps ? k_apply<PARTS, true> : k_apply<PARTS, false>)<<<blocks, kThreads, 0, stream>>>(l, ws, now, a, scale);
+    }
+}
+
 }  // namespace
 
 size_t ortho_workspace(const mlip_matrix_t *list, int32_t count)
 {
     int64_t most = kHead;
-    for (int32_t at = 0; at < count;) {
-        const Group g = group_of(list, count, at);
-        at = g.next;
-        if (g.bytes > most) most = g.bytes;
-    }
+    for (int way = 0; way < W_COUNT; ++way)
+        for (int32_t at = 0; at < count;) {
+            const Group g = group_of(list, count, at, way, false);
+            at = g.next;
+            if (g.bytes > most) most = g.bytes;
+        }
     return (size_t)most;
 }
 
@@ -296,28 +601,28 @@ int ortho_impl(const mlip_matrix_t *list, int32_t count, int32_t steps, const do
     double *norms = static_cast<double *>(workspace);
     P *ws = static_cast<P *>(workspace);
     const float a = (float)coef[0], b = (float)coef[1], c = (float)coef[2];
-    for (int32_t at = 0; at < count;) {
-        Group g = group_of(list, count, at);
-        at = g.next;
-        List &l = g.l;
-        if (!l.count) continue;
-        k_squares<<<dim3(kNormBlocks, l.count), kThreads, 0, stream>>>(l, norms);
-        if (!steps) {
-            k_normed<<<dim3(256, l.count), kThreads, 0, stream>>>(l, norms, eps, scale);
+    for (int way = 0; way < W_COUNT; ++way)
+        for (int32_t at = 0; at < count;) {
+            Group g = group_of(list, count, at, way, steps == 0);
+            at = g.next;
+            List &l = g.l;
+            if (!l.count) continue;
+            if (way < W_TWO && steps) {
+                (way == W_SMALL ? k_small<kSmallHalves> : k_small<kSmallMost>)<<<l.count, kSmallThreads, 0, stream>>>(l, eps, steps, a, b, c, scale);
+                MLIP_HIP(hipGetLastError());
+                continue;
+            }
+            k_squares<<<dim3(kNormBlocks, l.count), kThreads, 0, stream>>>(l, norms);
+            if (!steps) {
+                k_normed<<<dim3(256, l.count), kThreads, 0, stream>>>(l, norms, eps, scale);
+            } else {
+                const unsigned blocks = number_blocks(l, [](const Item &it) { return (int64_t)((it.m + 63) / 64) * (it.n_p / 64); });
+                k_start<<<blocks, kThreads, 0, stream>>>(l, norms, eps, ws);
+                if (way == W_TWO) steps_of<2>(l, ws, steps, a, b, c, scale, stream);
+                else steps_of<1>(l, ws, steps, a, b, c, scale, stream);
+            }
             MLIP_HIP(hipGetLastError());
-            continue;
         }
-        unsigned blocks = number_blocks(l, [](const Item &it) { return (int64_t)((it.m + 63) / 64) * (it.n_p / 64); });
-        k_start<<<blocks, kThreads, 0, stream>>>(l, norms, eps, ws);
-        for (int s = 0; s < steps; ++s) {
-            blocks = number_blocks(l, [](const Item &it) { const int64_t t = (it.m + 127) / 128; return t * (t + 1) / 2; });
-            k_symmetric<false><<<blocks, kThreads, 0, stream>>>(l, ws, s & 1, 0.f, 0.f);
-            k_symmetric<true><<<blocks, kThreads, 0, stream>>>(l, ws, s & 1, b, c);
-            blocks = number_blocks(l, [](const Item &it) { return (int64_t)((it.m + 127) / 128) * ((it.n_p + 127) / 128); });
-            (s + 1 == steps ? k_apply<true> : k_apply<false>)<<<blocks, kThreads, 0, stream>>>(l, ws, s & 1, a, scale);
-        }
-        MLIP_HIP(hipGetLastError());
-    }
     return MLIP_OK;
 }
 

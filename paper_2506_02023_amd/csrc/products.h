@@ -51,7 +51,7 @@ template <class T, int PARTS> __device__ inline void split(float v, T (&part)[PA
 #endif
 
 // Elements of K that one step takes: 64 of one part, 32 of several (LDS)
-template <int PARTS> constexpr int kStepK = PARTS == 1 ? 64 : 32;
+template <int PARTS, int LEAST> constexpr int kStepK = PARTS == 1 ? 64 : 32;
 // Columns that a panel with K in its columns is filled up to: a multiple of both
 constexpr int64_t kPadK = 64;
 inline int64_t pad_to(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
@@ -63,11 +63,11 @@ inline int64_t pad_to(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 template <class T, int PARTS, bool KC, int ROWS, int KT, int THREADS> struct Tile {
     static constexpr int kRow = KC ? KT : ROWS, kPieces = kRow / 8, kPart = ROWS * KT, kElems = PARTS * kPart;
     static constexpr int kLoads = PARTS * kPart / 8 / THREADS;
-    static_assert(kPart / 8 % THREADS == 0 && (kPieces == 4 || kPieces == 8 || kPieces % 16 == 0), "whole rounds of loads");
+    static_assert(kPart / 8 % THREADS == 0 && (kPieces == 2 || kPieces == 4 || kPieces == 8 || kPieces % 16 == 0), "whole rounds of loads");
 
     static __device__ inline int turn(int row)
     {
-        if constexpr (KC) return kPieces == 8 ? (row >> 1) & 7 : (row >> 2) & 3;
+        if constexpr (KC) return kPieces == 8 ? (row >> 1) & 7 : kPieces == 4 ? (row >> 2) & 3 : (row >> 3) & 1;
         else return kPieces == 8 ? ((row >> 1) & 1) * 4 : (row & 3) * 4;
     }
 
@@ -116,7 +116,7 @@ template <int PARTS, class Fn> __device__ inline void for_products(Fn &&f)
 // acc[i][j] += rows 32 i .. of A times rows 32 j .. of B, of a wavefront's WM x WN part of the block's BM x BN tile, summed over k in [k0, k1).
 // each(a fragments of part 0 .. PARTS - 1 of step kk): called once per fragment of A, for sums along its rows.
 template <class T, int PARTS, bool AKC, bool BKC, int BM, int BN, int WM, int WN> struct Product {
-    static constexpr int kWaves = (BM / WM) * (BN / WN), kThreads = kWaves * 64, KT = kStepK<PARTS>;
+    static constexpr int kWaves = (BM / WM) * (BN / WN), kThreads = kWaves * 64, KT = kStepK<PARTS, (BM < BN ? BM : BN)>;
     using TA = Tile<T, PARTS, AKC, BM, KT, kThreads>;
     using TB = Tile<T, PARTS, BKC, BN, KT, kThreads>;
     static constexpr int kStage = TA::kElems + TB::kElems;
