@@ -17,7 +17,7 @@ namespace {
 template <class T_, int PARTS_, class E_> struct Kind {
     using T = T_;
     using E = E_;
-    static constexpr int kParts = PARTS_;
+    static constexpr int kParts = PARTS_, kWide = 16 / sizeof(E_);   // elements of a lane's load or store
 };
 template <class Fn> int with_kind(int32_t dtype, Fn &&f)
 {
@@ -37,7 +37,7 @@ constexpr int kPackThreads = 256;
 
 // dst [rows][cols_p] in parts from src at (r, c) -> r rs + c cs, zeros from cols on; eight columns a thread
 template <class K> __global__ __launch_bounds__(kPackThreads) void k_pack_rows(const typename K::E *src, int64_t rs, int64_t cs, int64_t rows, int64_t cols, int64_t cols_p,
-                                                                             typename K::T *dst, int64_t part)
+                                                                             typename K::T *dst, int64_t ld, int64_t part)
 {
     const int64_t per_row = cols_p / 8, at = (int64_t)blockIdx.x * kPackThreads + threadIdx.x, r = at / per_row, c = at % per_row * 8;
     if (r >= rows) return;
@@ -51,13 +51,13 @@ template <class K> __global__ __launch_bounds__(kPackThreads) void k_pack_rows(c
         for (int p = 0; p < K::kParts; ++p) out[p][k] = v[p];
     }
 #pragma unroll
-    for (int p = 0; p < K::kParts; ++p) *reinterpret_cast<Half8<typename K::T> *>(dst + p * part + r * cols_p + c) = out[p];
+    for (int p = 0; p < K::kParts; ++p) *reinterpret_cast<Half8<typename K::T> *>(dst + p * part + r * ld + c) = out[p];
 }
 
 // A matrix of the weights' 32 x 32 squares: `across` [2 f][d_p] for g and v, `down` [d][2 f] for dx (either may be missing)
 template <class K> struct Weights {
     const typename K::E *wg, *wv;
-    int64_t g_rs, g_cs, v_rs, v_cs, d, f, d_p, f2;
+    int64_t g_rs, g_cs, v_rs, v_cs, d, f, d_ld, f2_ld;
     typename K::T *across, *down;
     int64_t across_part, down_part;
 };
@@ -78,10 +78,10 @@ template <class K> __global__ __launch_bounds__(kPackThreads) void k_pack_weight
     for (int i = b; i < 32; i += 8) {
         typename K::T v[K::kParts];
         split(tile[a][i], v);
-        for (int p = 0; p < K::kParts; ++p) w.across[p * w.across_part + (c0 + i) * w.d_p + d0 + a] = v[p];
+        for (int p = 0; p < K::kParts; ++p) w.across[p * w.across_part + (c0 + i) * w.d_ld + d0 + a] = v[p];
         if (w.down && d0 + i < w.d) {
             split(tile[i][a], v);
-            for (int p = 0; p < K::kParts; ++p) w.down[p * w.down_part + (d0 + i) * w.f2 + c0 + a] = v[p];
+            for (int p = 0; p < K::kParts; ++p) w.down[p * w.down_part + (d0 + i) * w.f2_ld + c0 + a] = v[p];
         }
     }
 }
@@ -131,91 +131,74 @@ template <class K> struct GateArgs {
     int64_t gv_ld, gv_part;
 };
 
-// Four elements from column c of a row on, zeros from `cols` on
-template <class E> __device__ inline void load4(float (&v)[4], const E *row, int64_t cs, int64_t c, int64_t cols)
-{
-    if (cs == 1 && c + 4 <= cols) {
-        const Cols<E, 4> w = *reinterpret_cast<const Far<E, 4> *>(row + c);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] = (float)w[k];
-        return;
-    }
-#pragma unroll
-    for (int k = 0; k < 4; ++k) v[k] = c + k < cols ? (float)row[(c + k) * cs] : 0.f;
-}
-template <class E> __device__ inline void store4(const float (&v)[4], E *row, int64_t c, int64_t cols)
-{
-    if (c + 4 <= cols) {
-        Cols<E, 4> w;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) w[k] = to_elem<E>(v[k]);
-        *reinterpret_cast<Far<E, 4> *>(row + c) = w;
-        return;
-    }
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-        if (c + k < cols) row[c + k] = to_elem<E>(v[k]);
-}
+// A block's tile: 128 x 128 in four wavefronts (64 x 256 where there are no more columns), or 256 x 256 in eight of 128 x 64 each.  The larger one brings half the bytes from the caches for the same
+// products, the smaller one shares a compute unit with another block and leaves no one idle where there are few.
+template <int COLS, int ROWS> struct Block {   // of the first operand and of the second
+    static constexpr int kCols = COLS, kRows = ROWS, kPer = COLS == 256 ? 128 : 64, kThreads = COLS / kPer * (ROWS / 64) * 64;   // kPer x 64: a wavefront's share
+    template <class K, bool AKC, bool BKC> using Of = Product<typename K::T, K::kParts, AKC, BKC, COLS, ROWS, kPer, 64>;
+    static __device__ inline int first(int wave) { return wave / (ROWS / 64) * kPer; }
+    static __device__ inline int second(int wave) { return wave % (ROWS / 64) * 64; }
+};
+using Narrow = Block<64, 256>;
+using Middle = Block<128, 128>;
+using Large = Block<256, 256>;
 
-// The weights are the products' first operand and the rows their second, so that a lane has four neighbouring features of one row in a row of
-// registers, and loads and stores them as one access.
-template <class K, bool BACK> __global__ __launch_bounds__(256) void k_gates(GateArgs<K> a)
+// The weights are the products' first operand and the rows their second; a lane ends with neighbouring features of a row.
+template <class K, class B, bool BACK> __global__ __launch_bounds__(B::kThreads) void k_gates(GateArgs<K> a)
 {
-    using P = Product<typename K::T, K::kParts, true, true, 128, 128, 64, 64>;
+    using T = typename K::T;
+    using P = typename B::template Of<K, true, true>;
     __shared__ typename P::Lds lds;
-    const int64_t tile = xcd_order(blockIdx.x, gridDim.x), m0 = tile / a.n_tiles * 128, n0 = tile % a.n_tiles * 128;
-    f32x16 acc[2][2] = {};
+    const int64_t tile = xcd_order(blockIdx.x, gridDim.x), m0 = tile / a.n_tiles * B::kRows, n0 = tile % a.n_tiles * B::kCols;
+    f32x16 acc[B::kPer / 32][2] = {};
     P::run(a.w, a.x, n0, m0, 0, a.d_p, lds, acc, NoEach{});
-    const int wave = threadIdx.x >> 6;
-    const int64_t col0 = n0 + wave / 2 * 64, f0 = col0 / 2 + acc_row(0);
-    if (col0 >= a.w.rows) return;
-    float bg[4][4] = {}, bv[4][4] = {};
+    __syncthreads();
+    constexpr int W = K::kWide, lanes = 32 / W;   // of a row
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, c = lane % lanes * W;
+    const Turned turned{reinterpret_cast<float *>(&lds) + wave * 4096};
+    auto finish = [&](const f32x16 (*part)[2], int64_t col0) {   // 64 columns of a wavefront
+        const int64_t f = col0 / 2 + c;
+        turned.put(part);
+        if (col0 >= a.w.rows) return;
+        float bg[W] = {}, bv[W] = {};
+        if (a.bg) load_cols(bg, a.bg, 1, f, a.f);
+        if (a.bv) load_cols(bv, a.bv, 1, f, a.f);
+        with_act(a.act, [&](auto act) {
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        if (a.bg) load4(bg[q], a.bg, 1, f0 + 8 * q, a.f);
-        if (a.bv) load4(bv[q], a.bv, 1, f0 + 8 * q, a.f);
-    }
-    with_act(a.act, [&](auto act) {
+            for (int k = 0; k < lanes; ++k) {
+                const int r = lane / lanes + 64 / lanes * k;
+                const int64_t row = m0 + B::second(wave) + r;
+                if (row >= a.x.rows) continue;
+                float g[W], v[W], bar[W];
+                turned.get(g, r, c);
+                turned.get(v, r, 32 + c);
+                if constexpr (BACK) load_cols(bar, a.bar + row * a.bar_rs, a.bar_cs, f, a.f);
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const int64_t row = m0 + wave % 2 * 64 + 32 * j + acc_col();
-            if (row >= a.x.rows) continue;
-            float bar[4][4];
-            if constexpr (BACK)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) load4(bar[q], a.bar + row * a.bar_rs, a.bar_cs, f0 + 8 * q, a.f);
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int64_t f = f0 + 8 * q;
-                float h[4];
-                Half4<typename K::T> g[K::kParts], v[K::kParts];
-#pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    const Phi y = phi<decltype(act)::value>(acc[0][j][4 * q + t] + bg[q][t], acc[1][j][4 * q + t] + bv[q][t]);
-                    if constexpr (!BACK) h[t] = y.h;
+                for (int t = 0; t < W; ++t) {
+                    const Phi y = phi<decltype(act)::value>(g[t] + bg[t], v[t] + bv[t]);
+                    if constexpr (!BACK) g[t] = y.h;
                     else {
-                        typename K::T gs[K::kParts], vs[K::kParts];
-                        split(f + t < a.f ? bar[q][t] * y.g : 0.f, gs);
-                        split(f + t < a.f ? bar[q][t] * y.v : 0.f, vs);
-#pragma unroll
-                        for (int p = 0; p < K::kParts; ++p) {
-                            g[p][t] = gs[p];
-                            v[p][t] = vs[p];
-                        }
+                        g[t] = f + t < a.f ? bar[t] * y.g : 0.f;
+                        v[t] = f + t < a.f ? bar[t] * y.v : 0.f;
                     }
                 }
-                if constexpr (!BACK) store4(h, a.out + row * a.out_rs, f, a.f);
+                if constexpr (!BACK) store_cols(g, a.out + row * a.out_rs, f, a.f);
                 else {
-                    typename K::T *to = a.gv + row * a.gv_ld + col0 + acc_row(4 * q);
+                    Cols<T, W> gp[K::kParts], vp[K::kParts];
+                    split_cols<T>(g, gp);
+                    split_cols<T>(v, vp);
+                    T *to = a.gv + row * a.gv_ld + col0 + c;
 #pragma unroll
                     for (int p = 0; p < K::kParts; ++p) {
-                        *reinterpret_cast<Half4<typename K::T> *>(to + p * a.gv_part) = g[p];
-                        *reinterpret_cast<Half4<typename K::T> *>(to + p * a.gv_part + 32) = v[p];
+                        *reinterpret_cast<Cols<T, W> *>(to + p * a.gv_part) = gp[p];
+                        *reinterpret_cast<Cols<T, W> *>(to + p * a.gv_part + 32) = vp[p];
                     }
                 }
             }
-        }
-    });
+        });
+    };
+    finish(&acc[0], n0 + B::first(wave));
+    if constexpr (B::kPer == 128) finish(&acc[2], n0 + B::first(wave) + 64);
 }
 
 // dx = [G V] [Wg Wv]^T
@@ -225,25 +208,29 @@ template <class K> struct RowBarArgs {
     typename K::E *out;
     int64_t out_rs;
 };
-template <class K, int BM, int BN> __global__ __launch_bounds__(256) void k_row_bars(RowBarArgs<K> a)
+template <class K, class B> __global__ __launch_bounds__(B::kThreads) void k_row_bars(RowBarArgs<K> a)
 {
-    using P = Product<typename K::T, K::kParts, true, true, BN, BM, 64, 64>;   // (d first, rows second, as above)
+    using P = typename B::template Of<K, true, true>;   // (d first, rows second)
     __shared__ typename P::Lds lds;
-    const int64_t tile = xcd_order(blockIdx.x, gridDim.x), m0 = tile / a.n_tiles * BM, n0 = tile % a.n_tiles * BN;
-    f32x16 acc[2][2] = {};
+    const int64_t tile = xcd_order(blockIdx.x, gridDim.x), m0 = tile / a.n_tiles * B::kRows, n0 = tile % a.n_tiles * B::kCols;
+    f32x16 acc[B::kPer / 32][2] = {};
     P::run(a.w, a.gv, n0, m0, 0, a.gv.cols, lds, acc, NoEach{});
-    const int wave = threadIdx.x >> 6;
+    __syncthreads();
+    constexpr int W = K::kWide, lanes = 64 / W;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, c = lane % lanes * W;
+    const Turned turned{reinterpret_cast<float *>(&lds) + wave * 4096};
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const int64_t row = m0 + wave % (BM / 64) * 64 + 32 * j + acc_col();
-        if (row >= a.gv.rows) continue;
+    for (int i = 0; i < B::kPer / 64; ++i) {
+        turned.put(&acc[2 * i]);
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const float v[4] = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
-                store4(v, a.out + row * a.out_rs, n0 + wave / (BM / 64) * 64 + 32 * i + acc_row(4 * q), a.w.rows);
-            }
+        for (int k = 0; k < lanes; ++k) {
+            const int r = lane / lanes + 64 / lanes * k;
+            const int64_t row = m0 + B::second(wave) + r;
+            if (row >= a.gv.rows) continue;
+            float v[W];
+            turned.get(v, r, c);
+            store_cols(v, a.out + row * a.out_rs, n0 + B::first(wave) + 64 * i + c, a.w.rows);
+        }
     }
 }
 
@@ -254,17 +241,17 @@ template <class K> struct WeightSumArgs {
     float *part, *bias;      // [splits][2 f][d], [splits][2 f]
     bool add;
 };
-template <class K, int BM, int BN> __global__ __launch_bounds__(256) void k_weight_sums(WeightSumArgs<K> a)
+template <class K, class B> __global__ __launch_bounds__(B::kThreads) void k_weight_sums(WeightSumArgs<K> a)
 {
-    using P = Product<typename K::T, K::kParts, false, false, BM, BN, 64, 64>;
+    using P = typename B::template Of<K, false, false>;   // (d first, the 2 f columns second)
     __shared__ typename P::Lds lds;
     const int64_t at = xcd_order(blockIdx.x, gridDim.x), tiles = a.m_tiles * a.n_tiles, s = at / tiles, tile = at % tiles;
-    const int64_t m0 = tile / a.n_tiles * BM, n0 = tile % a.n_tiles * BN;
+    const int64_t m0 = tile / a.n_tiles * B::kRows, n0 = tile % a.n_tiles * B::kCols;
     const int64_t k0 = s * a.run, k1 = k0 + a.run < a.gv.rows ? k0 + a.run : a.gv.rows;
-    const int wave = threadIdx.x >> 6, wn = wave % (BN / 64) * 64;
-    const bool sums = a.bias && n0 + wn == 0;
-    f32x16 acc[2][2] = {}, ones[2] = {};
-    P::run(a.gv, a.x, m0, n0, k0, k1, lds, acc, [&](auto &fa) {
+    const int wave = threadIdx.x >> 6;
+    const bool sums = a.bias && n0 + B::first(wave) == 0;
+    f32x16 acc[B::kPer / 32][2] = {}, ones[2] = {};
+    P::run(a.x, a.gv, n0, m0, k0, k1, lds, acc, [&](auto &fb) {
         if (!sums) return;
         Half8<typename K::T> one;
 #pragma unroll
@@ -272,26 +259,38 @@ template <class K, int BM, int BN> __global__ __launch_bounds__(256) void k_weig
 #pragma unroll
         for (int p = K::kParts - 1; p >= 0; --p)
 #pragma unroll
-            for (int i = 0; i < 2; ++i) ones[i] = mfma<typename K::T>(fa[i][p], one, ones[i]);
+            for (int j = 0; j < 2; ++j) ones[j] = mfma<typename K::T>(one, fb[j][p], ones[j]);
     });
-    const int64_t row0 = m0 + wave / (BN / 64) * 64, col0 = n0 + wn + acc_col();
+    __syncthreads();
+    constexpr int lanes = 16;
+    const int lane = threadIdx.x & 63, c = lane % lanes * 4;
+    const int64_t row0 = m0 + B::second(wave);
+    const Turned turned{reinterpret_cast<float *>(&lds) + wave * 4096};
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < B::kPer / 64; ++i) {
+        turned.put(&acc[2 * i]);
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const int64_t row = row0 + 32 * i + acc_row(r);
+        for (int k = 0; k < lanes; ++k) {
+            const int r = lane / lanes + 64 / lanes * k;
+            const int64_t row = row0 + r, col = n0 + B::first(wave) + 64 * i + c;
             if (row >= a.gv.cols) continue;
+            float v[4], old[4] = {};
+            turned.get(v, r, c);
+            float *to = a.part + (s * a.gv.cols + row) * a.d;
+            if (a.add) load_cols(old, to, 1, col, a.d);
 #pragma unroll
-            for (int j = 0; j < 2; ++j)
-                if (col0 + 32 * j < a.d) {
-                    float *to = a.part + (s * a.gv.cols + row) * a.d + col0 + 32 * j;
-                    *to = a.add ? *to + acc[i][j][r] : acc[i][j][r];
-                }
-            if (sums && acc_col() == 0) {
-                float *to = a.bias + s * a.gv.cols + row;
-                *to = a.add ? *to + ones[i][r] : ones[i][r];
-            }
+            for (int t = 0; t < 4; ++t) v[t] += old[t];
+            store_cols(v, to, col, a.d);
         }
+    }
+    if (sums && lane < 32) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int64_t row = row0 + 32 * j + lane;
+            float *to = a.bias + s * a.gv.cols + row;
+            if (row < a.gv.cols) *to = a.add ? *to + ones[j][0] : ones[j][0];
+        }
+    }
 }
 
 // The runs' shares added up, in their order
@@ -332,13 +331,13 @@ template <class K> __global__ __launch_bounds__(kPackThreads) void k_join(JoinAr
 
 // ---------------------------------------------------------------- a call's sizes and scratch memory
 
-constexpr int64_t kChunkBytes = 96 << 20;     // of x's parts, G and V of a chunk
+constexpr int64_t kChunkBytes = 1024 << 20;     // of x's parts, G and V of a chunk
 constexpr int64_t kMostTiles = 1 << 23;       // blocks of a launch
 
 struct Plan {
     int parts;
     bool pack_x;
-    int64_t d_p, f2, chunk;                    // columns of the laid out x and weights, rows of a chunk
+    int64_t d_p, f2, gv_ld, d_ld, chunk;       // columns of the laid out x and weights and where their rows lie, rows of a chunk
     int64_t splits, run;
     size_t across, down, xs, gv, part, bias, bytes;   // offsets
 };
@@ -350,6 +349,14 @@ bool reads_x(const GatedArgs &a)
            reinterpret_cast<uintptr_t>(a.x) % 16 == 0;
 }
 
+// f(Block{}) for a product of `cols` columns (of the first operand) and `rows` rows (of the second)
+template <class K, class Fn> void with_block(int64_t cols, int64_t rows, Fn &&f)
+{
+    if (K::kParts == 1 && cols >= 512 && rows >= 512) f(std::conditional_t<K::kParts == 1, Large, Middle>{});
+    else if (cols <= 64) f(Narrow{});
+    else f(Middle{});
+}
+
 Plan plan_of(const GatedArgs &a, bool grad)
 {
     Plan p{};
@@ -357,8 +364,10 @@ Plan plan_of(const GatedArgs &a, bool grad)
     p.pack_x = !reads_x(a);
     p.d_p = pad_to(a.d, kPadK);
     p.f2 = 2 * pad_to(a.f, 32);
+    p.gv_ld = pad_odd(p.f2);
+    p.d_ld = pad_odd(p.d_p);
     // (scratch memory does not depend on where x lies: a size asked for once holds for all)
-    const int64_t row_bytes = ((grad ? p.f2 : 0) + p.d_p) * p.parts * 2;
+    const int64_t row_bytes = ((grad ? p.gv_ld : 0) + p.d_ld) * p.parts * 2;
     p.chunk = pad_to(kChunkBytes / row_bytes + 1, 1024);
     const int64_t most = kMostTiles / ((p.f2 > p.d_p ? p.f2 : p.d_p) / 64 + 1) * 64 / 1024 * 1024;
     if (p.chunk > most) p.chunk = most;
@@ -366,12 +375,12 @@ Plan plan_of(const GatedArgs &a, bool grad)
     if (p.chunk > all) p.chunk = all;
     size_t at = 0;
     auto take = [&](int64_t bytes) { const size_t here = at; at += (size_t)pad_to(bytes, 256); return here; };
-    p.across = take(p.f2 * p.d_p * p.parts * 2);
-    p.xs = take(p.chunk * p.d_p * p.parts * 2);
+    p.across = take(p.f2 * p.d_ld * p.parts * 2);
+    p.xs = take(p.chunk * p.d_ld * p.parts * 2);
     if (grad) {
-        p.down = take(a.d * p.f2 * p.parts * 2);
-        p.gv = take(p.chunk * p.f2 * p.parts * 2);
-        const int64_t tiles = a.d <= 64 ? (p.f2 + 255) / 256 : (p.f2 + 127) / 128 * ((a.d + 127) / 128);
+        p.down = take(a.d * p.gv_ld * p.parts * 2);
+        p.gv = take(p.chunk * p.gv_ld * p.parts * 2);
+        const int64_t tiles = p.parts == 1 && a.d >= 512 && p.f2 >= 512 ? (p.f2 + 255) / 256 * ((a.d + 255) / 256) : a.d <= 64 ? (p.f2 + 255) / 256 : (p.f2 + 127) / 128 * ((a.d + 127) / 128);
         int64_t splits = 512 / tiles, most_splits = (p.chunk + 511) / 512;
         if (splits > most_splits) splits = most_splits;
         if (splits < 1) splits = 1;
@@ -393,10 +402,10 @@ template <class K> int launch(const GatedArgs &a, const GatedGrad *g)
     T *across = reinterpret_cast<T *>(ws + p.across), *down = g ? reinterpret_cast<T *>(ws + p.down) : nullptr, *xs = reinterpret_cast<T *>(ws + p.xs);
     T *gv = g ? reinterpret_cast<T *>(ws + p.gv) : nullptr;
     const bool rows = !g || g->dx, weights = g && (g->dwg || g->dwv || g->dbg || g->dbv);
-    const Weights<K> w = {static_cast<const E *>(a.wg), static_cast<const E *>(a.wv), a.wg_rs, a.wg_cs, a.wv_rs, a.wv_cs, a.d, a.f, p.d_p, p.f2,
-                          across, rows ? down : nullptr, p.f2 * p.d_p, a.d * p.f2};
+    const Weights<K> w = {static_cast<const E *>(a.wg), static_cast<const E *>(a.wv), a.wg_rs, a.wg_cs, a.wv_rs, a.wv_cs, a.d, a.f, p.d_ld, p.gv_ld,
+                          across, rows ? down : nullptr, p.f2 * p.d_ld, a.d * p.gv_ld};
     if (a.n > 0) k_pack_weights<K><<<dim3((unsigned)(p.f2 / 32), (unsigned)(p.d_p / 32)), kPackThreads, 0, a.stream>>>(w);
-    const Panel across_panel = {across, p.d_p, p.f2 * p.d_p, p.f2, p.d_p}, down_panel = {down, p.f2, a.d * p.f2, a.d, p.f2};
+    const Panel across_panel = {across, p.d_ld, p.f2 * p.d_ld, p.f2, p.d_p}, down_panel = {down, p.gv_ld, a.d * p.gv_ld, a.d, p.f2};
     int64_t first = 0;
     do {
         const int64_t n = a.n - first < p.chunk ? a.n - first : p.chunk;
@@ -405,42 +414,46 @@ template <class K> int launch(const GatedArgs &a, const GatedGrad *g)
         Panel xp = {x, a.x_rs, 0, n, a.d};
         if (p.pack_x && n > 0) {
             const int64_t threads = n * (p.d_p / 8);
-            k_pack_rows<K><<<(unsigned)((threads + kPackThreads - 1) / kPackThreads), kPackThreads, 0, a.stream>>>(x, a.x_rs, a.x_cs, n, a.d, p.d_p, xs, p.chunk * p.d_p);
-            xp = {xs, p.d_p, p.chunk * p.d_p, n, p.d_p};
+            k_pack_rows<K><<<(unsigned)((threads + kPackThreads - 1) / kPackThreads), kPackThreads, 0, a.stream>>>(x, a.x_rs, a.x_cs, n, a.d, p.d_p, xs, p.d_ld, p.chunk * p.d_ld);
+            xp = {xs, p.d_ld, p.chunk * p.d_ld, n, p.d_p};
         }
         if (n > 0) {
-            const int64_t n_tiles = (p.f2 + 127) / 128;
-            GateArgs<K> ga = {xp, across_panel, p.d_p, a.f, n_tiles, a.act, static_cast<const E *>(a.bg), static_cast<const E *>(a.bv)};
-            const unsigned blocks = (unsigned)((n + 127) / 128 * n_tiles);
+            GateArgs<K> ga = {xp, across_panel, p.d_p, a.f, 0, a.act, static_cast<const E *>(a.bg), static_cast<const E *>(a.bv)};
             if (!g) {
                 ga.out = static_cast<E *>(a.out) + first * a.out_rs;
                 ga.out_rs = a.out_rs;
-                k_gates<K, false><<<blocks, 256, 0, a.stream>>>(ga);
             } else {
                 ga.bar = static_cast<const E *>(g->bar) + first * g->bar_rs;
                 ga.bar_rs = g->bar_rs;
                 ga.bar_cs = g->bar_cs;
                 ga.gv = gv;
-                ga.gv_ld = p.f2;
-                ga.gv_part = p.chunk * p.f2;
-                k_gates<K, true><<<blocks, 256, 0, a.stream>>>(ga);
+                ga.gv_ld = p.gv_ld;
+                ga.gv_part = p.chunk * p.gv_ld;
             }
+            with_block<K>(p.f2, n, [&](auto block) {
+                using B = decltype(block);
+                ga.n_tiles = (p.f2 + B::kCols - 1) / B::kCols;
+                const unsigned blocks = (unsigned)((n + B::kRows - 1) / B::kRows * ga.n_tiles);
+                (g ? k_gates<K, B, true> : k_gates<K, B, false>)<<<blocks, B::kThreads, 0, a.stream>>>(ga);
+            });
         }
         if (g) {
-            const Panel gp = {gv, p.f2, p.chunk * p.f2, n, p.f2};
-            if (g->dx && n > 0) {
-                const bool narrow = a.d <= 64;
-                const int64_t bm = narrow ? 256 : 128, bn = narrow ? 64 : 128, n_tiles = (a.d + bn - 1) / bn;
-                const RowBarArgs<K> ra = {gp, down_panel, n_tiles, static_cast<E *>(g->dx) + first * g->dx_rs, g->dx_rs};
-                (narrow ? k_row_bars<K, 256, 64> : k_row_bars<K, 128, 128>)<<<(unsigned)((n + bm - 1) / bm * n_tiles), 256, 0, a.stream>>>(ra);
-            }
-            if (weights) {
-                const bool narrow = a.d <= 64;
-                const int64_t bm = narrow ? 256 : 128, bn = narrow ? 64 : 128, m_tiles = (p.f2 + bm - 1) / bm, n_tiles = (a.d + bn - 1) / bn;
-                const WeightSumArgs<K> wa = {gp, xp, a.d, m_tiles, n_tiles, p.run, reinterpret_cast<float *>(ws + p.part),
-                                             g->dbg || g->dbv ? reinterpret_cast<float *>(ws + p.bias) : nullptr, first > 0};
-                (narrow ? k_weight_sums<K, 256, 64> : k_weight_sums<K, 128, 128>)<<<(unsigned)(m_tiles * n_tiles * p.splits), 256, 0, a.stream>>>(wa);
-            }
+            const Panel gp = {gv, p.gv_ld, p.chunk * p.gv_ld, n, p.f2};
+            if (g->dx && n > 0)
+                with_block<K>(a.d, n, [&](auto block) {
+                    using B = decltype(block);
+                    const int64_t n_tiles = (a.d + B::kCols - 1) / B::kCols;
+                    const RowBarArgs<K> ra = {gp, down_panel, n_tiles, static_cast<E *>(g->dx) + first * g->dx_rs, g->dx_rs};
+                    k_row_bars<K, B><<<(unsigned)((n + B::kRows - 1) / B::kRows * n_tiles), B::kThreads, 0, a.stream>>>(ra);
+                });
+            if (weights)
+                with_block<K>(a.d, p.f2, [&](auto block) {
+                    using B = decltype(block);
+                    const int64_t m_tiles = (p.f2 + B::kRows - 1) / B::kRows, n_tiles = (a.d + B::kCols - 1) / B::kCols;
+                    const WeightSumArgs<K> wa = {gp, xp, a.d, m_tiles, n_tiles, p.run, reinterpret_cast<float *>(ws + p.part),
+                                                 g->dbg || g->dbv ? reinterpret_cast<float *>(ws + p.bias) : nullptr, first > 0};
+                    k_weight_sums<K, B><<<(unsigned)(m_tiles * n_tiles * p.splits), B::kThreads, 0, a.stream>>>(wa);
+                });
         }
         first += p.chunk;
     } while (first < a.n);

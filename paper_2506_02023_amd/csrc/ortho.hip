@@ -26,7 +26,7 @@ struct Item {
     void *dst;
     int64_t src_rs, src_cs, dst_rs, dst_cs;   // of the matrix with m <= n
     int64_t x[2], low[2], gram, poly, diag;   // places in scratch memory, in elements of 16 bits: X's high and low parts, now and next; A, B, their diagonals
-    int32_t m, n, m_p, n_p, dtype;
+    int32_t m, n, m_p, n_p, m_ld, n_ld, dtype;  // sizes, filled up with zeros to, rows apart
     float x_scale;
 };
 struct List {
@@ -34,7 +34,7 @@ struct List {
     uint32_t first[kList + 1];   // first block of every item
     Item item[kList];
 };
-static_assert(sizeof(List) <= 3800, "arguments of a launch");
+static_assert(sizeof(List) <= 3960, "arguments of a launch");
 
 // The item of a block, and the block's number among the item's
 __device__ inline int item_of(const List &l, uint32_t block, uint32_t &at)
@@ -145,7 +145,7 @@ __global__ __launch_bounds__(kThreads) void k_start(List l, const double *part, 
             hi[t] = v[0];
             lo[t] = v[1];
         }
-        const int64_t to = (int64_t)(r0 + r) * it.n_p + c0 + c;
+        const int64_t to = (int64_t)(r0 + r) * it.n_ld + c0 + c;
         *reinterpret_cast<Half8<P> *>(ws + it.x[0] + to) = hi;
         *reinterpret_cast<Half8<P> *>(ws + it.low[0] + to) = lo;
     }
@@ -156,8 +156,8 @@ __global__ __launch_bounds__(kThreads) void k_start(List l, const double *part, 
 struct NoEach { template <class F> __device__ inline void operator()(F &) const {} };
 
 // X, or A - diag A, or B - diag B
-__device__ inline Panel x_panel(const Item &it, const P *ws, int which) { return {ws + it.x[which], it.n_p, it.low[which] - it.x[which], it.m, it.n_p}; }
-__device__ inline Panel square_panel(const Item &it, const P *ws, int64_t at) { return {ws + at, it.m_p, (int64_t)it.m * it.m_p, it.m, it.m_p}; }
+__device__ inline Panel x_panel(const Item &it, const P *ws, int which) { return {ws + it.x[which], it.n_ld, it.low[which] - it.x[which], it.m, it.n_p}; }
+__device__ inline Panel square_panel(const Item &it, const P *ws, int64_t at) { return {ws + at, it.m_ld, (int64_t)it.m * it.m_ld, it.m, it.m_p}; }
 
 __device__ inline float both(P hi, P lo) { return (float)hi + (float)lo; }
 
@@ -188,61 +188,70 @@ template <int PARTS, bool SQUARE> __global__ __launch_bounds__(kThreads) void k_
     using M = Product<P, PARTS, true, true, 128, 128, 64, 64>;
     __shared__ typename M::Lds lds;
     uint32_t at;
-    const Item &it = l.item[item_of(l, blockIdx.x, at)];
+    const Item &it = l.item[item_of(l, (uint32_t)xcd_order(blockIdx.x, gridDim.x), at)];
     int ti, tj;
     triangle((int)at, (it.m + 127) / 128, ti, tj);
     const Panel from = SQUARE ? square_panel(it, ws, it.gram) : x_panel(it, ws, which);
     f32x16 acc[2][2] = {};
     M::run(from, from, tj * 128, ti * 128, 0, SQUARE ? it.m_p : it.n_p, lds, acc, NoEach{});
-    const int wave = threadIdx.x >> 6, m = it.m, m_p = it.m_p;
-    const int64_t part = (int64_t)m * m_p;
+    __syncthreads();
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, m = it.m, m_p = it.m_p, ld = it.m_ld, row0 = ti * 128 + wave % 2 * 64, col0 = tj * 128 + wave / 2 * 64;
+    const Turned turned{reinterpret_cast<float *>(&lds) + wave * 4096};
+    turned.put(acc);
+    const int64_t part = (int64_t)m * ld;
     P *to = ws + (SQUARE ? it.poly : it.gram);
     const P *gram = ws + it.gram;
     float *diag = reinterpret_cast<float *>(ws + it.diag);   // of A, then of B
     const float scale = SQUARE ? c / kGramScale : kGramScale / (it.x_scale * it.x_scale);
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const int row = ti * 128 + wave % 2 * 64 + 32 * j + acc_col();
+    for (int k = 0; k < 8; ++k) {
+        const int r = lane / 8 + 8 * k, row = row0 + r, col = col0 + lane % 8 * 8;
+        if (row >= m || col >= m_p) continue;
+        const int64_t here = (int64_t)row * ld + col;
+        float y[8];
+        turned.get(y, r, lane % 8 * 8);
+#pragma unroll
+        for (int t = 0; t < 8; ++t) y[t] *= scale;
+        float dr = 0.f;
+        if constexpr (SQUARE) {
+            const Half8<P> gh = *reinterpret_cast<const Half8<P> *>(gram + here), gl = *reinterpret_cast<const Half8<P> *>(gram + part + here);
+            float dc[8];
+            load_cols<float>(dc, diag, 1, col, m);
+            dr = diag[row];
+#pragma unroll
+            for (int t = 0; t < 8; ++t) y[t] = fmaf(fmaf(c, dr + dc[t], b), both(gh[t], gl[t]), y[t]);
+        }
+        if (row >= col && row < col + 8) {
+#pragma unroll
+            for (int t = 0; t < 8; ++t)
+                if (col + t == row) {
+                    const float d = y[t] * (1.f / kGramScale);
+                    diag[SQUARE ? m + row : row] = SQUARE ? fmaf(dr, fmaf(c, dr, b), d) : d;
+                    y[t] = 0.f;
+                }
+        }
+        if (col + 8 > m)
+#pragma unroll
+            for (int t = 0; t < 8; ++t) y[t] = col + t < m ? y[t] : 0.f;
+        Half8<P> v[2];
+        split_cols<P>(y, v);
+#pragma unroll
+        for (int p = 0; p < (SQUARE ? PARTS : 2); ++p) *reinterpret_cast<Half8<P> *>(to + p * part + here) = v[p];
+        if (tj > ti) turned.set(y, r, lane % 8 * 8);
+    }
+    if (tj == ti) return;
+    turned.fence();
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const int r = lane / 8 + 8 * k, row = col0 + r, col = row0 + lane % 8 * 8;   // (columns of the tile above the diagonal are whole: col + 8 <= m)
         if (row >= m) continue;
-        const float dr = SQUARE ? diag[row] : 0.f;
+        float y[8];
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int t = 0; t < 8; ++t) y[t] = turned.one(lane % 8 * 8 + t, r);
+        Half8<P> v[2];
+        split_cols<P>(y, v);
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int col = tj * 128 + wave / 2 * 64 + 32 * i + acc_row(4 * q);
-                if (col >= m_p) continue;
-                const int64_t here = (int64_t)row * m_p + col;
-                float y[4];
-                Half4<P> gh = {}, gl = {};
-                if constexpr (SQUARE) {
-                    gh = *reinterpret_cast<const Half4<P> *>(gram + here);
-                    gl = *reinterpret_cast<const Half4<P> *>(gram + part + here);
-                }
-#pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    y[t] = acc[i][j][4 * q + t] * scale;
-                    if (SQUARE && col + t < m) {
-                        const float dc = diag[col + t];
-                        y[t] = fmaf(fmaf(c, dr + dc, b), both(gh[t], gl[t]), y[t]);
-                    }
-                    if (col + t == row) {
-                        const float d = y[t] * (1.f / kGramScale);
-                        diag[SQUARE ? m + row : row] = SQUARE ? fmaf(dr, fmaf(c, dr, b), d) : d;
-                        y[t] = 0.f;
-                    }
-                    if (col + t >= m) y[t] = 0.f;
-                }
-                Half4<P> v[2];
-                split4(y, v[0], v[1]);
-#pragma unroll
-                for (int p = 0; p < (SQUARE ? PARTS : 2); ++p) {
-                    *reinterpret_cast<Half4<P> *>(to + p * part + here) = v[p];
-                    if (tj > ti)
-#pragma unroll
-                        for (int t = 0; t < 4; ++t)
-                            if (col + t < m) to[p * part + (int64_t)(col + t) * m_p + row] = v[p][t];
-                }
-            }
+        for (int p = 0; p < (SQUARE ? PARTS : 2); ++p) *reinterpret_cast<Half8<P> *>(to + p * part + (int64_t)row * ld + col) = v[p];
     }
 }
 
@@ -252,53 +261,48 @@ template <int PARTS, bool LAST> __global__ __launch_bounds__(kThreads) void k_ap
     using M = Product<P, PARTS, false, true, 128, 128, 64, 64>;
     __shared__ typename M::Lds lds;
     uint32_t at;
-    const Item &it = l.item[item_of(l, blockIdx.x, at)];
+    const Item &it = l.item[item_of(l, (uint32_t)xcd_order(blockIdx.x, gridDim.x), at)];
     const int tiles = (it.m + 127) / 128, m0 = at % tiles * 128, n0 = at / tiles * 128;   // (tiles of the same columns one after another)
     f32x16 acc[2][2] = {};
     M::run(x_panel(it, ws, which), square_panel(it, ws, it.poly), n0, m0, 0, it.m_p, lds, acc, NoEach{});
-    const int wave = threadIdx.x >> 6, n_p = it.n_p;
-    const P *old = ws + it.x[which];
-    const P *old_low = ws + it.low[which];
+    __syncthreads();
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, c = lane % 8 * 8, col = n0 + wave / 2 * 64 + c;
+    const Turned turned{reinterpret_cast<float *>(&lds) + wave * 4096};
+    turned.put(acc);
+    if (col >= it.n_p) return;
+    const P *old = ws + it.x[which], *old_low = ws + it.low[which];
     P *to = ws + it.x[which ^ 1], *to_low = ws + it.low[which ^ 1];   // (of one part the low ones stay where they are)
     const float *diag = reinterpret_cast<const float *>(ws + it.diag) + it.m;
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const int row = m0 + wave % 2 * 64 + 32 * j + acc_col();
+    for (int k = 0; k < 8; ++k) {
+        const int r = lane / 8 + 8 * k, row = m0 + wave % 2 * 64 + r;
         if (row >= it.m) continue;
+        const int64_t here = (int64_t)row * it.n_ld + col;
+        const Half8<P> hi = *reinterpret_cast<const Half8<P> *>(old + here), lo = *reinterpret_cast<const Half8<P> *>(old_low + here);
         const float f = a + diag[row];
+        float y[8];
+        turned.get(y, r, c);
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int t = 0; t < 8; ++t) y[t] = fmaf(f, both(hi[t], lo[t]), y[t] * (1.f / kGramScale));
+        if constexpr (LAST) {
+            device_elem(it.dtype, [&](auto e) {
+                using E = decltype(e);
+                E *dst = static_cast<E *>(it.dst) + row * it.dst_rs;
+                const float s = scale / it.x_scale;
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int col = n0 + wave / 2 * 64 + 32 * i + acc_row(4 * q);
-                if (col >= n_p) continue;
-                const int64_t here = (int64_t)row * n_p + col;
-                const Half4<P> hi = *reinterpret_cast<const Half4<P> *>(old + here), lo = *reinterpret_cast<const Half4<P> *>(old_low + here);
-                float y[4];
+                for (int t = 0; t < 8; ++t) y[t] *= s;
+                if (it.dst_cs == 1) store_cols<E>(y, dst, col, it.n);
+                else
 #pragma unroll
-                for (int t = 0; t < 4; ++t) y[t] = fmaf(f, both(hi[t], lo[t]), acc[i][j][4 * q + t] * (1.f / kGramScale));
-                if constexpr (LAST) {
-                    device_elem(it.dtype, [&](auto e) {
-                        using E = decltype(e);
-                        E *dst = static_cast<E *>(it.dst) + row * it.dst_rs + col * it.dst_cs;
-                        const float s = scale / it.x_scale;
-                        if (it.dst_cs == 1 && col + 4 <= it.n) {
-                            Cols<E, 4> w;
-#pragma unroll
-                            for (int t = 0; t < 4; ++t) w[t] = to_elem<E>(y[t] * s);
-                            *reinterpret_cast<Far<E, 4> *>(dst) = w;
-                        } else
-#pragma unroll
-                            for (int t = 0; t < 4; ++t)
-                                if (col + t < it.n) dst[t * it.dst_cs] = to_elem<E>(y[t] * s);
-                    });
-                } else {
-                    Half4<P> v[2];
-                    split4(y, v[0], v[1]);
-                    *reinterpret_cast<Half4<P> *>(to + here) = v[0];
-                    *reinterpret_cast<Half4<P> *>(to_low + here) = v[1];
-                }
-            }
+                    for (int t = 0; t < 8; ++t)
+                        if (col + t < it.n) dst[(col + t) * it.dst_cs] = to_elem<E>(y[t]);
+            });
+        } else {
+            Half8<P> v[2];
+            split_cols<P>(y, v);
+            *reinterpret_cast<Half8<P> *>(to + here) = v[0];
+            *reinterpret_cast<Half8<P> *>(to_low + here) = v[1];
+        }
     }
 }
 
@@ -535,13 +539,15 @@ Group group_of(const mlip_matrix_t *list, int32_t count, int32_t at, int way, bo
         it.dtype = x.dtype;
         it.m_p = (int32_t)pad_to(it.m, kPadK);
         it.n_p = (int32_t)pad_to(it.n, kPadK);
+        it.m_ld = (int32_t)pad_odd(it.m);
+        it.n_ld = (int32_t)pad_odd(it.n);
         int e = 4;
         while ((int64_t)1 << (2 * (e - 4)) < it.n) ++e;
         it.x_scale = (float)(1 << e);
         int64_t place = used;
         auto take = [&](int64_t bytes) { const int64_t here = place / 2; place += pad_to(bytes, 256); return here; };
         if (way >= W_TWO && !no_steps) {
-            const int64_t all = (int64_t)it.m * it.n_p * 2, square = (int64_t)it.m * it.m_p * 2;
+            const int64_t all = (int64_t)it.m * it.n_ld * 2, square = (int64_t)it.m * it.m_ld * 2;
             it.x[0] = take(all);
             it.low[0] = take(all);
             it.x[1] = take(all);

@@ -55,6 +55,8 @@ template <int PARTS, int LEAST> constexpr int kStepK = PARTS == 1 ? 64 : 32;
 // Columns that a panel with K in its columns is filled up to: a multiple of both
 constexpr int64_t kPadK = 64;
 inline int64_t pad_to(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
+// The same with an odd number of memory lines, so that the rows of a tile do not all lie in the same memory channels
+inline int64_t pad_odd(int64_t n) { return pad_to(n, 64) | 64; }
 
 #ifdef __HIPCC__
 // A tile of a panel in LDS: PARTS times ROWS rows of m (or n) by KT of k.  KC: the panel has k in its columns, the tile is [ROWS][KT];
@@ -114,7 +116,7 @@ template <int PARTS, class Fn> __device__ inline void for_products(Fn &&f)
 }
 
 // acc[i][j] += rows 32 i .. of A times rows 32 j .. of B, of a wavefront's WM x WN part of the block's BM x BN tile, summed over k in [k0, k1).
-// each(a fragments of part 0 .. PARTS - 1 of step kk): called once per fragment of A, for sums along its rows.
+// each(fragments of B): called in every step, for sums along K.
 template <class T, int PARTS, bool AKC, bool BKC, int BM, int BN, int WM, int WN> struct Product {
     static constexpr int kWaves = (BM / WM) * (BN / WN), kThreads = kWaves * 64, KT = kStepK<PARTS, (BM < BN ? BM : BN)>;
     using TA = Tile<T, PARTS, AKC, BM, KT, kThreads>;
@@ -155,7 +157,7 @@ template <class T, int PARTS, bool AKC, bool BKC, int BM, int BN, int WM, int WN
 #pragma unroll
                         for (int j = 0; j < WN / 32; ++j) acc[i][j] = mfma<T>(fa[i][p], fb[j][q], acc[i][j]);
                 });
-                each(fa);
+                each(fb);
             }
         }
     }
@@ -164,6 +166,84 @@ template <class T, int PARTS, bool AKC, bool BKC, int BM, int BN, int WM, int WN
 // Row and column of register r of a 32 x 32 result: the row of A and, in the lane, of B
 __device__ inline int acc_row(int r) { return 8 * (r >> 2) + 4 * ((threadIdx.x & 63) >> 5) + (r & 3); }
 __device__ inline int acc_col() { return threadIdx.x & 31; }
+
+// A wavefront's 64 x 64 result, turned around in 16 KB of LDS of its own so that memory is met in whole lines: lanes take four or eight neighbouring elements along the
+// first operand's rows ("columns" here) of one of the second's ("rows").  The caller has made sure that nobody reads what lay in the LDS before.  Four
+// columns together are a piece; which piece lies where is turned with the row so that writes and reads meet all banks.
+struct Turned {
+    float *at;
+    __device__ inline float *piece(int row, int p) const { return at + row * 64 + ((p ^ (row & 15)) << 2); }
+    __device__ inline void fence() const
+    {
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");   // a wavefront's LDS operations are done in order: this only keeps the compiler from moving them
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    }
+    __device__ inline void put(const f32x16 (*acc)[2]) const
+    {
+        fence();
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    *reinterpret_cast<Cols<float, 4> *>(piece(32 * j + acc_col(), (32 * i + acc_row(4 * q)) / 4)) =
+                        Cols<float, 4>{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+        fence();
+    }
+    template <int W> __device__ inline void get(float (&v)[W], int row, int col) const
+    {
+#pragma unroll
+        for (int p = 0; p < W / 4; ++p) {
+            const Cols<float, 4> w = *reinterpret_cast<const Cols<float, 4> *>(piece(row, col / 4 + p));
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[4 * p + k] = w[k];
+        }
+    }
+    __device__ inline void set(const float (&v)[8], int row, int col) const
+    {
+        *reinterpret_cast<Cols<float, 4> *>(piece(row, col / 4)) = Cols<float, 4>{v[0], v[1], v[2], v[3]};
+        *reinterpret_cast<Cols<float, 4> *>(piece(row, col / 4 + 1)) = Cols<float, 4>{v[4], v[5], v[6], v[7]};
+    }
+    __device__ inline float one(int row, int col) const { return piece(row, col >> 2)[col & 3]; }
+};
+
+// W elements from column c of a row on, zeros from `cols` on; and stored, those before `cols`
+template <class E, int W> __device__ inline void load_cols(float (&v)[W], const E *row, int64_t cs, int64_t c, int64_t cols)
+{
+    if (cs == 1 && c + W <= cols) {
+        const Cols<E, W> w = *reinterpret_cast<const Far<E, W> *>(row + c);
+#pragma unroll
+        for (int k = 0; k < W; ++k) v[k] = (float)w[k];
+        return;
+    }
+#pragma unroll
+    for (int k = 0; k < W; ++k) v[k] = c + k < cols ? (float)row[(c + k) * cs] : 0.f;
+}
+template <class E, int W> __device__ inline void store_cols(const float (&v)[W], E *row, int64_t c, int64_t cols)
+{
+    if (c + W <= cols) {
+        Cols<E, W> w;
+#pragma unroll
+        for (int k = 0; k < W; ++k) w[k] = to_elem<E>(v[k]);
+        *reinterpret_cast<Far<E, W> *>(row + c) = w;
+        return;
+    }
+#pragma unroll
+    for (int k = 0; k < W; ++k)
+        if (c + k < cols) row[c + k] = to_elem<E>(v[k]);
+}
+template <class T, int PARTS, int W> __device__ inline void split_cols(const float (&v)[W], Cols<T, W> (&part)[PARTS])
+{
+#pragma unroll
+    for (int k = 0; k < W; ++k) {
+        T s[PARTS];
+        split(v[k], s);
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p) part[p][k] = s[p];
+    }
+}
 
 // Block b of `blocks` takes place (b % 8) * (blocks / 8) + b / 8 of the order, as far as that divides: the blocks that an XCD gets lie one after another, so
 // that its L2 holds what neighbours share.
