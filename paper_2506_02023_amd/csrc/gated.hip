@@ -131,23 +131,11 @@ template <class K> struct GateArgs {
     int64_t gv_ld, gv_part;
 };
 
-// A block's tile: 128 x 128 in four wavefronts (64 x 256 where there are no more columns), or 256 x 256 in eight of 128 x 64 each.  The larger one brings half the bytes from the caches for the same
-// products, the smaller one shares a compute unit with another block and leaves no one idle where there are few.
-template <int COLS, int ROWS> struct Block {   // of the first operand and of the second
-    static constexpr int kCols = COLS, kRows = ROWS, kPer = COLS == 256 ? 128 : 64, kThreads = COLS / kPer * (ROWS / 64) * 64;   // kPer x 64: a wavefront's share
-    template <class K, bool AKC, bool BKC> using Of = Product<typename K::T, K::kParts, AKC, BKC, COLS, ROWS, kPer, 64>;
-    static __device__ inline int first(int wave) { return wave / (ROWS / 64) * kPer; }
-    static __device__ inline int second(int wave) { return wave % (ROWS / 64) * 64; }
-};
-using Narrow = Block<64, 256>;
-using Middle = Block<128, 128>;
-using Large = Block<256, 256>;
-
 // The weights are the products' first operand and the rows their second; a lane ends with neighbouring features of a row.
 template <class K, class B, bool BACK> __global__ __launch_bounds__(B::kThreads) void k_gates(GateArgs<K> a)
 {
     using T = typename K::T;
-    using P = typename B::template Of<K, true, true>;
+    using P = typename B::template Of<typename K::T, K::kParts, true, true>;
     __shared__ typename P::Lds lds;
     const int64_t tile = xcd_order(blockIdx.x, gridDim.x), m0 = tile / a.n_tiles * B::kRows, n0 = tile % a.n_tiles * B::kCols;
     f32x16 acc[B::kPer / 32][2] = {};
@@ -210,7 +198,7 @@ template <class K> struct RowBarArgs {
 };
 template <class K, class B> __global__ __launch_bounds__(B::kThreads) void k_row_bars(RowBarArgs<K> a)
 {
-    using P = typename B::template Of<K, true, true>;   // (d first, rows second)
+    using P = typename B::template Of<typename K::T, K::kParts, true, true>;   // (d first, rows second)
     __shared__ typename P::Lds lds;
     const int64_t tile = xcd_order(blockIdx.x, gridDim.x), m0 = tile / a.n_tiles * B::kRows, n0 = tile % a.n_tiles * B::kCols;
     f32x16 acc[B::kPer / 32][2] = {};
@@ -243,7 +231,7 @@ template <class K> struct WeightSumArgs {
 };
 template <class K, class B> __global__ __launch_bounds__(B::kThreads) void k_weight_sums(WeightSumArgs<K> a)
 {
-    using P = typename B::template Of<K, false, false>;   // (d first, the 2 f columns second)
+    using P = typename B::template Of<typename K::T, K::kParts, false, false>;   // (d first, the 2 f columns second)
     __shared__ typename P::Lds lds;
     const int64_t at = xcd_order(blockIdx.x, gridDim.x), tiles = a.m_tiles * a.n_tiles, s = at / tiles, tile = at % tiles;
     const int64_t m0 = tile / a.n_tiles * B::kRows, n0 = tile % a.n_tiles * B::kCols;
@@ -350,7 +338,7 @@ bool reads_x(const GatedArgs &a)
 }
 
 // f(Block{}) for a product of `cols` columns (of the first operand) and `rows` rows (of the second)
-template <class K, class Fn> void with_block(int64_t cols, int64_t rows, Fn &&f)
+template <class K, class Fn> void with_tile(int64_t cols, int64_t rows, Fn &&f)
 {
     if (K::kParts == 1 && cols >= 512 && rows >= 512) f(std::conditional_t<K::kParts == 1, Large, Middle>{});
     else if (cols <= 64) f(Narrow{});
@@ -381,7 +369,8 @@ Plan plan_of(const GatedArgs &a, bool grad)
         p.down = take(a.d * p.gv_ld * p.parts * 2);
         p.gv = take(p.chunk * p.gv_ld * p.parts * 2);
         const int64_t tiles = p.parts == 1 && a.d >= 512 && p.f2 >= 512 ? (p.f2 + 255) / 256 * ((a.d + 255) / 256) : a.d <= 64 ? (p.f2 + 255) / 256 : (p.f2 + 127) / 128 * ((a.d + 127) / 128);
-        int64_t splits = 512 / tiles, most_splits = (p.chunk + 511) / 512;
+        const int64_t blocks = p.parts == 1 && a.d >= 512 && p.f2 >= 512 ? 256 : 512;   // one or two to a compute unit
+        int64_t splits = blocks / tiles, most_splits = (p.chunk + 511) / 512;
         if (splits > most_splits) splits = most_splits;
         if (splits < 1) splits = 1;
         p.run = pad_to((p.chunk + splits - 1) / splits, 64);
@@ -430,7 +419,7 @@ template <class K> int launch(const GatedArgs &a, const GatedGrad *g)
                 ga.gv_ld = p.gv_ld;
                 ga.gv_part = p.chunk * p.gv_ld;
             }
-            with_block<K>(p.f2, n, [&](auto block) {
+            with_tile<K>(p.f2, n, [&](auto block) {
                 using B = decltype(block);
                 ga.n_tiles = (p.f2 + B::kCols - 1) / B::kCols;
                 const unsigned blocks = (unsigned)((n + B::kRows - 1) / B::kRows * ga.n_tiles);
@@ -440,14 +429,14 @@ template <class K> int launch(const GatedArgs &a, const GatedGrad *g)
         if (g) {
             const Panel gp = {gv, p.gv_ld, p.chunk * p.gv_ld, n, p.f2};
             if (g->dx && n > 0)
-                with_block<K>(a.d, n, [&](auto block) {
+                with_tile<K>(a.d, n, [&](auto block) {
                     using B = decltype(block);
                     const int64_t n_tiles = (a.d + B::kCols - 1) / B::kCols;
                     const RowBarArgs<K> ra = {gp, down_panel, n_tiles, static_cast<E *>(g->dx) + first * g->dx_rs, g->dx_rs};
                     k_row_bars<K, B><<<(unsigned)((n + B::kRows - 1) / B::kRows * n_tiles), B::kThreads, 0, a.stream>>>(ra);
                 });
             if (weights)
-                with_block<K>(a.d, p.f2, [&](auto block) {
+                with_tile<K>(a.d, p.f2, [&](auto block) {
                     using B = decltype(block);
                     const int64_t m_tiles = (p.f2 + B::kRows - 1) / B::kRows, n_tiles = (a.d + B::kCols - 1) / B::kCols;
                     const WeightSumArgs<K> wa = {gp, xp, a.d, m_tiles, n_tiles, p.run, reinterpret_cast<float *>(ws + p.part),

@@ -256,54 +256,58 @@ template <int PARTS, bool SQUARE> __global__ __launch_bounds__(kThreads) void k_
 }
 
 // X' = (a + diag B) X + (B - diag B) X; the last one to where it belongs, times `scale`.  Columns of X are the first operand, its rows the second.
-template <int PARTS, bool LAST> __global__ __launch_bounds__(kThreads) void k_apply(List l, P *ws, int which, float a, float scale)
+template <int PARTS, class B, bool LAST> __global__ __launch_bounds__(B::kThreads) void k_apply(List l, P *ws, int which, float a, float scale)
 {
-    using M = Product<P, PARTS, false, true, 128, 128, 64, 64>;
+    using M = typename B::template Of<P, PARTS, false, true>;
     __shared__ typename M::Lds lds;
     uint32_t at;
     const Item &it = l.item[item_of(l, (uint32_t)xcd_order(blockIdx.x, gridDim.x), at)];
-    const int tiles = (it.m + 127) / 128, m0 = at % tiles * 128, n0 = at / tiles * 128;   // (tiles of the same columns one after another)
-    f32x16 acc[2][2] = {};
+    const int tiles = (it.m + B::kRows - 1) / B::kRows, m0 = at % tiles * B::kRows, n0 = at / tiles * B::kCols;   // (tiles of the same columns one after another)
+    f32x16 acc[B::kPer / 32][2] = {};
     M::run(x_panel(it, ws, which), square_panel(it, ws, it.poly), n0, m0, 0, it.m_p, lds, acc, NoEach{});
     __syncthreads();
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, c = lane % 8 * 8, col = n0 + wave / 2 * 64 + c;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, c = lane % 8 * 8;
     const Turned turned{reinterpret_cast<float *>(&lds) + wave * 4096};
-    turned.put(acc);
-    if (col >= it.n_p) return;
     const P *old = ws + it.x[which], *old_low = ws + it.low[which];
     P *to = ws + it.x[which ^ 1], *to_low = ws + it.low[which ^ 1];   // (of one part the low ones stay where they are)
     const float *diag = reinterpret_cast<const float *>(ws + it.diag) + it.m;
+    auto finish = [&](const f32x16 (*part)[2], int col) {   // 64 columns of a wavefront
+        turned.put(part);
+        if (col >= it.n_p) return;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-        const int r = lane / 8 + 8 * k, row = m0 + wave % 2 * 64 + r;
-        if (row >= it.m) continue;
-        const int64_t here = (int64_t)row * it.n_ld + col;
-        const Half8<P> hi = *reinterpret_cast<const Half8<P> *>(old + here), lo = *reinterpret_cast<const Half8<P> *>(old_low + here);
-        const float f = a + diag[row];
-        float y[8];
-        turned.get(y, r, c);
+        for (int k = 0; k < 8; ++k) {
+            const int r = lane / 8 + 8 * k, row = m0 + B::second(wave) + r;
+            if (row >= it.m) continue;
+            const int64_t here = (int64_t)row * it.n_ld + col;
+            const Half8<P> hi = *reinterpret_cast<const Half8<P> *>(old + here), lo = *reinterpret_cast<const Half8<P> *>(old_low + here);
+            const float f = a + diag[row];
+            float y[8];
+            turned.get(y, r, c);
 #pragma unroll
-        for (int t = 0; t < 8; ++t) y[t] = fmaf(f, both(hi[t], lo[t]), y[t] * (1.f / kGramScale));
-        if constexpr (LAST) {
-            device_elem(it.dtype, [&](auto e) {
-                using E = decltype(e);
-                E *dst = static_cast<E *>(it.dst) + row * it.dst_rs;
-                const float s = scale / it.x_scale;
+            for (int t = 0; t < 8; ++t) y[t] = fmaf(f, both(hi[t], lo[t]), y[t] * (1.f / kGramScale));
+            if constexpr (LAST) {
+                device_elem(it.dtype, [&](auto e) {
+                    using E = decltype(e);
+                    E *dst = static_cast<E *>(it.dst) + row * it.dst_rs;
+                    const float s = scale / it.x_scale;
 #pragma unroll
-                for (int t = 0; t < 8; ++t) y[t] *= s;
-                if (it.dst_cs == 1) store_cols<E>(y, dst, col, it.n);
-                else
+                    for (int t = 0; t < 8; ++t) y[t] *= s;
+                    if (it.dst_cs == 1) store_cols<E>(y, dst, col, it.n);
+                    else
 #pragma unroll
-                    for (int t = 0; t < 8; ++t)
-                        if (col + t < it.n) dst[(col + t) * it.dst_cs] = to_elem<E>(y[t]);
-            });
-        } else {
-            Half8<P> v[2];
-            split_cols<P>(y, v);
-            *reinterpret_cast<Half8<P> *>(to + here) = v[0];
-            *reinterpret_cast<Half8<P> *>(to_low + here) = v[1];
+                        for (int t = 0; t < 8; ++t)
+                            if (col + t < it.n) dst[(col + t) * it.dst_cs] = to_elem<E>(y[t]);
+                });
+            } else {
+                Half8<P> v[2];
+                split_cols<P>(y, v);
+                *reinterpret_cast<Half8<P> *>(to + here) = v[0];
+                *reinterpret_cast<Half8<P> *>(to_low + here) = v[1];
+            }
         }
-    }
+    };
+    finish(&acc[0], n0 + B::first(wave) + c);
+    if constexpr (B::kPer == 128) finish(&acc[2], n0 + B::first(wave) + 64 + c);
 }
 
 // no steps: the matrix divided by its norm
@@ -504,12 +508,12 @@ template <int ELEMS> __global__ __launch_bounds__(kSmallThreads) void k_small(Li
 constexpr int64_t kHead = kList * kNormBlocks * 8;   // bytes of the norms' partial sums
 constexpr int64_t kMostBytes = (int64_t)1 << 31;    // of a group's scratch memory, where it has more than one matrix
 
-// How a matrix is taken: in one block (of the smaller or the larger amount of LDS), or by products of two parts or one
-enum { W_SMALL, W_MEDIUM, W_TWO, W_ONE, W_COUNT };
+// How a matrix is taken: in one block (of the smaller or the larger amount of LDS), or by products of two parts, or one (with smaller or larger tiles of X)
+enum { W_SMALL, W_MEDIUM, W_TWO, W_ONE, W_ONE_LARGE, W_COUNT };
 int way_of(const mlip_matrix_t &x)
 {
     const int64_t elems = x.rows < x.cols ? small_elems(x.rows, x.cols) : small_elems(x.cols, x.rows);
-    return elems <= kSmallHalves ? W_SMALL : elems <= kSmallMost ? W_MEDIUM : x.dtype == MLIP_DTYPE_BF16 ? W_ONE : W_TWO;
+    return elems <= kSmallHalves ? W_SMALL : elems <= kSmallMost ? W_MEDIUM : x.dtype != MLIP_DTYPE_BF16 ? W_TWO : x.rows < 512 || x.cols < 512 ? W_ONE : W_ONE_LARGE;
 }
 
 struct Group {
@@ -576,15 +580,15 @@ template <class Fn> unsigned number_blocks(List &l, Fn &&blocks_of)
     return at;
 }
 
-template <int PARTS> void steps_of(List &l, P *ws, int32_t steps, float a, float b, float c, float scale, hipStream_t stream)
+template <int PARTS, class B> void steps_of(List &l, P *ws, int32_t steps, float a, float b, float c, float scale, hipStream_t stream)
 {
     for (int s = 0; s < steps; ++s) {
         const int now = s & 1;
         unsigned blocks = number_blocks(l, [](const Item &it) { const int64_t t = (it.m + 127) / 128; return t * (t + 1) / 2; });
         k_symmetric<PARTS, false><<<blocks, kThreads, 0, stream>>>(l, ws, now, 0.f, 0.f);
         k_symmetric<PARTS, true><<<blocks, kThreads, 0, stream>>>(l, ws, now, b, c);
-        blocks = number_blocks(l, [](const Item &it) { return (int64_t)((it.m + 127) / 128) * ((it.n_p + 127) / 128); });
-        (s + 1 == steps ? k_apply<PARTS, true> : k_apply<PARTS, false>)<<<blocks, kThreads, 0, stream>>>(l, ws, now, a, scale);
+        blocks = number_blocks(l, [](const Item &it) { return (int64_t)((it.m + B::kRows - 1) / B::kRows) * ((it.n_p + B::kCols - 1) / B::kCols); });
+        (s + 1 == steps ? k_apply<PARTS, B, true> : k_apply<PARTS, B, false>)<<<blocks, B::kThreads, 0, stream>>>(l, ws, now, a, scale);
     }
 }
 
@@ -624,8 +628,9 @@ int ortho_impl(const mlip_matrix_t *list, int32_t count, int32_t steps, const do
             } else {
                 const unsigned blocks = number_blocks(l, [](const Item &it) { return (int64_t)((it.m + 63) / 64) * (it.n_p / 64); });
                 k_start<<<blocks, kThreads, 0, stream>>>(l, norms, eps, ws);
-                if (way == W_TWO) steps_of<2>(l, ws, steps, a, b, c, scale, stream);
-                else steps_of<1>(l, ws, steps, a, b, c, scale, stream);
+                if (way == W_TWO) steps_of<2, Middle>(l, ws, steps, a, b, c, scale, stream);
+                else if (way == W_ONE) steps_of<1, Middle>(l, ws, steps, a, b, c, scale, stream);
+                else steps_of<1, Large>(l, ws, steps, a, b, c, scale, stream);
             }
             MLIP_HIP(hipGetLastError());
         }

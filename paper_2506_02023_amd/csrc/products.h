@@ -163,6 +163,18 @@ template <class T, int PARTS, bool AKC, bool BKC, int BM, int BN, int WM, int WN
     }
 };
 
+// A block's tile: 128 x 128 in four wavefronts (64 x 256 where there are no more columns), or 256 x 256 in eight of 128 x 64 each.  The larger one brings half the bytes from the caches for the same
+// products, the smaller one shares a compute unit with another block and leaves no one idle where there are few.
+template <int COLS, int ROWS> struct Block {   // of the first operand and of the second
+    static constexpr int kCols = COLS, kRows = ROWS, kPer = COLS == 256 ? 128 : 64, kThreads = COLS / kPer * (ROWS / 64) * 64;   // kPer x 64: a wavefront's share
+    template <class T, int PARTS, bool AKC, bool BKC> using Of = Product<T, PARTS, AKC, BKC, COLS, ROWS, kPer, 64>;
+    static __device__ inline int first(int wave) { return wave / (ROWS / 64) * kPer; }
+    static __device__ inline int second(int wave) { return wave % (ROWS / 64) * 64; }
+};
+using Narrow = Block<64, 256>;
+using Middle = Block<128, 128>;
+using Large = Block<256, 256>;
+
 // Row and column of register r of a 32 x 32 result: the row of A and, in the lane, of B
 __device__ inline int acc_row(int r) { return 8 * (r >> 2) + 4 * ((threadIdx.x & 63) >> 5) + (r & 3); }
 __device__ inline int acc_col() { return threadIdx.x & 31; }
