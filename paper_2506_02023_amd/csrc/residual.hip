@@ -7,15 +7,19 @@
 //   dgate = factor scale p D, summed as the gate is spread;  dscale = sum over rows of factor gate p D
 //   dw_post = sum P zhat, db_post = sum P, dw_pre = sum dn yhat, db_pre = sum dn   (over rows)
 //
-// Bound by memory: every row is read once and stays in registers, 8 columns of a row in each of G lanes (rows of up to 512 columns in
-// part of a wavefront, wider ones in several), and all is fp32.  The gradient starts from x and z again, so the forward pass keeps nothing.
+// Bound by memory: every row is read once and stays in registers, four columns of it in a lane (rows of up to 256 columns in part of a
+// wavefront, wider ones in a block of their own), and all is fp32.  The gradient starts from x and z again, so the forward pass keeps nothing.  Up to 4096 columns the
+// next row is requested before the present one is worked on.
 // Sums over rows: each lane over the rows it meets, the lanes of a block joined in registers and LDS, the blocks in a second launch, all in a fixed order.
+#include <type_traits>
+
 #include "elem.h"
 
 namespace mlip {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kMostThreads = 1024;
 constexpr int kSums = 6;   // dscale, dw_post, db_post, dw_pre, db_pre, dgate of columns
 enum { S_SCALE, S_POST_W, S_POST_B, S_PRE_W, S_PRE_B, S_GATE };
 
@@ -37,272 +41,449 @@ struct Args {
     float eps, factor;
 };
 
-template <class E> __device__ inline void load8(float (&v)[8], const void *base, int64_t cs, int64_t at, int c, int width)
+template <class E> using Four = Cols<E, 4>;
+
+template <class E> __device__ inline Four<E> load4(const void *base, int64_t cs, int64_t at, int c, int width)
 {
     const E *p = static_cast<const E *>(base) + at;
-    if (cs == 1 && c + 8 <= width) {
-        const Cols<E, 8> w = *reinterpret_cast<const Far<E, 8> *>(p + c);
+    Four<E> w = {};
+    if (cs == 1 && c + 4 <= width) w = *reinterpret_cast<const Far<E, 4> *>(p + c);
+    else
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = (float)w[k];
-        return;
-    }
-#pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = c + k < width ? (float)p[(c + k) * cs] : 0.f;
+        for (int k = 0; k < 4; ++k)
+            if (c + k < width) w[k] = p[(c + k) * cs];
+    return w;
 }
-template <class E> __device__ inline void store8(const float (&v)[8], void *base, int64_t at, int c, int width)
+template <class E> __device__ inline Four<E> narrow(const float (&v)[4])
+{
+    if constexpr (std::is_same_v<E, __bf16>) return __builtin_convertvector(Four<float>{v[0], v[1], v[2], v[3]}, Four<__bf16>);
+    Four<E> w;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) w[k] = to_elem<E>(v[k]);
+    return w;
+}
+template <class E> __device__ inline void store4(Four<E> w, void *base, int64_t at, int c, int width)
 {
     E *p = static_cast<E *>(base) + at;
-    if (c + 8 <= width) {
-        Cols<E, 8> w;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) w[k] = to_elem<E>(v[k]);
-        *reinterpret_cast<Far<E, 8> *>(p + c) = w;
+    if (c + 4 <= width) {
+        *reinterpret_cast<Far<E, 4> *>(p + c) = w;
         return;
     }
 #pragma unroll
-    for (int k = 0; k < 8; ++k)
-        if (c + k < width) p[c + k] = to_elem<E>(v[k]);
+    for (int k = 0; k < 4; ++k)
+        if (c + k < width) p[c + k] = w[k];
+}
+// Four columns of a row of 4 or more, without a branch: past the end of the row the last four stand in, from which widen() takes those that belong, and zeros
+template <class E> __device__ inline Four<E> load4_within(const void *base, int64_t at, int c, int width)
+{
+    return *reinterpret_cast<const Far<E, 4> *>(static_cast<const E *>(base) + at + (c + 4 <= width ? c : width - 4));
+}
+// beyond: columns by which the load stands further left than its place; fix: whether any lane of the wavefront has such a load
+template <class E> __device__ inline void widen(float (&v)[4], Four<E> w, int beyond = 0, bool fix = false)
+{
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = (float)w[k];
+    if (fix) {
+        const float u[4] = {v[0], v[1], v[2], v[3]};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            v[k] = beyond == 0 ? u[k] : 0.f;
+#pragma unroll
+            for (int s = 1; s + k < 4; ++s) v[k] = beyond == s ? u[k + s] : v[k];
+        }
+    }
 }
 // A parameter's columns; `none` where there is no such parameter
-template <class E> __device__ inline void param8(float (&v)[8], const void *p, bool f32, int c, int width, float none)
+template <class E> __device__ inline void param4(float (&v)[4], const void *p, bool f32, int c, int width, float none)
 {
     if (!p) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = none;
-    } else if (f32) load8<float>(v, p, 1, 0, c, width);
-    else load8<E>(v, p, 1, 0, c, width);
+        for (int k = 0; k < 4; ++k) v[k] = none;
+    } else if (f32) widen<float>(v, load4<float>(p, 1, 0, c, width));
+    else widen<E>(v, load4<E>(p, 1, 0, c, width));
 }
 
-// Lanes of a row: G, in one wavefront or several; N vectors of 8 columns each
+// Lanes of a row: G of a wavefront, or (0) all of the block; N vectors of 4 columns each
 template <int G_, int N_> struct Shape {
-    static constexpr int G = G_, N = N_, kBlock = G > kThreads ? G : kThreads, kRows = kBlock / G;
-    static constexpr int kWaves = kBlock / 64;
+    static constexpr int G = G_, N = N_;
+    static constexpr bool kWide = G == 0;
+    static constexpr int kBlock = kWide ? kMostThreads : kThreads;   // at most
+    static __device__ inline int lanes() { return kWide ? (int)blockDim.x : G; }
+    static __device__ inline int lane() { return kWide ? (int)threadIdx.x : (int)threadIdx.x % (kWide ? 1 : G); }
+    static constexpr int kRows = kWide ? 1 : kThreads / (kWide ? 1 : G);
 };
 
-template <class S> struct Red { float v[2][2][S::kWaves]; };
-
-// Sums of a and b over the lanes of a row; turn: which half of the scratch memory, the other one than the last time
-template <class S> __device__ inline void row_sum(float &a, float &b, Red<S> &red, int &turn)
+// Sum over G neighbouring lanes, for all of them
+template <int G> __device__ inline float lanes_sum(float v)
 {
-    constexpr int in_wave = S::G < 64 ? S::G : 64;
-#pragma unroll
-    for (int d = in_wave / 2; d; d >>= 1) {
-        a += __shfl_xor(a, d);
-        b += __shfl_xor(b, d);
-    }
-    if constexpr (S::G > 64) {
-        const int wave = threadIdx.x >> 6, first = threadIdx.x / S::G * (S::G / 64);
-        if ((threadIdx.x & 63) == 0) {
-            red.v[turn][0][wave] = a;
-            red.v[turn][1][wave] = b;
-        }
-        __syncthreads();
-        a = b = 0.f;
-#pragma unroll
-        for (int w = 0; w < S::G / 64; ++w) {
-            a += red.v[turn][0][first + w];
-            b += red.v[turn][1][first + w];
-        }
-        turn ^= 1;
-    }
+    auto moved = [](float x, auto way) { return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), decltype(way)::value, 0xf, 0xf, true)); };
+    if constexpr (G >= 2) v += moved(v, std::integral_constant<int, 0xb1>{});    // neighbours in pairs,
+    if constexpr (G >= 4) v += moved(v, std::integral_constant<int, 0x4e>{});    // pairs in fours,
+    if constexpr (G >= 8) v += moved(v, std::integral_constant<int, 0x141>{});   // halves of eight mirrored,
+    if constexpr (G >= 16) v += moved(v, std::integral_constant<int, 0x140>{});  // and of sixteen
+    if constexpr (G >= 32) v += __builtin_bit_cast(float, __builtin_amdgcn_ds_swizzle(__builtin_bit_cast(int, v), 0x401f));   // lane ^ 16
+    if constexpr (G >= 64) v += __shfl_xor(v, 32);
+    return v;
 }
 
-// t becomes that; returns r
-template <class S> __device__ inline float normalise(float (&t)[S::N][8], const Args &a, int c0, float inv, Red<S> &red, int &turn)
+// Columns of a row that wavefront w of its block has
+template <class S> __device__ inline float row_cols(int w, int width)
+{
+    int cols = 0;
+#pragma unroll
+    for (int i = 0; i < S::N; ++i) {
+        const int from = (i * S::lanes() + w * 64) * 4, left = width - from;
+        cols += left < 0 ? 0 : left < 256 ? left : 256;
+    }
+    return (float)cols;
+}
+
+// What the wavefronts of a row exchange: two values of each, in the half of the memory that was not used last
+struct Exchange {
+    float (*at)[2][kMostThreads / 64];   // [2]
+    int turn;
+    __device__ inline void put(float a, float b)
+    {
+        turn ^= 1;
+        if ((threadIdx.x & 63) == 0) {
+            at[turn][0][threadIdx.x >> 6] = a;
+            at[turn][1][threadIdx.x >> 6] = b;
+        }
+        // a barrier for what lies in LDS alone: loads and stores of rows go on
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+    }
+};
+
+// Sums of a and b over the lanes of a row
+template <class S> __device__ inline void row_sum(float &a, float &b, Exchange &x)
+{
+    a = lanes_sum<S::kWide ? 64 : S::G>(a);
+    b = lanes_sum<S::kWide ? 64 : S::G>(b);
+    if constexpr (S::kWide) {
+        x.put(a, b);
+        a = b = 0.f;
+        for (int w = 0; w < (int)blockDim.x / 64; ++w) {
+            a += x.at[x.turn][0][w];
+            b += x.at[x.turn][1][w];
+        }
+    }
+}
+template <class S> __device__ inline float row_sum(float a, Exchange &x)
 {
     float none = 0.f;
+    if constexpr (!S::kWide) return lanes_sum<S::G>(a);
+    row_sum<S>(a, none, x);
+    return a;
+}
+
+// t becomes that; returns r.  Over several wavefronts the squares are summed about each wavefront's own mean, and the means' about the row's, so that one exchange
+// will do: mine = columns of this wavefront.
+template <class S> __device__ inline float normalise(float (&t)[S::N][4], const Args &a, float inv, bool ragged, float mine, Exchange &x)
+{
+    constexpr int G = S::kWide ? 64 : S::G;
+    const int c0 = S::lane() * 4, step = S::lanes() * 4;
+    float sum = 0.f, mean = 0.f, sq = 0.f;
     if (a.layer) {
-        float sum = 0.f;
 #pragma unroll
         for (int i = 0; i < S::N; ++i)
 #pragma unroll
-            for (int k = 0; k < 8; ++k) sum += t[i][k];
-        row_sum<S>(sum, none, red, turn);
-        const float mean = sum * inv;
+            for (int k = 0; k < 4; ++k) sum += t[i][k];
+        sum = lanes_sum<G>(sum);
+        mean = S::kWide ? sum / fmaxf(mine, 1.f) : sum * inv;
 #pragma unroll
         for (int i = 0; i < S::N; ++i)
 #pragma unroll
-            for (int k = 0; k < 8; ++k) t[i][k] = c0 + i * S::G * 8 + k < a.width ? t[i][k] - mean : 0.f;
+            for (int k = 0; k < 4; ++k) t[i][k] -= mean;
+        if (ragged)
+#pragma unroll
+            for (int i = 0; i < S::N; ++i)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) t[i][k] = c0 + i * step + k < a.width ? t[i][k] : 0.f;
     }
-    float sq = 0.f;
 #pragma unroll
     for (int i = 0; i < S::N; ++i)
 #pragma unroll
-        for (int k = 0; k < 8; ++k) sq = fmaf(t[i][k], t[i][k], sq);
-    row_sum<S>(sq, none, red, turn);
+        for (int k = 0; k < 4; ++k) sq = fmaf(t[i][k], t[i][k], sq);
+    sq = lanes_sum<G>(sq);
+    if constexpr (S::kWide) {
+        x.put(sq, sum);
+        const int waves = blockDim.x / 64;
+        float all = 0.f;
+        sq = 0.f;
+        for (int w = 0; w < waves; ++w) {
+            sq += x.at[x.turn][0][w];
+            all += x.at[x.turn][1][w];
+        }
+        if (a.layer) {
+            all *= inv;   // the row's mean
+            for (int w = 0; w < waves; ++w) {
+                const float cols = row_cols<S>(w, a.width), d = x.at[x.turn][1][w] / fmaxf(cols, 1.f) - all;
+                sq = fmaf(cols * d, d, sq);
+            }
+            const float shift = mean - all;
+#pragma unroll
+            for (int i = 0; i < S::N; ++i)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) t[i][k] = !ragged || c0 + i * step + k < a.width ? t[i][k] + shift : 0.f;
+        }
+    }
     const float r = 1.f / sqrtf(fmaf(sq, inv, a.eps));
 #pragma unroll
     for (int i = 0; i < S::N; ++i)
 #pragma unroll
-        for (int k = 0; k < 8; ++k) t[i][k] *= r;
+        for (int k = 0; k < 4; ++k) t[i][k] *= r;
     return r;
 }
 
 // bar, the gradient of that, becomes the gradient of t
-template <class S> __device__ inline void normalise_back(float (&bar)[S::N][8], const float (&hat)[S::N][8], float r, const Args &a, int c0, float inv, Red<S> &red, int &turn)
+template <class S> __device__ inline void normalise_back(float (&bar)[S::N][4], const float (&hat)[S::N][4], float r, const Args &a, float inv, bool ragged, Exchange &x)
 {
+    const int c0 = S::lane() * 4, step = S::lanes() * 4;
     float s0 = 0.f, s1 = 0.f;
 #pragma unroll
     for (int i = 0; i < S::N; ++i)
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            s0 += bar[i][k];
-            s1 = fmaf(bar[i][k], hat[i][k], s1);
-        }
-    row_sum<S>(s0, s1, red, turn);
-    const float mean = a.layer ? s0 * inv : 0.f, along = s1 * inv;
+        for (int k = 0; k < 4; ++k) s1 = fmaf(bar[i][k], hat[i][k], s1);
+    if (a.layer) {
+#pragma unroll
+        for (int i = 0; i < S::N; ++i)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) s0 += bar[i][k];
+        row_sum<S>(s0, s1, x);
+    } else s1 = row_sum<S>(s1, x);
+    const float mean = s0 * inv, along = s1 * inv;
 #pragma unroll
     for (int i = 0; i < S::N; ++i)
 #pragma unroll
-        for (int k = 0; k < 8; ++k) bar[i][k] = c0 + i * S::G * 8 + k < a.width ? r * (bar[i][k] - fmaf(hat[i][k], along, mean)) : 0.f;
+        for (int k = 0; k < 4; ++k) bar[i][k] = r * (bar[i][k] - fmaf(hat[i][k], along, mean));   // (a row of equal gradients comes out as zeros)
+    if (ragged)
+#pragma unroll
+        for (int i = 0; i < S::N; ++i)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) bar[i][k] = c0 + i * step + k < a.width ? bar[i][k] : 0.f;
 }
 
-template <class E, class S, bool BACK> __global__ __launch_bounds__(S::kBlock) void k_residual(Args a, Back b)
+// PLAIN: rows of four columns or more, the columns one after another in all inputs
+template <class E, class S, bool BACK, bool PLAIN> __global__ __launch_bounds__(S::kBlock, S::kWide ? 4 : 1) void k_residual(Args a, Back b)
 {
-    __shared__ Red<S> red;
-    __shared__ float sums[BACK && S::kRows > 1 ? S::kWaves : 1][BACK && S::kRows > 1 ? S::G * 8 * S::N : 1];
-    int turn = 0;
-    const int lane = threadIdx.x % S::G, c0 = lane * 8;
-    const float inv = 1.f / (float)a.width;
-    auto col = [&](int i) { return c0 + i * S::G * 8; };
-    float scale[S::N][8], post_w[S::N][8], post_b[S::N][8], pre_w[S::N][8], pre_b[S::N][8], gate_c[S::N][8];
+    constexpr int N = S::N;
+    __shared__ float between[2][2][kMostThreads / 64];
+    __shared__ float sums[BACK && !S::kWide ? kThreads / 64 : 1][BACK && !S::kWide ? S::G * 4 : 1];
+    Exchange ex{between, 0};
+    const int c0 = S::lane() * 4, step = S::lanes() * 4;
+    const float inv = 1.f / (float)a.width, mine = S::kWide ? row_cols<S>(threadIdx.x >> 6, a.width) : 0.f;
+    const bool ragged = a.width != N * step;
+    auto col = [&](int i) { return c0 + i * step; };
+    const bool gate_cols = a.gate_kind == MLIP_RESIDUAL_GATE_COL, gate_full = a.gate_kind == MLIP_RESIDUAL_GATE_FULL, gate_row = a.gate_kind == MLIP_RESIDUAL_GATE_ROW;
+
+    // the parameters' columns stay in registers where a lane has four, and come from the caches where it has more.
+    struct Params { float scale[4], gate[4], post_w[4], post_b[4], pre_w[4], pre_b[4]; };
+    auto params_of = [&](Params &p, int i) {
+        param4<E>(p.scale, a.scale, a.params_f32, col(i), a.width, 1.f);
+        param4<E>(p.gate, gate_cols ? a.gate.p : nullptr, false, col(i), a.width, 1.f);
+        param4<E>(p.post_w, a.post_w, a.params_f32, col(i), a.width, 1.f);
+        param4<E>(p.post_b, a.post_b, a.params_f32, col(i), a.width, 0.f);
+        param4<E>(p.pre_w, a.pre_w, a.params_f32, col(i), a.width, 1.f);
+        param4<E>(p.pre_b, a.pre_b, a.params_f32, col(i), a.width, 0.f);
+    };
+    Params held;
+    if constexpr (N == 1) params_of(held, 0);
+
+    struct Raw { Four<E> x[N], z[N], gate[N], dy[N], dn[N]; E g; };
+    int beyond[N];
+    bool fix[N];
 #pragma unroll
-    for (int i = 0; i < S::N; ++i) {
-        param8<E>(scale[i], a.scale, a.params_f32, col(i), a.width, 1.f);
-        param8<E>(post_w[i], a.post_w, a.params_f32, col(i), a.width, 1.f);
-        param8<E>(post_b[i], a.post_b, a.params_f32, col(i), a.width, 0.f);
-        param8<E>(pre_w[i], a.pre_w, a.params_f32, col(i), a.width, 1.f);
-        param8<E>(pre_b[i], a.pre_b, a.params_f32, col(i), a.width, 0.f);
-        param8<E>(gate_c[i], a.gate_kind == MLIP_RESIDUAL_GATE_COL ? a.gate.p : nullptr, false, col(i), a.width, 1.f);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) scale[i][k] *= a.factor;
+    for (int i = 0; i < N; ++i) {
+        beyond[i] = PLAIN && col(i) + 4 > a.width ? col(i) + 4 - a.width : 0;
+        fix[i] = __ballot(beyond[i] != 0) != 0;
     }
-    float sum[BACK ? kSums : 1][S::N][8] = {};
+    auto load = [&](Raw &w, int64_t r0) {
+        int64_t row = r0 + (S::kWide ? 0 : threadIdx.x / (S::kWide ? 1 : S::G));
+        if (row >= a.n) row = a.n - 1;
+        auto take = [&](Four<E> (&to)[N], const Input &from) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                if constexpr (PLAIN) to[i] = load4_within<E>(from.p, row * from.rs, col(i), a.width);
+                else to[i] = load4<E>(from.p, from.cs, row * from.rs, col(i), a.width);
+            }
+        };
+        take(w.x, a.x);
+        if (a.z.p) take(w.z, a.z);
+        if (gate_full) take(w.gate, a.gate);
+        if constexpr (BACK) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) w.dy[i] = w.dn[i] = Four<E>{};
+            if (b.dy.p) take(w.dy, b.dy);
+            if (b.dn.p) take(w.dn, b.dn);
+        }
+        if (gate_row) w.g = static_cast<const E *>(a.gate.p)[row * a.gate.rs];
+    };
+
+    // A row's results are stored when the next row has come: a wait for loads is one for all stores made before them, which take longest.
+    struct Done { Four<E> first[N], second[N], gate[N]; } done;   // y and norm, or dx, dz and dgate
+    int64_t done_row = -1;
+    auto store = [&] {
+        if (done_row < 0) return;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            if constexpr (BACK) {
+                if (b.dx) store4<E>(done.first[i], b.dx, done_row * b.dx_rs, col(i), a.width);
+                if (b.dz) store4<E>(done.second[i], b.dz, done_row * b.dz_rs, col(i), a.width);
+                if (gate_full && b.dgate) store4<E>(done.gate[i], b.dgate, done_row * b.dgate_rs, col(i), a.width);
+            } else {
+                if (a.y) store4<E>(done.first[i], a.y, done_row * a.y_rs, col(i), a.width);
+                if (a.pre) store4<E>(done.second[i], a.norm, done_row * a.norm_rs, col(i), a.width);
+            }
+        }
+    };
+
+    float sum[BACK ? kSums : 1][N][4] = {};
+    const int64_t stride = (int64_t)gridDim.x * S::kRows;
+    Raw next;
+    int64_t r0 = (int64_t)blockIdx.x * S::kRows;
+    if (N == 1 && r0 < a.n) load(next, r0);
     // (all lanes of a block make the same number of rounds: rows of several wavefronts meet at barriers)
-    for (int64_t r0 = (int64_t)blockIdx.x * S::kRows; r0 < a.n; r0 += (int64_t)gridDim.x * S::kRows) {
-        const int64_t row_at = r0 + threadIdx.x / S::G;
-        const bool there = row_at < a.n;
-        const int64_t row = there ? row_at : a.n - 1;
-        float y[S::N][8], zh[S::N][8], gate[S::N][8], dy[S::N][8], dn[S::N][8];
+    for (; r0 < a.n; r0 += stride) {
+        const int64_t row = r0 + (S::kWide ? 0 : threadIdx.x / (S::kWide ? 1 : S::G));
+        const bool there = row < a.n;
+        float y[N][4], zh[N][4], gate[N][4], dy[N][4], dn[N][4];
+        if (N > 1) load(next, r0);
 #pragma unroll
-        for (int i = 0; i < S::N; ++i) {
-            load8<E>(y[i], a.x.p, a.x.cs, row * a.x.rs, col(i), a.width);
-            if (a.z.p) load8<E>(zh[i], a.z.p, a.z.cs, row * a.z.rs, col(i), a.width);
-            if (a.gate_kind == MLIP_RESIDUAL_GATE_FULL) load8<E>(gate[i], a.gate.p, a.gate.cs, row * a.gate.rs, col(i), a.width);
+        for (int i = 0; i < N; ++i) {
+            widen<E>(y[i], next.x[i], beyond[i], fix[i]);
+            if (a.z.p) widen<E>(zh[i], next.z[i], beyond[i], fix[i]);
+            if (gate_full) widen<E>(gate[i], next.gate[i], beyond[i], fix[i]);
             else {
-                const float g = a.gate_kind == MLIP_RESIDUAL_GATE_ROW ? (float)static_cast<const E *>(a.gate.p)[row * a.gate.rs] : 1.f;
+                const float g = gate_row ? (float)next.g : 1.f;
 #pragma unroll
-                for (int k = 0; k < 8; ++k) gate[i][k] = gate_c[i][k] * g;
+                for (int k = 0; k < 4; ++k) gate[i][k] = g;
             }
             if constexpr (BACK) {
-#pragma unroll
-                for (int k = 0; k < 8; ++k) dy[i][k] = dn[i][k] = 0.f;
-                if (b.dy.p) load8<E>(dy[i], b.dy.p, b.dy.cs, row * b.dy.rs, col(i), a.width);
-                if (b.dn.p) load8<E>(dn[i], b.dn.p, b.dn.cs, row * b.dn.rs, col(i), a.width);
+                widen<E>(dy[i], next.dy[i], beyond[i], fix[i]);
+                widen<E>(dn[i], next.dn[i], beyond[i], fix[i]);
             }
         }
+        store();
+        done_row = there ? row : -1;
+        if (N == 1 && r0 + stride < a.n) load(next, r0 + stride);
         float rz = 1.f;
         if (a.z.p) {
-            if (a.post) rz = normalise<S>(zh, a, c0, inv, red, turn);
+            if (a.post) rz = normalise<S>(zh, a, inv, ragged, mine, ex);
 #pragma unroll
-            for (int i = 0; i < S::N; ++i)
+            for (int i = 0; i < N; ++i) {
+                if constexpr (N > 1) params_of(held, i);
 #pragma unroll
-                for (int k = 0; k < 8; ++k) y[i][k] = fmaf(gate[i][k] * scale[i][k], fmaf(zh[i][k], post_w[i][k], post_b[i][k]), y[i][k]);
+                for (int k = 0; k < 4; ++k) {
+                    gate[i][k] *= held.gate[k] * a.factor;   // (from here on with the factor)
+                    y[i][k] = fmaf(gate[i][k] * held.scale[k], fmaf(zh[i][k], held.post_w[k], held.post_b[k]), y[i][k]);
+                }
+            }
         }
         if constexpr (!BACK) {
-            if (a.y && there)
 #pragma unroll
-                for (int i = 0; i < S::N; ++i) store8<E>(y[i], a.y, row * a.y_rs, col(i), a.width);
+            for (int i = 0; i < N; ++i) done.first[i] = narrow<E>(y[i]);
             if (!a.pre) continue;
-            normalise<S>(y, a, c0, inv, red, turn);
-            if (there)
+            normalise<S>(y, a, inv, ragged, mine, ex);
 #pragma unroll
-                for (int i = 0; i < S::N; ++i) {
+            for (int i = 0; i < N; ++i) {
+                if constexpr (N > 1) params_of(held, i);
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) y[i][k] = fmaf(y[i][k], pre_w[i][k], pre_b[i][k]);
-                    store8<E>(y[i], a.norm, row * a.norm_rs, col(i), a.width);
-                }
+                for (int k = 0; k < 4; ++k) y[i][k] = fmaf(y[i][k], held.pre_w[k], held.pre_b[k]);
+                done.second[i] = narrow<E>(y[i]);
+            }
         } else {
             if (a.pre) {
-                const float ry = normalise<S>(y, a, c0, inv, red, turn);
+                const float ry = normalise<S>(y, a, inv, ragged, mine, ex);
 #pragma unroll
-                for (int i = 0; i < S::N; ++i)
+                for (int i = 0; i < N; ++i) {
+                    if (there && b.sum[S_PRE_W])
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        if (there) {
-                            sum[S_PRE_W][i][k] = fmaf(dn[i][k], y[i][k], sum[S_PRE_W][i][k]);
-                            sum[S_PRE_B][i][k] += dn[i][k];
-                        }
-                        dn[i][k] *= pre_w[i][k];
-                    }
-                normalise_back<S>(dn, y, ry, a, c0, inv, red, turn);
+                        for (int k = 0; k < 4; ++k) sum[S_PRE_W][i][k] = fmaf(dn[i][k], y[i][k], sum[S_PRE_W][i][k]);
+                    if (there && b.sum[S_PRE_B])
 #pragma unroll
-                for (int i = 0; i < S::N; ++i)
+                        for (int k = 0; k < 4; ++k) sum[S_PRE_B][i][k] += dn[i][k];
+                    if constexpr (N > 1) params_of(held, i);
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) dy[i][k] += dn[i][k];
-            }
-            if (b.dx && there)
-#pragma unroll
-                for (int i = 0; i < S::N; ++i) store8<E>(dy[i], b.dx, row * b.dx_rs, col(i), a.width);
-            if (!a.z.p) continue;
-            float gate_sum = 0.f, none = 0.f;
-#pragma unroll
-            for (int i = 0; i < S::N; ++i) {
-                float dgate[8];
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    const float pd = fmaf(zh[i][k], post_w[i][k], post_b[i][k]) * dy[i][k];
-                    dgate[k] = pd * scale[i][k];
-                    if (col(i) + k >= a.width) dgate[k] = 0.f;
-                    const float bar = dy[i][k] * gate[i][k] * scale[i][k];
-                    if (there) {
-                        sum[S_SCALE][i][k] = fmaf(pd * a.factor, gate[i][k], sum[S_SCALE][i][k]);
-                        sum[S_GATE][i][k] += dgate[k];
-                        sum[S_POST_W][i][k] = fmaf(bar, zh[i][k], sum[S_POST_W][i][k]);
-                        sum[S_POST_B][i][k] += bar;
-                    }
-                    gate_sum += dgate[k];
-                    dy[i][k] = a.post ? bar * post_w[i][k] : bar;
+                    for (int k = 0; k < 4; ++k) dn[i][k] *= held.pre_w[k];
                 }
-                if (b.dgate && a.gate_kind == MLIP_RESIDUAL_GATE_FULL && there) store8<E>(dgate, b.dgate, row * b.dgate_rs, col(i), a.width);
-            }
-            if (a.gate_kind == MLIP_RESIDUAL_GATE_ROW && b.dgate) {
-                row_sum<S>(gate_sum, none, red, turn);
-                if (there && lane == 0) static_cast<E *>(b.dgate)[row * b.dgate_rs] = to_elem<E>(gate_sum);
-            }
-            if (a.post) normalise_back<S>(dy, zh, rz, a, c0, inv, red, turn);
-            if (b.dz && there)
+                normalise_back<S>(dn, y, ry, a, inv, ragged, ex);
 #pragma unroll
-                for (int i = 0; i < S::N; ++i) store8<E>(dy[i], b.dz, row * b.dz_rs, col(i), a.width);
+                for (int i = 0; i < N; ++i)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) dy[i][k] += dn[i][k];
+            }
+#pragma unroll
+            for (int i = 0; i < N; ++i) done.first[i] = narrow<E>(dy[i]);
+            if (!a.z.p) continue;
+            float gate_sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                if constexpr (N > 1) params_of(held, i);
+                float pd[4], bar[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    pd[k] = fmaf(zh[i][k], held.post_w[k], held.post_b[k]) * dy[i][k];
+                    bar[k] = dy[i][k] * gate[i][k] * held.scale[k];
+                }
+                if (there && b.sum[S_SCALE])
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) sum[S_SCALE][i][k] = fmaf(pd[k], gate[i][k], sum[S_SCALE][i][k]);
+                if (there && b.sum[S_POST_W])
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) sum[S_POST_W][i][k] = fmaf(bar[k], zh[i][k], sum[S_POST_W][i][k]);
+                if (there && b.sum[S_POST_B])
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) sum[S_POST_B][i][k] += bar[k];
+                if (a.gate_kind != MLIP_RESIDUAL_GATE_NONE) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        pd[k] *= held.scale[k] * a.factor;
+                        gate_sum += pd[k];
+                    }
+                    if (there && b.sum[S_GATE])
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) sum[S_GATE][i][k] += pd[k];
+                    done.gate[i] = narrow<E>(pd);
+                }
+#pragma unroll
+                for (int k = 0; k < 4; ++k) dy[i][k] = a.post ? bar[k] * held.post_w[k] : bar[k];
+            }
+            if (gate_row && b.dgate) {
+                gate_sum = row_sum<S>(gate_sum, ex);
+                if (there && S::lane() == 0) static_cast<E *>(b.dgate)[row * b.dgate_rs] = to_elem<E>(gate_sum);
+            }
+            if (a.post && b.dz) normalise_back<S>(dy, zh, rz, a, inv, ragged, ex);
+#pragma unroll
+            for (int i = 0; i < N; ++i) done.second[i] = narrow<E>(dy[i]);
         }
     }
+    store();
     if constexpr (BACK) {
 #pragma unroll
         for (int s = 0; s < kSums; ++s) {
             if (!b.sum[s]) continue;
             const bool f32 = b.part || (a.params_f32 && s != S_GATE);
             void *to = b.part ? static_cast<void *>(b.part + ((int64_t)blockIdx.x * kSums + s) * a.width) : b.sum[s];
-            if constexpr (S::kRows == 1) {
+            if constexpr (S::kWide) {
 #pragma unroll
-                for (int i = 0; i < S::N; ++i) {
-                    if (f32) store8<float>(sum[s][i], to, 0, col(i), a.width);
-                    else store8<E>(sum[s][i], to, 0, col(i), a.width);
+                for (int i = 0; i < N; ++i) {
+                    if (f32) store4<float>(narrow<float>(sum[s][i]), to, 0, col(i), a.width);
+                    else store4<E>(narrow<E>(sum[s][i]), to, 0, col(i), a.width);
                 }
             } else {
-                constexpr int in_wave = S::G < 64 ? S::G : 64, step = S::G > 64 ? S::G / 64 : 1;
 #pragma unroll
-                for (int i = 0; i < S::N; ++i)
+                for (int k = 0; k < 4; ++k) {
+                    float v = sum[s][0][k];
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        float v = sum[s][i][k];
-#pragma unroll
-                        for (int d = in_wave; d < 64; d <<= 1) v += __shfl_xor(v, d);
-                        if ((int)(threadIdx.x & 63) < in_wave) sums[threadIdx.x >> 6][col(i) + k] = v;
-                    }
+                    for (int d = S::G; d < 64; d <<= 1) v += __shfl_xor(v, d);
+                    if ((int)(threadIdx.x & 63) < S::G) sums[threadIdx.x >> 6][c0 + k] = v;
+                }
                 __syncthreads();
-                for (int c = threadIdx.x; c < a.width; c += S::kBlock) {
+                for (int c = threadIdx.x; c < a.width; c += kThreads) {
                     float v = 0.f;
-                    for (int w = S::G > 64 ? c / 8 % S::G / 64 : 0; w < S::kWaves; w += step) v += sums[w][c];
+                    for (int w = 0; w < kThreads / 64; ++w) v += sums[w][c];
                     if (f32) static_cast<float *>(to)[c] = v;
                     else static_cast<E *>(to)[c] = to_elem<E>(v);
                 }
@@ -328,29 +509,26 @@ template <class E> __global__ __launch_bounds__(kThreads) void k_residual_join(B
     else static_cast<E *>(b.sum[s])[c] = to_elem<E>(sum);
 }
 
+// f(Shape{}, threads of a block)
 template <class Fn> void with_shape(int64_t width, Fn &&f)
 {
-    if (width <= 8) f(Shape<1, 1>{});
-    else if (width <= 16) f(Shape<2, 1>{});
-    else if (width <= 32) f(Shape<4, 1>{});
-    else if (width <= 64) f(Shape<8, 1>{});
-    else if (width <= 128) f(Shape<16, 1>{});
-    else if (width <= 256) f(Shape<32, 1>{});
-    else if (width <= 512) f(Shape<64, 1>{});
-    else if (width <= 1024) f(Shape<128, 1>{});
-    else if (width <= 2048) f(Shape<256, 1>{});
-    else if (width <= 4096) f(Shape<256, 2>{});
-    else f(Shape<512, 2>{});
+    if (width <= 8) f(Shape<2, 1>{}, kThreads);
+    else if (width <= 16) f(Shape<4, 1>{}, kThreads);
+    else if (width <= 32) f(Shape<8, 1>{}, kThreads);
+    else if (width <= 64) f(Shape<16, 1>{}, kThreads);
+    else if (width <= 128) f(Shape<32, 1>{}, kThreads);
+    else if (width <= 256) f(Shape<64, 1>{}, kThreads);
+    else if (width <= 4096) f(Shape<0, 1>{}, (int)(width + 255) / 256 * 64);   // wavefronts of 256 columns, or of 512
+    else f(Shape<0, 2>{}, (int)(width + 511) / 512 * 64);
 }
 
-// Blocks of the gradient: a block's sums take as much as a few dozen rows
+// Blocks of the gradient: a block's sums take as much as a few rows
 int64_t back_blocks(int64_t n, int64_t width)
 {
     int64_t blocks = 0;
-    with_shape(width, [&](auto s) {
-        using S = decltype(s);
-        const int64_t rounds = (n + S::kRows - 1) / S::kRows;
-        const int64_t most = 1024;
+    with_shape(width, [&](auto s, int threads) {
+        const int64_t rounds = (n + decltype(s)::kRows - 1) / decltype(s)::kRows;
+        const int64_t most = 256 * (1024 / threads);   // sixteen wavefronts to a compute unit
         blocks = (rounds + 3) / 4;
         if (blocks > most) blocks = most;
     });
@@ -359,13 +537,15 @@ int64_t back_blocks(int64_t n, int64_t width)
 
 template <bool BACK> int run(const ResidualArgs &a, const Back &b0, int64_t blocks)
 {
+    auto along = [](const Input &m) { return !m.p || m.cs == 1; };
+    const bool plain = a.width >= 4 && a.x_cs == 1 && (!a.z || a.z_cs == 1) && (a.gate_kind != MLIP_RESIDUAL_GATE_FULL || a.gate_cs == 1) && along(b0.dy) && along(b0.dn);
     Args d{{a.x, a.x_rs, a.x_cs}, {a.z, a.z_rs, a.z_cs}, {a.gate, a.gate_rs, a.gate_cs}, a.scale, a.post_w, a.post_b, a.pre_w, a.pre_b, a.y, a.norm, a.y_rs, a.norm_rs, a.n,
            (int32_t)a.width, a.gate_kind, a.param_dtype == MLIP_DTYPE_F32, a.kind == MLIP_NORM_LAYER, a.post, a.pre, a.eps, a.factor};
     with_elem(a.dtype, [&](auto e) {
         using E = decltype(e);
-        with_shape(a.width, [&](auto s) {
+        with_shape(a.width, [&](auto s, int threads) {
             using S = decltype(s);
-            k_residual<E, S, BACK><<<(unsigned)blocks, S::kBlock, 0, a.stream>>>(d, b0);
+            (plain ? k_residual<E, S, BACK, true> : k_residual<E, S, BACK, false>)<<<(unsigned)blocks, threads, 0, a.stream>>>(d, b0);
         });
         if (BACK && b0.part)
             k_residual_join<E><<<dim3((unsigned)((a.width + 31) / 32), kSums), kThreads, 0, a.stream>>>(b0, (int32_t)blocks, (int32_t)a.width, d.params_f32);
@@ -386,7 +566,7 @@ int residual_impl(const ResidualArgs &a)
 {
     if (a.n == 0) return MLIP_OK;
     int64_t blocks = 0;
-    with_shape(a.width, [&](auto s) { blocks = (a.n + decltype(s)::kRows - 1) / decltype(s)::kRows; });
+    with_shape(a.width, [&](auto s, int) { blocks = (a.n + decltype(s)::kRows - 1) / decltype(s)::kRows; });
     const int64_t most = 2048;
     return run<false>(a, Back{}, blocks < most ? blocks : most);
 }
