@@ -189,6 +189,169 @@ template <class K, class B, bool BACK> __global__ __launch_bounds__(B::kThreads)
     if constexpr (B::kPer == 128) finish(&acc[2], n0 + B::first(wave) + 64);
 }
 
+// Rows of up to 128 features, one after another in x and in the gradient: a block keeps the weights of PAIRS times 32 + 32 columns in LDS, in the order in which the lanes take them, and its
+// wavefronts go over the rows, 32 at a time and without a barrier, each with its rows in registers (fp32 split there).  Such calls are bound by memory: rows come and go
+// once for each such group of columns (from the L2 for all but the first), and nothing is laid out before.
+template <class K, int STEPS> struct NarrowShape {
+    static constexpr int kDp = STEPS * 16, kPairs = (K::kParts == 1 ? 256 : 128) / kDp, kFrags = kPairs * 2 * STEPS * K::kParts;   // 32 or 48 KB of weights
+    static constexpr int kStage = 32 * 72;   // elements of 16 bits for a wavefront's results on their way out: 32 rows of 64 and 8 (or of 32 and 4 fp32)
+};
+template <class K> struct NarrowArgs {
+    GateArgs<K> a;           // (x: rows of the chunk as the caller has them)
+    int64_t groups, tiles;   // groups of columns; runs of 32 rows
+    int32_t blocks;          // of a group
+};
+
+template <class K, int STEPS, bool BACK> __global__ __launch_bounds__(256, K::kParts == 1 && !BACK ? 3 : 2) void k_gates_narrow(NarrowArgs<K> na)
+{
+    using T = typename K::T;
+    using E = typename K::E;
+    using S = NarrowShape<K, STEPS>;
+    constexpr int PARTS = K::kParts;
+    __shared__ alignas(16) T weights[S::kFrags * 512];
+    __shared__ alignas(16) T stage_[4 * S::kStage];
+    __shared__ alignas(16) float bias[2][S::kPairs * 32];
+    const GateArgs<K> &a = na.a;
+    const int64_t at = xcd_order(blockIdx.x, gridDim.x);
+    const int64_t group = at % na.groups, col_first = group * S::kPairs * 64;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, half = lane >> 5, d = (int)a.x.cols;
+    const T *across = static_cast<const T *>(a.w.p);
+    for (int k = threadIdx.x; k < S::kFrags * 64; k += 256) {
+        const int l = k & 63, f = k >> 6, p = f % PARTS, kk = f / PARTS % STEPS, c = f / PARTS / STEPS;
+        const int64_t col = col_first + c * 32 + (l & 31);
+        Half8<T> w = {};
+        if (col < a.w.rows && kk * 16 < a.w.cols) w = *reinterpret_cast<const Half8<T> *>(across + p * a.w.part + col * a.w.ld + kk * 16 + (l >> 5) * 8);
+        *reinterpret_cast<Half8<T> *>(weights + k * 8) = w;
+    }
+    for (int k = threadIdx.x; k < S::kPairs * 32; k += 256) {
+        const int64_t f = col_first / 2 + k;
+        bias[0][k] = a.bg && f < a.f ? (float)a.bg[f] : 0.f;
+        bias[1][k] = a.bv && f < a.f ? (float)a.bv[f] : 0.f;
+    }
+    __syncthreads();
+    T *stage = stage_ + wave * S::kStage;
+    const E *x = static_cast<const E *>(a.x.p);
+    auto fence = [] {
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    };
+    for (int64_t tile = at / na.groups * 4 + wave; tile < na.tiles; tile += (int64_t)na.blocks * 4) {
+        const int64_t row0 = tile * 32, mine = row0 + (lane & 31), row = mine < a.x.rows ? mine : a.x.rows - 1;
+        Half8<T> fx[STEPS][PARTS];
+#pragma unroll
+        for (int kk = 0; kk < STEPS; ++kk) {
+            if constexpr (PARTS == 1) {
+                const int c = kk * 16 + half * 8;
+                const E *p = x + row * a.x.ld;
+                if (c + 8 <= d) fx[kk][0] = *reinterpret_cast<const Far<E, 8> *>(p + c);
+                else
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) fx[kk][0][k] = c + k < d ? p[c + k] : (E)0.f;
+            } else {
+                float v[8];
+                load_cols(v, x + row * a.x.ld, 1, kk * 16 + half * 8, d);
+                split_cols<T>(v, fx[kk]);
+            }
+        }
+#pragma unroll 1
+        for (int pair = 0; pair < S::kPairs; ++pair) {
+            const int64_t col0 = col_first + pair * 64, f0 = col0 / 2;
+            if (col0 >= a.w.rows) break;
+            float bar[4][4];
+            if constexpr (BACK)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) load_cols(bar[q], a.bar + row * a.bar_rs, 1, f0 + acc_row(4 * q), a.f);
+            f32x16 g = {}, v = {};
+#pragma unroll
+            for (int kk = 0; kk < STEPS; ++kk) {
+                Half8<T> wg[PARTS], wv[PARTS];
+#pragma unroll
+                for (int p = 0; p < PARTS; ++p) {
+                    wg[p] = *reinterpret_cast<const Half8<T> *>(weights + (((pair * 2 * STEPS + kk) * PARTS + p) * 64 + lane) * 8);
+                    wv[p] = *reinterpret_cast<const Half8<T> *>(weights + ((((pair * 2 + 1) * STEPS + kk) * PARTS + p) * 64 + lane) * 8);
+                }
+                for_products<PARTS>([&](int p, int q) {
+                    g = mfma<T>(wg[p], fx[kk][q], g);
+                    v = mfma<T>(wv[p], fx[kk][q], v);
+                });
+                if (kk % 2) __builtin_amdgcn_sched_barrier(0);   // (else all fragments are fetched at once, into registers that there are not)
+            }
+            // bias, phi: registers 4 q + t have feature f0 + acc_row(4 q) + t of the lane's row
+            with_act(a.act, [&](auto act) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int64_t f = f0 + acc_row(4 * q);
+                    const int c = pair * 32 + acc_row(4 * q);
+                    const Cols<float, 4> bg = *reinterpret_cast<const Cols<float, 4> *>(bias[0] + c), bv = *reinterpret_cast<const Cols<float, 4> *>(bias[1] + c);
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) {
+                        const Phi y = phi<decltype(act)::value>(g[4 * q + t] + bg[t], v[4 * q + t] + bv[t]);
+                        if constexpr (!BACK) g[4 * q + t] = y.h;
+                        else {
+                            g[4 * q + t] = f + t < a.f ? bar[q][t] * y.g : 0.f;
+                            v[4 * q + t] = f + t < a.f ? bar[q][t] * y.v : 0.f;
+                        }
+                    }
+                }
+            });
+            if constexpr (!BACK) {
+                constexpr int W = K::kWide, lanes = 32 / W, ld = 32 + W;   // of a row in the stage
+                E *st = reinterpret_cast<E *>(stage);
+                fence();
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    Cols<E, 4> h;
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) h[t] = to_elem<E>(g[4 * q + t]);
+                    *reinterpret_cast<Cols<E, 4> *>(st + (lane & 31) * ld + acc_row(4 * q)) = h;
+                }
+                fence();
+#pragma unroll
+                for (int k = 0; k < lanes / 2; ++k) {
+                    const int r = lane / lanes + 64 / lanes * k, c = lane % lanes * W;
+                    if (row0 + r >= a.x.rows) continue;
+                    const Cols<E, W> h = *reinterpret_cast<const Cols<E, W> *>(st + r * ld + c);
+                    E *to = a.out + (row0 + r) * a.out_rs + f0;
+                    if (f0 + c + W <= a.f) *reinterpret_cast<Far<E, W> *>(to + c) = h;
+                    else
+#pragma unroll
+                        for (int t = 0; t < W; ++t)
+                            if (f0 + c + t < a.f) to[c + t] = h[t];
+                }
+            } else {
+#pragma unroll
+                for (int p = 0; p < PARTS; ++p) {
+                    fence();
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        Half4<T> gp, vp;
+#pragma unroll
+                        for (int t = 0; t < 4; ++t) {
+                            gp[t] = to_elem<T>(g[4 * q + t]);
+                            vp[t] = to_elem<T>(v[4 * q + t]);
+                            if (p + 1 < PARTS) {
+                                g[4 * q + t] -= (float)gp[t];
+                                v[4 * q + t] -= (float)vp[t];
+                            }
+                        }
+                        *reinterpret_cast<Half4<T> *>(stage + (lane & 31) * 72 + acc_row(4 * q)) = gp;
+                        *reinterpret_cast<Half4<T> *>(stage + (lane & 31) * 72 + 32 + acc_row(4 * q)) = vp;
+                    }
+                    fence();
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const int r = lane / 8 + 8 * k, c = lane % 8 * 8;
+                        if (row0 + r < a.x.rows)
+                            *reinterpret_cast<Half8<T> *>(a.gv + p * a.gv_part + (row0 + r) * a.gv_ld + col0 + c) = *reinterpret_cast<const Half8<T> *>(stage + r * 72 + c);
+                    }
+                }
+            }
+        }
+    }
+}
+
 // dx = [G V] [Wg Wv]^T
 template <class K> struct RowBarArgs {
     Panel gv, w;             // [rows][2 f], [d][2 f]
@@ -290,37 +453,35 @@ template <class K> struct JoinArgs {
 };
 template <class K> __global__ __launch_bounds__(kPackThreads) void k_join(JoinArgs<K> a)
 {
-    __shared__ float tile[32][33];
-    const int64_t c0 = (int64_t)blockIdx.x * 32, d0 = (int64_t)blockIdx.y * 32, f0 = feature_of(c0);
+    __shared__ float tile[8][33];
+    const int64_t c0 = (int64_t)blockIdx.x * 8, d0 = (int64_t)blockIdx.y * 32, f0 = feature_of(c0);
     const bool value = is_value(c0);
     typename K::E *dw = value ? a.dwv : a.dwg, *db = value ? a.dbv : a.dbg;
     const int64_t rs = value ? a.v_rs : a.g_rs, cs = value ? a.v_cs : a.g_cs;
     const int p = threadIdx.x & 31, q = threadIdx.x >> 5;
     if (dw) {
-        for (int i = q; i < 32; i += 8) {
-            float sum = 0.f;
-            if (d0 + p < a.d)
-                in_steps<4>(0, a.splits, 1, [&](int64_t s) { return a.part[(s * a.f2 + c0 + i) * a.d + d0 + p]; }, [&](float x) { sum += x; });
-            tile[i][p] = sum;   // [feature][d]
-        }
+        float sum = 0.f;
+        if (d0 + p < a.d)
+            in_steps<8>(0, a.splits, 1, [&](int64_t s) { return a.part[(s * a.f2 + c0 + q) * a.d + d0 + p]; }, [&](float x) { sum += x; });
+        tile[q][p] = sum;   // [feature][d]
         __syncthreads();
         const bool by_row = cs <= rs;
-        for (int i = q; i < 32; i += 8) {
-            const int dd = by_row ? i : p, ff = by_row ? p : i;
-            if (d0 + dd < a.d && f0 + ff < a.f) dw[(d0 + dd) * rs + (f0 + ff) * cs] = to_elem<typename K::E>(tile[ff][dd]);
-        }
+        const int dd = by_row ? (int)threadIdx.x >> 3 : p, ff = by_row ? (int)threadIdx.x & 7 : q;
+        if (d0 + dd < a.d && f0 + ff < a.f) dw[(d0 + dd) * rs + (f0 + ff) * cs] = to_elem<typename K::E>(tile[ff][dd]);
     }
-    if (db && d0 == 0 && q == 0 && f0 + p < a.f) {
+    if (db && d0 == 0 && threadIdx.x < 8 && f0 + threadIdx.x < a.f) {
         float sum = 0.f;
-        for (int64_t s = 0; s < a.splits; ++s) sum += a.bias[s * a.f2 + c0 + p];
-        db[f0 + p] = to_elem<typename K::E>(sum);
+        in_steps<8>(0, a.splits, 1, [&](int64_t s) { return a.bias[s * a.f2 + c0 + threadIdx.x]; }, [&](float x) { sum += x; });
+        db[f0 + threadIdx.x] = to_elem<typename K::E>(sum);
     }
 }
 
 // ---------------------------------------------------------------- a call's sizes and scratch memory
 
-constexpr int64_t kChunkBytes = 1024 << 20;     // of x's parts, G and V of a chunk
+constexpr int64_t kChunkBytes = (int64_t)4 << 30;     // of x's parts, G and V of a chunk
 constexpr int64_t kMostTiles = 1 << 23;       // blocks of a launch
+constexpr int64_t kNarrow = 128;              // d up to which rows stay in registers
+constexpr int64_t kNarrowBlocks = 1024;       // blocks of such a launch
 
 struct Plan {
     int parts;
@@ -370,7 +531,7 @@ Plan plan_of(const GatedArgs &a, bool grad)
         p.gv = take(p.chunk * p.gv_ld * p.parts * 2);
         const int64_t tiles = p.parts == 1 && a.d >= 512 && p.f2 >= 512 ? (p.f2 + 255) / 256 * ((a.d + 255) / 256) : a.d <= 64 ? (p.f2 + 255) / 256 : (p.f2 + 127) / 128 * ((a.d + 127) / 128);
         const int64_t blocks = p.parts == 1 && a.d >= 512 && p.f2 >= 512 ? 256 : 512;   // one or two to a compute unit
-        int64_t splits = blocks / tiles, most_splits = (p.chunk + 511) / 512;
+        int64_t splits = blocks / tiles, most_splits = (p.chunk + 127) / 128;
         if (splits > most_splits) splits = most_splits;
         if (splits < 1) splits = 1;
         p.run = pad_to((p.chunk + splits - 1) / splits, 64);
@@ -390,6 +551,7 @@ template <class K> int launch(const GatedArgs &a, const GatedGrad *g)
     char *ws = static_cast<char *>(a.workspace);
     T *across = reinterpret_cast<T *>(ws + p.across), *down = g ? reinterpret_cast<T *>(ws + p.down) : nullptr, *xs = reinterpret_cast<T *>(ws + p.xs);
     T *gv = g ? reinterpret_cast<T *>(ws + p.gv) : nullptr;
+    const bool in_registers = a.d <= kNarrow && a.x_cs == 1 && (!g || g->bar_cs == 1);
     const bool rows = !g || g->dx, weights = g && (g->dwg || g->dwv || g->dbg || g->dbv);
     const Weights<K> w = {static_cast<const E *>(a.wg), static_cast<const E *>(a.wv), a.wg_rs, a.wg_cs, a.wv_rs, a.wv_cs, a.d, a.f, p.d_ld, p.gv_ld,
                           across, rows ? down : nullptr, p.f2 * p.d_ld, a.d * p.gv_ld};
@@ -401,7 +563,7 @@ template <class K> int launch(const GatedArgs &a, const GatedGrad *g)
         if (n <= 0 && a.n > 0) break;
         const E *x = static_cast<const E *>(a.x) + first * a.x_rs;
         Panel xp = {x, a.x_rs, 0, n, a.d};
-        if (p.pack_x && n > 0) {
+        if (p.pack_x && n > 0 && (weights || !in_registers)) {
             const int64_t threads = n * (p.d_p / 8);
             k_pack_rows<K><<<(unsigned)((threads + kPackThreads - 1) / kPackThreads), kPackThreads, 0, a.stream>>>(x, a.x_rs, a.x_cs, n, a.d, p.d_p, xs, p.d_ld, p.chunk * p.d_ld);
             xp = {xs, p.d_ld, p.chunk * p.d_ld, n, p.d_p};
@@ -419,7 +581,17 @@ template <class K> int launch(const GatedArgs &a, const GatedGrad *g)
                 ga.gv_ld = p.gv_ld;
                 ga.gv_part = p.chunk * p.gv_ld;
             }
-            with_tile<K>(p.f2, n, [&](auto block) {
+            auto narrow = [&](auto steps) {
+                constexpr int STEPS = decltype(steps)::value;
+                NarrowArgs<K> na = {ga, (p.f2 + NarrowShape<K, STEPS>::kPairs * 64 - 1) / (NarrowShape<K, STEPS>::kPairs * 64), (n + 31) / 32, 0};
+                na.a.x = {x, a.x_rs, 0, n, a.d};
+                const int64_t most = kNarrowBlocks / na.groups > 0 ? kNarrowBlocks / na.groups : 1, blocks = (na.tiles + 3) / 4;
+                na.blocks = (int32_t)(blocks < most ? blocks : most);
+                (g ? k_gates_narrow<K, STEPS, true> : k_gates_narrow<K, STEPS, false>)<<<(unsigned)(na.blocks * na.groups), 256, 0, a.stream>>>(na);
+            };
+            if (in_registers && a.d <= 64) narrow(std::integral_constant<int, 4>{});
+            else if (in_registers) narrow(std::integral_constant<int, 8>{});
+            else with_tile<K>(p.f2, n, [&](auto block) {
                 using B = decltype(block);
                 ga.n_tiles = (p.f2 + B::kCols - 1) / B::kCols;
                 const unsigned blocks = (unsigned)((n + B::kRows - 1) / B::kRows * ga.n_tiles);
@@ -449,7 +621,7 @@ template <class K> int launch(const GatedArgs &a, const GatedGrad *g)
     if (weights) {
         const JoinArgs<K> ja = {reinterpret_cast<float *>(ws + p.part), reinterpret_cast<float *>(ws + p.bias), p.splits, a.d, a.f, p.f2, static_cast<E *>(g->dwg),
                                 static_cast<E *>(g->dwv), static_cast<E *>(g->dbg), static_cast<E *>(g->dbv), g->dwg_rs, g->dwg_cs, g->dwv_rs, g->dwv_cs};
-        k_join<K><<<dim3((unsigned)(p.f2 / 32), (unsigned)((a.d + 31) / 32)), kPackThreads, 0, a.stream>>>(ja);
+        k_join<K><<<dim3((unsigned)(p.f2 / 8), (unsigned)((a.d + 31) / 32)), kPackThreads, 0, a.stream>>>(ja);
     }
     MLIP_HIP(hipGetLastError());
     return MLIP_OK;

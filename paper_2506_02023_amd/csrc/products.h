@@ -50,8 +50,9 @@ template <class T, int PARTS> __device__ inline void split(float v, T (&part)[PA
 }
 #endif
 
-// Elements of K that one step takes: 64 of one part, 32 of several (LDS)
-template <int PARTS, int LEAST> constexpr int kStepK = PARTS == 1 ? 64 : 32;
+// Elements of K that one step takes: 64 of one part, 32 of several (LDS), 16 of several where both panels have K in their rows, so that two blocks share a compute
+// unit (202,612 rows of 128 x 704 of three parts: 507 us in steps of 32, 312 here; panels with K in their columns would be read in quarters of lines)
+template <int PARTS, bool KC, int LEAST> constexpr int kStepK = PARTS == 1 ? 64 : KC || LEAST < 128 ? 32 : 16;
 // Columns that a panel with K in its columns is filled up to: a multiple of both
 constexpr int64_t kPadK = 64;
 inline int64_t pad_to(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
@@ -118,11 +119,12 @@ template <int PARTS, class Fn> __device__ inline void for_products(Fn &&f)
 // acc[i][j] += rows 32 i .. of A times rows 32 j .. of B, of a wavefront's WM x WN part of the block's BM x BN tile, summed over k in [k0, k1).
 // each(fragments of B): called in every step, for sums along K.
 template <class T, int PARTS, bool AKC, bool BKC, int BM, int BN, int WM, int WN> struct Product {
-    static constexpr int kWaves = (BM / WM) * (BN / WN), kThreads = kWaves * 64, KT = kStepK<PARTS, (BM < BN ? BM : BN)>;
+    static constexpr int kWaves = (BM / WM) * (BN / WN), kThreads = kWaves * 64, KT = kStepK<PARTS, AKC || BKC, (BM < BN ? BM : BN)>;
     using TA = Tile<T, PARTS, AKC, BM, KT, kThreads>;
     using TB = Tile<T, PARTS, BKC, BN, KT, kThreads>;
     static constexpr int kStage = TA::kElems + TB::kElems;
-    struct alignas(16) Lds { T e[2 * kStage]; };
+    static constexpr int kTurned = kWaves * 64 * 64 * 2;   // what Turned takes of it afterwards
+    struct alignas(16) Lds { T e[2 * kStage > kTurned ? 2 * kStage : kTurned]; };
 
     template <class Each>
     static __device__ inline void run(const Panel &a, const Panel &b, int64_t m0, int64_t n0, int64_t k0, int64_t k1, Lds &lds, f32x16 (&acc)[WM / 32][WN / 32],
