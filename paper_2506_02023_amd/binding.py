@@ -786,35 +786,46 @@ def mlip_gated_grad(grad, x, w_gate, w_value, b_gate=None, b_value=None, act="si
 
 def _residual_call(x, z, gate, scale, post, pre, kind, eps, factor):
     """(the call's structure, its tensors)"""
-    if x.dim() != 2 or x.dtype not in _DTYPES:
+    dtype = _DTYPES.get(x.dtype)
+    if dtype is None or x.dim() != 2:
         _refuse("x must be a matrix of float32, bfloat16 or float16")
     if kind not in _KINDS:
         _refuse(f"kind must be one of {', '.join(_KINDS)}")
-    n, width = x.shape
-    z_rs, z_cs = _rows_of(z, "z", (n, width), x.dtype) if z is not None else (0, 0)
-    gate_kind, g_rs, g_cs = 0, 0, 0
+    shape = n, width = x.shape
+    tensors = [x]
+    z_rs = z_cs = gate_kind = g_rs = g_cs = 0
+    z_at = gate_at = None
+    if z is not None:
+        z_rs, z_cs = _rows_of(z, "z", shape, x.dtype)
+        z_at = z.data_ptr()
+        tensors.append(z)
     if gate is not None:
         if gate.dtype is not x.dtype:
             _refuse("gate must be of the type of x")
-        shape = tuple(gate.shape)
-        if shape == (n, width):
+        if gate.shape == shape:
             gate_kind, g_rs, g_cs = 1, *gate.stride()
-        elif shape == (n, 1):
+        elif gate.shape == (n, 1):
             gate_kind, g_rs = 2, gate.stride(0)
-        elif shape in ((width,), (1, width)) and gate.is_contiguous():
+        elif gate.shape in ((width,), (1, width)) and gate.is_contiguous():
             gate_kind = 3
         else:
             _refuse("gate must have a value for each element, row ([n, 1]) or column (contiguous [width] or [1, width])")
-    params = [scale, *(post or (None, None)), *(pre or (None, None))]
-    there = [p for p in params if p is not None]
-    param_dtype = there[0].dtype if there else x.dtype
-    if param_dtype is not torch.float32 and param_dtype is not x.dtype:
-        _refuse("scale and the norms' parameters must be float32 or of the type of x")
-    for p in there:
-        _vector_of(p, "scale and the norms' parameters", width, param_dtype)
-    call = _Residual(_DTYPES[x.dtype], _DTYPES[param_dtype], _KINDS[kind], gate_kind, post is not None, pre is not None, n, width, eps, factor, x.data_ptr(), *x.stride(),
-                     _address(z), z_rs, z_cs, _address(gate), g_rs, g_cs, *map(_address, params))
-    return call, [t for t in (x, z, gate, *there) if t is not None]
+        gate_at = gate.data_ptr()
+        tensors.append(gate)
+    param_dtype, at = None, []
+    for p in (scale, *(post or (None, None)), *(pre or (None, None))):
+        if p is None:
+            at.append(None)
+            continue
+        if param_dtype is None:
+            param_dtype = p.dtype
+            if param_dtype is not torch.float32 and param_dtype is not x.dtype:
+                _refuse("scale and the norms' parameters must be float32 or of the type of x")
+        at.append(_vector_of(p, "scale and the norms' parameters", width, param_dtype).data_ptr())
+        tensors.append(p)
+    call = _Residual(dtype, dtype if param_dtype is None else _DTYPES[param_dtype], _KINDS[kind], gate_kind, post is not None, pre is not None, n, width, eps, factor,
+                     x.data_ptr(), *x.stride(), z_at, z_rs, z_cs, gate_at, g_rs, g_cs, *at)
+    return call, tensors
 
 
 def _residual_forward(x, z, gate, scale, post, pre, kind, eps, factor):
@@ -829,14 +840,23 @@ def _residual_forward(x, z, gate, scale, post, pre, kind, eps, factor):
 def _residual_backward(dy, dn, x, z, gate, scale, post, pre, kind, eps, factor, needs):
     """Gradients of (x, z, gate, scale, post_w, post_b, pre_w, pre_b) where `needs` says so, else None"""
     call, tensors = _residual_call(x, z, gate, scale, post, pre, kind, eps, factor)
-    bars = [(*_rows_of(t, what, x.shape, x.dtype), t) if t is not None else (0, 0, None) for t, what in ((dy, "dy"), (dn, "dn"))]
-    stream = _stream_of(*[b[2] for b in bars if b[2] is not None], *tensors)
-    params = (scale, *(post or (None, None)), *(pre or (None, None)))
-    outs = [t.new_empty(t.shape) if need and t is not None else None for t, need in zip((x, z, gate, *params), needs)]
-    gate_rs = outs[2].stride(0) if outs[2] is not None else 0
-    g = _ResidualGrad(_address(dy), *bars[0][:2], _address(dn), *bars[1][:2], _address(outs[0]), call.width, _address(outs[1]), call.width, _address(outs[2]), gate_rs,
-                      *map(_address, outs[3:]))
-    need = lib().mlip_residual_grad_workspace(call.n, call.width)
+    dy_rs = dy_cs = dn_rs = dn_cs = 0
+    dy_at = dn_at = None
+    if dy is not None:
+        dy_rs, dy_cs = _rows_of(dy, "dy", x.shape, x.dtype)
+        dy_at = dy.data_ptr()
+        tensors.append(dy)
+    if dn is not None:
+        dn_rs, dn_cs = _rows_of(dn, "dn", x.shape, x.dtype)
+        dn_at = dn.data_ptr()
+        tensors.append(dn)
+    stream = _stream_of(*tensors)
+    inputs = (x, z, gate, scale, *(post or (None, None)), *(pre or (None, None)))
+    outs = [t.new_empty(t.shape) if need and t is not None else None for t, need in zip(inputs, needs)]
+    dx, dz, dgate, *rest = [None if t is None else t.data_ptr() for t in outs]
+    width = call.width
+    g = _ResidualGrad(dy_at, dy_rs, dy_cs, dn_at, dn_rs, dn_cs, dx, width, dz, width, dgate, outs[2].stride(0) if dgate is not None else 0, *rest)
+    need = lib().mlip_residual_grad_workspace(call.n, width)
     ws, at = _scratch(need)
     _check(lib().mlip_residual_grad(call, g, at, need, stream))
     return outs

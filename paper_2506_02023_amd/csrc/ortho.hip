@@ -350,7 +350,7 @@ __device__ inline Half8<P> across(const P *p, int ld, int col, int k)
 template <int ELEMS> __global__ __launch_bounds__(kSmallThreads) void k_small(List l, double eps, int steps, float a, float b, float c, float scale)
 {
     __shared__ alignas(16) P lds[ELEMS];
-    __shared__ float diag[2][128];
+    __shared__ alignas(16) float diag[2][128];
     __shared__ double red[kSmallWaves];
     const Item &it = l.item[blockIdx.x];
     const int m = it.m, n = it.n, mp = (m + 31) / 32 * 32, np = (n + 31) / 32 * 32, xs = np + 8, as = mp + 8, mb = mp / 32, nb = np / 32;
@@ -392,6 +392,7 @@ template <int ELEMS> __global__ __launch_bounds__(kSmallThreads) void k_small(Li
             const int sq = wave + s * kSmallWaves, i0 = sq / mb * 32, j0 = sq % mb * 32;
             if (sq >= mb * mb) break;
             f32x16 acc = {};
+#pragma unroll 4
             for (int k = 0; k < np; k += 16) {
                 const Half8<P> u0 = along(x[0], xs, i0, k), u1 = along(x[1], xs, i0, k), v0 = along(x[0], xs, j0, k), v1 = along(x[1], xs, j0, k);
                 acc = mfma<P>(u1, v0, acc);
@@ -422,6 +423,7 @@ template <int ELEMS> __global__ __launch_bounds__(kSmallThreads) void k_small(Li
         for (int s = 0; s < 2; ++s) {   // B
             const int sq = wave + s * kSmallWaves, i0 = sq / mb * 32, j0 = sq % mb * 32;
             if (sq >= mb * mb) break;
+#pragma unroll 2
             for (int k = 0; k < mp; k += 16) {
                 const Half8<P> u0 = along(q[0], as, i0, k), u1 = along(q[1], as, i0, k), v0 = along(q[0], as, j0, k), v1 = along(q[1], as, j0, k);
                 poly[s] = mfma<P>(u1, v0, poly[s]);
@@ -431,14 +433,19 @@ template <int ELEMS> __global__ __launch_bounds__(kSmallThreads) void k_small(Li
             const int row = j0 + acc_col();
             const float dr = diag[0][row];
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int col = i0 + acc_row(r);
-                float y = fmaf(fmaf(c, dr + diag[0][col], b), both(q[0][row * as + col], q[1][row * as + col]), poly[s][r] * (c / kGramScale));
-                if (col == row) {
-                    diag[1][row] = fmaf(dr, fmaf(c, dr, b), y * (1.f / kGramScale));
-                    y = 0.f;
+            for (int g = 0; g < 4; ++g) {
+                const int col = i0 + acc_row(4 * g);
+                const Half4<P> gh = *reinterpret_cast<const Half4<P> *>(q[0] + row * as + col), gl = *reinterpret_cast<const Half4<P> *>(q[1] + row * as + col);
+                const Cols<float, 4> dc = *reinterpret_cast<const Cols<float, 4> *>(diag[0] + col);
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    float y = fmaf(fmaf(c, dr + dc[t], b), both(gh[t], gl[t]), poly[s][4 * g + t] * (c / kGramScale));
+                    if (col + t == row) {
+                        diag[1][row] = fmaf(dr, fmaf(c, dr, b), y * (1.f / kGramScale));
+                        y = 0.f;
+                    }
+                    poly[s][4 * g + t] = y;
                 }
-                poly[s][r] = y;
             }
         }
         __syncthreads();
@@ -461,6 +468,7 @@ template <int ELEMS> __global__ __launch_bounds__(kSmallThreads) void k_small(Li
         for (int s = 0; s < 4; ++s) {   // X: columns i0, rows j0
             const int sq = wave + s * kSmallWaves, i0 = sq / mb * 32, j0 = sq % mb * 32;
             if (sq >= mb * nb) break;
+#pragma unroll 2
             for (int k = 0; k < mp; k += 16) {
                 const Half8<P> u0 = across(x[0], xs, i0, k), u1 = across(x[1], xs, i0, k), v0 = along(q[0], as, j0, k), v1 = along(q[1], as, j0, k);
                 next[s] = mfma<P>(u1, v0, next[s]);
@@ -470,9 +478,11 @@ template <int ELEMS> __global__ __launch_bounds__(kSmallThreads) void k_small(Li
             const int row = j0 + acc_col();
             const float f = a + diag[1][row];
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int at = row * xs + i0 + acc_row(r);
-                next[s][r] = fmaf(f, both(x[0][at], x[1][at]), next[s][r] * (1.f / kGramScale));
+            for (int g = 0; g < 4; ++g) {
+                const int at = row * xs + i0 + acc_row(4 * g);
+                const Half4<P> hi = *reinterpret_cast<const Half4<P> *>(x[0] + at), lo = *reinterpret_cast<const Half4<P> *>(x[1] + at);
+#pragma unroll
+                for (int t = 0; t < 4; ++t) next[s][4 * g + t] = fmaf(f, both(hi[t], lo[t]), next[s][4 * g + t] * (1.f / kGramScale));
             }
         }
         __syncthreads();

@@ -529,7 +529,7 @@ int64_t back_blocks(int64_t n, int64_t width)
     with_shape(width, [&](auto s, int threads) {
         const int64_t rounds = (n + decltype(s)::kRows - 1) / decltype(s)::kRows;
         const int64_t most = 256 * (1024 / threads);   // sixteen wavefronts to a compute unit
-        blocks = (rounds + 3) / 4;
+        blocks = rounds <= 8 ? 1 : (rounds + 3) / 4;   // (one block needs no second launch)
         if (blocks > most) blocks = most;
     });
     return blocks < 1 ? 1 : blocks;
