@@ -202,8 +202,8 @@ def lib():
         L.mlip_residual.argtypes = [ref(_Residual), vp, i64, vp, i64, vp]
         L.mlip_residual_grad_workspace.argtypes, L.mlip_residual_grad_workspace.restype = [i64, i64], size
         L.mlip_residual_grad.argtypes = [ref(_Residual), ref(_ResidualGrad), vp, size, vp]
-        L.mlip_orthogonalise_workspace.argtypes, L.mlip_orthogonalise_workspace.restype = [ref(_Matrix), i32], size
-        L.mlip_orthogonalise.argtypes = [ref(_Matrix), i32, i32, ref(ctypes.c_double), ctypes.c_double, f32, vp, size, vp]
+        L.mlip_orthogonalise_workspace.argtypes, L.mlip_orthogonalise_workspace.restype = [vp, i32], size
+        L.mlip_orthogonalise.argtypes = [vp, i32, i32, ref(ctypes.c_double), ctypes.c_double, f32, vp, size, vp]
         L.mlip_embed.argtypes = [vp, i32, i64, i64, i64, i64, vp, i32, i64, f32, vp, i32, i64, vp]
         L.mlip_embed_grad_workspace.argtypes = [i64, i64, i64]
         L.mlip_embed_grad_workspace.restype = size
@@ -931,16 +931,6 @@ def mlip_norm_grad(grad, x, weight=None, bias=None, kind="rms", eps=1e-6):
     return d[0], d[6], d[7]
 
 
-def _matrices(tensors, what):
-    """The matrices of an iterable of matrices and stacks of matrices"""
-    out = []
-    for t in tensors:
-        if t.dim() not in (2, 3):
-            _refuse(f"{what} must be matrices, or stacks of matrices")
-        out += [t] if t.dim() == 2 else list(t.unbind(0))
-    return out
-
-
 def mlip_orthogonalise(updates, steps=5, coefficients=(3.4445, -4.7750, 2.0315), eps=1e-7, scale=1.0, out=None):
     """Orthogonalises matrices (gradients or their running means, before an update): X = G / max(|G|, eps), then `steps` times
     X <- (a + b X X^T + c (X X^T)^2) X, of the transpose where a matrix has more rows than columns; times `scale`.
@@ -948,17 +938,27 @@ def mlip_orthogonalise(updates, steps=5, coefficients=(3.4445, -4.7750, 2.0315),
     updates, out: iterables of cuda matrices [rows, cols] or stacks of them [k, rows, cols], float32, bfloat16 or float16, any strides.  In place, or
     into the tensors of `out` (of the same types and shapes).  Not recorded by autograd.  Returns the list of results."""
     updates = _listed(updates)
-    out = updates if out is None else _listed(out)
-    if [(t.dtype, t.shape) for t in updates] != [(t.dtype, t.shape) for t in out]:
+    given, out = out is not None, updates if out is None else _listed(out)
+    if given and [(t.dtype, t.shape) for t in updates] != [(t.dtype, t.shape) for t in out]:
         _refuse("out must have a tensor for each update, of its type and shape")
-    if any(t.dtype not in _DTYPES for t in updates):
+    codes = list(map(_DTYPES.get, map(_dtype_of, updates)))
+    if None in codes:
         _refuse("updates must be float32, bfloat16 or float16")
+    if not {2, 3}.issuperset(map(_Tensor_of.dim, updates)):
+        _refuse("updates must be matrices, or stacks of matrices")
+    if not {torch.cuda.current_device()}.issuperset(map(_Tensor_of.get_device, itertools.chain(updates, out if given else ()))):
+        _refuse("tensors must be on the current GPU")
     a, b, c = coefficients
-    src, dst = _matrices(updates, "updates"), _matrices(out, "out")
-    stream = _stream_of(*src, *dst)
-    list_ = (_Matrix * len(src))(*[_Matrix(s.data_ptr(), d.data_ptr(), *s.shape, *s.stride(), *d.stride(), _DTYPES[s.dtype]) for s, d in zip(src, dst)])
-    need = lib().mlip_orthogonalise_workspace(list_, len(src))
-    ws, at = _scratch(need)
-    _check(lib().mlip_orthogonalise(list_, len(src), steps, (ctypes.c_double * 3)(a, b, c), eps, scale, at, need, stream))
+    words = array.array("q")      # mlip_matrix_t as 64-bit words
+    for src, dst, code in zip(updates, out, codes):
+        if src.dim() == 2:
+            words.extend((src.data_ptr(), dst.data_ptr(), *src.shape, *src.stride(), *dst.stride(), code))
+        else:
+            for s, d in zip(src.unbind(0), dst.unbind(0)):
+                words.extend((s.data_ptr(), d.data_ptr(), *s.shape, *s.stride(), *d.stride(), code))
+    at, count = words.buffer_info()[0], len(words) // 9
+    need = lib().mlip_orthogonalise_workspace(at, count)
+    ws, ws_at = _scratch(need)
+    _check(lib().mlip_orthogonalise(at, count, steps, (ctypes.c_double * 3)(a, b, c), eps, scale, ws_at, need, _stream()))
     _written(out)
     return out

@@ -359,11 +359,11 @@ template <class K> struct RowBarArgs {
     typename K::E *out;
     int64_t out_rs;
 };
-template <class K, class B> __global__ __launch_bounds__(B::kThreads) void k_row_bars(RowBarArgs<K> a)
+template <class K, class B> using RowBars = typename B::template Of<typename K::T, K::kParts, true, true>;   // (d first, rows second)
+template <class K, class B> __device__ inline void row_bars(const RowBarArgs<K> &a, int64_t tile, typename RowBars<K, B>::Lds &lds)
 {
-    using P = typename B::template Of<typename K::T, K::kParts, true, true>;   // (d first, rows second)
-    __shared__ typename P::Lds lds;
-    const int64_t tile = xcd_order(blockIdx.x, gridDim.x), m0 = tile / a.n_tiles * B::kRows, n0 = tile % a.n_tiles * B::kCols;
+    using P = RowBars<K, B>;
+    const int64_t m0 = tile / a.n_tiles * B::kRows, n0 = tile % a.n_tiles * B::kCols;
     f32x16 acc[B::kPer / 32][2] = {};
     P::run(a.w, a.gv, n0, m0, 0, a.gv.cols, lds, acc, NoEach{});
     __syncthreads();
@@ -392,11 +392,11 @@ template <class K> struct WeightSumArgs {
     float *part, *bias;      // [splits][2 f][d], [splits][2 f]
     bool add;
 };
-template <class K, class B> __global__ __launch_bounds__(B::kThreads) void k_weight_sums(WeightSumArgs<K> a)
+template <class K, class B> using WeightSums = typename B::template Of<typename K::T, K::kParts, false, false>;   // (d first, the 2 f columns second)
+template <class K, class B> __device__ inline void weight_sums(const WeightSumArgs<K> &a, int64_t at, typename WeightSums<K, B>::Lds &lds)
 {
-    using P = typename B::template Of<typename K::T, K::kParts, false, false>;   // (d first, the 2 f columns second)
-    __shared__ typename P::Lds lds;
-    const int64_t at = xcd_order(blockIdx.x, gridDim.x), tiles = a.m_tiles * a.n_tiles, s = at / tiles, tile = at % tiles;
+    using P = WeightSums<K, B>;
+    const int64_t tiles = a.m_tiles * a.n_tiles, s = at / tiles, tile = at % tiles;
     const int64_t m0 = tile / a.n_tiles * B::kRows, n0 = tile % a.n_tiles * B::kCols;
     const int64_t k0 = s * a.run, k1 = k0 + a.run < a.gv.rows ? k0 + a.run : a.gv.rows;
     const int wave = threadIdx.x >> 6;
@@ -444,6 +444,28 @@ template <class K, class B> __global__ __launch_bounds__(B::kThreads) void k_wei
     }
 }
 
+template <class K, class B> __global__ __launch_bounds__(B::kThreads) void k_row_bars(RowBarArgs<K> a)
+{
+    __shared__ typename RowBars<K, B>::Lds lds;
+    row_bars<K, B>(a, xcd_order(blockIdx.x, gridDim.x), lds);
+}
+template <class K, class B> __global__ __launch_bounds__(B::kThreads) void k_weight_sums(WeightSumArgs<K> a)
+{
+    __shared__ typename WeightSums<K, B>::Lds lds;
+    weight_sums<K, B>(a, xcd_order(blockIdx.x, gridDim.x), lds);
+}
+// Both at once, where neither fills the chip
+template <class K, class B> __global__ __launch_bounds__(B::kThreads) void k_row_bars_and_weight_sums(RowBarArgs<K> r, WeightSumArgs<K> w, unsigned of_rows)
+{
+    __shared__ union Both {
+        typename RowBars<K, B>::Lds r;
+        typename WeightSums<K, B>::Lds w;
+        __device__ Both() {}
+    } lds;
+    if (blockIdx.x < of_rows) row_bars<K, B>(r, blockIdx.x, lds.r);
+    else weight_sums<K, B>(w, blockIdx.x - of_rows, lds.w);
+}
+
 // The runs' shares added up, in their order
 template <class K> struct JoinArgs {
     const float *part, *bias;
@@ -480,6 +502,7 @@ template <class K> __global__ __launch_bounds__(kPackThreads) void k_join(JoinAr
 
 constexpr int64_t kChunkBytes = (int64_t)4 << 30;     // of x's parts, G and V of a chunk
 constexpr int64_t kMostTiles = 1 << 23;       // blocks of a launch
+constexpr int64_t kFull = 256;                // blocks that leave no compute unit idle
 constexpr int64_t kNarrow = 128;              // d up to which rows stay in registers
 constexpr int64_t kNarrowBlocks = 1024;       // blocks of such a launch
 
@@ -600,20 +623,38 @@ template <class K> int launch(const GatedArgs &a, const GatedGrad *g)
         }
         if (g) {
             const Panel gp = {gv, p.gv_ld, p.chunk * p.gv_ld, n, p.f2};
-            if (g->dx && n > 0)
-                with_tile<K>(a.d, n, [&](auto block) {
+            auto row_args = [&](auto block) {
+                using B = decltype(block);
+                return RowBarArgs<K>{gp, down_panel, (a.d + B::kCols - 1) / B::kCols, static_cast<E *>(g->dx) + first * g->dx_rs, g->dx_rs};
+            };
+            auto row_blocks = [&](auto block) {
+                using B = decltype(block);
+                return (n + B::kRows - 1) / B::kRows * ((a.d + B::kCols - 1) / B::kCols);
+            };
+            auto weight_args = [&](auto block) {
+                using B = decltype(block);
+                return WeightSumArgs<K>{gp, xp, a.d, (p.f2 + B::kRows - 1) / B::kRows, (a.d + B::kCols - 1) / B::kCols, p.run, reinterpret_cast<float *>(ws + p.part),
+                                        g->dbg || g->dbv ? reinterpret_cast<float *>(ws + p.bias) : nullptr, first > 0};
+            };
+            bool together = false;
+            if (g->dx && n > 0 && weights)
+                with_tile<K>(a.d, n < p.f2 ? n : p.f2, [&](auto block) {
                     using B = decltype(block);
-                    const int64_t n_tiles = (a.d + B::kCols - 1) / B::kCols;
-                    const RowBarArgs<K> ra = {gp, down_panel, n_tiles, static_cast<E *>(g->dx) + first * g->dx_rs, g->dx_rs};
-                    k_row_bars<K, B><<<(unsigned)((n + B::kRows - 1) / B::kRows * n_tiles), B::kThreads, 0, a.stream>>>(ra);
+                    const WeightSumArgs<K> wa = weight_args(block);
+                    const int64_t rb = row_blocks(block), wb = wa.m_tiles * wa.n_tiles * p.splits;
+                    together = rb < kFull && wb < kFull && B::kThreads == 256;
+                    if constexpr (B::kThreads == 256) {
+                        if (together) k_row_bars_and_weight_sums<K, B><<<(unsigned)(rb + wb), B::kThreads, 0, a.stream>>>(row_args(block), wa, (unsigned)rb);
+                    }
                 });
-            if (weights)
+            if (g->dx && n > 0 && !together)
+                with_tile<K>(a.d, n, [&](auto block) {
+                    k_row_bars<K, decltype(block)><<<(unsigned)row_blocks(block), decltype(block)::kThreads, 0, a.stream>>>(row_args(block));
+                });
+            if (weights && !together)
                 with_tile<K>(a.d, p.f2, [&](auto block) {
-                    using B = decltype(block);
-                    const int64_t m_tiles = (p.f2 + B::kRows - 1) / B::kRows, n_tiles = (a.d + B::kCols - 1) / B::kCols;
-                    const WeightSumArgs<K> wa = {gp, xp, a.d, m_tiles, n_tiles, p.run, reinterpret_cast<float *>(ws + p.part),
-                                                 g->dbg || g->dbv ? reinterpret_cast<float *>(ws + p.bias) : nullptr, first > 0};
-                    k_weight_sums<K, B><<<(unsigned)(m_tiles * n_tiles * p.splits), B::kThreads, 0, a.stream>>>(wa);
+                    const WeightSumArgs<K> wa = weight_args(block);
+                    k_weight_sums<K, decltype(block)><<<(unsigned)(wa.m_tiles * wa.n_tiles * p.splits), decltype(block)::kThreads, 0, a.stream>>>(wa);
                 });
         }
         first += p.chunk;

@@ -356,32 +356,46 @@ template <int ELEMS> __global__ __launch_bounds__(kSmallThreads) void k_small(Li
     const int m = it.m, n = it.n, mp = (m + 31) / 32 * 32, np = (n + 31) / 32 * 32, xs = np + 8, as = mp + 8, mb = mp / 32, nb = np / 32;
     P *x[2] = {lds, lds + mp * xs}, *q[2] = {lds + 2 * mp * xs, lds + 2 * mp * xs + mp * as};
     const int wave = threadIdx.x >> 6;
-    const bool by_row = it.src_cs <= it.src_rs;
-    const int in = by_row ? np : mp, all = mp * np;
+    for (int k = threadIdx.x; k < mp * xs / 4; k += kSmallThreads) *reinterpret_cast<Half8<P> *>(lds + 8 * k) = Half8<P>{};   // what the matrix does not fill stays zero
     device_elem(it.dtype, [&](auto e) {
         using E = decltype(e);
         const E *src = static_cast<const E *>(it.src);
-        auto value = [&](int k, int &r, int &col) {
-            r = by_row ? k / in : k % in;
-            col = by_row ? k % in : k / in;
-            return r < m && col < n ? (float)src[r * it.src_rs + col * it.src_cs] : 0.f;
+        // eight neighbours at a time, along rows or columns
+        const bool by_row = it.src_cs <= it.src_rs;
+        const unsigned inner = by_row ? n : m, outer = by_row ? m : n, pieces = (inner + 7) / 8, total = pieces * outer;
+        const int64_t is = by_row ? it.src_cs : it.src_rs, os = by_row ? it.src_rs : it.src_cs;
+        auto load = [&](unsigned k, float (&v)[8]) {
+            const unsigned o = k / pieces, i = k % pieces * 8;
+            load_cols(v, src + o * os, is, i, inner);
         };
         double sum = 0.0;
-        int r, col;
-        in_steps<4>(threadIdx.x, all, kSmallThreads, [&](int64_t k) { return value((int)k, r, col); }, [&](float v) { sum = fma((double)v, (double)v, sum); });
+#pragma unroll 2
+        for (unsigned k = threadIdx.x; k < total; k += kSmallThreads) {
+            float v[8];
+            load(k, v);
+#pragma unroll
+            for (int t = 0; t < 8; ++t) sum = fma((double)v[t], (double)v[t], sum);
+        }
         for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
         if ((threadIdx.x & 63) == 0) red[wave] = sum;
         __syncthreads();
         sum = 0.0;
         for (int w = 0; w < kSmallWaves; ++w) sum += red[w];
         const double f = start_scale(sum, eps, it.x_scale);
-#pragma unroll 4
-        for (int k = threadIdx.x; k < all; k += kSmallThreads) {
-            P v[2];
-            const float t = value(k, r, col);
-            split((float)(t * f), v);
-            x[0][r * xs + col] = v[0];
-            x[1][r * xs + col] = v[1];
+#pragma unroll 2
+        for (unsigned k = threadIdx.x; k < total; k += kSmallThreads) {
+            const int o = k / pieces, i = k % pieces * 8;
+            float v[8];
+            load(k, v);
+            const int at = by_row ? o * xs + i : i * xs + o, step = by_row ? 1 : xs;
+#pragma unroll
+            for (int t = 0; t < 8; ++t)
+                if (i + t < (int)inner) {
+                    P w[2];
+                    split((float)(v[t] * f), w);
+                    x[0][at + t * step] = w[0];
+                    x[1][at + t * step] = w[1];
+                }
         }
     });
     const float from_gram = kGramScale / (it.x_scale * it.x_scale);
@@ -391,14 +405,15 @@ template <int ELEMS> __global__ __launch_bounds__(kSmallThreads) void k_small(Li
         for (int s = 0; s < 2; ++s) {   // A
             const int sq = wave + s * kSmallWaves, i0 = sq / mb * 32, j0 = sq % mb * 32;
             if (sq >= mb * mb) break;
-            f32x16 acc = {};
+            f32x16 acc = {}, cross = {};   // (two sums, so that a product does not wait for the one before)
 #pragma unroll 4
             for (int k = 0; k < np; k += 16) {
                 const Half8<P> u0 = along(x[0], xs, i0, k), u1 = along(x[1], xs, i0, k), v0 = along(x[0], xs, j0, k), v1 = along(x[1], xs, j0, k);
-                acc = mfma<P>(u1, v0, acc);
-                acc = mfma<P>(u0, v1, acc);
+                cross = mfma<P>(u1, v0, cross);
                 acc = mfma<P>(u0, v0, acc);
+                cross = mfma<P>(u0, v1, cross);
             }
+            acc += cross;
             const int row = j0 + acc_col();
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
@@ -423,13 +438,15 @@ template <int ELEMS> __global__ __launch_bounds__(kSmallThreads) void k_small(Li
         for (int s = 0; s < 2; ++s) {   // B
             const int sq = wave + s * kSmallWaves, i0 = sq / mb * 32, j0 = sq % mb * 32;
             if (sq >= mb * mb) break;
+            f32x16 cross = {};
 #pragma unroll 2
             for (int k = 0; k < mp; k += 16) {
                 const Half8<P> u0 = along(q[0], as, i0, k), u1 = along(q[1], as, i0, k), v0 = along(q[0], as, j0, k), v1 = along(q[1], as, j0, k);
-                poly[s] = mfma<P>(u1, v0, poly[s]);
-                poly[s] = mfma<P>(u0, v1, poly[s]);
+                cross = mfma<P>(u1, v0, cross);
                 poly[s] = mfma<P>(u0, v0, poly[s]);
+                cross = mfma<P>(u0, v1, cross);
             }
+            poly[s] += cross;
             const int row = j0 + acc_col();
             const float dr = diag[0][row];
 #pragma unroll
@@ -468,13 +485,15 @@ template <int ELEMS> __global__ __launch_bounds__(kSmallThreads) void k_small(Li
         for (int s = 0; s < 4; ++s) {   // X: columns i0, rows j0
             const int sq = wave + s * kSmallWaves, i0 = sq / mb * 32, j0 = sq % mb * 32;
             if (sq >= mb * nb) break;
+            f32x16 cross = {};
 #pragma unroll 2
             for (int k = 0; k < mp; k += 16) {
                 const Half8<P> u0 = across(x[0], xs, i0, k), u1 = across(x[1], xs, i0, k), v0 = along(q[0], as, j0, k), v1 = along(q[1], as, j0, k);
-                next[s] = mfma<P>(u1, v0, next[s]);
-                next[s] = mfma<P>(u0, v1, next[s]);
+                cross = mfma<P>(u1, v0, cross);
                 next[s] = mfma<P>(u0, v0, next[s]);
+                cross = mfma<P>(u0, v1, cross);
             }
+            next[s] += cross;
             const int row = j0 + acc_col();
             const float f = a + diag[1][row];
 #pragma unroll
@@ -503,12 +522,25 @@ template <int ELEMS> __global__ __launch_bounds__(kSmallThreads) void k_small(Li
     __syncthreads();
     device_elem(it.dtype, [&](auto e) {   // (X has 22 bits: fp32 results too)
         using E = decltype(e);
-        const bool rows = it.dst_cs <= it.dst_rs;
-        const int inner = rows ? n : m, total = m * n;
+        const bool by_row = it.dst_cs <= it.dst_rs;
+        const unsigned inner = by_row ? n : m, outer = by_row ? m : n, pieces = (inner + 7) / 8, total = pieces * outer;
+        const int64_t is = by_row ? it.dst_cs : it.dst_rs, os = by_row ? it.dst_rs : it.dst_cs;
         const float to = scale / it.x_scale;
-        for (int k = threadIdx.x; k < total; k += kSmallThreads) {
-            const int r = rows ? k / inner : k % inner, col = rows ? k % inner : k / inner, at = r * xs + col;
-            static_cast<E *>(it.dst)[r * it.dst_rs + col * it.dst_cs] = to_elem<E>(both(x[0][at], x[1][at]) * to);
+#pragma unroll 2
+        for (unsigned k = threadIdx.x; k < total; k += kSmallThreads) {
+            const int o = k / pieces, i = k % pieces * 8, at = by_row ? o * xs + i : i * xs + o, step = by_row ? 1 : xs;
+            E *dst = static_cast<E *>(it.dst) + o * os;
+            float v[8];
+#pragma unroll
+            for (int t = 0; t < 8; ++t) {
+                const int from = i + t < (int)inner ? at + t * step : at;
+                v[t] = both(x[0][from], x[1][from]) * to;
+            }
+            if (is == 1) store_cols<E>(v, dst, i, inner);
+            else
+#pragma unroll
+                for (int t = 0; t < 8; ++t)
+                    if (i + t < (int)inner) dst[(i + t) * is] = to_elem<E>(v[t]);
         }
     });
 }
