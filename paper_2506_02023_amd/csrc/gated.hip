@@ -26,6 +26,10 @@ template <class Fn> int with_kind(int32_t dtype, Fn &&f)
     return f(Kind<_Float16, 1, _Float16>{});
 }
 int parts_of(int32_t dtype) { return dtype == MLIP_DTYPE_F32 ? 3 : 1; }
+// Wide fp32 rows of the forward call: two fp16 parts (22 bits) and three products, half the matrix time.  Every row of x and column of the weights is brought by a
+// power of two to a largest value in [2^13, 2^14), so that a value has its 22 bits down to 2^-24 of its row's largest and is off by 2^-38 of that below.
+// (32,768 x 512 x 1365: 381 us, with three bf16 parts 712.)
+using Scaled = Kind<_Float16, 2, float>;
 
 // Column c of the 2 f: the feature, and whether of v
 __host__ __device__ inline int64_t feature_of(int64_t c) { return c / 64 * 32 + c % 32; }
@@ -34,6 +38,7 @@ __host__ __device__ inline bool is_value(int64_t c) { return c & 32; }
 // ---------------------------------------------------------------- layouts
 
 constexpr int kPackThreads = 256;
+constexpr int64_t kNarrow = 128;              // d up to which rows stay in registers
 
 // dst [rows][cols_p] in parts from src at (r, c) -> r rs + c cs, zeros from cols on; eight columns a thread
 template <class K> __global__ __launch_bounds__(kPackThreads) void k_pack_rows(const typename K::E *src, int64_t rs, int64_t cs, int64_t rows, int64_t cols, int64_t cols_p,
@@ -60,6 +65,7 @@ template <class K> struct Weights {
     int64_t g_rs, g_cs, v_rs, v_cs, d, f, d_ld, f2_ld;
     typename K::T *across, *down;
     int64_t across_part, down_part;
+    const float *scale;      // of the columns, or NULL
 };
 template <class K> __global__ __launch_bounds__(kPackThreads) void k_pack_weights(Weights<K> w)
 {
@@ -77,12 +83,82 @@ template <class K> __global__ __launch_bounds__(kPackThreads) void k_pack_weight
     __syncthreads();
     for (int i = b; i < 32; i += 8) {
         typename K::T v[K::kParts];
-        split(tile[a][i], v);
+        split(w.scale ? tile[a][i] * w.scale[c0 + i] : tile[a][i], v);
         for (int p = 0; p < K::kParts; ++p) w.across[p * w.across_part + (c0 + i) * w.d_ld + d0 + a] = v[p];
         if (w.down && d0 + i < w.d) {
             split(tile[i][a], v);
             for (int p = 0; p < K::kParts; ++p) w.down[p * w.down_part + (d0 + i) * w.f2_ld + c0 + a] = v[p];
         }
+    }
+}
+
+// The power of two that brings a largest value to [2^13, 2^14) (1 for none, and for one that is not finite), and its inverse
+__device__ inline float scale_for(float largest, float &inverse)
+{
+    const int e = largest > 0.f && largest < __builtin_inff() ? 13 - ilogbf(largest) : 0, s = e > 110 ? 110 : e < -110 ? -110 : e;
+    inverse = ldexpf(1.f, -s);
+    return ldexpf(1.f, s);
+}
+
+// Scales of 32 columns of the weights
+__global__ __launch_bounds__(kPackThreads) void k_column_scales(Weights<Scaled> w, float *scale, float *inverse)
+{
+    __shared__ float most[kPackThreads];
+    const int64_t c = (int64_t)blockIdx.x * 32 + (threadIdx.x & 31), f = feature_of(c);
+    const bool value = is_value(c);
+    const float *src = value ? w.wv : w.wg;
+    const int64_t rs = value ? w.v_rs : w.g_rs, cs = value ? w.v_cs : w.g_cs;
+    float m = 0.f;
+    if (f < w.f) in_steps<8>(threadIdx.x >> 5, w.d, kPackThreads / 32, [&](int64_t d) { return src[d * rs + f * cs]; }, [&](float x) { m = fmaxf(m, fabsf(x)); });
+    most[threadIdx.x] = m;
+    __syncthreads();
+    if (threadIdx.x >= 32) return;
+    for (int k = 32; k < kPackThreads; k += 32) m = fmaxf(m, most[threadIdx.x + k]);
+    float inv;
+    scale[c] = scale_for(m, inv);
+    inverse[c] = inv;
+}
+
+// Rows of x scaled and in parts, a wavefront each; zeros from `cols` on
+__global__ __launch_bounds__(kPackThreads) void k_pack_scaled_rows(const float *src, int64_t rs, int64_t cs, int64_t rows, int64_t cols, int64_t cols_p, _Float16 *dst, int64_t ld, int64_t part,
+                                                                   float *inverse)
+{
+    const int64_t r = (int64_t)blockIdx.x * (kPackThreads / 64) + (threadIdx.x >> 6);
+    if (r >= rows) return;
+    const int lane = threadIdx.x & 63;
+    const float *row = src + r * rs;
+    constexpr int kHeld = 4;   // pieces of four columns that a lane keeps from the first look to the second: rows of up to 1024
+    float v[kHeld][4], m = 0.f;
+    auto look = [&](float (&x)[4], int64_t c) {
+        load_cols(x, row, cs, c, cols);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) m = fmaxf(m, fabsf(x[t]));
+    };
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k) look(v[k], (k * 64 + lane) * 4);
+    for (int64_t c = (kHeld * 64 + lane) * 4; c < cols; c += 256) {
+        float x[4];
+        look(x, c);
+    }
+    for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
+    float inv;
+    const float scale = scale_for(m, inv);
+    if (lane == 0) inverse[r] = inv;
+    auto put = [&](float (&x)[4], int64_t c) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t) x[t] *= scale;
+        Cols<_Float16, 4> p[2];
+        split_cols<_Float16>(x, p);
+        *reinterpret_cast<Cols<_Float16, 4> *>(dst + r * ld + c) = p[0];
+        *reinterpret_cast<Cols<_Float16, 4> *>(dst + part + r * ld + c) = p[1];
+    };
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k)
+        if ((k * 64 + lane) * 4 < cols_p) put(v[k], (k * 64 + lane) * 4);
+    for (int64_t c = (kHeld * 64 + lane) * 4; c < cols_p; c += 256) {
+        float x[4];
+        load_cols(x, row, cs, c, cols);
+        put(x, c);
     }
 }
 
@@ -129,6 +205,7 @@ template <class K> struct GateArgs {
     int64_t bar_rs, bar_cs;
     typename K::T *gv;
     int64_t gv_ld, gv_part;
+    const float *x_inverse, *w_inverse;   // scales to take off again (Scaled)
 };
 
 // The weights are the products' first operand and the rows their second; a lane ends with neighbouring features of a row.
@@ -151,6 +228,11 @@ template <class K, class B, bool BACK> __global__ __launch_bounds__(B::kThreads)
         float bg[W] = {}, bv[W] = {};
         if (a.bg) load_cols(bg, a.bg, 1, f, a.f);
         if (a.bv) load_cols(bv, a.bv, 1, f, a.f);
+        float ig[W], iv[W];
+        if constexpr (std::is_same_v<K, Scaled>) {
+            load_cols(ig, a.w_inverse, 1, col0 + c, a.w.rows);
+            load_cols(iv, a.w_inverse, 1, col0 + 32 + c, a.w.rows);
+        }
         with_act(a.act, [&](auto act) {
 #pragma unroll
             for (int k = 0; k < lanes; ++k) {
@@ -160,6 +242,14 @@ template <class K, class B, bool BACK> __global__ __launch_bounds__(B::kThreads)
                 float g[W], v[W], bar[W];
                 turned.get(g, r, c);
                 turned.get(v, r, 32 + c);
+                if constexpr (std::is_same_v<K, Scaled>) {
+                    const float ix = a.x_inverse[row];
+#pragma unroll
+                    for (int t = 0; t < W; ++t) {
+                        g[t] *= ix * ig[t];
+                        v[t] *= ix * iv[t];
+                    }
+                }
                 if constexpr (BACK) load_cols(bar, a.bar + row * a.bar_rs, a.bar_cs, f, a.f);
 #pragma unroll
                 for (int t = 0; t < W; ++t) {
@@ -503,7 +593,6 @@ template <class K> __global__ __launch_bounds__(kPackThreads) void k_join(JoinAr
 constexpr int64_t kChunkBytes = (int64_t)4 << 30;     // of x's parts, G and V of a chunk
 constexpr int64_t kMostTiles = 1 << 23;       // blocks of a launch
 constexpr int64_t kFull = 256;                // blocks that leave no compute unit idle
-constexpr int64_t kNarrow = 128;              // d up to which rows stay in registers
 constexpr int64_t kNarrowBlocks = 1024;       // blocks of such a launch
 
 struct Plan {
@@ -511,8 +600,11 @@ struct Plan {
     bool pack_x;
     int64_t d_p, f2, gv_ld, d_ld, chunk;       // columns of the laid out x and weights and where their rows lie, rows of a chunk
     int64_t splits, run;
-    size_t across, down, xs, gv, part, bias, bytes;   // offsets
+    size_t across, down, xs, gv, part, bias, x_inverse, w_scale, bytes;   // offsets
 };
+
+// Whether a call goes by Scaled: long enough for its one more launch to pay (1024 x 130 x 20: 23 us, 22 without; 3000 x 256 x 256: 25, 28 without)
+bool by_scale(const GatedArgs &a, bool grad) { return a.dtype == MLIP_DTYPE_F32 && !grad && a.d > kNarrow && a.n >= 1024; }
 
 // x is read where it lies if its rows are whole lines of pieces and steps
 bool reads_x(const GatedArgs &a)
@@ -521,10 +613,11 @@ bool reads_x(const GatedArgs &a)
            reinterpret_cast<uintptr_t>(a.x) % 16 == 0;
 }
 
-// f(Block{}) for a product of `cols` columns (of the first operand) and `rows` rows (of the second)
-template <class K, class Fn> void with_tile(int64_t cols, int64_t rows, Fn &&f)
+// f(Block{}) for a product of `cols` columns (of the first operand) and `rows` rows (of the second).  Large tiles if there are enough for half the compute units, or K is
+// split for more (1500 x 300 x 700 in fp32: 44 us by 36 large tiles, 30 by 144).
+template <class K, class Fn> void with_tile(int64_t cols, int64_t rows, bool split, Fn &&f)
 {
-    if (K::kParts == 1 && cols >= 512 && rows >= 512) f(std::conditional_t<K::kParts == 1, Large, Middle>{});
+    if (K::kParts <= 2 && cols >= 512 && rows >= 512 && (split || (double)cols * (double)rows >= 128.0 * 65536.0)) f(std::conditional_t<K::kParts <= 2, Large, Middle>{});
     else if (cols <= 64) f(Narrow{});
     else f(Middle{});
 }
@@ -532,7 +625,7 @@ template <class K, class Fn> void with_tile(int64_t cols, int64_t rows, Fn &&f)
 Plan plan_of(const GatedArgs &a, bool grad)
 {
     Plan p{};
-    p.parts = parts_of(a.dtype);
+    p.parts = by_scale(a, grad) ? Scaled::kParts : parts_of(a.dtype);
     p.pack_x = !reads_x(a);
     p.d_p = pad_to(a.d, kPadK);
     p.f2 = 2 * pad_to(a.f, 32);
@@ -549,6 +642,10 @@ Plan plan_of(const GatedArgs &a, bool grad)
     auto take = [&](int64_t bytes) { const size_t here = at; at += (size_t)pad_to(bytes, 256); return here; };
     p.across = take(p.f2 * p.d_ld * p.parts * 2);
     p.xs = take(p.chunk * p.d_ld * p.parts * 2);
+    if (by_scale(a, grad)) {
+        p.x_inverse = take(p.chunk * 4);
+        p.w_scale = take(2 * p.f2 * 4);
+    }
     if (grad) {
         p.down = take(a.d * p.gv_ld * p.parts * 2);
         p.gv = take(p.chunk * p.gv_ld * p.parts * 2);
@@ -614,7 +711,7 @@ template <class K> int launch(const GatedArgs &a, const GatedGrad *g)
             };
             if (in_registers && a.d <= 64) narrow(std::integral_constant<int, 4>{});
             else if (in_registers) narrow(std::integral_constant<int, 8>{});
-            else with_tile<K>(p.f2, n, [&](auto block) {
+            else with_tile<K>(p.f2, n, false, [&](auto block) {
                 using B = decltype(block);
                 ga.n_tiles = (p.f2 + B::kCols - 1) / B::kCols;
                 const unsigned blocks = (unsigned)((n + B::kRows - 1) / B::kRows * ga.n_tiles);
@@ -638,7 +735,7 @@ template <class K> int launch(const GatedArgs &a, const GatedGrad *g)
             };
             bool together = false;
             if (g->dx && n > 0 && weights)
-                with_tile<K>(a.d, n < p.f2 ? n : p.f2, [&](auto block) {
+                with_tile<K>(a.d, n < p.f2 ? n : p.f2, false, [&](auto block) {
                     using B = decltype(block);
                     const WeightSumArgs<K> wa = weight_args(block);
                     const int64_t rb = row_blocks(block), wb = wa.m_tiles * wa.n_tiles * p.splits;
@@ -648,11 +745,11 @@ template <class K> int launch(const GatedArgs &a, const GatedGrad *g)
                     }
                 });
             if (g->dx && n > 0 && !together)
-                with_tile<K>(a.d, n, [&](auto block) {
+                with_tile<K>(a.d, n, false, [&](auto block) {
                     k_row_bars<K, decltype(block)><<<(unsigned)row_blocks(block), decltype(block)::kThreads, 0, a.stream>>>(row_args(block));
                 });
             if (weights && !together)
-                with_tile<K>(a.d, p.f2, [&](auto block) {
+                with_tile<K>(a.d, p.f2, true, [&](auto block) {
                     const WeightSumArgs<K> wa = weight_args(block);
                     k_weight_sums<K, decltype(block)><<<(unsigned)(wa.m_tiles * wa.n_tiles * p.splits), decltype(block)::kThreads, 0, a.stream>>>(wa);
                 });
@@ -668,6 +765,36 @@ template <class K> int launch(const GatedArgs &a, const GatedGrad *g)
     return MLIP_OK;
 }
 
+int launch_scaled(const GatedArgs &a)
+{
+    const Plan p = plan_of(a, false);
+    char *ws = static_cast<char *>(a.workspace);
+    _Float16 *across = reinterpret_cast<_Float16 *>(ws + p.across), *xs = reinterpret_cast<_Float16 *>(ws + p.xs);
+    float *x_inverse = reinterpret_cast<float *>(ws + p.x_inverse), *w_scale = reinterpret_cast<float *>(ws + p.w_scale), *w_inverse = w_scale + p.f2;
+    const Weights<Scaled> w = {static_cast<const float *>(a.wg), static_cast<const float *>(a.wv), a.wg_rs, a.wg_cs, a.wv_rs, a.wv_cs, a.d, a.f, p.d_ld, p.gv_ld,
+                               across, nullptr, p.f2 * p.d_ld, 0, w_scale};
+    k_column_scales<<<(unsigned)(p.f2 / 32), kPackThreads, 0, a.stream>>>(w, w_scale, w_inverse);
+    k_pack_weights<Scaled><<<dim3((unsigned)(p.f2 / 32), (unsigned)(p.d_p / 32)), kPackThreads, 0, a.stream>>>(w);
+    for (int64_t first = 0; first < a.n; first += p.chunk) {
+        const int64_t n = a.n - first < p.chunk ? a.n - first : p.chunk;
+        k_pack_scaled_rows<<<(unsigned)((n + kPackThreads / 64 - 1) / (kPackThreads / 64)), kPackThreads, 0, a.stream>>>(
+            static_cast<const float *>(a.x) + first * a.x_rs, a.x_rs, a.x_cs, n, a.d, p.d_p, xs, p.d_ld, p.chunk * p.d_ld, x_inverse);
+        GateArgs<Scaled> ga = {{xs, p.d_ld, p.chunk * p.d_ld, n, p.d_p}, {across, p.d_ld, p.f2 * p.d_ld, p.f2, p.d_p}, p.d_p, a.f, 0, a.act,
+                               static_cast<const float *>(a.bg), static_cast<const float *>(a.bv)};
+        ga.out = static_cast<float *>(a.out) + first * a.out_rs;
+        ga.out_rs = a.out_rs;
+        ga.x_inverse = x_inverse;
+        ga.w_inverse = w_inverse;
+        with_tile<Scaled>(p.f2, n, false, [&](auto block) {
+            using B = decltype(block);
+            ga.n_tiles = (p.f2 + B::kCols - 1) / B::kCols;
+            k_gates<Scaled, B, false><<<(unsigned)((n + B::kRows - 1) / B::kRows * ga.n_tiles), B::kThreads, 0, a.stream>>>(ga);
+        });
+    }
+    MLIP_HIP(hipGetLastError());
+    return MLIP_OK;
+}
+
 }  // namespace
 
 size_t gated_workspace(const GatedArgs &a, bool grad) { return plan_of(a, grad).bytes; }
@@ -675,6 +802,7 @@ size_t gated_workspace(const GatedArgs &a, bool grad) { return plan_of(a, grad).
 int gated_impl(const GatedArgs &a)
 {
     if (a.n == 0) return MLIP_OK;
+    if (by_scale(a, false)) return launch_scaled(a);
     return with_kind(a.dtype, [&](auto kind) { return launch<decltype(kind)>(a, nullptr); });
 }
 

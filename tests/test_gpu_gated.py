@@ -103,10 +103,61 @@ def test_layouts(dtype, turned, gap):
     _both(190, 128, 72, dtype, "silu", turned=turned, gap=gap)
 
 
+@pytest.mark.parametrize("n,d,f", [(1024, 129, 33), (1100, 200, 100), (1030, 1025, 40), (1500, 2050, 64), (1200, 300, 700), (3000, 256, 600)])
+@pytest.mark.parametrize("turned", [False, True])
+def test_wide_fp32_rows(n, d, f, turned):
+    """(the terms that two parts of 22 bits leave out are below 12 2^-24 of the terms' sizes, of 2 (d + 8) 2^-24 counted)"""
+    _both(n, d, f, "float32", ACTS[(n + d) % 4], turned=turned, gap=(n + f) % 3, bias=n % 4 == 0)
+
+
+def test_wide_fp32_rows_of_all_sizes():
+    """Rows and columns from 2^-40 to 2^40, some of them zero or not finite: each as exact as if it were alone"""
+    import torch
+    import paper_2506_02023_amd as M
+    bar, (x, wg, wv, _, _) = _make(1100, 160, 64, torch.float32, bias=False)
+    x = x * torch.exp2(torch.arange(1100, device="cuda") % 81 - 40.0)[:, None]
+    wv = wv * torch.exp2(torch.arange(64, device="cuda") - 32.0)[None, :]
+    x[5], wv[:, 7] = 0.0, 0.0
+    h, tol, _, _ = _reference(bar, (x, wg, wv, None, None), "sigmoid")
+    got = M.mlip_gated(x, wg, wv, act="sigmoid")
+    _check(got, h, tol, "h")
+    assert bool((got[5] == 0).all()) and bool((got[:, 7] == 0).all())
+    x2 = x.clone()
+    x2[17, 3], x2[1099, 159] = float("nan"), float("inf")
+    got2 = M.mlip_gated(x2, wg, wv, act="sigmoid")
+    keep = torch.ones(1100, dtype=torch.bool, device="cuda")
+    keep[[17, 1099]] = False
+    assert torch.equal(got2[keep], got[keep]) and got2[17].isnan().all() and got2[1099].isnan().all()
+
+
 @pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
-def test_several_chunks(dtype):
-    """More rows than a chunk has, whose last one is ragged"""
+def test_many_rows(dtype):
     _both(50_001 if dtype == "float32" else 70_001, 64, 512 if dtype == "float32" else 1024, dtype, "silu")
+
+
+def test_several_chunks():
+    """More rows than a chunk has (4 GB of parts): gradients of whole numbers, all sums exact, against those of the two halves, which are one chunk each.
+    (sigmoid(0) = 1/2; with x, H in -1 .. 1 and |v| <= 128 every sum is a multiple of 1/4 below 2^22.)"""
+    import torch
+    import paper_2506_02023_amd as M
+    n, d, f = 100_000, 64, 4096
+    g = torch.Generator(device="cuda").manual_seed(3)
+
+    def whole(low, high, *shape):
+        return torch.randint(low, high + 1, shape, generator=g, device="cuda").float()
+    x, bar, wv, wg = whole(-1, 1, n, d), whole(-1, 1, n, f), whole(-2, 2, d, f), torch.zeros(d, f, device="cuda")
+    bias = torch.zeros(f, device="cuda")
+    assert n * (2 * f + d) * 6 > 4 << 30 > n // 2 * (2 * f + 128) * 6
+    dx, *dw = M.mlip_gated_grad(bar, x, wg, wv, bias, bias, act="sigmoid")
+    halves = [M.mlip_gated_grad(bar[k], x[k], wg, wv, bias, bias, act="sigmoid") for k in (slice(0, n // 2), slice(n // 2, n))]
+    assert torch.equal(dx, torch.cat([h[0] for h in halves]))
+    for k, w in enumerate(dw):
+        assert torch.equal(w, halves[0][k + 1] + halves[1][k + 1]) and bool((w != 0).any())
+
+
+@pytest.mark.parametrize("n,d,f,dtype", [(4100, 640, 1100, "bfloat16"), (4097, 513, 1025, "float16"), (8200, 530, 530, "float32"), (600, 1030, 300, "bfloat16")])
+def test_large_tiles(n, d, f, dtype):
+    _both(n, d, f, dtype, "gelu", bias=n != 4100, gap=n % 2)
 
 
 @pytest.mark.parametrize("dtype", ["float32", "bfloat16"])

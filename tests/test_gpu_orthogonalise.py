@@ -1,7 +1,9 @@
 """Orthogonal updates against the same iteration in 64 bits.
 
 Tolerance, in the norm of all elements: a step's result is off by 2^-18 |X_k| at most (parts of 22 bits: three roundings of 2^-22 of sizes up to
-|a| + |b| + |c| = 10.3 times |X_k|, and fp32 sums), later steps stretch that by a = 3.4445 at most each, and the last rounding adds half a step."""
+|a| + |b| + |c| = 10.3 times |X_k|, and fp32 sums), later steps stretch that by a = 3.4445 at most each, and the last rounding adds half a step.  Of bf16
+matrices the products take parts of 11 bits; what that brings (0.4 to 1.2e-3 of the norm) and the 1.7e-3 of the result's own rounding together
+lie within the half step of 3.9e-3 that is counted for the latter."""
 import numpy as np
 import pytest
 
@@ -72,6 +74,19 @@ def test_a_list_of_all_shapes_and_types():
             _check(t, g, k)
             assert torch.equal(M.mlip_orthogonalise([g.clone()])[0], t)
     assert M.mlip_orthogonalise([]) == []
+
+
+def test_matrices_beyond_the_scratch_memory_of_a_group():
+    """Four matrices of 560 MB of scratch memory each are taken in two groups: the same bits as alone"""
+    import torch
+    import paper_2506_02023_amd as M
+    from paper_2506_02023_amd import binding as B
+    g = torch.Generator(device="cuda").manual_seed(1)
+    list_ = [torch.randn(5000, 9000, generator=g, device="cuda") for _ in range(4)]
+    a = (B._Matrix * 4)(*[B._Matrix(t.data_ptr(), t.data_ptr(), *t.shape, *t.stride(), *t.stride(), 0) for t in list_])
+    assert 1 << 30 < B.lib().mlip_orthogonalise_workspace(a, 4) <= 1 << 31
+    alone = [M.mlip_orthogonalise([t], steps=2, out=[torch.empty_like(t)])[0] for t in list_]
+    assert all(torch.equal(x, y) for x, y in zip(M.mlip_orthogonalise(list_, steps=2), alone))
 
 
 def test_singular_values():
