@@ -92,16 +92,15 @@ template <class K> __global__ __launch_bounds__(kPackThreads) void k_pack_weight
     }
 }
 
-// The power of two that brings a largest value to [2^13, 2^14) (1 for none, and for one that is not finite), and its inverse
-__device__ inline float scale_for(float largest, float &inverse)
+// The power of two that brings a largest value to [2^13, 2^14), as its exponent (0 for none, and for one that is not finite)
+__device__ inline int scale_for(float largest)
 {
-    const int e = largest > 0.f && largest < __builtin_inff() ? 13 - ilogbf(largest) : 0, s = e > 110 ? 110 : e < -110 ? -110 : e;
-    inverse = ldexpf(1.f, -s);
-    return ldexpf(1.f, s);
+    const int e = largest > 0.f && largest < __builtin_inff() ? 13 - ilogbf(largest) : 0;
+    return e > 110 ? 110 : e;
 }
 
 // Scales of 32 columns of the weights
-__global__ __launch_bounds__(kPackThreads) void k_column_scales(Weights<Scaled> w, float *scale, float *inverse)
+__global__ __launch_bounds__(kPackThreads) void k_column_scales(Weights<Scaled> w, float *scale, float *exponent)
 {
     __shared__ float most[kPackThreads];
     const int64_t c = (int64_t)blockIdx.x * 32 + (threadIdx.x & 31), f = feature_of(c);
@@ -114,14 +113,14 @@ __global__ __launch_bounds__(kPackThreads) void k_column_scales(Weights<Scaled> 
     __syncthreads();
     if (threadIdx.x >= 32) return;
     for (int k = 32; k < kPackThreads; k += 32) m = fmaxf(m, most[threadIdx.x + k]);
-    float inv;
-    scale[c] = scale_for(m, inv);
-    inverse[c] = inv;
+    const int e = scale_for(m);
+    scale[c] = ldexpf(1.f, e);
+    exponent[c] = (float)e;
 }
 
 // Rows of x scaled and in parts, a wavefront each; zeros from `cols` on
 __global__ __launch_bounds__(kPackThreads) void k_pack_scaled_rows(const float *src, int64_t rs, int64_t cs, int64_t rows, int64_t cols, int64_t cols_p, _Float16 *dst, int64_t ld, int64_t part,
-                                                                   float *inverse)
+                                                                   float *exponent)
 {
     const int64_t r = (int64_t)blockIdx.x * (kPackThreads / 64) + (threadIdx.x >> 6);
     if (r >= rows) return;
@@ -141,9 +140,9 @@ __global__ __launch_bounds__(kPackThreads) void k_pack_scaled_rows(const float *
         look(x, c);
     }
     for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
-    float inv;
-    const float scale = scale_for(m, inv);
-    if (lane == 0) inverse[r] = inv;
+    const int e = scale_for(m);
+    const float scale = ldexpf(1.f, e);
+    if (lane == 0) exponent[r] = (float)e;
     auto put = [&](float (&x)[4], int64_t c) {
 #pragma unroll
         for (int t = 0; t < 4; ++t) x[t] *= scale;
@@ -205,7 +204,7 @@ template <class K> struct GateArgs {
     int64_t bar_rs, bar_cs;
     typename K::T *gv;
     int64_t gv_ld, gv_part;
-    const float *x_inverse, *w_inverse;   // scales to take off again (Scaled)
+    const float *x_exponent, *w_exponent;   // of the scales to take off again (Scaled)
 };
 
 // The weights are the products' first operand and the rows their second; a lane ends with neighbouring features of a row.
@@ -228,10 +227,10 @@ template <class K, class B, bool BACK> __global__ __launch_bounds__(B::kThreads)
         float bg[W] = {}, bv[W] = {};
         if (a.bg) load_cols(bg, a.bg, 1, f, a.f);
         if (a.bv) load_cols(bv, a.bv, 1, f, a.f);
-        float ig[W], iv[W];
+        float eg[W], ev[W];
         if constexpr (std::is_same_v<K, Scaled>) {
-            load_cols(ig, a.w_inverse, 1, col0 + c, a.w.rows);
-            load_cols(iv, a.w_inverse, 1, col0 + 32 + c, a.w.rows);
+            load_cols(eg, a.w_exponent, 1, col0 + c, a.w.rows);
+            load_cols(ev, a.w_exponent, 1, col0 + 32 + c, a.w.rows);
         }
         with_act(a.act, [&](auto act) {
 #pragma unroll
@@ -243,11 +242,11 @@ template <class K, class B, bool BACK> __global__ __launch_bounds__(B::kThreads)
                 turned.get(g, r, c);
                 turned.get(v, r, 32 + c);
                 if constexpr (std::is_same_v<K, Scaled>) {
-                    const float ix = a.x_inverse[row];
+                    const float ex = a.x_exponent[row];
 #pragma unroll
                     for (int t = 0; t < W; ++t) {
-                        g[t] *= ix * ig[t];
-                        v[t] *= ix * iv[t];
+                        g[t] = ldexpf(g[t], -(int)(ex + eg[t]));
+                        v[t] = ldexpf(v[t], -(int)(ex + ev[t]));
                     }
                 }
                 if constexpr (BACK) load_cols(bar, a.bar + row * a.bar_rs, a.bar_cs, f, a.f);
@@ -600,7 +599,7 @@ struct Plan {
     bool pack_x;
     int64_t d_p, f2, gv_ld, d_ld, chunk;       // columns of the laid out x and weights and where their rows lie, rows of a chunk
     int64_t splits, run;
-    size_t across, down, xs, gv, part, bias, x_inverse, w_scale, bytes;   // offsets
+    size_t across, down, xs, gv, part, bias, x_exponent, w_scale, bytes;   // offsets
 };
 
 // Whether a call goes by Scaled: long enough for its one more launch to pay (1024 x 130 x 20: 23 us, 22 without; 3000 x 256 x 256: 25, 28 without)
@@ -643,7 +642,7 @@ Plan plan_of(const GatedArgs &a, bool grad)
     p.across = take(p.f2 * p.d_ld * p.parts * 2);
     p.xs = take(p.chunk * p.d_ld * p.parts * 2);
     if (by_scale(a, grad)) {
-        p.x_inverse = take(p.chunk * 4);
+        p.x_exponent = take(p.chunk * 4);
         p.w_scale = take(2 * p.f2 * 4);
     }
     if (grad) {
@@ -770,21 +769,21 @@ int launch_scaled(const GatedArgs &a)
     const Plan p = plan_of(a, false);
     char *ws = static_cast<char *>(a.workspace);
     _Float16 *across = reinterpret_cast<_Float16 *>(ws + p.across), *xs = reinterpret_cast<_Float16 *>(ws + p.xs);
-    float *x_inverse = reinterpret_cast<float *>(ws + p.x_inverse), *w_scale = reinterpret_cast<float *>(ws + p.w_scale), *w_inverse = w_scale + p.f2;
+    float *x_exponent = reinterpret_cast<float *>(ws + p.x_exponent), *w_scale = reinterpret_cast<float *>(ws + p.w_scale), *w_exponent = w_scale + p.f2;
     const Weights<Scaled> w = {static_cast<const float *>(a.wg), static_cast<const float *>(a.wv), a.wg_rs, a.wg_cs, a.wv_rs, a.wv_cs, a.d, a.f, p.d_ld, p.gv_ld,
                                across, nullptr, p.f2 * p.d_ld, 0, w_scale};
-    k_column_scales<<<(unsigned)(p.f2 / 32), kPackThreads, 0, a.stream>>>(w, w_scale, w_inverse);
+    k_column_scales<<<(unsigned)(p.f2 / 32), kPackThreads, 0, a.stream>>>(w, w_scale, w_exponent);
     k_pack_weights<Scaled><<<dim3((unsigned)(p.f2 / 32), (unsigned)(p.d_p / 32)), kPackThreads, 0, a.stream>>>(w);
     for (int64_t first = 0; first < a.n; first += p.chunk) {
         const int64_t n = a.n - first < p.chunk ? a.n - first : p.chunk;
         k_pack_scaled_rows<<<(unsigned)((n + kPackThreads / 64 - 1) / (kPackThreads / 64)), kPackThreads, 0, a.stream>>>(
-            static_cast<const float *>(a.x) + first * a.x_rs, a.x_rs, a.x_cs, n, a.d, p.d_p, xs, p.d_ld, p.chunk * p.d_ld, x_inverse);
+            static_cast<const float *>(a.x) + first * a.x_rs, a.x_rs, a.x_cs, n, a.d, p.d_p, xs, p.d_ld, p.chunk * p.d_ld, x_exponent);
         GateArgs<Scaled> ga = {{xs, p.d_ld, p.chunk * p.d_ld, n, p.d_p}, {across, p.d_ld, p.f2 * p.d_ld, p.f2, p.d_p}, p.d_p, a.f, 0, a.act,
                                static_cast<const float *>(a.bg), static_cast<const float *>(a.bv)};
         ga.out = static_cast<float *>(a.out) + first * a.out_rs;
         ga.out_rs = a.out_rs;
-        ga.x_inverse = x_inverse;
-        ga.w_inverse = w_inverse;
+        ga.x_exponent = x_exponent;
+        ga.w_exponent = w_exponent;
         with_tile<Scaled>(p.f2, n, false, [&](auto block) {
             using B = decltype(block);
             ga.n_tiles = (p.f2 + B::kCols - 1) / B::kCols;
