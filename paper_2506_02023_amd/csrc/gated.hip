@@ -26,10 +26,12 @@ template <class Fn> int with_kind(int32_t dtype, Fn &&f)
     return f(Kind<_Float16, 1, _Float16>{});
 }
 int parts_of(int32_t dtype) { return dtype == MLIP_DTYPE_F32 ? 3 : 1; }
-// Wide fp32 rows of the forward call: two fp16 parts (22 bits) and three products, half the matrix time.  Every row of x and column of the weights is brought by a
-// power of two to a largest value in [2^13, 2^14), so that a value has its 22 bits down to 2^-24 of its row's largest and is off by 2^-38 of that below.
-// (32,768 x 512 x 1365: 381 us, with three bf16 parts 712.)
+// g and v of fp32 arrays: two fp16 parts (22 bits) and three products, half the matrix time, where that is what bounds (wide rows of the forward call) or registers are
+// short (rows of up to 128 features).  Every row of x and column of the weights is brought by a power of two to a largest value in [2^13, 2^14), so that a value has its 22 bits
+// down to 2^-24 of its row's largest and is off by 2^-38 of that below.  (32,768 x 512 x 1365: 381 us, with three bf16 parts 712; 300,000 x 128 x 256: 214 and 361; the gradient's
+// g and v of 202,612 x 128 x 341: 421 and 588.)
 using Scaled = Kind<_Float16, 2, float>;
+template <class K> using Inner = std::conditional_t<K::kParts == 3, Scaled, K>;   // in what k_gates_narrow computes g and v
 
 // Column c of the 2 f: the feature, and whether of v
 __host__ __device__ inline int64_t feature_of(int64_t c) { return c / 64 * 32 + c % 32; }
@@ -116,6 +118,51 @@ __global__ __launch_bounds__(kPackThreads) void k_column_scales(Weights<Scaled> 
     const int e = scale_for(m);
     scale[c] = ldexpf(1.f, e);
     exponent[c] = (float)e;
+}
+
+// The weights for k_gates_narrow in fp32, all of up to 128 rows of 32 columns in a block: `across` scaled and in two fp16 parts, the scales' exponents, and `down` as
+// k_pack_weights makes it
+template <class K> __global__ __launch_bounds__(kPackThreads) void k_pack_scaled_weights(Weights<K> w, int64_t d_p, _Float16 *across, float *exponent)
+{
+    __shared__ float tile[kNarrow][33], most[kPackThreads / 32][32];
+    const int64_t c0 = (int64_t)blockIdx.x * 32, f0 = feature_of(c0);
+    const bool value = is_value(c0);
+    const typename K::E *src = value ? w.wv : w.wg;
+    const int64_t rs = value ? w.v_rs : w.g_rs, cs = value ? w.v_cs : w.g_cs;
+    const int a = threadIdx.x & 31, b = threadIdx.x >> 5;
+    const bool by_row = cs <= rs;
+#pragma unroll
+    for (int k = 0; k < kNarrow / 32; ++k) {
+        if (k * 32 >= d_p) break;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int i = b + 8 * j, dd = k * 32 + (by_row ? i : a), ff = by_row ? a : i;
+            tile[dd][ff] = dd < w.d && f0 + ff < w.f ? (float)src[dd * rs + (f0 + ff) * cs] : 0.f;
+        }
+    }
+    __syncthreads();
+    float m = 0.f;
+    for (int dd = b; dd < d_p; dd += 8) m = fmaxf(m, fabsf(tile[dd][a]));
+    most[b][a] = m;
+    __syncthreads();
+    for (int j = 0; j < 4; ++j) {
+        const int i = b + 8 * j;   // column
+        m = 0.f;
+        for (int k = 0; k < kPackThreads / 32; ++k) m = fmaxf(m, most[k][i]);
+        const int e = scale_for(m);
+        if (a == 0) exponent[c0 + i] = (float)e;
+        for (int64_t dd = a; dd < d_p; dd += 32) {
+            _Float16 v[2];
+            split(tile[dd][i] * ldexpf(1.f, e), v);
+            for (int p = 0; p < 2; ++p) across[p * w.across_part + (c0 + i) * w.d_ld + dd] = v[p];
+        }
+    }
+    if (!w.down) return;
+    for (int64_t dd = b; dd < w.d; dd += 8) {
+        typename K::T v[K::kParts];
+        split(tile[dd][a], v);
+        for (int p = 0; p < K::kParts; ++p) w.down[p * w.down_part + dd * w.f2_ld + c0 + a] = v[p];
+    }
 }
 
 // Rows of x scaled and in parts, a wavefront each; zeros from `cols` on
@@ -278,44 +325,53 @@ template <class K, class B, bool BACK> __global__ __launch_bounds__(B::kThreads)
     if constexpr (B::kPer == 128) finish(&acc[2], n0 + B::first(wave) + 64);
 }
 
-// Rows of up to 128 features, one after another in x and in the gradient: a block keeps the weights of PAIRS times 32 + 32 columns in LDS, in the order in which the lanes take them, and its
+// Rows of up to 128 features (STRIDED: which, or those of the gradient, do not lie one after another; the same bits): a block keeps the weights of PAIRS times 32 + 32 columns in LDS, in the order in which the lanes take them, and its
 // wavefronts go over the rows, 32 at a time and without a barrier, each with its rows in registers (fp32 split there).  Such calls are bound by memory: rows come and go
 // once for each such group of columns (from the L2 for all but the first), and nothing is laid out before.
 template <class K, int STEPS> struct NarrowShape {
-    static constexpr int kDp = STEPS * 16, kPairs = (K::kParts == 1 ? 256 : 128) / kDp, kFrags = kPairs * 2 * STEPS * K::kParts;   // 32 or 48 KB of weights
+    static constexpr int kDp = STEPS * 16, kPairs = (K::kParts == 1 ? 256 : 128) / kDp, kFrags = kPairs * 2 * STEPS * Inner<K>::kParts;   // 32 KB of weights
     static constexpr int kStage = 32 * 72;   // elements of 16 bits for a wavefront's results on their way out: 32 rows of 64 and 8 (or of 32 and 4 fp32)
 };
 template <class K> struct NarrowArgs {
     GateArgs<K> a;           // (x: rows of the chunk as the caller has them)
-    int64_t groups, tiles;   // groups of columns; runs of 32 rows
+    int64_t x_cs, groups, tiles;   // groups of columns; runs of 32 rows
     int32_t blocks;          // of a group
 };
 
-template <class K, int STEPS, bool BACK> __global__ __launch_bounds__(256, K::kParts == 1 && !BACK ? 3 : 2) void k_gates_narrow(NarrowArgs<K> na)
+template <class K, int STEPS, bool BACK, bool STRIDED> __global__ __launch_bounds__(256, K::kParts == 1 && !BACK ? 3 : 2) void k_gates_narrow(NarrowArgs<K> na)
 {
     using T = typename K::T;
     using E = typename K::E;
+    using C = typename Inner<K>::T;
     using S = NarrowShape<K, STEPS>;
-    constexpr int PARTS = K::kParts;
-    __shared__ alignas(16) T weights[S::kFrags * 512];
+    constexpr int PARTS = Inner<K>::kParts;
+    constexpr bool SCALED = std::is_same_v<Inner<K>, Scaled>;
+    __shared__ alignas(16) C weights[S::kFrags * 512];
+    __shared__ alignas(16) float exponents[2][SCALED ? S::kPairs * 32 : 4];
     __shared__ alignas(16) T stage_[4 * S::kStage];
     __shared__ alignas(16) float bias[2][S::kPairs * 32];
     const GateArgs<K> &a = na.a;
     const int64_t at = xcd_order(blockIdx.x, gridDim.x);
     const int64_t group = at % na.groups, col_first = group * S::kPairs * 64;
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, half = lane >> 5, d = (int)a.x.cols;
-    const T *across = static_cast<const T *>(a.w.p);
+    const C *across = static_cast<const C *>(a.w.p);
+#pragma unroll 4
     for (int k = threadIdx.x; k < S::kFrags * 64; k += 256) {
         const int l = k & 63, f = k >> 6, p = f % PARTS, kk = f / PARTS % STEPS, c = f / PARTS / STEPS;
         const int64_t col = col_first + c * 32 + (l & 31);
-        Half8<T> w = {};
-        if (col < a.w.rows && kk * 16 < a.w.cols) w = *reinterpret_cast<const Half8<T> *>(across + p * a.w.part + col * a.w.ld + kk * 16 + (l >> 5) * 8);
-        *reinterpret_cast<Half8<T> *>(weights + k * 8) = w;
+        Half8<C> w = {};
+        if (col < a.w.rows && kk * 16 < a.w.cols) w = *reinterpret_cast<const Half8<C> *>(across + p * a.w.part + col * a.w.ld + kk * 16 + (l >> 5) * 8);
+        *reinterpret_cast<Half8<C> *>(weights + k * 8) = w;
     }
     for (int k = threadIdx.x; k < S::kPairs * 32; k += 256) {
         const int64_t f = col_first / 2 + k;
         bias[0][k] = a.bg && f < a.f ? (float)a.bg[f] : 0.f;
         bias[1][k] = a.bv && f < a.f ? (float)a.bv[f] : 0.f;
+        if constexpr (SCALED) {
+            const int64_t col = col_first + k / 32 * 64 + k % 32;
+            exponents[0][k] = col < a.w.rows ? a.w_exponent[col] : 0.f;
+            exponents[1][k] = col < a.w.rows ? a.w_exponent[col + 32] : 0.f;
+        }
     }
     __syncthreads();
     T *stage = stage_ + wave * S::kStage;
@@ -327,20 +383,35 @@ template <class K, int STEPS, bool BACK> __global__ __launch_bounds__(256, K::kP
     };
     for (int64_t tile = at / na.groups * 4 + wave; tile < na.tiles; tile += (int64_t)na.blocks * 4) {
         const int64_t row0 = tile * 32, mine = row0 + (lane & 31), row = mine < a.x.rows ? mine : a.x.rows - 1;
-        Half8<T> fx[STEPS][PARTS];
+        Half8<C> fx[STEPS][PARTS];
+        float ex = 0.f;
+        if constexpr (!SCALED) {
 #pragma unroll
-        for (int kk = 0; kk < STEPS; ++kk) {
-            if constexpr (PARTS == 1) {
+            for (int kk = 0; kk < STEPS; ++kk) {
                 const int c = kk * 16 + half * 8;
                 const E *p = x + row * a.x.ld;
-                if (c + 8 <= d) fx[kk][0] = *reinterpret_cast<const Far<E, 8> *>(p + c);
+                if (!STRIDED && c + 8 <= d) fx[kk][0] = *reinterpret_cast<const Far<E, 8> *>(p + c);
                 else
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) fx[kk][0][k] = c + k < d ? p[c + k] : (E)0.f;
-            } else {
-                float v[8];
-                load_cols(v, x + row * a.x.ld, 1, kk * 16 + half * 8, d);
-                split_cols<T>(v, fx[kk]);
+                    for (int k = 0; k < 8; ++k) fx[kk][0][k] = c + k < d ? p[(c + k) * (STRIDED ? na.x_cs : 1)] : (E)0.f;
+            }
+        } else {   // (the two halves of the wavefront have half of a row's features each)
+            float v[STEPS][8], m = 0.f;
+#pragma unroll
+            for (int kk = 0; kk < STEPS; ++kk) load_cols(v[kk], x + row * a.x.ld, STRIDED ? na.x_cs : 1, kk * 16 + half * 8, d);
+#pragma unroll
+            for (int kk = 0; kk < STEPS; ++kk)
+#pragma unroll
+                for (int k = 0; k < 8; ++k) m = fmaxf(m, fabsf(v[kk][k]));
+            m = fmaxf(m, __shfl_xor(m, 32));
+            const int e = scale_for(m);
+            const float scale = ldexpf(1.f, e);
+            ex = (float)e;
+#pragma unroll
+            for (int kk = 0; kk < STEPS; ++kk) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[kk][k] *= scale;
+                split_cols<C>(v[kk], fx[kk]);
             }
         }
 #pragma unroll 1
@@ -350,19 +421,19 @@ template <class K, int STEPS, bool BACK> __global__ __launch_bounds__(256, K::kP
             float bar[4][4];
             if constexpr (BACK)
 #pragma unroll
-                for (int q = 0; q < 4; ++q) load_cols(bar[q], a.bar + row * a.bar_rs, 1, f0 + acc_row(4 * q), a.f);
+                for (int q = 0; q < 4; ++q) load_cols(bar[q], a.bar + row * a.bar_rs, STRIDED ? a.bar_cs : 1, f0 + acc_row(4 * q), a.f);
             f32x16 g = {}, v = {};
 #pragma unroll
             for (int kk = 0; kk < STEPS; ++kk) {
-                Half8<T> wg[PARTS], wv[PARTS];
+                Half8<C> wg[PARTS], wv[PARTS];
 #pragma unroll
                 for (int p = 0; p < PARTS; ++p) {
-                    wg[p] = *reinterpret_cast<const Half8<T> *>(weights + (((pair * 2 * STEPS + kk) * PARTS + p) * 64 + lane) * 8);
-                    wv[p] = *reinterpret_cast<const Half8<T> *>(weights + ((((pair * 2 + 1) * STEPS + kk) * PARTS + p) * 64 + lane) * 8);
+                    wg[p] = *reinterpret_cast<const Half8<C> *>(weights + (((pair * 2 * STEPS + kk) * PARTS + p) * 64 + lane) * 8);
+                    wv[p] = *reinterpret_cast<const Half8<C> *>(weights + ((((pair * 2 + 1) * STEPS + kk) * PARTS + p) * 64 + lane) * 8);
                 }
                 for_products<PARTS>([&](int p, int q) {
-                    g = mfma<T>(wg[p], fx[kk][q], g);
-                    v = mfma<T>(wv[p], fx[kk][q], v);
+                    g = mfma<C>(wg[p], fx[kk][q], g);
+                    v = mfma<C>(wv[p], fx[kk][q], v);
                 });
                 if (kk % 2) __builtin_amdgcn_sched_barrier(0);   // (else all fragments are fetched at once, into registers that there are not)
             }
@@ -373,6 +444,14 @@ template <class K, int STEPS, bool BACK> __global__ __launch_bounds__(256, K::kP
                     const int64_t f = f0 + acc_row(4 * q);
                     const int c = pair * 32 + acc_row(4 * q);
                     const Cols<float, 4> bg = *reinterpret_cast<const Cols<float, 4> *>(bias[0] + c), bv = *reinterpret_cast<const Cols<float, 4> *>(bias[1] + c);
+                    if constexpr (SCALED) {
+                        const Cols<float, 4> eg = *reinterpret_cast<const Cols<float, 4> *>(exponents[0] + c), ev = *reinterpret_cast<const Cols<float, 4> *>(exponents[1] + c);
+#pragma unroll
+                        for (int t = 0; t < 4; ++t) {
+                            g[4 * q + t] = ldexpf(g[4 * q + t], -(int)(ex + eg[t]));
+                            v[4 * q + t] = ldexpf(v[4 * q + t], -(int)(ex + ev[t]));
+                        }
+                    }
                     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                     for (int t = 0; t < 4; ++t) {
@@ -411,7 +490,7 @@ template <class K, int STEPS, bool BACK> __global__ __launch_bounds__(256, K::kP
                 }
             } else {
 #pragma unroll
-                for (int p = 0; p < PARTS; ++p) {
+                for (int p = 0; p < K::kParts; ++p) {
                     fence();
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
@@ -420,7 +499,7 @@ template <class K, int STEPS, bool BACK> __global__ __launch_bounds__(256, K::kP
                         for (int t = 0; t < 4; ++t) {
                             gp[t] = to_elem<T>(g[4 * q + t]);
                             vp[t] = to_elem<T>(v[4 * q + t]);
-                            if (p + 1 < PARTS) {
+                            if (p + 1 < K::kParts) {
                                 g[4 * q + t] -= (float)gp[t];
                                 v[4 * q + t] -= (float)vp[t];
                             }
@@ -641,10 +720,8 @@ Plan plan_of(const GatedArgs &a, bool grad)
     auto take = [&](int64_t bytes) { const size_t here = at; at += (size_t)pad_to(bytes, 256); return here; };
     p.across = take(p.f2 * p.d_ld * p.parts * 2);
     p.xs = take(p.chunk * p.d_ld * p.parts * 2);
-    if (by_scale(a, grad)) {
-        p.x_exponent = take(p.chunk * 4);
-        p.w_scale = take(2 * p.f2 * 4);
-    }
+    if (by_scale(a, grad)) p.x_exponent = take(p.chunk * 4);
+    if (a.dtype == MLIP_DTYPE_F32) p.w_scale = take(2 * p.f2 * 4);
     if (grad) {
         p.down = take(a.d * p.gv_ld * p.parts * 2);
         p.gv = take(p.chunk * p.gv_ld * p.parts * 2);
@@ -670,11 +747,15 @@ template <class K> int launch(const GatedArgs &a, const GatedGrad *g)
     char *ws = static_cast<char *>(a.workspace);
     T *across = reinterpret_cast<T *>(ws + p.across), *down = g ? reinterpret_cast<T *>(ws + p.down) : nullptr, *xs = reinterpret_cast<T *>(ws + p.xs);
     T *gv = g ? reinterpret_cast<T *>(ws + p.gv) : nullptr;
-    const bool in_registers = a.d <= kNarrow && a.x_cs == 1 && (!g || g->bar_cs == 1);
+    const bool in_registers = a.d <= kNarrow, strided = a.x_cs != 1 || (g && g->bar_cs != 1);
     const bool rows = !g || g->dx, weights = g && (g->dwg || g->dwv || g->dbg || g->dbv);
     const Weights<K> w = {static_cast<const E *>(a.wg), static_cast<const E *>(a.wv), a.wg_rs, a.wg_cs, a.wv_rs, a.wv_cs, a.d, a.f, p.d_ld, p.gv_ld,
                           across, rows ? down : nullptr, p.f2 * p.d_ld, a.d * p.gv_ld};
-    if (a.n > 0) k_pack_weights<K><<<dim3((unsigned)(p.f2 / 32), (unsigned)(p.d_p / 32)), kPackThreads, 0, a.stream>>>(w);
+    float *w_exponent = reinterpret_cast<float *>(ws + p.w_scale);
+    if (a.n > 0 && in_registers && K::kParts == 3) {
+        if constexpr (K::kParts == 3)
+            k_pack_scaled_weights<K><<<(unsigned)(p.f2 / 32), kPackThreads, 0, a.stream>>>(w, p.d_p, reinterpret_cast<_Float16 *>(across), w_exponent);
+    } else if (a.n > 0) k_pack_weights<K><<<dim3((unsigned)(p.f2 / 32), (unsigned)(p.d_p / 32)), kPackThreads, 0, a.stream>>>(w);
     const Panel across_panel = {across, p.d_ld, p.f2 * p.d_ld, p.f2, p.d_p}, down_panel = {down, p.gv_ld, a.d * p.gv_ld, a.d, p.f2};
     int64_t first = 0;
     do {
@@ -702,11 +783,13 @@ template <class K> int launch(const GatedArgs &a, const GatedGrad *g)
             }
             auto narrow = [&](auto steps) {
                 constexpr int STEPS = decltype(steps)::value;
-                NarrowArgs<K> na = {ga, (p.f2 + NarrowShape<K, STEPS>::kPairs * 64 - 1) / (NarrowShape<K, STEPS>::kPairs * 64), (n + 31) / 32, 0};
+                NarrowArgs<K> na = {ga, a.x_cs, (p.f2 + NarrowShape<K, STEPS>::kPairs * 64 - 1) / (NarrowShape<K, STEPS>::kPairs * 64), (n + 31) / 32, 0};
                 na.a.x = {x, a.x_rs, 0, n, a.d};
+                na.a.w_exponent = w_exponent;
                 const int64_t most = kNarrowBlocks / na.groups > 0 ? kNarrowBlocks / na.groups : 1, blocks = (na.tiles + 3) / 4;
                 na.blocks = (int32_t)(blocks < most ? blocks : most);
-                (g ? k_gates_narrow<K, STEPS, true> : k_gates_narrow<K, STEPS, false>)<<<(unsigned)(na.blocks * na.groups), 256, 0, a.stream>>>(na);
+                (strided ? g ? k_gates_narrow<K, STEPS, true, true> : k_gates_narrow<K, STEPS, false, true>
+                         : g ? k_gates_narrow<K, STEPS, true, false> : k_gates_narrow<K, STEPS, false, false>)<<<(unsigned)(na.blocks * na.groups), 256, 0, a.stream>>>(na);
             };
             if (in_registers && a.d <= 64) narrow(std::integral_constant<int, 4>{});
             else if (in_registers) narrow(std::integral_constant<int, 8>{});

@@ -110,24 +110,25 @@ def test_wide_fp32_rows(n, d, f, turned):
     _both(n, d, f, "float32", ACTS[(n + d) % 4], turned=turned, gap=(n + f) % 3, bias=n % 4 == 0)
 
 
-def test_wide_fp32_rows_of_all_sizes():
+@pytest.mark.parametrize("d", [160, 128, 61])
+def test_fp32_rows_of_all_sizes(d):
     """Rows from 2^-90 to 2^122 and columns from 2^-32 to 2^31, some of them zero or not finite: each as exact as if it were alone"""
     import torch
     import paper_2506_02023_amd as M
-    bar, (x, wg, wv, _, _) = _make(1100, 160, 64, torch.float32, bias=False)
+    bar, (x, wg, wv, _, _) = _make(1100, d, 64, torch.float32, bias=False)
     x = x * torch.exp2(torch.arange(1100, device="cuda") % 213 - 90.0)[:, None]
     wv = wv * torch.exp2(torch.arange(64, device="cuda") - 32.0)[None, :]
     wv[:, 40:] *= torch.exp2(torch.tensor(-90.0, device="cuda"))      # (columns from 2^-82 on)
     x[5], wv[:, 7] = 0.0, 0.0
     h, tol, _, _ = _reference(bar, (x, wg, wv, None, None), "sigmoid")
     got = M.mlip_gated(x, wg, wv, act="sigmoid")
-    # v itself has to be an fp32 number: with rows of 2^122, columns of 2^31 and 160 terms it reaches 2^160, beyond 2^128 it is infinite in fp32 and sigmoid(g) = 0 times it NaN
+    # v itself has to be an fp32 number: with rows of 2^122, columns of 2^31 and d terms it reaches 2^153 and more, beyond 2^128 it is infinite in fp32 and sigmoid(g) = 0 times it NaN
     fits = (x.double() @ wv.double()).abs() < 2.0 ** 126
     _check(torch.where(fits, got, 0.0), torch.where(fits, h, 0.0), tol + 2.0 ** -140, "h")      # (what is below the normal numbers may go to zero)
     assert bool(fits[:, :30].double().mean() > 0.5) and bool(fits[:, 40:].all())
     assert bool((got[5] == 0).all()) and bool((got[:, 7] == 0).all())
     x2 = x.clone()
-    x2[17, 3], x2[1099, 159] = float("nan"), float("inf")
+    x2[17, 3], x2[1099, d - 1] = float("nan"), float("inf")
     got2 = M.mlip_gated(x2, wg, wv, act="sigmoid")
     keep = torch.ones(1100, dtype=torch.bool, device="cuda")
     keep[[17, 1099]] = False
