@@ -96,8 +96,8 @@ __global__ __launch_bounds__(kThreads) void k_squares(List l, double *part)
 // What X_0 is G times, x_scale included
 __device__ inline double start_scale(double squares, double eps, float x_scale)
 {
-    const double norm = sqrt(squares);
-    return (double)x_scale / (norm > eps || norm != norm ? norm : eps);
+    const double norm = sqrt(squares), by = norm > eps || norm != norm ? norm : eps;
+    return by == 0.0 ? (double)x_scale : (double)x_scale / by;   // (zeros stay zeros)
 }
 
 // X_0 in parts: tiles of 64 rows and 64 columns, zeros up to n_p.  Loads and stores go along what lies close together, eight elements a thread.
@@ -315,8 +315,7 @@ template <int PARTS, class B, bool LAST> __global__ __launch_bounds__(B::kThread
 __global__ __launch_bounds__(kThreads) void k_normed(List l, const double *part, double eps, float scale)
 {
     const Item &it = l.item[blockIdx.y];
-    const double norm = sqrt(block_sum(threadIdx.x < kNormBlocks ? part[blockIdx.y * kNormBlocks + threadIdx.x] : 0.0));
-    const double f = (double)scale / (norm > eps || norm != norm ? norm : eps);
+    const double f = start_scale(block_sum(threadIdx.x < kNormBlocks ? part[blockIdx.y * kNormBlocks + threadIdx.x] : 0.0), eps, scale);
     device_elem(it.dtype, [&](auto e) {
         using E = decltype(e);
         const int64_t total = (int64_t)it.m * it.n;

@@ -121,7 +121,8 @@ def test_sizes_of_gradients():
             assert torch.equal(M.mlip_orthogonalise([g * f], eps=0.0)[0], one)
         small = g / g.norm() * 1e-9
         _check(M.mlip_orthogonalise([small.clone()], eps=1e-7)[0], small, eps=1e-7)
-        assert bool((M.mlip_orthogonalise([torch.zeros(shape, device="cuda")])[0] == 0).all())
+        for eps, steps in ((1e-7, 5), (0.0, 5), (0.0, 0)):
+            assert bool((M.mlip_orthogonalise([torch.zeros(shape, device="cuda")], eps=eps, steps=steps)[0] == 0).all())
 
 
 def test_decaying_singular_values():
