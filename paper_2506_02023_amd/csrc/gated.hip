@@ -337,7 +337,7 @@ template <class K, int STEPS> struct NarrowShape {
 template <class K> struct NarrowArgs {
     GateArgs<K> a;           // (x: rows of the chunk as the caller has them)
     int64_t x_cs, groups, tiles;   // groups of columns; runs of 32 rows
-    int32_t blocks;          // of a group
+    int32_t blocks, pairs;   // of a group; pairs of 32 columns in a group, NarrowShape's or, where that leaves compute units idle, one
 };
 
 template <class K, int STEPS, bool BACK, bool STRIDED> __global__ __launch_bounds__(256, K::kParts == 1 && !BACK ? 3 : 2) void k_gates_narrow(NarrowArgs<K> na)
@@ -354,18 +354,19 @@ template <class K, int STEPS, bool BACK, bool STRIDED> __global__ __launch_bound
     __shared__ alignas(16) float bias[2][S::kPairs * 32];
     const GateArgs<K> &a = na.a;
     const int64_t at = xcd_order(blockIdx.x, gridDim.x);
-    const int64_t group = at % na.groups, col_first = group * S::kPairs * 64;
+    const int pairs = S::kPairs == 1 ? 1 : na.pairs;
+    const int64_t group = at % na.groups, col_first = group * pairs * 64;
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, half = lane >> 5, d = (int)a.x.cols;
     const C *across = static_cast<const C *>(a.w.p);
 #pragma unroll 4
-    for (int k = threadIdx.x; k < S::kFrags * 64; k += 256) {
+    for (int k = threadIdx.x; k < pairs * (2 * STEPS * PARTS * 64); k += 256) {
         const int l = k & 63, f = k >> 6, p = f % PARTS, kk = f / PARTS % STEPS, c = f / PARTS / STEPS;
         const int64_t col = col_first + c * 32 + (l & 31);
         Half8<C> w = {};
         if (col < a.w.rows && kk * 16 < a.w.cols) w = *reinterpret_cast<const Half8<C> *>(across + p * a.w.part + col * a.w.ld + kk * 16 + (l >> 5) * 8);
         *reinterpret_cast<Half8<C> *>(weights + k * 8) = w;
     }
-    for (int k = threadIdx.x; k < S::kPairs * 32; k += 256) {
+    for (int k = threadIdx.x; k < pairs * 32; k += 256) {
         const int64_t f = col_first / 2 + k;
         bias[0][k] = a.bg && f < a.f ? (float)a.bg[f] : 0.f;
         bias[1][k] = a.bv && f < a.f ? (float)a.bv[f] : 0.f;
@@ -417,7 +418,7 @@ template <class K, int STEPS, bool BACK, bool STRIDED> __global__ __launch_bound
             }
         }
 #pragma unroll 1
-        for (int pair = 0; pair < S::kPairs; ++pair) {
+        for (int pair = 0; pair < pairs; ++pair) {
             const int64_t col0 = col_first + pair * 64, f0 = col0 / 2;
             if (col0 >= a.w.rows) break;
             float bar[4][4];
@@ -786,7 +787,8 @@ template <class K> int launch(const GatedArgs &a, const GatedGrad *g)
             }
             auto narrow = [&](auto steps) {
                 constexpr int STEPS = decltype(steps)::value;
-                NarrowArgs<K> na = {ga, a.x_cs, (p.f2 + NarrowShape<K, STEPS>::kPairs * 64 - 1) / (NarrowShape<K, STEPS>::kPairs * 64), (n + 31) / 32, 0};
+                const int64_t tiles = (n + 31) / 32, all = p.f2 / 64, pairs = (tiles + 3) / 4 * all < kFull ? 1 : NarrowShape<K, STEPS>::kPairs;
+                NarrowArgs<K> na = {ga, a.x_cs, (all + pairs - 1) / pairs, tiles, 0, (int32_t)pairs};
                 na.a.x = {x, a.x_rs, 0, n, a.d};
                 na.a.w_exponent = w_exponent;
                 const int64_t most = kNarrowBlocks / na.groups > 0 ? kNarrowBlocks / na.groups : 1, blocks = (na.tiles + 3) / 4;
