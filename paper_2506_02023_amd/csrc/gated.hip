@@ -645,28 +645,38 @@ template <class K> struct JoinArgs {
     typename K::E *dwg, *dwv, *dbg, *dbv;
     int64_t g_rs, g_cs, v_rs, v_cs;
 };
-template <class K> __global__ __launch_bounds__(kPackThreads) void k_join(JoinArgs<K> a)
+// RUNS: of splits that a block's threads take side by side and then join in order: four for 32 splits and more (512 splits of 256 x 64: 19 us, 57 one after another), else one
+template <class K, int RUNS> __global__ __launch_bounds__(256 * RUNS) void k_join(JoinArgs<K> a)
 {
-    __shared__ float tile[8][33];
+    __shared__ float tile[RUNS][8][33], sums[RUNS][8];
     const int64_t c0 = (int64_t)blockIdx.x * 8, d0 = (int64_t)blockIdx.y * 32, f0 = feature_of(c0);
     const bool value = is_value(c0);
     typename K::E *dw = value ? a.dwv : a.dwg, *db = value ? a.dbv : a.dbg;
     const int64_t rs = value ? a.v_rs : a.g_rs, cs = value ? a.v_cs : a.g_cs;
-    const int p = threadIdx.x & 31, q = threadIdx.x >> 5;
-    if (dw) {
-        float sum = 0.f;
-        if (d0 + p < a.d)
-            in_steps<8>(0, a.splits, 1, [&](int64_t s) { return a.part[(s * a.f2 + c0 + q) * a.d + d0 + p]; }, [&](float x) { sum += x; });
-        tile[q][p] = sum;   // [feature][d]
-        __syncthreads();
-        const bool by_row = cs <= rs;
-        const int dd = by_row ? (int)threadIdx.x >> 3 : p, ff = by_row ? (int)threadIdx.x & 7 : q;
-        if (d0 + dd < a.d && f0 + ff < a.f) dw[(d0 + dd) * rs + (f0 + ff) * cs] = to_elem<typename K::E>(tile[ff][dd]);
+    const int run = threadIdx.x >> 8, t = threadIdx.x & 255, p = t & 31, q = t >> 5;
+    const int64_t each = (a.splits + RUNS - 1) / RUNS, from = run * each, end = from + each < a.splits ? from + each : a.splits;
+    float sum = 0.f;
+    if (dw && d0 + p < a.d) in_steps<8>(from, end, 1, [&](int64_t s) { return a.part[(s * a.f2 + c0 + q) * a.d + d0 + p]; }, [&](float x) { sum += x; });
+    tile[run][q][p] = sum;   // [feature][d]
+    const bool bias = db && d0 == 0;
+    if (bias && t < 8) {
+        sum = 0.f;
+        in_steps<8>(from, end, 1, [&](int64_t s) { return a.bias[s * a.f2 + c0 + t]; }, [&](float x) { sum += x; });
+        sums[run][t] = sum;
     }
-    if (db && d0 == 0 && threadIdx.x < 8 && f0 + threadIdx.x < a.f) {
-        float sum = 0.f;
-        in_steps<8>(0, a.splits, 1, [&](int64_t s) { return a.bias[s * a.f2 + c0 + threadIdx.x]; }, [&](float x) { sum += x; });
-        db[f0 + threadIdx.x] = to_elem<typename K::E>(sum);
+    __syncthreads();
+    if (run) return;
+    const bool by_row = cs <= rs;
+    const int dd = by_row ? t >> 3 : p, ff = by_row ? t & 7 : q;
+    if (dw && d0 + dd < a.d && f0 + ff < a.f) {
+        sum = tile[0][ff][dd];
+        for (int k = 1; k < RUNS; ++k) sum += tile[k][ff][dd];
+        dw[(d0 + dd) * rs + (f0 + ff) * cs] = to_elem<typename K::E>(sum);
+    }
+    if (bias && t < 8 && f0 + t < a.f) {
+        sum = sums[0][t];
+        for (int k = 1; k < RUNS; ++k) sum += sums[k][t];
+        db[f0 + t] = to_elem<typename K::E>(sum);
     }
 }
 
@@ -846,7 +856,9 @@ template <class K> int launch(const GatedArgs &a, const GatedGrad *g)
     if (weights) {
         const JoinArgs<K> ja = {reinterpret_cast<float *>(ws + p.part), reinterpret_cast<float *>(ws + p.bias), p.splits, a.d, a.f, p.f2, static_cast<E *>(g->dwg),
                                 static_cast<E *>(g->dwv), static_cast<E *>(g->dbg), static_cast<E *>(g->dbv), g->dwg_rs, g->dwg_cs, g->dwv_rs, g->dwv_cs};
-        k_join<K><<<dim3((unsigned)(p.f2 / 8), (unsigned)((a.d + 31) / 32)), kPackThreads, 0, a.stream>>>(ja);
+        const dim3 blocks((unsigned)(p.f2 / 8), (unsigned)((a.d + 31) / 32));
+        if (p.splits >= 32) k_join<K, 4><<<blocks, 1024, 0, a.stream>>>(ja);
+        else k_join<K, 1><<<blocks, 256, 0, a.stream>>>(ja);
     }
     MLIP_HIP(hipGetLastError());
     return MLIP_OK;
