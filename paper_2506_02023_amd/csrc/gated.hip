@@ -255,7 +255,7 @@ template <class K> struct GateArgs {
 };
 
 // The weights are the products' first operand and the rows their second; a lane ends with neighbouring features of a row.  Bound by the matrix units, the activations behind
-// them: 32,768 x 1024 x 4096 bf16, backward, 729 us (0.75 PF; 1250 in tiles of 128 with four features a store).
+// them: 32,768 x 1024 x 4096 bf16, backward, 706 us (0.78 PF; 1250 in tiles of 128 with four features a store).
 template <class K, class B, bool BACK> __global__ __launch_bounds__(B::kThreads) void k_gates(GateArgs<K> a)
 {
     using T = typename K::T;
@@ -523,7 +523,7 @@ template <class K, int STEPS, bool BACK, bool STRIDED> __global__ __launch_bound
     }
 }
 
-// dx = [G V] [Wg Wv]^T.  32,768 x 8192 by 1024 bf16: 486 us (1.13 PF; in tiles of 128 690); 202,612 x 704 by 128 of three parts: 327 us (0.67 PF)
+// dx = [G V] [Wg Wv]^T.  32,768 x 8192 by 1024 bf16: 490 us (1.12 PF; in tiles of 128 690); 202,612 x 704 by 128 of three parts: 320 us (0.68 PF)
 template <class K> struct RowBarArgs {
     Panel gv, w;             // [rows][2 f], [d][2 f]
     int64_t n_tiles;
@@ -557,7 +557,7 @@ template <class K, class B> __device__ inline void row_bars(const RowBarArgs<K> 
 }
 
 // The chunk's share of [dWg dWv]^T = [G V]^T x, [2 f][d], its rows in `splits` runs; and of the biases' gradients, the column sums of G and V.
-// 32,768 x 8192 by 1024 bf16: 674 us (0.81 PF; in tiles of 128 773); 202,612 x 704 by 128 of three parts: 319 us
+// 32,768 x 8192 by 1024 bf16: 655 us (0.84 PF; in tiles of 128 773); 202,612 x 704 by 128 of three parts: 316 us
 template <class K> struct WeightSumArgs {
     Panel gv, x;             // [rows][2 f], [rows][d]
     int64_t d, m_tiles, n_tiles, run;   // rows of a run, a multiple of a step
