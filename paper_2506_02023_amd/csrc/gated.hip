@@ -733,7 +733,7 @@ Plan plan_of(const GatedArgs &a, bool grad)
     size_t at = 0;
     auto take = [&](int64_t bytes) { const size_t here = at; at += (size_t)pad_to(bytes, 256); return here; };
     p.across = take(p.f2 * p.d_ld * p.parts * 2);
-    p.xs = take(p.chunk * p.d_ld * p.parts * 2);
+    if (grad || a.d > kNarrow) p.xs = take(p.chunk * p.d_ld * p.parts * 2);
     if (by_scale(a, grad)) p.x_exponent = take(p.chunk * 4);
     if (a.dtype == MLIP_DTYPE_F32) p.w_scale = take(2 * p.f2 * 4);
     if (grad) {
