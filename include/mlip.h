@@ -580,8 +580,8 @@ typedef struct {
 /*
  * Orthogonalises the matrices of a list (gradients or their running means, before an optimiser's update): X_0 = G / max(|G|, eps) with |G| the root of the sum of
  * squares, then `steps` times X <- (a + b X X^T + c (X X^T)^2) X, of the transpose where a matrix has more rows than columns; dst = scale * X.
- * |G| is summed in fp64.  X and the products X X^T are held in two fp16 parts (22 bits), sums are fp32; the products of bf16 matrices that have more than a few ten thousand
- * elements take one part of X and of what is off the diagonals, which leaves the result off by about 1e-3 (norm of the difference by norm) beside its own rounding's 1.7e-3.
+ * |G| is summed in fp64.  X and the products X X^T are held in two fp16 parts (22 bits), sums are fp32, for matrices of all types: results are as of fp32 arithmetic, rounded
+ * to the type once.
  * Entries of X must stay below 2^11 / sqrt(columns) and those off the diagonals of the polynomials below 2^7, which coefficients hold that keep singular values
  * in [0, 1] below 1.3 (larger ones become infinite or NaN).
  * A matrix with values that are not finite gets none that is; one of zeros stays so.  The same matrix must not be in the list twice.

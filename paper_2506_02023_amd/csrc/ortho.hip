@@ -4,10 +4,9 @@
 // A step is three products: A = X X^T and B = b A + c A A, which are symmetric (the tiles above the diagonal are computed and written twice), and
 // a X + B X.  The steps stretch small singular values by a each, up to a^5 = 485 times in all, and with them what a rounding of X put there: X is
 // therefore held in two fp16 parts (22 bits).  The diagonals of A and B, which are large against the rest, are kept in fp32 beside them and enter the
-// next result element by element: X' = (a + diag B) X + (B - diag B) X.  Only what is left goes through the matrix units,
-//   fp32 and fp16 matrices: in two parts each, three products, at the precision of fp32;
-//   bf16 matrices: rounded to fp16, one product.  The result is then off by 0.4 to 1.2e-3 (norm of the difference by norm; gradients of shared directions
-//   and noise 5e-4, singular values down to 10^-5 1.2e-3) beside the 1.7e-3 of its own rounding; with the diagonals rounded too it would be 2e-3.
+// next result element by element: X' = (a + diag B) X + (B - diag B) X.  Only what is left goes through the matrix units, in two parts and three
+// products, at the precision of fp32 for all types.  (One part would do for bf16 matrices of noise: 5e-4 of the norm beside the 1.7e-3 of the result's own rounding, in half the
+// time.  But where elements share a few sizes, as in a matrix of ones and signs, their roundings do not average out, and the result is off by 1.2e-2.)
 // Powers of two bring the entries into the range of fp16: X holds at most |X| <= 1.3 (for coefficients that keep it there), entries of the size 1/sqrt(n).
 #include "products.h"
 
@@ -182,10 +181,10 @@ __device__ inline void triangle(int t, int tiles, int &i, int &j)
 }
 
 // SQUARE: B = b A + c A A; else A = X X^T.  Off the diagonal with D = diag A, R = A - D:  A A = R R + (D_i + D_j) R_ij, on it D_i^2 + (R R)_ii.
-// Twelve matrices of 1024 x 4096, one part: A 85 us (0.60 PF), B 31.
-template <int PARTS, bool SQUARE> __global__ __launch_bounds__(kThreads) void k_symmetric(List l, P *ws, int which, float b, float c)
+// Twelve matrices of 1024 x 4096: A 201 us (0.86 PF), B 63.
+template <bool SQUARE> __global__ __launch_bounds__(kThreads) void k_symmetric(List l, P *ws, int which, float b, float c)
 {
-    using M = Product<P, PARTS, true, true, 128, 128, 64, 64>;
+    using M = Product<P, 2, true, true, 128, 128, 64, 64>;
     __shared__ typename M::Lds lds;
     uint32_t at;
     const Item &it = l.item[item_of(l, (uint32_t)xcd_order(blockIdx.x, gridDim.x), at)];
@@ -236,7 +235,7 @@ template <int PARTS, bool SQUARE> __global__ __launch_bounds__(kThreads) void k_
         Half8<P> v[2];
         split_cols<P>(y, v);
 #pragma unroll
-        for (int p = 0; p < (SQUARE ? PARTS : 2); ++p) *reinterpret_cast<Half8<P> *>(to + p * part + here) = v[p];
+        for (int p = 0; p < 2; ++p) *reinterpret_cast<Half8<P> *>(to + p * part + here) = v[p];
         if (tj > ti) turned.set(y, r, lane % 8 * 8);
     }
     if (tj == ti) return;
@@ -251,64 +250,63 @@ template <int PARTS, bool SQUARE> __global__ __launch_bounds__(kThreads) void k_
         Half8<P> v[2];
         split_cols<P>(y, v);
 #pragma unroll
-        for (int p = 0; p < (SQUARE ? PARTS : 2); ++p) *reinterpret_cast<Half8<P> *>(to + p * part + (int64_t)row * ld + col) = v[p];
+        for (int p = 0; p < 2; ++p) *reinterpret_cast<Half8<P> *>(to + p * part + (int64_t)row * ld + col) = v[p];
     }
 }
 
 // X' = (a + diag B) X + (B - diag B) X; the last one to where it belongs, times `scale`.  Columns of X are the first operand, its rows the second.
-// Twelve matrices of 1024 x 4096, one part: 194 us, of which both parts of X read and written (400 MB) are 80; in tiles of 128 214.
-template <int PARTS, class B, bool LAST> __global__ __launch_bounds__(B::kThreads) void k_apply(List l, P *ws, int which, float a, float scale)
+// Twelve matrices of 1024 x 4096: 387 us (0.80 PF), of which both parts of X read and written (400 MB) are 80.  (In tiles of 256 the whole call takes 2.99 ms for 3.08, but lists of
+// fewer or smaller ones leave compute units idle: two of 1024 x 1024 766 us for 552, 24 of 512 x 512 520 for 420.)
+template <bool LAST> __global__ __launch_bounds__(Middle::kThreads) void k_apply(List l, P *ws, int which, float a, float scale)
 {
-    using M = typename B::template Of<P, PARTS, false, true>;
+    using B = Middle;
+    using M = typename B::template Of<P, 2, false, true>;
     __shared__ typename M::Lds lds;
     uint32_t at;
     const Item &it = l.item[item_of(l, (uint32_t)xcd_order(blockIdx.x, gridDim.x), at)];
     const int tiles = (it.m + B::kRows - 1) / B::kRows, m0 = at % tiles * B::kRows, n0 = at / tiles * B::kCols;   // (tiles of the same columns one after another)
-    f32x16 acc[B::kPer / 32][2] = {};
+    f32x16 acc[2][2] = {};
     M::run(x_panel(it, ws, which), square_panel(it, ws, it.poly), n0, m0, 0, it.m_p, lds, acc, NoEach{});
     __syncthreads();
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, c = lane % 8 * 8;
     const Turned turned{reinterpret_cast<float *>(&lds) + wave * 4096};
     const P *old = ws + it.x[which], *old_low = ws + it.low[which];
-    P *to = ws + it.x[which ^ 1], *to_low = ws + it.low[which ^ 1];   // (of one part the low ones stay where they are)
+    P *to = ws + it.x[which ^ 1], *to_low = ws + it.low[which ^ 1];
     const float *diag = reinterpret_cast<const float *>(ws + it.diag) + it.m;
-    auto finish = [&](const f32x16 (*part)[2], int col) {   // 64 columns of a wavefront
-        turned.put(part);
-        if (col >= it.n_p) return;
+    turned.put(acc);
+    const int col = n0 + B::first(wave) + c;
+    if (col >= it.n_p) return;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const int r = lane / 8 + 8 * k, row = m0 + B::second(wave) + r;
-            if (row >= it.m) continue;
-            const int64_t here = (int64_t)row * it.n_ld + col;
-            const Half8<P> hi = *reinterpret_cast<const Half8<P> *>(old + here), lo = *reinterpret_cast<const Half8<P> *>(old_low + here);
-            const float f = a + diag[row];
-            float y[8];
-            turned.get(y, r, c);
+    for (int k = 0; k < 8; ++k) {
+        const int r = lane / 8 + 8 * k, row = m0 + B::second(wave) + r;
+        if (row >= it.m) continue;
+        const int64_t here = (int64_t)row * it.n_ld + col;
+        const Half8<P> hi = *reinterpret_cast<const Half8<P> *>(old + here), lo = *reinterpret_cast<const Half8<P> *>(old_low + here);
+        const float f = a + diag[row];
+        float y[8];
+        turned.get(y, r, c);
 #pragma unroll
-            for (int t = 0; t < 8; ++t) y[t] = fmaf(f, both(hi[t], lo[t]), y[t] * (1.f / kGramScale));
-            if constexpr (LAST) {
-                device_elem(it.dtype, [&](auto e) {
-                    using E = decltype(e);
-                    E *dst = static_cast<E *>(it.dst) + row * it.dst_rs;
-                    const float s = scale / it.x_scale;
+        for (int t = 0; t < 8; ++t) y[t] = fmaf(f, both(hi[t], lo[t]), y[t] * (1.f / kGramScale));
+        if constexpr (LAST) {
+            device_elem(it.dtype, [&](auto e) {
+                using E = decltype(e);
+                E *dst = static_cast<E *>(it.dst) + row * it.dst_rs;
+                const float s = scale / it.x_scale;
 #pragma unroll
-                    for (int t = 0; t < 8; ++t) y[t] *= s;
-                    if (it.dst_cs == 1) store_cols<E>(y, dst, col, it.n);
-                    else
+                for (int t = 0; t < 8; ++t) y[t] *= s;
+                if (it.dst_cs == 1) store_cols<E>(y, dst, col, it.n);
+                else
 #pragma unroll
-                        for (int t = 0; t < 8; ++t)
-                            if (col + t < it.n) dst[(col + t) * it.dst_cs] = to_elem<E>(y[t]);
-                });
-            } else {
-                Half8<P> v[2];
-                split_cols<P>(y, v);
-                *reinterpret_cast<Half8<P> *>(to + here) = v[0];
-                *reinterpret_cast<Half8<P> *>(to_low + here) = v[1];
-            }
+                    for (int t = 0; t < 8; ++t)
+                        if (col + t < it.n) dst[(col + t) * it.dst_cs] = to_elem<E>(y[t]);
+            });
+        } else {
+            Half8<P> v[2];
+            split_cols<P>(y, v);
+            *reinterpret_cast<Half8<P> *>(to + here) = v[0];
+            *reinterpret_cast<Half8<P> *>(to_low + here) = v[1];
         }
-    };
-    finish(&acc[0], n0 + B::first(wave) + c);
-    if constexpr (B::kPer == 128) finish(&acc[2], n0 + B::first(wave) + 64 + c);
+    }
 }
 
 // no steps: the matrix divided by its norm
@@ -550,12 +548,12 @@ template <int ELEMS> __global__ __launch_bounds__(kSmallThreads) void k_small(Li
 constexpr int64_t kHead = kList * kNormBlocks * 8;   // bytes of the norms' partial sums
 constexpr int64_t kMostBytes = (int64_t)1 << 31;    // of a group's scratch memory, where it has more than one matrix
 
-// How a matrix is taken: in one block (of the smaller or the larger amount of LDS), or by products of two parts, or one (with smaller or larger tiles of X)
-enum { W_SMALL, W_MEDIUM, W_TWO, W_ONE, W_ONE_LARGE, W_COUNT };
+// How a matrix is taken: in one block (of the smaller or the larger amount of LDS), or by products in tiles
+enum { W_SMALL, W_MEDIUM, W_TILES, W_COUNT };
 int way_of(const mlip_matrix_t &x)
 {
     const int64_t elems = x.rows < x.cols ? small_elems(x.rows, x.cols) : small_elems(x.cols, x.rows);
-    return elems <= kSmallHalves ? W_SMALL : elems <= kSmallMost ? W_MEDIUM : x.dtype != MLIP_DTYPE_BF16 ? W_TWO : x.rows < 512 || x.cols < 512 ? W_ONE : W_ONE_LARGE;
+    return elems <= kSmallHalves ? W_SMALL : elems <= kSmallMost ? W_MEDIUM : W_TILES;
 }
 
 struct Group {
@@ -592,14 +590,14 @@ Group group_of(const mlip_matrix_t *list, int32_t count, int32_t at, int way, bo
         it.x_scale = (float)(1 << e);
         int64_t place = used;
         auto take = [&](int64_t bytes) { const int64_t here = place / 2; place += pad_to(bytes, 256); return here; };
-        if (way >= W_TWO && !no_steps) {
+        if (way == W_TILES && !no_steps) {
             const int64_t all = (int64_t)it.m * it.n_ld * 2, square = (int64_t)it.m * it.m_ld * 2;
             it.x[0] = take(all);
             it.low[0] = take(all);
             it.x[1] = take(all);
-            it.low[1] = way == W_TWO ? take(all) : it.low[0];
+            it.low[1] = take(all);
             it.gram = take(2 * square);
-            it.poly = take((way == W_TWO ? 2 : 1) * square);
+            it.poly = take(2 * square);
             it.diag = take((int64_t)it.m * 8);
         }
         if (g.l.count && place > kMostBytes) break;
@@ -622,15 +620,15 @@ template <class Fn> unsigned number_blocks(List &l, Fn &&blocks_of)
     return at;
 }
 
-template <int PARTS, class B> void steps_of(List &l, P *ws, int32_t steps, float a, float b, float c, float scale, hipStream_t stream)
+void steps_of(List &l, P *ws, int32_t steps, float a, float b, float c, float scale, hipStream_t stream)
 {
     for (int s = 0; s < steps; ++s) {
         const int now = s & 1;
         unsigned blocks = number_blocks(l, [](const Item &it) { const int64_t t = (it.m + 127) / 128; return t * (t + 1) / 2; });
-        k_symmetric<PARTS, false><<<blocks, kThreads, 0, stream>>>(l, ws, now, 0.f, 0.f);
-        k_symmetric<PARTS, true><<<blocks, kThreads, 0, stream>>>(l, ws, now, b, c);
-        blocks = number_blocks(l, [](const Item &it) { return (int64_t)((it.m + B::kRows - 1) / B::kRows) * ((it.n_p + B::kCols - 1) / B::kCols); });
-        (s + 1 == steps ? k_apply<PARTS, B, true> : k_apply<PARTS, B, false>)<<<blocks, B::kThreads, 0, stream>>>(l, ws, now, a, scale);
+        k_symmetric<false><<<blocks, kThreads, 0, stream>>>(l, ws, now, 0.f, 0.f);
+        k_symmetric<true><<<blocks, kThreads, 0, stream>>>(l, ws, now, b, c);
+        blocks = number_blocks(l, [](const Item &it) { return (int64_t)((it.m + Middle::kRows - 1) / Middle::kRows) * ((it.n_p + Middle::kCols - 1) / Middle::kCols); });
+        (s + 1 == steps ? k_apply<true> : k_apply<false>)<<<blocks, Middle::kThreads, 0, stream>>>(l, ws, now, a, scale);
     }
 }
 
@@ -659,7 +657,7 @@ int ortho_impl(const mlip_matrix_t *list, int32_t count, int32_t steps, const do
             at = g.next;
             List &l = g.l;
             if (!l.count) continue;
-            if (way < W_TWO && steps) {
+            if (way != W_TILES && steps) {
                 (way == W_SMALL ? k_small<kSmallHalves> : k_small<kSmallMost>)<<<l.count, kSmallThreads, 0, stream>>>(l, eps, steps, a, b, c, scale);
                 MLIP_HIP(hipGetLastError());
                 continue;
@@ -670,9 +668,7 @@ int ortho_impl(const mlip_matrix_t *list, int32_t count, int32_t steps, const do
             } else {
                 const unsigned blocks = number_blocks(l, [](const Item &it) { return (int64_t)((it.m + 63) / 64) * (it.n_p / 64); });
                 k_start<<<blocks, kThreads, 0, stream>>>(l, norms, eps, ws);
-                if (way == W_TWO) steps_of<2, Middle>(l, ws, steps, a, b, c, scale, stream);
-                else if (way == W_ONE) steps_of<1, Middle>(l, ws, steps, a, b, c, scale, stream);
-                else steps_of<1, Large>(l, ws, steps, a, b, c, scale, stream);
+                steps_of(l, ws, steps, a, b, c, scale, stream);
             }
             MLIP_HIP(hipGetLastError());
         }
