@@ -474,9 +474,9 @@ int mlip_clip_grads(const mlip_tensor_t *tensors, int32_t count, float max_norm,
  *   MLIP_GATE_SIGMOID       sigmoid(g) v
  *   MLIP_GATE_SILU_SIGMOID  sigmoid(g) silu(v)
  * All arrays are of type dtype; products are exact, sums fp32.  fp32 arrays: products of three bf16 parts each, all terms down to 2^-24; those that make
- * g and v where d <= 128, and of mlip_gated where n >= 1024, of two fp16 parts of values brought by powers of two into their range row by row of x and column by column of the weights (22 bits,
- * down to 2^-24 of the row's or column's largest value, which may not be below 2^-97).  A value that is infinite, or beyond the bf16 range of 3.39e38, makes its row of x, or
- * its column of the weights, NaN.
+ * g and v where d <= 128, and of mlip_gated where n d f >= 5e8, of two fp16 parts (22 bits) of values brought by powers of two into their range row by row of x and column by column
+ * of the weights, except in the rows and columns whose values differ too much in size for that, where they are products of fp32 values; what is left out or rounded is below 2^-20 of
+ * the sum of the terms' sizes.  A value that is infinite, or beyond the bf16 range of 3.39e38, makes its row of x, or its column of the weights, NaN.
  *   x        DEVICE [n][d], any strides;  w_gate, w_value DEVICE [d][f], any strides (so that weights kept as [f][d] serve as well)
  *   b_gate, b_value   DEVICE [f], one element after another, or NULL
  *   out      DEVICE [n][f], element (i, k) at i * out_row_stride + k

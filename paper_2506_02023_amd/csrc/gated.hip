@@ -27,9 +27,12 @@ template <class Fn> int with_kind(int32_t dtype, Fn &&f)
 }
 int parts_of(int32_t dtype) { return dtype == MLIP_DTYPE_F32 ? 3 : 1; }
 // g and v of fp32 arrays: two fp16 parts (22 bits) and three products, half the matrix time, where that is what bounds (wide rows of the forward call) or registers are
-// short (rows of up to 128 features).  Every row of x and column of the weights is brought by a power of two to a largest value in [2^13, 2^14), so that a value has its 22 bits
-// down to 2^-24 of its row's largest and is off by 2^-38 of that below.  (32,768 x 512 x 1365: 381 us, with three bf16 parts 712; 300,000 x 128 x 256: 214 and 361; the gradient's
-// g and v of 202,612 x 128 x 341: 421 and 588.)
+// short (rows of up to 128 features).  Every row of x and column of the weights is brought by a power of two to a largest value in [2^13, 2^14).  A value then has its 22 bits
+// down to 2^-3; what is below is off by up to 2^-25.  That is nothing beside a sum of large terms, but it is all there is of a sum whose row is large where the column is small
+// and the other way round.  So values of 2^7 and more are counted: of a column all but t (an eighth) shall be that large, of a row t and an eighth of those that are not zero.
+// Then an eighth of the row's terms at least are 2^14 and more, and what is lost, twice 2^-25 2^14 a term at most, is below 2^-21 of the terms' sizes.  The results of a row or
+// column that falls short are computed again by the fp32 matrix instruction.  (32,768 x 512 x 1365: 381 us, with three bf16 parts 712; 300,000 x 128 x 256: 214 and 361; the
+// gradient's g and v of 202,612 x 128 x 341: 421 and 588.)
 using Scaled = Kind<_Float16, 2, float>;
 template <class K> using Inner = std::conditional_t<K::kParts == 3, Scaled, K>;   // in what k_gates_narrow computes g and v
 
@@ -95,34 +98,103 @@ template <class K> __global__ __launch_bounds__(kPackThreads) void k_pack_weight
 }
 
 // The power of two that brings a largest value to [2^13, 2^14), as its exponent (0 for none, and for one that is not finite)
+constexpr int kMostExponent = 110;
 __device__ inline int scale_for(float largest)
 {
     const int e = largest > 0.f && largest < __builtin_inff() ? 13 - ilogbf(largest) : 0;
-    return e > 110 ? 110 : e;
+    return e > kMostExponent ? kMostExponent : e;
+}
+// Scaled values of a row or column of the weights, counted
+constexpr float kLarge = 128.f;
+struct Counts {
+    int large = 0, there = 0;
+    __device__ inline void add(float scaled)
+    {
+        large += fabsf(scaled) >= kLarge;
+        there += scaled != 0.f;
+    }
+    __device__ inline void join(int lane_step)   // with those of lane ^ lane_step
+    {
+        large += __shfl_xor(large, lane_step);
+        there += __shfl_xor(there, lane_step);
+    }
+};
+// Whether the d values of a row (or column) fall short; `largest` before they were scaled.  (Not if one is infinite: their results are NaN either way.)
+__device__ inline bool cannot_be_scaled(float largest, int e) { return e == kMostExponent && ldexpf(largest, e) < 8192.f; }
+__device__ inline int spared(int d) { return d / 8 + 1 < d / 4 ? d / 8 + 1 : d / 4; }
+__device__ inline bool row_falls_short(float largest, int e, Counts n, int d)
+{
+    return largest > 0.f && largest < __builtin_inff() && (8 * (n.large - spared(d)) < n.there || cannot_be_scaled(largest, e));
+}
+__device__ inline bool column_falls_short(float largest, int e, Counts n, int d)
+{
+    return largest > 0.f && largest < __builtin_inff() && (d - n.large > spared(d) || cannot_be_scaled(largest, e));
 }
 
-// Scales of 32 columns of the weights
-__global__ __launch_bounds__(kPackThreads) void k_column_scales(Weights<Scaled> w, float *scale, float *exponent)
+// fp32 weights as the caller has them
+struct Plain {
+    const float *wg, *wv;
+    int64_t g_rs, g_cs, v_rs, v_cs;
+    int32_t d, f;
+};
+
+// g and v of 32 features from f0 on and of a lane's row (32 of them) by the fp32 matrix instruction, in the same order whatever the strides
+__device__ inline void plain_products(const Plain &w, const float *row, int64_t x_cs, int64_t f0, f32x16 &g, f32x16 &v)
 {
-    __shared__ float most[kPackThreads];
+    const int k_lane = (threadIdx.x & 63) >> 5 << 2;
+    const int64_t f = f0 + (threadIdx.x & 31), f_within = f < w.f ? f : w.f - 1;
+    const float *wg = w.wg + f_within * w.g_cs, *wv = w.wv + f_within * w.v_cs;
+    g = v = f32x16{};
+#pragma unroll 2
+    for (int k0 = 0; k0 < w.d; k0 += 8) {
+        float x[4], a[4], b[4];
+        load_cols(x, row, x_cs, k0 + k_lane, w.d);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            const int64_t k = k0 + k_lane + t, within = k < w.d ? k : w.d - 1;
+            a[t] = wg[within * w.g_rs];
+            b[t] = wv[within * w.v_rs];
+            if (k >= w.d || f >= w.f) a[t] = b[t] = 0.f;
+        }
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            g = __builtin_amdgcn_mfma_f32_32x32x2f32(a[t], x[t], g, 0, 0, 0);
+            v = __builtin_amdgcn_mfma_f32_32x32x2f32(b[t], x[t], v, 0, 0, 0);
+        }
+    }
+}
+
+// Scales of 32 columns of the weights, and whether they fall short
+constexpr int kScaleThreads = 1024;
+__global__ __launch_bounds__(kScaleThreads) void k_column_scales(Weights<Scaled> w, float *scale, float *exponent, int32_t *short_of)
+{
+    __shared__ float most[kScaleThreads];
+    __shared__ int counts[kScaleThreads];   // of large ones
     const int64_t c = (int64_t)blockIdx.x * 32 + (threadIdx.x & 31), f = feature_of(c);
     const bool value = is_value(c);
     const float *src = value ? w.wv : w.wg;
     const int64_t rs = value ? w.v_rs : w.g_rs, cs = value ? w.v_cs : w.g_cs;
     float m = 0.f;
-    if (f < w.f) in_steps<8>(threadIdx.x >> 5, w.d, kPackThreads / 32, [&](int64_t d) { return src[d * rs + f * cs]; }, [&](float x) { m = fmaxf(m, fabsf(x)); });
+    if (f < w.f) in_steps<8>(threadIdx.x >> 5, w.d, kScaleThreads / 32, [&](int64_t d) { return src[d * rs + f * cs]; }, [&](float x) { m = fmaxf(m, fabsf(x)); });
     most[threadIdx.x] = m;
     __syncthreads();
-    if (threadIdx.x >= 32) return;
-    for (int k = 32; k < kPackThreads; k += 32) m = fmaxf(m, most[threadIdx.x + k]);
+    for (int k = threadIdx.x & 31; k < kScaleThreads; k += 32) m = fmaxf(m, most[k]);
     const int e = scale_for(m);
-    scale[c] = ldexpf(1.f, e);
+    const float by = ldexpf(1.f, e);
+    Counts n;
+    if (f < w.f) in_steps<8>(threadIdx.x >> 5, w.d, kScaleThreads / 32, [&](int64_t d) { return src[d * rs + f * cs]; }, [&](float x) { n.add(x * by); });
+    counts[threadIdx.x] = n.large;
+    __syncthreads();
+    if (threadIdx.x >= 32) return;
+    for (int k = 32; k < kScaleThreads; k += 32) n.large += counts[threadIdx.x + k];
+    scale[c] = by;
     exponent[c] = (float)e;
+    short_of[c] = column_falls_short(m, e, n, (int)w.d);
 }
 
-// The weights for k_gates_narrow in fp32, all of up to 128 rows of 32 columns in a block: `across` scaled and in two fp16 parts, the scales' exponents, and `down` as
-// k_pack_weights makes it
-template <class K> __global__ __launch_bounds__(kPackThreads) void k_pack_scaled_weights(Weights<K> w, int64_t d_p, _Float16 *across, float *exponent)
+// The weights for k_gates_narrow in fp32, all of up to 128 rows of 32 columns in a block: `across` scaled and in two fp16 parts, the scales' exponents, which columns fall short,
+// and `down` as k_pack_weights makes it
+template <class K> __global__ __launch_bounds__(kPackThreads) void k_pack_scaled_weights(Weights<K> w, int64_t d_p, _Float16 *across, float *exponent, int32_t *short_of)
 {
     __shared__ float tile[kNarrow][33], most[kPackThreads / 32][32];
     const int64_t c0 = (int64_t)blockIdx.x * 32, f0 = feature_of(c0);
@@ -150,11 +222,18 @@ template <class K> __global__ __launch_bounds__(kPackThreads) void k_pack_scaled
         m = 0.f;
         for (int k = 0; k < kPackThreads / 32; ++k) m = fmaxf(m, most[k][i]);
         const int e = scale_for(m);
-        if (a == 0) exponent[c0 + i] = (float)e;
+        Counts n;
         for (int64_t dd = a; dd < d_p; dd += 32) {
+            const float x = tile[dd][i] * ldexpf(1.f, e);
             _Float16 v[2];
-            split(tile[dd][i] * ldexpf(1.f, e), v);
+            n.add(x);
+            split(x, v);
             for (int p = 0; p < 2; ++p) across[p * w.across_part + (c0 + i) * w.d_ld + dd] = v[p];
+        }
+        for (int k = 16; k; k >>= 1) n.join(k);
+        if (a == 0) {
+            exponent[c0 + i] = (float)e;
+            short_of[c0 + i] = m == __builtin_inff() ? -1 : column_falls_short(m, e, n, (int)w.d);
         }
     }
     if (!w.down) return;
@@ -167,7 +246,7 @@ template <class K> __global__ __launch_bounds__(kPackThreads) void k_pack_scaled
 
 // Rows of x scaled and in parts, a wavefront each; zeros from `cols` on
 __global__ __launch_bounds__(kPackThreads) void k_pack_scaled_rows(const float *src, int64_t rs, int64_t cs, int64_t rows, int64_t cols, int64_t cols_p, _Float16 *dst, int64_t ld, int64_t part,
-                                                                   float *exponent)
+                                                                   float *exponent, int32_t *short_of)
 {
     const int64_t r = (int64_t)blockIdx.x * (kPackThreads / 64) + (threadIdx.x >> 6);
     if (r >= rows) return;
@@ -189,10 +268,13 @@ __global__ __launch_bounds__(kPackThreads) void k_pack_scaled_rows(const float *
     for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
     const int e = scale_for(m);
     const float scale = ldexpf(1.f, e);
-    if (lane == 0) exponent[r] = (float)e;
+    Counts n;
     auto put = [&](float (&x)[4], int64_t c) {
 #pragma unroll
-        for (int t = 0; t < 4; ++t) x[t] *= scale;
+        for (int t = 0; t < 4; ++t) {
+            x[t] *= scale;
+            n.add(x[t]);
+        }
         Cols<_Float16, 4> p[2];
         split_cols<_Float16>(x, p);
         *reinterpret_cast<Cols<_Float16, 4> *>(dst + r * ld + c) = p[0];
@@ -205,6 +287,11 @@ __global__ __launch_bounds__(kPackThreads) void k_pack_scaled_rows(const float *
         float x[4];
         load_cols(x, row, cs, c, cols);
         put(x, c);
+    }
+    for (int d = 32; d; d >>= 1) n.join(d);
+    if (lane == 0) {
+        exponent[r] = (float)e;
+        short_of[r] = row_falls_short(m, e, n, (int)cols);
     }
 }
 
@@ -251,7 +338,12 @@ template <class K> struct GateArgs {
     int64_t bar_rs, bar_cs;
     typename K::T *gv;
     int64_t gv_ld, gv_part;
-    const float *x_exponent, *w_exponent;   // of the scales to take off again (Scaled)
+    // Scaled: the exponents of the scales to take off again, which rows and columns fall short, x and the weights as the caller has them
+    const float *x_exponent, *w_exponent;
+    const int32_t *x_short, *w_short;
+    const float *x_plain;
+    int64_t x_rs, x_cs;
+    Plain plain;
 };
 
 // The weights are the products' first operand and the rows their second; a lane ends with neighbouring features of a row.  Bound by the matrix units, the activations behind
@@ -268,10 +360,31 @@ template <class K, class B, bool BACK> __global__ __launch_bounds__(B::kThreads)
     constexpr int W = K::kWide, lanes = 32 / W;   // of a row
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, c = lane % lanes * W;
     const Turned turned{reinterpret_cast<float *>(&lds) + wave * 4096};
-    auto finish = [&](const f32x16 (*part)[2], int64_t col0) {   // 64 columns of a wavefront
+    auto finish = [&](f32x16 (*part)[2], int64_t col0) {   // 64 columns of a wavefront
         const int64_t f = col0 / 2 + c;
-        turned.put(part);
         if (col0 >= a.w.rows) return;
+        if constexpr (std::is_same_v<K, Scaled>) {
+            const uint64_t columns = __ballot(a.w_short[col0 + lane]);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                int64_t row = m0 + B::second(wave) + 32 * j + (lane & 31);
+                if (row >= a.x.rows) row = a.x.rows - 1;
+                const bool short_row = a.x_short[row];
+                if (!__ballot(short_row) && !columns) continue;
+                const float ex = a.x_exponent[row];
+                f32x16 g, v;
+                plain_products(a.plain, a.x_plain + row * a.x_rs, a.x_cs, col0 / 2, g, v);
+#pragma unroll
+                for (int k = 0; k < 16; ++k) {
+                    const int q = acc_row(k);
+                    if (!short_row && !(columns >> q & 0x100000001)) continue;
+                    // (brought to the others' scale; NaN, of an infinity in the row or column, stays)
+                    if (part[0][j][k] == part[0][j][k]) part[0][j][k] = ldexpf(g[k], (int)(ex + a.w_exponent[col0 + q]));
+                    if (part[1][j][k] == part[1][j][k]) part[1][j][k] = ldexpf(v[k], (int)(ex + a.w_exponent[col0 + 32 + q]));
+                }
+            }
+        }
+        turned.put(part);
         float bg[W] = {}, bv[W] = {};
         if (a.bg) load_cols(bg, a.bg, 1, f, a.f);
         if (a.bv) load_cols(bv, a.bv, 1, f, a.f);
@@ -340,6 +453,90 @@ template <class K> struct NarrowArgs {
     int32_t blocks, pairs;   // of a group; pairs of 32 columns in a group, NarrowShape's or, where that leaves compute units idle, one
 };
 
+// What a wavefront has to compute again of its rows and group of columns, stored over what it has stored before.  (Not in the kernel's loop, which has no registers to spare for
+// it.  What has an infinity in its row or column has become NaN and stays so: `lost` features.)  1,000,188 x 64 -> 128 with four of five features zero: 1.05 ms, 0.23 with none.
+template <class K, int STEPS, bool BACK>
+__device__ inline void gates_again(const NarrowArgs<K> &na, const uint32_t *short_of, const uint32_t *lost, const float (*bias)[NarrowShape<K, STEPS>::kPairs * 32], int pairs, int64_t col_first,
+                                   int64_t first_tile, int64_t stride)
+{
+    const GateArgs<K> &a = na.a;
+    const Plain &w = a.plain;
+    const int lane = threadIdx.x & 63, half = lane >> 5, d = w.d;
+    __threadfence();   // (the earlier stores are other lanes')
+    for (int64_t tile = first_tile; tile < na.tiles; tile += stride) {
+        const int64_t mine = tile * 32 + (lane & 31), row = mine < a.x.rows ? mine : a.x.rows - 1;
+        float x[STEPS][8], m = 0.f;
+#pragma unroll
+        for (int kk = 0; kk < STEPS; ++kk) load_cols(x[kk], static_cast<const float *>(a.x.p) + row * a.x.ld, na.x_cs, kk * 16 + half * 8, d);
+#pragma unroll
+        for (int kk = 0; kk < STEPS; ++kk)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) m = fmaxf(m, fabsf(x[kk][k]));
+        m = fmaxf(m, __shfl_xor(m, 32));
+        const int e = scale_for(m);
+        const float scale = ldexpf(1.f, e);
+        Counts n;
+#pragma unroll
+        for (int kk = 0; kk < STEPS; ++kk)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) n.add(x[kk][k] * scale);
+        n.join(32);
+        const bool short_row = row_falls_short(m, e, n, d), rows = __ballot(short_row) != 0, leave = mine >= a.x.rows || m == __builtin_inff();
+        for (int pair = 0; pair < pairs; ++pair) {
+            const int64_t col0 = col_first + pair * 64, f0 = col0 / 2, f_mine = f0 + (lane & 31);
+            if (col0 >= a.w.rows) break;
+            if (!rows && !short_of[pair]) continue;
+            const int64_t f = f_mine < w.f ? f_mine : w.f - 1;
+            f32x16 g = {}, v = {};
+#pragma unroll
+            for (int kk = 0; kk < STEPS; ++kk) {
+                float ag[8], av[8];
+                int from = half * 8;
+                __builtin_amdgcn_sched_barrier(0);
+                asm volatile("" : "+v"(from));   // (else all addresses are worked out before the loops, for registers that there are not)
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const int at = kk * 16 + from + k, within = at < d ? at : d - 1;
+                    ag[k] = w.wg[within * w.g_rs + f * w.g_cs];
+                    av[k] = w.wv[within * w.v_rs + f * w.v_cs];
+                    if (at >= d || f_mine >= w.f) ag[k] = av[k] = 0.f;
+                }
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    g = __builtin_amdgcn_mfma_f32_32x32x2f32(ag[k], x[kk][k], g, 0, 0, 0);
+                    v = __builtin_amdgcn_mfma_f32_32x32x2f32(av[k], x[kk][k], v, 0, 0, 0);
+                }
+            }
+            const uint32_t mask = (leave ? 0 : short_row ? ~0u : short_of[pair]) & ~lost[pair];   // of the row's features
+            with_act(a.act, [&](auto act) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int c = acc_row(4 * q);
+                    float bar[4];
+                    if constexpr (BACK) load_cols(bar, a.bar + row * a.bar_rs, a.bar_cs, f0 + c, a.f);
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) {
+                        const Phi y = phi<decltype(act)::value>(g[4 * q + t] + bias[0][pair * 32 + c + t], v[4 * q + t] + bias[1][pair * 32 + c + t]);
+                        if (!(mask >> (c + t) & 1) || f0 + c + t >= a.f) continue;
+                        if constexpr (!BACK) a.out[row * a.out_rs + f0 + c + t] = y.h;
+                        else {
+                            typename K::T gp[K::kParts], vp[K::kParts];
+                            split(bar[t] * y.g, gp);
+                            split(bar[t] * y.v, vp);
+#pragma unroll
+                            for (int p = 0; p < K::kParts; ++p) {
+                                typename K::T *to = a.gv + p * a.gv_part + row * a.gv_ld + col0 + c + t;
+                                to[0] = gp[p];
+                                to[32] = vp[p];
+                            }
+                        }
+                    }
+                }
+            });
+        }
+    }
+}
+
 template <class K, int STEPS, bool BACK, bool STRIDED> __global__ __launch_bounds__(256, K::kParts == 1 && !BACK ? 3 : 2) void k_gates_narrow(NarrowArgs<K> na)
 {
     using T = typename K::T;
@@ -352,6 +549,7 @@ template <class K, int STEPS, bool BACK, bool STRIDED> __global__ __launch_bound
     __shared__ alignas(16) float exponents[2][SCALED ? S::kPairs * 32 : 4];
     __shared__ alignas(16) T stage_[4 * S::kStage];
     __shared__ alignas(16) float bias[2][S::kPairs * 32];
+    __shared__ uint32_t short_of[SCALED ? S::kPairs : 1], lost[SCALED ? S::kPairs : 1];   // features whose columns fall short, or hold an infinity, a bit each
     const GateArgs<K> &a = na.a;
     const int64_t at = xcd_order(blockIdx.x, gridDim.x);
     const int pairs = S::kPairs == 1 ? 1 : na.pairs;
@@ -374,6 +572,12 @@ template <class K, int STEPS, bool BACK, bool STRIDED> __global__ __launch_bound
             const int64_t col = col_first + k / 32 * 64 + k % 32;
             exponents[0][k] = col < a.w.rows ? a.w_exponent[col] : 0.f;
             exponents[1][k] = col < a.w.rows ? a.w_exponent[col + 32] : 0.f;
+            const int32_t sg = col < a.w.rows ? a.w_short[col] : 0, sv = col < a.w.rows ? a.w_short[col + 32] : 0;
+            const uint64_t some = __ballot(sg > 0 || sv > 0), none = __ballot(sg < 0 || sv < 0);
+            if (k % 32 == 0) {
+                short_of[k / 32] = (uint32_t)(some >> (lane & 32));
+                lost[k / 32] = (uint32_t)(none >> (lane & 32));
+            }
         }
     }
     __syncthreads();
@@ -384,7 +588,9 @@ template <class K, int STEPS, bool BACK, bool STRIDED> __global__ __launch_bound
         __builtin_amdgcn_wave_barrier();
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
     };
-    for (int64_t tile = at / na.groups * 4 + wave; tile < na.tiles; tile += (int64_t)na.blocks * 4) {
+    bool again = false;   // whether there may be something that falls short
+    const int64_t first_tile = at / na.groups * 4 + wave, stride = (int64_t)na.blocks * 4;
+    for (int64_t tile = first_tile; tile < na.tiles; tile += stride) {
         const int64_t row0 = tile * 32, mine = row0 + (lane & 31), row = mine < a.x.rows ? mine : a.x.rows - 1;
         Half8<C> fx[STEPS][PARTS];
         float ex = 0.f;
@@ -410,12 +616,19 @@ template <class K, int STEPS, bool BACK, bool STRIDED> __global__ __launch_bound
             const int e = scale_for(m);
             const float scale = ldexpf(1.f, e);
             ex = (float)e;
+            Counts n;
+            n.there = d;   // (at most: gates_again looks closer)
 #pragma unroll
             for (int kk = 0; kk < STEPS; ++kk) {
 #pragma unroll
-                for (int k = 0; k < 8; ++k) v[kk][k] *= scale;
+                for (int k = 0; k < 8; ++k) {
+                    v[kk][k] *= scale;
+                    n.large += fabsf(v[kk][k]) >= kLarge;
+                }
                 split_cols<C>(v[kk], fx[kk]);
             }
+            n.large += __shfl_xor(n.large, 32);
+            again |= __ballot(row_falls_short(m, e, n, d)) != 0;
         }
 #pragma unroll 1
         for (int pair = 0; pair < pairs; ++pair) {
@@ -520,6 +733,10 @@ template <class K, int STEPS, bool BACK, bool STRIDED> __global__ __launch_bound
                 }
             }
         }
+    }
+    if constexpr (SCALED) {
+        for (int pair = 0; pair < pairs; ++pair) again |= short_of[pair] != 0;
+        if (again) gates_again<K, STEPS, BACK>(na, short_of, lost, bias, pairs, col_first, first_tile, stride);
     }
 }
 
@@ -692,11 +909,12 @@ struct Plan {
     bool pack_x;
     int64_t d_p, f2, gv_ld, d_ld, chunk;       // columns of the laid out x and weights and where their rows lie, rows of a chunk
     int64_t splits, run;
-    size_t across, down, xs, gv, part, bias, x_exponent, w_scale, bytes;   // offsets
+    size_t across, down, xs, gv, part, bias, x_exponent, w_scale, bytes;   // offsets (x_exponent: and which rows fall short; w_scale: scales, exponents, which columns do)
 };
 
-// Whether a call goes by Scaled: long enough for its one more launch to pay (1024 x 130 x 20: 23 us, 22 without; 3000 x 256 x 256: 25, 28 without)
-bool by_scale(const GatedArgs &a, bool grad) { return a.dtype == MLIP_DTYPE_F32 && !grad && a.d > kNarrow && a.n >= 1024; }
+// Whether a call goes by Scaled: large enough for its one more launch and the counts to pay (us, and by three bf16 parts: 3000 x 256 x 256 28 and 26, 4000 x 256 x 512 30 and 30,
+// 2000 x 512 x 1024 42 and 44, 1024 x 1024 x 4096 111 and 135, 32,768 x 512 x 1365 343 and 635)
+bool by_scale(const GatedArgs &a, bool grad) { return a.dtype == MLIP_DTYPE_F32 && !grad && a.d > kNarrow && (double)a.n * (double)a.d * (double)a.f >= 5e8; }
 
 // x is read where it lies if its rows are whole lines of pieces and steps
 bool reads_x(const GatedArgs &a)
@@ -734,8 +952,8 @@ Plan plan_of(const GatedArgs &a, bool grad)
     auto take = [&](int64_t bytes) { const size_t here = at; at += (size_t)pad_to(bytes, 256); return here; };
     p.across = take(p.f2 * p.d_ld * p.parts * 2);
     if (grad || a.d > kNarrow) p.xs = take(p.chunk * p.d_ld * p.parts * 2);
-    if (by_scale(a, grad)) p.x_exponent = take(p.chunk * 4);
-    if (a.dtype == MLIP_DTYPE_F32) p.w_scale = take(2 * p.f2 * 4);
+    if (by_scale(a, grad)) p.x_exponent = take(2 * p.chunk * 4);
+    if (a.dtype == MLIP_DTYPE_F32) p.w_scale = take(3 * p.f2 * 4);
     if (grad) {
         p.down = take(a.d * p.gv_ld * p.parts * 2);
         p.gv = take(p.chunk * p.gv_ld * p.parts * 2);
@@ -753,6 +971,11 @@ Plan plan_of(const GatedArgs &a, bool grad)
     return p;
 }
 
+Plain plain_of(const GatedArgs &a)
+{
+    return {static_cast<const float *>(a.wg), static_cast<const float *>(a.wv), a.wg_rs, a.wg_cs, a.wv_rs, a.wv_cs, (int32_t)a.d, (int32_t)a.f};
+}
+
 template <class K> int launch(const GatedArgs &a, const GatedGrad *g)
 {
     using E = typename K::E;
@@ -766,9 +989,10 @@ template <class K> int launch(const GatedArgs &a, const GatedGrad *g)
     const Weights<K> w = {static_cast<const E *>(a.wg), static_cast<const E *>(a.wv), a.wg_rs, a.wg_cs, a.wv_rs, a.wv_cs, a.d, a.f, p.d_ld, p.gv_ld,
                           across, rows ? down : nullptr, p.f2 * p.d_ld, a.d * p.gv_ld};
     float *w_exponent = reinterpret_cast<float *>(ws + p.w_scale);
+    int32_t *w_short = reinterpret_cast<int32_t *>(w_exponent + p.f2);
     if (a.n > 0 && in_registers && K::kParts == 3) {
         if constexpr (K::kParts == 3)
-            k_pack_scaled_weights<K><<<(unsigned)(p.f2 / 32), kPackThreads, 0, a.stream>>>(w, p.d_p, reinterpret_cast<_Float16 *>(across), w_exponent);
+            k_pack_scaled_weights<K><<<(unsigned)(p.f2 / 32), kPackThreads, 0, a.stream>>>(w, p.d_p, reinterpret_cast<_Float16 *>(across), w_exponent, w_short);
     } else if (a.n > 0) k_pack_weights<K><<<dim3((unsigned)(p.f2 / 32), (unsigned)(p.d_p / 32)), kPackThreads, 0, a.stream>>>(w);
     const Panel across_panel = {across, p.d_ld, p.f2 * p.d_ld, p.f2, p.d_p}, down_panel = {down, p.gv_ld, a.d * p.gv_ld, a.d, p.f2};
     int64_t first = 0;
@@ -801,6 +1025,8 @@ template <class K> int launch(const GatedArgs &a, const GatedGrad *g)
                 NarrowArgs<K> na = {ga, a.x_cs, (all + pairs - 1) / pairs, tiles, 0, (int32_t)pairs};
                 na.a.x = {x, a.x_rs, 0, n, a.d};
                 na.a.w_exponent = w_exponent;
+                na.a.w_short = w_short;
+                na.a.plain = plain_of(a);
                 const int64_t most = kNarrowBlocks / na.groups > 0 ? kNarrowBlocks / na.groups : 1, blocks = (na.tiles + 3) / 4;
                 na.blocks = (int32_t)(blocks < most ? blocks : most);
                 (strided ? g ? k_gates_narrow<K, STEPS, true, true> : k_gates_narrow<K, STEPS, false, true>
@@ -870,20 +1096,27 @@ int launch_scaled(const GatedArgs &a)
     char *ws = static_cast<char *>(a.workspace);
     _Float16 *across = reinterpret_cast<_Float16 *>(ws + p.across), *xs = reinterpret_cast<_Float16 *>(ws + p.xs);
     float *x_exponent = reinterpret_cast<float *>(ws + p.x_exponent), *w_scale = reinterpret_cast<float *>(ws + p.w_scale), *w_exponent = w_scale + p.f2;
+    int32_t *x_short = reinterpret_cast<int32_t *>(x_exponent + p.chunk), *w_short = reinterpret_cast<int32_t *>(w_exponent + p.f2);
     const Weights<Scaled> w = {static_cast<const float *>(a.wg), static_cast<const float *>(a.wv), a.wg_rs, a.wg_cs, a.wv_rs, a.wv_cs, a.d, a.f, p.d_ld, p.gv_ld,
                                across, nullptr, p.f2 * p.d_ld, 0, w_scale};
-    k_column_scales<<<(unsigned)(p.f2 / 32), kPackThreads, 0, a.stream>>>(w, w_scale, w_exponent);
+    k_column_scales<<<(unsigned)(p.f2 / 32), kScaleThreads, 0, a.stream>>>(w, w_scale, w_exponent, w_short);
     k_pack_weights<Scaled><<<dim3((unsigned)(p.f2 / 32), (unsigned)(p.d_p / 32)), kPackThreads, 0, a.stream>>>(w);
     for (int64_t first = 0; first < a.n; first += p.chunk) {
         const int64_t n = a.n - first < p.chunk ? a.n - first : p.chunk;
         k_pack_scaled_rows<<<(unsigned)((n + kPackThreads / 64 - 1) / (kPackThreads / 64)), kPackThreads, 0, a.stream>>>(
-            static_cast<const float *>(a.x) + first * a.x_rs, a.x_rs, a.x_cs, n, a.d, p.d_p, xs, p.d_ld, p.chunk * p.d_ld, x_exponent);
+            static_cast<const float *>(a.x) + first * a.x_rs, a.x_rs, a.x_cs, n, a.d, p.d_p, xs, p.d_ld, p.chunk * p.d_ld, x_exponent, x_short);
         GateArgs<Scaled> ga = {{xs, p.d_ld, p.chunk * p.d_ld, n, p.d_p}, {across, p.d_ld, p.f2 * p.d_ld, p.f2, p.d_p}, p.d_p, a.f, 0, a.act,
                                static_cast<const float *>(a.bg), static_cast<const float *>(a.bv)};
         ga.out = static_cast<float *>(a.out) + first * a.out_rs;
         ga.out_rs = a.out_rs;
         ga.x_exponent = x_exponent;
         ga.w_exponent = w_exponent;
+        ga.x_short = x_short;
+        ga.w_short = w_short;
+        ga.x_plain = static_cast<const float *>(a.x) + first * a.x_rs;
+        ga.x_rs = a.x_rs;
+        ga.x_cs = a.x_cs;
+        ga.plain = plain_of(a);
         with_tile<Scaled>(p.f2, n, false, [&](auto block) {
             using B = decltype(block);
             ga.n_tiles = (p.f2 + B::kCols - 1) / B::kCols;
