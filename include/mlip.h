@@ -499,7 +499,7 @@ int mlip_gated(const mlip_gated_t *call, void *out, int64_t out_row_stride, void
 
 /*
  * Its gradient, from the gradient of out.  The products are computed again: nothing is kept from the forward call.  The gradients of g and v are rounded
- * to the arrays' type (fp32: not rounded) before the products with x and the weights take them up.
+ * before the products with x and the weights take them up: of bf16 arrays to bf16, of fp16 arrays to 16 bits with the range of fp32, of fp32 arrays not at all.
  *   grad     DEVICE [n][f], any strides
  *   x        DEVICE [n][d], element (i, k) at i * x_row_stride + k;  w_gate, w_value DEVICE [d][f], any strides that keep elements apart
  *   b_gate, b_value   DEVICE [f]

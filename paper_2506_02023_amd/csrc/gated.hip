@@ -19,13 +19,18 @@ template <class T_, int PARTS_, class E_> struct Kind {
     using E = E_;
     static constexpr int kParts = PARTS_, kWide = 16 / sizeof(E_);   // elements of a lane's load or store
 };
-template <class Fn> int with_kind(int32_t dtype, Fn &&f)
+using Half = Kind<_Float16, 1, _Float16>;
+// Gradients of fp16 arrays: G and V, which are not bounded by what the arrays hold, may be larger or smaller than fp16 numbers.  They go in two bf16 parts (16 bits, the range of fp32),
+// and with them x and the weights, exactly: three products for one.  (32,768 x 1024 x 4096: 3.99 ms, 1.85 in one fp16 part; 1,000,188 x 64 x 128: 935 us and 516.)  Those of bf16 arrays have the range, and
+// are rounded to bf16 as any network's are that computes its gradients in that type.
+using HalfBack = Kind<__bf16, 2, _Float16>;
+template <bool BACK, class Fn> int with_kind(int32_t dtype, Fn &&f)
 {
     if (dtype == MLIP_DTYPE_F32) return f(Kind<__bf16, 3, float>{});
     if (dtype == MLIP_DTYPE_BF16) return f(Kind<__bf16, 1, __bf16>{});
-    return f(Kind<_Float16, 1, _Float16>{});
+    return f(std::conditional_t<BACK, HalfBack, Half>{});
 }
-int parts_of(int32_t dtype) { return dtype == MLIP_DTYPE_F32 ? 3 : 1; }
+int parts_of(int32_t dtype, bool grad) { return dtype == MLIP_DTYPE_F32 ? 3 : dtype == MLIP_DTYPE_F16 && grad ? 2 : 1; }
 // g and v of fp32 arrays: two fp16 parts (22 bits) and three products, half the matrix time, where that is what bounds (wide rows of the forward call) or registers are
 // short (rows of up to 128 features).  Every row of x and column of the weights is brought by a power of two to a largest value in [2^13, 2^14).  A value then has its 22 bits
 // down to 2^-3; what is below is off by up to 2^-25.  That is nothing beside a sum of large terms, but it is all there is of a sum whose row is large where the column is small
@@ -34,7 +39,9 @@ int parts_of(int32_t dtype) { return dtype == MLIP_DTYPE_F32 ? 3 : 1; }
 // column that falls short are computed again by the fp32 matrix instruction.  (32,768 x 512 x 1365: 381 us, with three bf16 parts 712; 300,000 x 128 x 256: 214 and 361; the
 // gradient's g and v of 202,612 x 128 x 341: 421 and 588.)
 using Scaled = Kind<_Float16, 2, float>;
-template <class K> using Inner = std::conditional_t<K::kParts == 3, Scaled, K>;   // in what k_gates_narrow computes g and v
+// In what g and v are computed, by tiles and by k_gates_narrow
+template <class K> using InTiles = std::conditional_t<std::is_same_v<K, HalfBack>, Half, K>;
+template <class K> using Inner = std::conditional_t<K::kParts == 3, Scaled, InTiles<K>>;
 
 // Column c of the 2 f: the feature, and whether of v
 __host__ __device__ inline int64_t feature_of(int64_t c) { return c / 64 * 32 + c % 32; }
@@ -68,7 +75,8 @@ template <class K> __global__ __launch_bounds__(kPackThreads) void k_pack_rows(c
 template <class K> struct Weights {
     const typename K::E *wg, *wv;
     int64_t g_rs, g_cs, v_rs, v_cs, d, f, d_ld, f2_ld;
-    typename K::T *across, *down;
+    typename InTiles<K>::T *across;
+    typename K::T *down;
     int64_t across_part, down_part;
     const float *scale;      // of the columns, or NULL
 };
@@ -87,9 +95,10 @@ template <class K> __global__ __launch_bounds__(kPackThreads) void k_pack_weight
     }
     __syncthreads();
     for (int i = b; i < 32; i += 8) {
+        typename InTiles<K>::T u[InTiles<K>::kParts];
         typename K::T v[K::kParts];
-        split(w.scale ? tile[a][i] * w.scale[c0 + i] : tile[a][i], v);
-        for (int p = 0; p < K::kParts; ++p) w.across[p * w.across_part + (c0 + i) * w.d_ld + d0 + a] = v[p];
+        split(w.scale ? tile[a][i] * w.scale[c0 + i] : tile[a][i], u);
+        for (int p = 0; p < InTiles<K>::kParts; ++p) w.across[p * w.across_part + (c0 + i) * w.d_ld + d0 + a] = u[p];
         if (w.down && d0 + i < w.d) {
             split(tile[i][a], v);
             for (int p = 0; p < K::kParts; ++p) w.down[p * w.down_part + (d0 + i) * w.f2_ld + c0 + a] = v[p];
@@ -351,7 +360,7 @@ template <class K> struct GateArgs {
 template <class K, class B, bool BACK> __global__ __launch_bounds__(B::kThreads) void k_gates(GateArgs<K> a)
 {
     using T = typename K::T;
-    using P = typename B::template Of<typename K::T, K::kParts, true, true>;
+    using P = typename B::template Of<typename InTiles<K>::T, InTiles<K>::kParts, true, true>;
     __shared__ typename P::Lds lds;
     const int64_t tile = xcd_order(blockIdx.x, gridDim.x), m0 = tile / a.n_tiles * B::kRows, n0 = tile % a.n_tiles * B::kCols;
     f32x16 acc[B::kPer / 32][2] = {};
@@ -444,7 +453,7 @@ template <class K, class B, bool BACK> __global__ __launch_bounds__(B::kThreads)
 // once for each such group of columns (from the L2 for all but the first), and nothing but the weights is laid out before.  1,000,188 x 64 -> 128 bf16: 124 us (3.1 TB/s; 189 by k_gates,
 // whose blocks have one step of products each).
 template <class K, int STEPS> struct NarrowShape {
-    static constexpr int kDp = STEPS * 16, kPairs = (K::kParts == 1 ? 256 : 128) / kDp, kFrags = kPairs * 2 * STEPS * Inner<K>::kParts;   // 32 KB of weights
+    static constexpr int kDp = STEPS * 16, kPairs = (Inner<K>::kParts == 1 ? 256 : 128) / kDp, kFrags = kPairs * 2 * STEPS * Inner<K>::kParts;   // 32 KB of weights
     static constexpr int kStage = 32 * 72;   // elements of 16 bits for a wavefront's results on their way out: 32 rows of 64 and 8 (or of 32 and 4 fp32)
 };
 template <class K> struct NarrowArgs {
@@ -905,11 +914,11 @@ constexpr int64_t kFull = 256;                // blocks that leave no compute un
 constexpr int64_t kNarrowBlocks = 1024;       // blocks of such a launch
 
 struct Plan {
-    int parts;
+    int parts;                                 // of G, V and what they are multiplied with (without a gradient: of g's and v's factors)
     bool pack_x;
     int64_t d_p, f2, gv_ld, d_ld, chunk;       // columns of the laid out x and weights and where their rows lie, rows of a chunk
     int64_t splits, run;
-    size_t across, down, xs, gv, part, bias, x_exponent, w_scale, bytes;   // offsets (x_exponent: and which rows fall short; w_scale: scales, exponents, which columns do)
+    size_t across, down, x_tiles, xs, gv, part, bias, x_exponent, w_scale, bytes;   // offsets (x_exponent: and which rows fall short; w_scale: scales, exponents, which columns do)
 };
 
 // Whether a call goes by Scaled: large enough for its one more launch and the counts to pay (us, and by three bf16 parts: 3000 x 256 x 256 28 and 26, 4000 x 256 x 512 30 and 30,
@@ -935,7 +944,8 @@ template <class K, class Fn> void with_tile(int64_t cols, int64_t rows, bool spl
 Plan plan_of(const GatedArgs &a, bool grad)
 {
     Plan p{};
-    p.parts = by_scale(a, grad) ? Scaled::kParts : parts_of(a.dtype);
+    const bool half_back = a.dtype == MLIP_DTYPE_F16 && grad;
+    p.parts = by_scale(a, grad) ? Scaled::kParts : parts_of(a.dtype, grad);
     p.pack_x = !reads_x(a);
     p.d_p = pad_to(a.d, kPadK);
     p.f2 = 2 * pad_to(a.f, 32);
@@ -950,15 +960,16 @@ Plan plan_of(const GatedArgs &a, bool grad)
     if (p.chunk > all) p.chunk = all;
     size_t at = 0;
     auto take = [&](int64_t bytes) { const size_t here = at; at += (size_t)pad_to(bytes, 256); return here; };
-    p.across = take(p.f2 * p.d_ld * p.parts * 2);
+    p.across = take(p.f2 * p.d_ld * (half_back ? 1 : p.parts) * 2);
+    if (half_back && a.d > kNarrow) p.x_tiles = take(p.chunk * p.d_ld * 2);
     if (grad || a.d > kNarrow) p.xs = take(p.chunk * p.d_ld * p.parts * 2);
     if (by_scale(a, grad)) p.x_exponent = take(2 * p.chunk * 4);
     if (a.dtype == MLIP_DTYPE_F32) p.w_scale = take(3 * p.f2 * 4);
     if (grad) {
         p.down = take(a.d * p.gv_ld * p.parts * 2);
         p.gv = take(p.chunk * p.gv_ld * p.parts * 2);
-        const int64_t tiles = p.parts == 1 && a.d >= 512 && p.f2 >= 512 ? (p.f2 + 255) / 256 * ((a.d + 255) / 256) : a.d <= 64 ? (p.f2 + 255) / 256 : (p.f2 + 127) / 128 * ((a.d + 127) / 128);
-        const int64_t blocks = p.parts == 1 && a.d >= 512 && p.f2 >= 512 ? 256 : 512;   // one or two to a compute unit
+        const int64_t tiles = p.parts <= 2 && a.d >= 512 && p.f2 >= 512 ? (p.f2 + 255) / 256 * ((a.d + 255) / 256) : a.d <= 64 ? (p.f2 + 255) / 256 : (p.f2 + 127) / 128 * ((a.d + 127) / 128);
+        const int64_t blocks = p.parts <= 2 && a.d >= 512 && p.f2 >= 512 ? 256 : 512;   // one or two to a compute unit
         int64_t splits = blocks / tiles, most_splits = (p.chunk + 127) / 128;
         if (splits > most_splits) splits = most_splits;
         if (splits < 1) splits = 1;
@@ -976,18 +987,21 @@ Plain plain_of(const GatedArgs &a)
     return {static_cast<const float *>(a.wg), static_cast<const float *>(a.wv), a.wg_rs, a.wg_cs, a.wv_rs, a.wv_cs, (int32_t)a.d, (int32_t)a.f};
 }
 
-template <class K> int launch(const GatedArgs &a, const GatedGrad *g)
+// g: of a gradient (BACK)
+template <class K, bool BACK> int launch(const GatedArgs &a, const GatedGrad *g)
 {
     using E = typename K::E;
     using T = typename K::T;
-    const Plan p = plan_of(a, g != nullptr);
+    const Plan p = plan_of(a, BACK);
     char *ws = static_cast<char *>(a.workspace);
-    T *across = reinterpret_cast<T *>(ws + p.across), *down = g ? reinterpret_cast<T *>(ws + p.down) : nullptr, *xs = reinterpret_cast<T *>(ws + p.xs);
-    T *gv = g ? reinterpret_cast<T *>(ws + p.gv) : nullptr;
-    const bool in_registers = a.d <= kNarrow, strided = a.x_cs != 1 || (g && g->bar_cs != 1);
-    const bool rows = !g || g->dx, weights = g && (g->dwg || g->dwv || g->dbg || g->dbv);
+    using Tiles = InTiles<K>;
+    constexpr bool apart = !std::is_same_v<K, Tiles>;   // whether the products with G and V have x in other parts than those that make g and v
+    typename Tiles::T *across = reinterpret_cast<typename Tiles::T *>(ws + p.across), *x_tiles = reinterpret_cast<typename Tiles::T *>(ws + (apart ? p.x_tiles : p.xs));
+    T *down = reinterpret_cast<T *>(ws + p.down), *xs = reinterpret_cast<T *>(ws + p.xs), *gv = reinterpret_cast<T *>(ws + p.gv);
+    const bool in_registers = a.d <= kNarrow, strided = a.x_cs != 1 || (BACK && g->bar_cs != 1);
+    const bool weights = BACK && (g->dwg || g->dwv || g->dbg || g->dbv);
     const Weights<K> w = {static_cast<const E *>(a.wg), static_cast<const E *>(a.wv), a.wg_rs, a.wg_cs, a.wv_rs, a.wv_cs, a.d, a.f, p.d_ld, p.gv_ld,
-                          across, rows ? down : nullptr, p.f2 * p.d_ld, a.d * p.gv_ld};
+                          across, BACK && g->dx ? down : nullptr, p.f2 * p.d_ld, a.d * p.gv_ld};
     float *w_exponent = reinterpret_cast<float *>(ws + p.w_scale);
     int32_t *w_short = reinterpret_cast<int32_t *>(w_exponent + p.f2);
     if (a.n > 0 && in_registers && K::kParts == 3) {
@@ -1000,15 +1014,19 @@ template <class K> int launch(const GatedArgs &a, const GatedGrad *g)
         const int64_t n = a.n - first < p.chunk ? a.n - first : p.chunk;
         if (n <= 0 && a.n > 0) break;
         const E *x = static_cast<const E *>(a.x) + first * a.x_rs;
-        Panel xp = {x, a.x_rs, 0, n, a.d};
-        if (p.pack_x && n > 0 && (weights || !in_registers)) {
-            const int64_t threads = n * (p.d_p / 8);
-            k_pack_rows<K><<<(unsigned)((threads + kPackThreads - 1) / kPackThreads), kPackThreads, 0, a.stream>>>(x, a.x_rs, a.x_cs, n, a.d, p.d_p, xs, p.d_ld, p.chunk * p.d_ld);
-            xp = {xs, p.d_ld, p.chunk * p.d_ld, n, p.d_p};
+        Panel xp = {x, a.x_rs, 0, n, a.d}, xw = xp;
+        const unsigned pack_blocks = (unsigned)((n * (p.d_p / 8) + kPackThreads - 1) / kPackThreads);
+        if (p.pack_x && n > 0 && (!in_registers || (weights && !apart))) {
+            k_pack_rows<Tiles><<<pack_blocks, kPackThreads, 0, a.stream>>>(x, a.x_rs, a.x_cs, n, a.d, p.d_p, x_tiles, p.d_ld, p.chunk * p.d_ld);
+            xp = xw = {x_tiles, p.d_ld, p.chunk * p.d_ld, n, p.d_p};
+        }
+        if (apart && n > 0 && weights) {
+            k_pack_rows<K><<<pack_blocks, kPackThreads, 0, a.stream>>>(x, a.x_rs, a.x_cs, n, a.d, p.d_p, xs, p.d_ld, p.chunk * p.d_ld);
+            xw = {xs, p.d_ld, p.chunk * p.d_ld, n, p.d_p};
         }
         if (n > 0) {
             GateArgs<K> ga = {xp, across_panel, p.d_p, a.f, 0, a.act, static_cast<const E *>(a.bg), static_cast<const E *>(a.bv)};
-            if (!g) {
+            if constexpr (!BACK) {
                 ga.out = static_cast<E *>(a.out) + first * a.out_rs;
                 ga.out_rs = a.out_rs;
             } else {
@@ -1029,19 +1047,18 @@ template <class K> int launch(const GatedArgs &a, const GatedGrad *g)
                 na.a.plain = plain_of(a);
                 const int64_t most = kNarrowBlocks / na.groups > 0 ? kNarrowBlocks / na.groups : 1, blocks = (na.tiles + 3) / 4;
                 na.blocks = (int32_t)(blocks < most ? blocks : most);
-                (strided ? g ? k_gates_narrow<K, STEPS, true, true> : k_gates_narrow<K, STEPS, false, true>
-                         : g ? k_gates_narrow<K, STEPS, true, false> : k_gates_narrow<K, STEPS, false, false>)<<<(unsigned)(na.blocks * na.groups), 256, 0, a.stream>>>(na);
+                (strided ? k_gates_narrow<K, STEPS, BACK, true> : k_gates_narrow<K, STEPS, BACK, false>)<<<(unsigned)(na.blocks * na.groups), 256, 0, a.stream>>>(na);
             };
             if (in_registers && a.d <= 64) narrow(std::integral_constant<int, 4>{});
             else if (in_registers) narrow(std::integral_constant<int, 8>{});
-            else with_tile<K>(p.f2, n, false, [&](auto block) {
+            else with_tile<Tiles>(p.f2, n, false, [&](auto block) {
                 using B = decltype(block);
                 ga.n_tiles = (p.f2 + B::kCols - 1) / B::kCols;
                 const unsigned blocks = (unsigned)((n + B::kRows - 1) / B::kRows * ga.n_tiles);
-                (g ? k_gates<K, B, true> : k_gates<K, B, false>)<<<blocks, B::kThreads, 0, a.stream>>>(ga);
+                k_gates<K, B, BACK><<<blocks, B::kThreads, 0, a.stream>>>(ga);
             });
         }
-        if (g) {
+        if constexpr (BACK) {
             const Panel gp = {gv, p.gv_ld, p.chunk * p.gv_ld, n, p.f2};
             auto row_args = [&](auto block) {
                 using B = decltype(block);
@@ -1053,7 +1070,7 @@ template <class K> int launch(const GatedArgs &a, const GatedGrad *g)
             };
             auto weight_args = [&](auto block) {
                 using B = decltype(block);
-                return WeightSumArgs<K>{gp, xp, a.d, (p.f2 + B::kRows - 1) / B::kRows, (a.d + B::kCols - 1) / B::kCols, p.run, reinterpret_cast<float *>(ws + p.part),
+                return WeightSumArgs<K>{gp, xw, a.d, (p.f2 + B::kRows - 1) / B::kRows, (a.d + B::kCols - 1) / B::kCols, p.run, reinterpret_cast<float *>(ws + p.part),
                                         g->dbg || g->dbv ? reinterpret_cast<float *>(ws + p.bias) : nullptr, first > 0};
             };
             bool together = false;
@@ -1079,7 +1096,7 @@ template <class K> int launch(const GatedArgs &a, const GatedGrad *g)
         }
         first += p.chunk;
     } while (first < a.n);
-    if (weights) {
+    if constexpr (BACK) if (weights) {
         const JoinArgs<K> ja = {reinterpret_cast<float *>(ws + p.part), reinterpret_cast<float *>(ws + p.bias), p.splits, a.d, a.f, p.f2, static_cast<E *>(g->dwg),
                                 static_cast<E *>(g->dwv), static_cast<E *>(g->dbg), static_cast<E *>(g->dbv), g->dwg_rs, g->dwg_cs, g->dwv_rs, g->dwv_cs};
         const dim3 blocks((unsigned)(p.f2 / 8), (unsigned)((a.d + 31) / 32));
@@ -1135,12 +1152,12 @@ int gated_impl(const GatedArgs &a)
 {
     if (a.n == 0) return MLIP_OK;
     if (by_scale(a, false)) return launch_scaled(a);
-    return with_kind(a.dtype, [&](auto kind) { return launch<decltype(kind)>(a, nullptr); });
+    return with_kind<false>(a.dtype, [&](auto kind) { return launch<decltype(kind), false>(a, nullptr); });
 }
 
 int gated_grad_impl(const GatedArgs &a, const GatedGrad &g)
 {
-    return with_kind(a.dtype, [&](auto kind) { return launch<decltype(kind)>(a, &g); });
+    return with_kind<true>(a.dtype, [&](auto kind) { return launch<decltype(kind), true>(a, &g); });
 }
 
 }  // namespace mlip
