@@ -307,20 +307,44 @@ __global__ __launch_bounds__(kPackThreads) void k_pack_scaled_rows(const float *
 // ---------------------------------------------------------------- phi
 
 __device__ inline float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.f + __expf(-x)); }
+// sigmoid(x) and 1 - sigmoid(x), the latter to its own size's precision
+struct Sigmoid { float s, rest; };
+__device__ inline Sigmoid sigmoid_both(float x)
+{
+    const float e = __expf(-fabsf(x)), r = __builtin_amdgcn_rcpf(1.f + e), q = e * r;
+    return x < 0.f ? Sigmoid{q, r} : Sigmoid{r, q};
+}
 
-struct Phi { float h, g, v; };   // phi, its derivatives
+// Phi(x), the normal distribution function, given e = exp(-x^2 / 2): Phi(-|x|) is e times a function that falls like 1 / |x|, here a polynomial in u = 1 / (1 + 0.35 |x|) of
+// least relative error for |x| <= 14.5 (2^-25, in fp32 2^-21.5; 1 + erf would cancel in the tail; 1,000,188 x 64 -> 128 bf16 142 us, with erf 170, with erfc 198)
+__device__ inline float normal(float x, float e)
+{
+    constexpr float c[9] = {0.139621302f, 0.139863521f, 0.119821288f, 0.105552502f, -0.0232123528f, 0.159319699f, -0.25583899f, 0.144030914f, -0.0291578863f};
+    const float u = __builtin_amdgcn_rcpf(fmaf(0.35f, fabsf(x), 1.f));
+    float q = c[8];
+#pragma unroll
+    for (int k = 7; k >= 0; --k) q = fmaf(q, u, c[k]);
+    q *= u * e;
+    return x < 0.f ? q : 1.f - q;
+}
 
-template <int ACT> __device__ inline Phi phi(float g, float v)
+struct Phi { float h, g, v; };   // phi, its derivatives (BACK)
+
+template <int ACT, bool BACK> __device__ inline Phi phi(float g, float v)
 {
     if constexpr (ACT == MLIP_GATE_GELU) {
-        const float c = 0.5f + 0.5f * erff(g * 0.70710678f);
-        return {g * c * v, (c + g * __expf(-0.5f * g * g) * 0.39894228f) * v, g * c};
+        const float e = __expf(-0.5f * g * g), c = normal(g, e);
+        return {g * c * v, (c + g * e * 0.39894228f) * v, g * c};
     }
-    const float s = sigmoid(g);
-    if constexpr (ACT == MLIP_GATE_SILU) return {g * s * v, s * (1.f + g * (1.f - s)) * v, g * s};
-    if constexpr (ACT == MLIP_GATE_SIGMOID) return {s * v, s * (1.f - s) * v, s};
-    const float t = sigmoid(v), b = v * t;
-    return {s * b, s * (1.f - s) * b, s * t * (1.f + v * (1.f - t))};
+    Sigmoid s{}, t{};
+    if constexpr (BACK) s = sigmoid_both(g);
+    else s.s = sigmoid(g);
+    if constexpr (ACT == MLIP_GATE_SILU) return {g * s.s * v, s.s * (1.f + g * s.rest) * v, g * s.s};
+    if constexpr (ACT == MLIP_GATE_SIGMOID) return {s.s * v, s.s * s.rest * v, s.s};
+    if constexpr (BACK) t = sigmoid_both(v);
+    else t.s = sigmoid(v);
+    const float b = v * t.s;
+    return {s.s * b, s.s * s.rest * b, s.s * t.s * (1.f + v * t.rest)};
 }
 
 template <class Fn> __device__ inline void with_act(int act, Fn &&f)
@@ -422,7 +446,7 @@ template <class K, class B, bool BACK> __global__ __launch_bounds__(B::kThreads)
                 if constexpr (BACK) load_cols(bar, a.bar + row * a.bar_rs, a.bar_cs, f, a.f);
 #pragma unroll
                 for (int t = 0; t < W; ++t) {
-                    const Phi y = phi<decltype(act)::value>(g[t] + bg[t], v[t] + bv[t]);
+                    const Phi y = phi<decltype(act)::value, BACK>(g[t] + bg[t], v[t] + bv[t]);
                     if constexpr (!BACK) g[t] = y.h;
                     else {
                         g[t] = f + t < a.f ? bar[t] * y.g : 0.f;
@@ -525,7 +549,7 @@ __device__ inline void gates_again(const NarrowArgs<K> &na, const uint32_t *shor
                     if constexpr (BACK) load_cols(bar, a.bar + row * a.bar_rs, a.bar_cs, f0 + c, a.f);
 #pragma unroll
                     for (int t = 0; t < 4; ++t) {
-                        const Phi y = phi<decltype(act)::value>(g[4 * q + t] + bias[0][pair * 32 + c + t], v[4 * q + t] + bias[1][pair * 32 + c + t]);
+                        const Phi y = phi<decltype(act)::value, BACK>(g[4 * q + t] + bias[0][pair * 32 + c + t], v[4 * q + t] + bias[1][pair * 32 + c + t]);
                         if (!(mask >> (c + t) & 1) || f0 + c + t >= a.f) continue;
                         if constexpr (!BACK) a.out[row * a.out_rs + f0 + c + t] = y.h;
                         else {
@@ -680,7 +704,7 @@ template <class K, int STEPS, bool BACK, bool STRIDED> __global__ __launch_bound
                     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                     for (int t = 0; t < 4; ++t) {
-                        const Phi y = phi<decltype(act)::value>(g[4 * q + t] + bg[t], v[4 * q + t] + bv[t]);
+                        const Phi y = phi<decltype(act)::value, BACK>(g[4 * q + t] + bg[t], v[4 * q + t] + bv[t]);
                         if constexpr (!BACK) g[4 * q + t] = y.h;
                         else {
                             g[4 * q + t] = f + t < a.f ? bar[q][t] * y.g : 0.f;
