@@ -92,10 +92,11 @@ __global__ __launch_bounds__(kThreads) void k_squares(List l, double *part)
     if (threadIdx.x == 0) part[blockIdx.y * kNormBlocks + blockIdx.x] = sum;
 }
 
-// What X_0 is G times, x_scale included
+// What X_0 is G times, x_scale included; NaN for a matrix with an infinity or NaN (squares of fp32 values do not overflow)
 __device__ inline double start_scale(double squares, double eps, float x_scale)
 {
-    const double norm = sqrt(squares), by = norm > eps || norm != norm ? norm : eps;
+    if (!(squares < __builtin_inf())) return __builtin_nan("");
+    const double norm = sqrt(squares), by = norm > eps ? norm : eps;
     return by == 0.0 ? (double)x_scale : (double)x_scale / by;   // (zeros stay zeros)
 }
 
