@@ -581,7 +581,9 @@ int residual_grad_impl(const ResidualArgs &a, const ResidualGrad &g)
     for (void *s : b.sum) any |= s != nullptr;
     if (any && blocks > 1) b.part = static_cast<float *>(g.workspace);
     if (a.n == 0 && !any) return MLIP_OK;
-    return run<true>(a, b, blocks);
+    ResidualArgs used = a;
+    used.pre = a.pre && g.dn;   // a norm that nobody used: nothing comes back through it, not even where it is NaN
+    return run<true>(used, b, blocks);
 }
 
 }  // namespace mlip
