@@ -784,6 +784,14 @@ def mlip_gated_grad(grad, x, w_gate, w_value, b_gate=None, b_value=None, act="si
     return _gated_grad(grad, (x, w_gate, w_value, b_gate, b_value), act, (True,) * 5)
 
 
+def _params_of(post, pre):
+    """(post weights, post biases, pre weights, pre biases), None for what there is not"""
+    for norm, what in ((post, "post"), (pre, "pre")):
+        if norm is not None and (not isinstance(norm, (tuple, list)) or len(norm) != 2):
+            _refuse(f"{what} must be None or a pair (weights, biases)")
+    return (*((None, None) if post is None else post), *((None, None) if pre is None else pre))
+
+
 def _residual_call(x, z, gate, scale, post, pre, kind, eps, factor):
     """(the call's structure, its tensors)"""
     dtype = _DTYPES.get(x.dtype)
@@ -813,7 +821,7 @@ def _residual_call(x, z, gate, scale, post, pre, kind, eps, factor):
         gate_at = gate.data_ptr()
         tensors.append(gate)
     param_dtype, at = None, []
-    for p in (scale, *(post or (None, None)), *(pre or (None, None))):
+    for p in (scale, *_params_of(post, pre)):
         if p is None:
             at.append(None)
             continue
@@ -851,7 +859,7 @@ def _residual_backward(dy, dn, x, z, gate, scale, post, pre, kind, eps, factor, 
         dn_at = dn.data_ptr()
         tensors.append(dn)
     stream = _stream_of(*tensors)
-    inputs = (x, z, gate, scale, *(post or (None, None)), *(pre or (None, None)))
+    inputs = (x, z, gate, scale, *_params_of(post, pre))
     outs = [t.new_empty(t.shape) if need and t is not None else None for t, need in zip(inputs, needs)]
     dx, dz, dgate, *rest = [None if t is None else t.data_ptr() for t in outs]
     width = call.width
@@ -890,7 +898,7 @@ class _ResidualFn(torch.autograd.Function):
 
 def _residual_any(x, z, gate, scale, post, pre, kind, eps, factor):
     """The outputs that there are"""
-    params = (*(post or (None, None)), *(pre or (None, None)))
+    params = _params_of(post, pre)
     if _wants_graph(x, z, gate, scale, *params):
         return _ResidualFn.apply((post is not None, pre is not None, kind, eps, factor), x, z, gate, scale, *params)
     return tuple(t for t in _residual_forward(x, z, gate, scale, post, pre, kind, eps, factor) if t is not None)
