@@ -943,7 +943,7 @@ def mlip_orthogonalise(updates, steps=5, coefficients=(3.4445, -4.7750, 2.0315),
     """Orthogonalises matrices (gradients or their running means, before an update): X = G / max(|G|, eps), then `steps` times
     X <- (a + b X X^T + c (X X^T)^2) X, of the transpose where a matrix has more rows than columns; times `scale`.
 
-    updates, out: iterables of cuda matrices [rows, cols] or stacks of them [k, rows, cols], float32, bfloat16 or float16, any strides.  In place, or
+    updates, out: iterables of cuda matrices [rows, cols] or stacks of them [k, rows, cols], float32, bfloat16 or float16, any strides, each matrix once.  In place, or
     into the tensors of `out` (of the same types and shapes).  Not recorded by autograd.  Returns the list of results."""
     updates = _listed(updates)
     given, out = out is not None, updates if out is None else _listed(out)
@@ -965,6 +965,12 @@ def mlip_orthogonalise(updates, steps=5, coefficients=(3.4445, -4.7750, 2.0315),
             for s, d in zip(src.unbind(0), dst.unbind(0)):
                 words.extend((s.data_ptr(), d.data_ptr(), *s.shape, *s.stride(), *d.stride(), code))
     at, count = words.buffer_info()[0], len(words) // 9
+    src, dst = words[::9], words[1::9]
+    if len(set(dst)) < count or (given and not set(src).isdisjoint(dst)):
+        there = [k for k in range(count) if words[9 * k + 2] and words[9 * k + 3]]      # (those with elements)
+        written = {dst[k]: k for k in there}
+        if len(written) < len(there) or any(written.get(src[k], k) != k for k in there):
+            _refuse("a matrix must not be in the list twice, or be another one's result")
     need = lib().mlip_orthogonalise_workspace(at, count)
     ws, ws_at = _scratch(need)
     _check(lib().mlip_orthogonalise(at, count, steps, (ctypes.c_double * 3)(a, b, c), eps, scale, ws_at, need, _stream()))
