@@ -726,7 +726,24 @@ def _gated_call(x, w_gate, w_value, b_gate, b_value, act):
 
 
 def _wants_graph(*tensors):
-    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
+    if torch.is_grad_enabled():
+        for t in tensors:
+            if t is not None and t.requires_grad:
+                return True
+    return False
+
+
+class _GradFn(torch.autograd.Function):
+    """A gradient call of these operators in an autograd graph: its results need a gradient where its inputs do, and there is none to be had"""
+
+    @staticmethod
+    def forward(ctx, name, call, *inputs):
+        ctx.name = name
+        return call()
+
+    @staticmethod
+    def backward(ctx, *bars):
+        _refuse(f"{ctx.name} cannot be differentiated (there are no second derivatives)")
 
 
 class _GatedFn(torch.autograd.Function):
@@ -780,16 +797,19 @@ def _gated_grad(grad, inputs, act, needs):
 
 
 def mlip_gated_grad(grad, x, w_gate, w_value, b_gate=None, b_value=None, act="silu"):
-    """Gradients of mlip_gated for x, w_gate, w_value, b_gate and b_value (None for a bias that is None) from grad, the gradient of its result."""
-    return _gated_grad(grad, (x, w_gate, w_value, b_gate, b_value), act, (True,) * 5)
+    """Gradients of mlip_gated for x, w_gate, w_value, b_gate and b_value (None for a bias that is None) from grad, the gradient of its result.  Not differentiable."""
+    inputs = x, w_gate, w_value, b_gate, b_value
+    if _wants_graph(grad, *inputs):
+        return _GradFn.apply("mlip_gated_grad", lambda: _gated_grad(grad, inputs, act, (True,) * 5), grad, *inputs)
+    return _gated_grad(grad, inputs, act, (True,) * 5)
 
 
 def _params_of(post, pre):
-    """(post weights, post biases, pre weights, pre biases), None for what there is not"""
+    """(post weights, post biases, pre weights, pre biases), None for what there is not; checks that they are pairs"""
     for norm, what in ((post, "post"), (pre, "pre")):
         if norm is not None and (not isinstance(norm, (tuple, list)) or len(norm) != 2):
             _refuse(f"{what} must be None or a pair (weights, biases)")
-    return (*((None, None) if post is None else post), *((None, None) if pre is None else pre))
+    return *(post or (None, None)), *(pre or (None, None))
 
 
 def _residual_call(x, z, gate, scale, post, pre, kind, eps, factor):
@@ -821,7 +841,7 @@ def _residual_call(x, z, gate, scale, post, pre, kind, eps, factor):
         gate_at = gate.data_ptr()
         tensors.append(gate)
     param_dtype, at = None, []
-    for p in (scale, *_params_of(post, pre)):
+    for p in (scale, *(post or (None, None)), *(pre or (None, None))):
         if p is None:
             at.append(None)
             continue
@@ -859,7 +879,7 @@ def _residual_backward(dy, dn, x, z, gate, scale, post, pre, kind, eps, factor, 
         dn_at = dn.data_ptr()
         tensors.append(dn)
     stream = _stream_of(*tensors)
-    inputs = (x, z, gate, scale, *_params_of(post, pre))
+    inputs = (x, z, gate, scale, *(post or (None, None)), *(pre or (None, None)))
     outs = [t.new_empty(t.shape) if need and t is not None else None for t, need in zip(inputs, needs)]
     dx, dz, dgate, *rest = [None if t is None else t.data_ptr() for t in outs]
     width = call.width
@@ -916,13 +936,21 @@ def mlip_residual(x, z, gate=None, scale=None, post=None, pre=None, kind="rms", 
     return outs if pre is not None else outs[0]
 
 
+def _residual_grads(name, *args):
+    dy, dn, x, z, gate, scale, post, pre, *_ = args
+    inputs = dy, dn, x, z, gate, scale, *_params_of(post, pre)
+    if _wants_graph(*inputs):
+        return _GradFn.apply(name, lambda: tuple(_residual_backward(*args, (True,) * 8)), *inputs)
+    return _residual_backward(*args, (True,) * 8)
+
+
 def mlip_residual_grad(dy, dn, x, z, gate=None, scale=None, post=None, pre=None, kind="rms", eps=1e-6, factor=1.0):
     """Gradients of mlip_residual from those of its sum (dy) and of the norm (dn; either may be None, not both).
 
-    Returns (dx, dz, dgate, dscale, (d post weights, d post biases), (d pre weights, d pre biases)), None for what there is not."""
+    Returns (dx, dz, dgate, dscale, (d post weights, d post biases), (d pre weights, d pre biases)), None for what there is not.  Not differentiable."""
     if z is None:
         _refuse("mlip_residual_grad needs z (a norm alone: mlip_norm_grad)")
-    dx, dz, dgate, dscale, *d = _residual_backward(dy, dn, x, z, gate, scale, post, pre, kind, eps, factor, (True,) * 8)
+    dx, dz, dgate, dscale, *d = _residual_grads("mlip_residual_grad", dy, dn, x, z, gate, scale, post, pre, kind, eps, factor)
     return dx, dz, dgate, dscale, tuple(d[:2]) if post is not None else None, tuple(d[2:]) if pre is not None else None
 
 
@@ -934,8 +962,8 @@ def mlip_norm(x, weight=None, bias=None, kind="rms", eps=1e-6):
 
 
 def mlip_norm_grad(grad, x, weight=None, bias=None, kind="rms", eps=1e-6):
-    """Gradients of mlip_norm for x, weight and bias (None for one that is None) from grad, the gradient of its result."""
-    d = _residual_backward(None, grad, x, None, None, None, None, (weight, bias), kind, eps, 1.0, (True,) * 8)
+    """Gradients of mlip_norm for x, weight and bias (None for one that is None) from grad, the gradient of its result.  Not differentiable."""
+    d = _residual_grads("mlip_norm_grad", None, grad, x, None, None, None, None, (weight, bias), kind, eps, 1.0)
     return d[0], d[6], d[7]
 
 
