@@ -725,12 +725,20 @@ def _gated_call(x, w_gate, w_value, b_gate, b_value, act):
     return call, [t for t in (x, w_gate, w_value, b_gate, b_value) if t is not None]
 
 
+def _forward_level():
+    """Below 0 where there is no forward-mode differentiation"""
+    return getattr(torch.autograd.forward_ad, "_current_level", 0)
+
+
 def _wants_graph(*tensors):
+    """Whether autograd has to know of a call with these tensors"""
     if torch.is_grad_enabled():
         for t in tensors:
             if t is not None and t.requires_grad:
                 return True
-    return False
+    if _forward_level() < 0:
+        return False
+    return any(t is not None and torch.autograd.forward_ad.unpack_dual(t).tangent is not None for t in tensors)     # (which these functions then refuse)
 
 
 class _GradFn(torch.autograd.Function):

@@ -43,3 +43,20 @@ def test_results_of_gradient_calls_stay_in_the_graph(name):
             got[0].sum().backward()
         with torch.no_grad():
             assert not any(t.requires_grad for t in _flat(call(here)))
+
+
+def test_forward_mode_is_refused():
+    """A dual tensor's tangent is not lost in silence"""
+    import torch
+    import torch.autograd.forward_ad as fwd
+    import paper_2506_02023_amd as M
+    v = _inputs()
+    calls = [lambda x: M.mlip_gated(x, v["wg"], v["wv"]), lambda x: M.mlip_residual(x, v["z"]), lambda x: M.mlip_norm(x), lambda x: M.mlip_gated_grad(v["grad"], x, v["wg"], v["wv"]),
+             lambda x: M.mlip_residual_grad(v["dy"], None, x, v["z"]), lambda x: M.mlip_norm_grad(v["dn"], x)]
+    plain = [_flat(c(v["x"])) for c in calls]
+    with fwd.dual_level():
+        dual = fwd.make_dual(v["x"], torch.ones_like(v["x"]))
+        for call, want in zip(calls, plain):
+            with pytest.raises((RuntimeError, NotImplementedError)):
+                call(dual)
+            assert all(torch.equal(a, b) for a, b in zip(_flat(call(v["x"])), want))       # (others' calls go on)
