@@ -789,19 +789,15 @@ def _gated_grad(grad, inputs, act, needs):
     call, tensors = _gated_call(*inputs, act)
     rs, cs = _rows_of(grad, "grad", (call.n, call.f), inputs[0].dtype)
     stream = _stream_of(grad, *tensors)
-    outs = [torch.empty_like(t) if need and t is not None else None for t, need in zip(inputs, needs)]
-    if outs[0] is not None:
-        outs[0] = inputs[0].new_empty(inputs[0].shape)
-    for k in (1, 2):
-        if outs[k] is not None and not _dense(outs[k]):
-            outs[k] = inputs[k].new_empty(inputs[k].shape)
-    dx, dwg, dwv, dbg, dbv = outs
+    # (the weights' in the order of the weights: empty_like() of any strides is dense)
+    dx = inputs[0].new_empty(inputs[0].shape) if needs[0] else None
+    dwg, dwv, dbg, dbv = (torch.empty_like(t) if need and t is not None else None for t, need in zip(inputs[1:], needs[1:]))
     strides = [t.stride() if t is not None else (0, 0) for t in (dwg, dwv)]
     g = _GatedGrad(grad.data_ptr(), rs, cs, _address(dx), call.d, _address(dwg), *strides[0], _address(dwv), *strides[1], _address(dbg), _address(dbv))
     need = lib().mlip_gated_workspace(call, 1)
     ws, at = _scratch(need)
     _check(lib().mlip_gated_grad(call, g, at, need, stream))
-    return tuple(outs)
+    return dx, dwg, dwv, dbg, dbv
 
 
 def mlip_gated_grad(grad, x, w_gate, w_value, b_gate=None, b_value=None, act="silu"):
