@@ -183,15 +183,23 @@ __global__ __launch_bounds__(kScaleThreads) void k_column_scales(Weights<Scaled>
     const bool value = is_value(c);
     const float *src = value ? w.wv : w.wg;
     const int64_t rs = value ? w.v_rs : w.g_rs, cs = value ? w.v_cs : w.g_cs;
-    float m = 0.f;
-    if (f < w.f) in_steps<8>(threadIdx.x >> 5, w.d, kScaleThreads / 32, [&](int64_t d) { return src[d * rs + f * cs]; }, [&](float x) { m = fmaxf(m, fabsf(x)); });
+    constexpr int kHeld = 16, kStep = kScaleThreads / 32;   // values that a thread keeps from the first look to the second: columns of up to 512
+    const int first = threadIdx.x >> 5;
+    float held[kHeld], m = 0.f;
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k) held[k] = f < w.f && first + k * kStep < w.d ? src[(first + k * kStep) * rs + f * cs] : 0.f;
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k) m = fmaxf(m, fabsf(held[k]));
+    if (f < w.f) in_steps<8>(first + kHeld * kStep, w.d, kStep, [&](int64_t d) { return src[d * rs + f * cs]; }, [&](float x) { m = fmaxf(m, fabsf(x)); });
     most[threadIdx.x] = m;
     __syncthreads();
     for (int k = threadIdx.x & 31; k < kScaleThreads; k += 32) m = fmaxf(m, most[k]);
     const int e = scale_for(m);
     const float by = ldexpf(1.f, e);
     Counts n;
-    if (f < w.f) in_steps<8>(threadIdx.x >> 5, w.d, kScaleThreads / 32, [&](int64_t d) { return src[d * rs + f * cs]; }, [&](float x) { n.add(x * by); });
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k) n.add(held[k] * by);
+    if (f < w.f) in_steps<8>(first + kHeld * kStep, w.d, kStep, [&](int64_t d) { return src[d * rs + f * cs]; }, [&](float x) { n.add(x * by); });
     counts[threadIdx.x] = n.large;
     __syncthreads();
     if (threadIdx.x >= 32) return;
