@@ -480,7 +480,9 @@ int mlip_clip_grads(const mlip_tensor_t *tensors, int32_t count, float max_norm,
  *   x        DEVICE [n][d], any strides;  w_gate, w_value DEVICE [d][f], any strides (so that weights kept as [f][d] serve as well)
  *   b_gate, b_value   DEVICE [f], one element after another, or NULL
  *   out      DEVICE [n][f], element (i, k) at i * out_row_stride + k
- * 0 <= n < 2^31, 1 <= d, f <= 65536.  mlip_gated_workspace returns 0 for calls that are refused.
+ * 0 <= n < 2^31, 1 <= d, f <= 65536.  mlip_gated_workspace returns 0 for calls that are refused.  It asks for the weights once more (fp32: in parts) and, where they are laid out
+ * first, for x, gradients also for 4 f values a row and for the weights' gradients in fp32 as many times as rows are split for them; of many rows, those of one chunk, 4 GB
+ * (32,768 x 1024 -> 4096 bf16: 89 MB, its gradient 714; 1,000,188 x 64 -> 128 fp32: 0.1 MB and 2.3 GB).
  */
 enum { MLIP_GATE_SILU = 0, MLIP_GATE_GELU = 1, MLIP_GATE_SIGMOID = 2, MLIP_GATE_SILU_SIGMOID = 3 };
 typedef struct {

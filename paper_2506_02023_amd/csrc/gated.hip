@@ -2,12 +2,11 @@
 //
 // With g = x Wg + bg, v = x Wv + bv and the incoming gradient H of h:
 //   G = H phi_g(g, v), V = H phi_v(g, v);  dx = G Wg^T + V Wv^T;  dWg = x^T G, dWv = x^T V;  dbg, dbv = column sums of G, V.
-// The gradient computes g and v again: 4 n d f of its 12 n d f operations, in place of 2 n f values that a forward pass would have to keep and
-// both to move, which costs more where d is small, as it is here.
+// The gradient computes g and v again: 4 n d f of its 12 n d f operations, in place of 2 n f values that a forward pass would have to keep until then.
 //
 // Both matrices are laid out as one of 2 f columns, 32 of Wg and 32 of Wv in turn, so that a lane has g and v of the same feature in two
-// registers; G and V lie the same way.  Rows go through in chunks whose G and V stay in the caches between the kernel that makes them and
-// the two products that read them.
+// registers; G and V lie the same way.  Rows go through in chunks that take up to 4 GB of scratch memory; the kernel that makes G and V writes them there, and the two products each
+// read them again.  Where d is small that is what takes the time: 1,000,188 x 64 x 128 bf16 528 us, of which the call's own bytes would take 100.
 #include "products.h"
 
 namespace mlip {
@@ -21,8 +20,9 @@ template <class T_, int PARTS_, class E_> struct Kind {
 };
 using Half = Kind<_Float16, 1, _Float16>;
 // Gradients of fp16 arrays: G and V, which are not bounded by what the arrays hold, may be larger or smaller than fp16 numbers.  They go in two bf16 parts (16 bits, the range of fp32),
-// and with them x and the weights, exactly: three products for one.  (32,768 x 1024 x 4096: 3.99 ms, 1.85 in one fp16 part; 1,000,188 x 64 x 128: 935 us and 516.)  Those of bf16 arrays have the range, and
-// are rounded to bf16 as any network's are that computes its gradients in that type.
+// and with them x and the weights, exactly: three products for one.  (32,768 x 1024 x 4096: 3.95 ms, 1.85 in one fp16 part; 1,000,188 x 64 x 128: 935 us and 516.)  G and V of bf16 arrays have the range in one
+// part and are rounded to it, as a network's are that keeps its gradients in that type: results are off by 2.35e-3 of the norm, by 1.66e-3 (their own rounding) in two parts, which
+// would take 3.77 ms for 1.76 and 935 us for 520.
 using HalfBack = Kind<__bf16, 2, _Float16>;
 template <bool BACK, class Fn> int with_kind(int32_t dtype, Fn &&f)
 {
@@ -36,8 +36,8 @@ int parts_of(int32_t dtype, bool grad) { return dtype == MLIP_DTYPE_F32 ? 3 : dt
 // down to 2^-3; what is below is off by up to 2^-25.  That is nothing beside a sum of large terms, but it is all there is of a sum whose row is large where the column is small
 // and the other way round.  So values of 2^7 and more are counted: of a column all but t (an eighth) shall be that large, of a row t and an eighth of those that are not zero.
 // Then an eighth of the row's terms at least are 2^14 and more, and what is lost, twice 2^-25 2^14 a term at most, is below 2^-21 of the terms' sizes.  The results of a row or
-// column that falls short are computed again by the fp32 matrix instruction.  (32,768 x 512 x 1365: 381 us, with three bf16 parts 712; 300,000 x 128 x 256: 214 and 361; the
-// gradient's g and v of 202,612 x 128 x 341: 421 and 588.)
+// column that falls short are computed again by the fp32 matrix instruction.  (32,768 x 512 x 1365: 343 us, with three bf16 parts 635; 300,000 x 128 x 256: 236 and
+// 361; the gradient's g and v of 202,612 x 128 x 341: 458 and 588.)
 using Scaled = Kind<_Float16, 2, float>;
 // In what g and v are computed, by tiles and by k_gates_narrow
 template <class K> using InTiles = std::conditional_t<std::is_same_v<K, HalfBack>, Half, K>;
@@ -495,7 +495,7 @@ template <class K> struct NarrowArgs {
 };
 
 // What a wavefront has to compute again of its rows and group of columns, stored over what it has stored before.  (Not in the kernel's loop, which has no registers to spare for
-// it.  What has an infinity in its row or column has become NaN and stays so: `lost` features.)  1,000,188 x 64 -> 128 with four of five features zero: 1.05 ms, 0.23 with none.
+// it.  What has an infinity in its row or column has become NaN and stays so: `lost` features.)  1,000,188 x 64 -> 128 with four of five features zero: 1.05 ms, 0.24 with none.
 template <class K, int STEPS, bool BACK>
 __device__ inline void gates_again(const NarrowArgs<K> &na, const uint32_t *short_of, const uint32_t *lost, const float (*bias)[NarrowShape<K, STEPS>::kPairs * 32], int pairs, int64_t col_first,
                                    int64_t first_tile, int64_t stride)

@@ -8,7 +8,8 @@
 //   dw_post = sum P zhat, db_post = sum P, dw_pre = sum dn yhat, db_pre = sum dn   (over rows)
 //
 // Bound by memory: every row is read once and stays in registers, four columns of it in a lane (rows of up to 256 columns in part of a
-// wavefront, wider ones in a block of their own), and all is fp32.  The gradient starts from x and z again, so the forward pass keeps nothing.  Up to 4096 columns the
+// wavefront, wider ones in a block of their own), and all is fp32.  Wider rows have 128 registers a lane, because a block may have 1024 threads: the fp32 gradient spills 14 of them up
+// to 4096 columns, all types 26 to 123 beyond (eight columns a lane; 16,384 x 8192 bf16: 697 us, its gradient 1.83 ms, floors 263 and 421).  The gradient starts from x and z again, so the forward pass keeps nothing.  Up to 4096 columns the
 // next row is requested before the present one is worked on.
 // 1,000,188 x 64 bf16 with both norms: 125 us (4.1 TB/s; 8 columns a lane 157), its gradient with 128 columns 433 us (4.7 TB/s; 8 columns a lane, each row loaded when its turn comes, 728).
 // Sums over rows: each lane over the rows it meets, the lanes of a block joined in registers and LDS, the blocks in a second launch, all in a fixed order.
