@@ -155,6 +155,22 @@ __global__ __launch_bounds__(kThreads) void k_start(List l, const double *part, 
 
 struct NoEach { template <class F> __device__ inline void operator()(F &) const {} };
 
+// A tile's product over k in [0, k1), in runs that are summed by themselves first: what one fp32 sum loses grows with its terms, and where they are alike (a matrix of ones) it
+// loses the same way every time (1 x 2^20: 4.4e-3 of the result in one run, 2e-5 so)
+constexpr int64_t kRun = 4096;
+template <class M> __device__ inline void product(const Panel &a, const Panel &b, int64_t m0, int64_t n0, int64_t k1, typename M::Lds &lds, f32x16 (&sum)[2][2])
+{
+    for (int64_t k = 0; k < k1; k += kRun) {
+        f32x16 acc[2][2] = {};
+        M::run(a, b, m0, n0, k, k + kRun < k1 ? k + kRun : k1, lds, acc, NoEach{});
+        __syncthreads();   // nobody reads the tiles any more
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) sum[i][j] += acc[i][j];
+    }
+}
+
 // X, or A - diag A, or B - diag B
 __device__ inline Panel x_panel(const Item &it, const P *ws, int which) { return {ws + it.x[which], it.n_ld, it.low[which] - it.x[which], it.m, it.n_p}; }
 __device__ inline Panel square_panel(const Item &it, const P *ws, int64_t at) { return {ws + at, it.m_ld, (int64_t)it.m * it.m_ld, it.m, it.m_p}; }
@@ -193,8 +209,7 @@ template <bool SQUARE> __global__ __launch_bounds__(kThreads) void k_symmetric(L
     triangle((int)at, (it.m + 127) / 128, ti, tj);
     const Panel from = SQUARE ? square_panel(it, ws, it.gram) : x_panel(it, ws, which);
     f32x16 acc[2][2] = {};
-    M::run(from, from, tj * 128, ti * 128, 0, SQUARE ? it.m_p : it.n_p, lds, acc, NoEach{});
-    __syncthreads();
+    product<M>(from, from, tj * 128, ti * 128, SQUARE ? it.m_p : it.n_p, lds, acc);
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, m = it.m, m_p = it.m_p, ld = it.m_ld, row0 = ti * 128 + wave % 2 * 64, col0 = tj * 128 + wave / 2 * 64;
     const Turned turned{reinterpret_cast<float *>(&lds) + wave * 4096};
     turned.put(acc);
@@ -267,8 +282,7 @@ template <bool LAST> __global__ __launch_bounds__(Middle::kThreads) void k_apply
     const Item &it = l.item[item_of(l, (uint32_t)xcd_order(blockIdx.x, gridDim.x), at)];
     const int tiles = (it.m + B::kRows - 1) / B::kRows, m0 = at % tiles * B::kRows, n0 = at / tiles * B::kCols;   // (tiles of the same columns one after another)
     f32x16 acc[2][2] = {};
-    M::run(x_panel(it, ws, which), square_panel(it, ws, it.poly), n0, m0, 0, it.m_p, lds, acc, NoEach{});
-    __syncthreads();
+    product<M>(x_panel(it, ws, which), square_panel(it, ws, it.poly), n0, m0, it.m_p, lds, acc);
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, c = lane % 8 * 8;
     const Turned turned{reinterpret_cast<float *>(&lds) + wave * 4096};
     const P *old = ws + it.x[which], *old_low = ws + it.low[which];
