@@ -481,8 +481,8 @@ int mlip_clip_grads(const mlip_tensor_t *tensors, int32_t count, float max_norm,
  *   b_gate, b_value   DEVICE [f], one element after another, or NULL
  *   out      DEVICE [n][f], element (i, k) at i * out_row_stride + k
  * 0 <= n < 2^31, 1 <= d, f <= 65536.  mlip_gated_workspace returns 0 for calls that are refused.  It asks for the weights once more (fp32: in parts) and, where they are laid out
- * first, for x, gradients also for 4 f values a row and for the weights' gradients in fp32 as many times as rows are split for them; of many rows, those of one chunk, 4 GB
- * (32,768 x 1024 -> 4096 bf16: 89 MB, its gradient 714; 1,000,188 x 64 -> 128 fp32: 0.1 MB and 2.3 GB).
+ * first, for x, gradients also for 4 f values of 16 bits a row (fp32: 6 f) and for the weights' gradients in fp32 as many times as rows are split for them; of many rows, those of one chunk, 4 GB
+ * (32,768 x 1024 -> 4096 bf16: 89 MB, its gradient 1255 MB; 1,000,188 x 64 -> 128 fp32: 0.1 MB and 2.3 GB).
  */
 enum { MLIP_GATE_SILU = 0, MLIP_GATE_GELU = 1, MLIP_GATE_SIGMOID = 2, MLIP_GATE_SILU_SIGMOID = 3 };
 typedef struct {
@@ -501,7 +501,7 @@ int mlip_gated(const mlip_gated_t *call, void *out, int64_t out_row_stride, void
 
 /*
  * Its gradient, from the gradient of out.  The products are computed again: nothing is kept from the forward call.  The gradients of g and v are rounded
- * before the products with x and the weights take them up: of bf16 arrays to bf16, of fp16 arrays to 16 bits with the range of fp32, of fp32 arrays not at all.
+ * before the products with x and the weights take them up, of 16-bit arrays to 16 bits with the range of fp32, of fp32 arrays not at all.
  *   grad     DEVICE [n][f], any strides
  *   x        DEVICE [n][d], element (i, k) at i * x_row_stride + k;  w_gate, w_value DEVICE [d][f], any strides that keep elements apart
  *   b_gate, b_value   DEVICE [f]

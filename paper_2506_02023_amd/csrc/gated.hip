@@ -6,31 +6,32 @@
 //
 // Both matrices are laid out as one of 2 f columns, 32 of Wg and 32 of Wv in turn, so that a lane has g and v of the same feature in two
 // registers; G and V lie the same way.  Rows go through in chunks that take up to 4 GB of scratch memory; the kernel that makes G and V writes them there, and the two products each
-// read them again.  Where d is small that is what takes the time: 1,000,188 x 64 x 128 bf16 528 us, of which the call's own bytes would take 100.
+// read them again.  Where d is small that is what takes the time: 1,000,188 x 64 x 128 bf16 809 us, of which the call's own bytes would take 100.
 #include "products.h"
 
 namespace mlip {
 namespace {
 
-// The types of a call: E of its arrays, T of the parts
-template <class T_, int PARTS_, class E_> struct Kind {
+// The types of a call: E of its arrays, T of the parts; parts of g's and v's factors, or of G and V, and of what those are multiplied with
+template <class T_, int PARTS_, class E_, int FACTORS_ = PARTS_> struct Kind {
     using T = T_;
     using E = E_;
-    static constexpr int kParts = PARTS_, kWide = 16 / sizeof(E_);   // elements of a lane's load or store
+    static constexpr int kParts = PARTS_, kFactors = FACTORS_, kWide = 16 / sizeof(E_);   // kWide: elements of a lane's load or store
 };
+using Brain = Kind<__bf16, 1, __bf16>;
 using Half = Kind<_Float16, 1, _Float16>;
-// Gradients of fp16 arrays: G and V, which are not bounded by what the arrays hold, may be larger or smaller than fp16 numbers.  They go in two bf16 parts (16 bits, the range of fp32),
-// and with them x and the weights, exactly: three products for one.  (32,768 x 1024 x 4096: 3.95 ms, 1.85 in one fp16 part; 1,000,188 x 64 x 128: 935 us and 516.)  G and V of bf16 arrays have the range in one
-// part and are rounded to it, as a network's are that keeps its gradients in that type: results are off by 2.35e-3 of the norm, by 1.66e-3 (their own rounding) in two parts, which
-// would take 3.77 ms for 1.76 and 935 us for 520.
+// Gradients of 16-bit arrays: G and V go in two bf16 parts (16 bits, the range of fp32).  Rounded to the arrays' type they would lose what sums over many terms of both signs leave (bf16:
+// up to a tenth of such a result in 30,000 drawn calls; 2.35e-3 of the norm usually, of which a result's own rounding is 1.66e-3), and of fp16 what lies outside of its range, as they may on
+// both sides.  x and the weights beside them are bf16, or exactly two bf16 parts: two products, or three, for one.  (32,768 x 1024 x 4096 bf16: 2.74 ms, 1.77 rounded to
+// bf16; fp16 3.54, 1.85 rounded to fp16; 1,000,188 x 64 x 128: 809 and 520 us, fp16 930 and 516.)
+using BrainBack = Kind<__bf16, 2, __bf16, 1>;
 using HalfBack = Kind<__bf16, 2, _Float16>;
 template <bool BACK, class Fn> int with_kind(int32_t dtype, Fn &&f)
 {
     if (dtype == MLIP_DTYPE_F32) return f(Kind<__bf16, 3, float>{});
-    if (dtype == MLIP_DTYPE_BF16) return f(Kind<__bf16, 1, __bf16>{});
+    if (dtype == MLIP_DTYPE_BF16) return f(std::conditional_t<BACK, BrainBack, Brain>{});
     return f(std::conditional_t<BACK, HalfBack, Half>{});
 }
-int parts_of(int32_t dtype, bool grad) { return dtype == MLIP_DTYPE_F32 ? 3 : dtype == MLIP_DTYPE_F16 && grad ? 2 : 1; }
 // g and v of fp32 arrays: two fp16 parts (22 bits) and three products, half the matrix time, where that is what bounds (wide rows of the forward call) or registers are
 // short (rows of up to 128 features).  Every row of x and column of the weights is brought by a power of two to a largest value in [2^13, 2^14).  A value then has its 22 bits
 // down to 2^-3; what is below is off by up to 2^-25.  That is nothing beside a sum of large terms, but it is all there is of a sum whose row is large where the column is small
@@ -40,7 +41,7 @@ int parts_of(int32_t dtype, bool grad) { return dtype == MLIP_DTYPE_F32 ? 3 : dt
 // 361; the gradient's g and v of 202,612 x 128 x 341: 458 and 588.)
 using Scaled = Kind<_Float16, 2, float>;
 // In what g and v are computed, by tiles and by k_gates_narrow
-template <class K> using InTiles = std::conditional_t<std::is_same_v<K, HalfBack>, Half, K>;
+template <class K> using InTiles = std::conditional_t<std::is_same_v<K, HalfBack>, Half, std::conditional_t<std::is_same_v<K, BrainBack>, Brain, K>>;
 template <class K> using Inner = std::conditional_t<K::kParts == 3, Scaled, InTiles<K>>;
 
 // Column c of the 2 f: the feature, and whether of v
@@ -96,12 +97,12 @@ template <class K> __global__ __launch_bounds__(kPackThreads) void k_pack_weight
     __syncthreads();
     for (int i = b; i < 32; i += 8) {
         typename InTiles<K>::T u[InTiles<K>::kParts];
-        typename K::T v[K::kParts];
+        typename K::T v[K::kFactors];
         split(w.scale ? tile[a][i] * w.scale[c0 + i] : tile[a][i], u);
         for (int p = 0; p < InTiles<K>::kParts; ++p) w.across[p * w.across_part + (c0 + i) * w.d_ld + d0 + a] = u[p];
         if (w.down && d0 + i < w.d) {
             split(tile[i][a], v);
-            for (int p = 0; p < K::kParts; ++p) w.down[p * w.down_part + (d0 + i) * w.f2_ld + c0 + a] = v[p];
+            for (int p = 0; p < K::kFactors; ++p) w.down[p * w.down_part + (d0 + i) * w.f2_ld + c0 + a] = v[p];
         }
     }
 }
@@ -388,11 +389,11 @@ template <class K> struct GateArgs {
 };
 
 // The weights are the products' first operand and the rows their second; a lane ends with neighbouring features of a row.  Bound by the matrix units, the activations behind
-// them: 32,768 x 1024 x 4096 bf16, backward, 706 us (0.78 PF; 1250 in tiles of 128 with four features a store).
+// them: 32,768 x 1024 x 4096 bf16, backward, 799 us (0.69 PF; with one part of G and V 706, and 1250 in tiles of 128 with four features a store).
 template <class K, class B, bool BACK> __global__ __launch_bounds__(B::kThreads) void k_gates(GateArgs<K> a)
 {
     using T = typename K::T;
-    using P = typename B::template Of<typename InTiles<K>::T, InTiles<K>::kParts, true, true>;
+    using P = typename B::template Of<typename InTiles<K>::T, InTiles<K>::kParts, InTiles<K>::kParts, true, true>;
     __shared__ typename P::Lds lds;
     const int64_t tile = xcd_order(blockIdx.x, gridDim.x), m0 = tile / a.n_tiles * B::kRows, n0 = tile % a.n_tiles * B::kCols;
     f32x16 acc[B::kPer / 32][2] = {};
@@ -688,7 +689,7 @@ template <class K, int STEPS, bool BACK, bool STRIDED> __global__ __launch_bound
                     wg[p] = *reinterpret_cast<const Half8<C> *>(weights + (((pair * 2 * STEPS + kk) * PARTS + p) * 64 + lane) * 8);
                     wv[p] = *reinterpret_cast<const Half8<C> *>(weights + ((((pair * 2 + 1) * STEPS + kk) * PARTS + p) * 64 + lane) * 8);
                 }
-                for_products<PARTS>([&](int p, int q) {
+                for_products<PARTS, PARTS>([&](int p, int q) {
                     g = mfma<C>(wg[p], fx[kk][q], g);
                     v = mfma<C>(wv[p], fx[kk][q], v);
                 });
@@ -781,14 +782,14 @@ template <class K, int STEPS, bool BACK, bool STRIDED> __global__ __launch_bound
     }
 }
 
-// dx = [G V] [Wg Wv]^T.  32,768 x 8192 by 1024 bf16: 490 us (1.12 PF; in tiles of 128 690); 202,612 x 704 by 128 of three parts: 320 us (0.68 PF)
+// dx = [G V] [Wg Wv]^T.  32,768 x 8192 in two parts by 1024 in one: 931 us (1.18 PF); 202,612 x 704 by 128 of three parts: 320 us (0.68 PF)
 template <class K> struct RowBarArgs {
     Panel gv, w;             // [rows][2 f], [d][2 f]
     int64_t n_tiles;
     typename K::E *out;
     int64_t out_rs;
 };
-template <class K, class B> using RowBars = typename B::template Of<typename K::T, K::kParts, true, true>;   // (d first, rows second)
+template <class K, class B> using RowBars = typename B::template Of<typename K::T, K::kFactors, K::kParts, true, true>;   // (d first, rows second)
 template <class K, class B> __device__ inline void row_bars(const RowBarArgs<K> &a, int64_t tile, typename RowBars<K, B>::Lds &lds)
 {
     using P = RowBars<K, B>;
@@ -815,14 +816,14 @@ template <class K, class B> __device__ inline void row_bars(const RowBarArgs<K> 
 }
 
 // The chunk's share of [dWg dWv]^T = [G V]^T x, [2 f][d], its rows in `splits` runs; and of the biases' gradients, the column sums of G and V.
-// 32,768 x 8192 by 1024 bf16: 655 us (0.84 PF; in tiles of 128 773); 202,612 x 704 by 128 of three parts: 316 us
+// 32,768 x 8192 in two parts by 1024 in one: 1115 us (0.99 PF); 202,612 x 704 by 128 of three parts: 316 us
 template <class K> struct WeightSumArgs {
     Panel gv, x;             // [rows][2 f], [rows][d]
     int64_t d, m_tiles, n_tiles, run;   // rows of a run, a multiple of a step
     float *part, *bias;      // [splits][2 f][d], [splits][2 f]
     bool add;
 };
-template <class K, class B> using WeightSums = typename B::template Of<typename K::T, K::kParts, false, false>;   // (d first, the 2 f columns second)
+template <class K, class B> using WeightSums = typename B::template Of<typename K::T, K::kFactors, K::kParts, false, false>;   // (d first, the 2 f columns second)
 template <class K, class B> __device__ inline void weight_sums(const WeightSumArgs<K> &a, int64_t at, typename WeightSums<K, B>::Lds &lds)
 {
     using P = WeightSums<K, B>;
@@ -976,15 +977,16 @@ template <class K, class Fn> void with_tile(int64_t cols, int64_t rows, bool spl
 Plan plan_of(const GatedArgs &a, bool grad)
 {
     Plan p{};
-    const bool half_back = a.dtype == MLIP_DTYPE_F16 && grad;
-    p.parts = by_scale(a, grad) ? Scaled::kParts : parts_of(a.dtype, grad);
+    const bool f32 = a.dtype == MLIP_DTYPE_F32, apart = a.dtype == MLIP_DTYPE_F16 && grad;
+    const int factors = by_scale(a, grad) ? Scaled::kParts : f32 ? 3 : apart ? 2 : 1, tiles_parts = apart ? 1 : factors;   // parts of x and weights, and of those that make g and v
+    p.parts = f32 || !grad ? factors : 2;
     p.pack_x = !reads_x(a);
     p.d_p = pad_to(a.d, kPadK);
     p.f2 = 2 * pad_to(a.f, 32);
     p.gv_ld = pad_odd(p.f2);
     p.d_ld = pad_odd(p.d_p);
     // (scratch memory does not depend on where x lies: a size asked for once holds for all)
-    const int64_t row_bytes = ((grad ? p.gv_ld : 0) + p.d_ld) * p.parts * 2;
+    const int64_t row_bytes = ((grad ? p.gv_ld : 0) * p.parts + p.d_ld * factors) * 2;
     p.chunk = pad_to(kChunkBytes / row_bytes + 1, 1024);
     const int64_t most = kMostTiles / ((p.f2 > p.d_p ? p.f2 : p.d_p) / 64 + 1) * 64 / 1024 * 1024;
     if (p.chunk > most) p.chunk = most;
@@ -992,13 +994,13 @@ Plan plan_of(const GatedArgs &a, bool grad)
     if (p.chunk > all) p.chunk = all;
     size_t at = 0;
     auto take = [&](int64_t bytes) { const size_t here = at; at += (size_t)pad_to(bytes, 256); return here; };
-    p.across = take(p.f2 * p.d_ld * (half_back ? 1 : p.parts) * 2);
-    if (half_back && a.d > kNarrow) p.x_tiles = take(p.chunk * p.d_ld * 2);
-    if (grad || a.d > kNarrow) p.xs = take(p.chunk * p.d_ld * p.parts * 2);
+    p.across = take(p.f2 * p.d_ld * tiles_parts * 2);
+    if (apart && a.d > kNarrow) p.x_tiles = take(p.chunk * p.d_ld * 2);
+    if (grad || a.d > kNarrow) p.xs = take(p.chunk * p.d_ld * factors * 2);
     if (by_scale(a, grad)) p.x_exponent = take(2 * p.chunk * 4);
     if (a.dtype == MLIP_DTYPE_F32) p.w_scale = take(3 * p.f2 * 4);
     if (grad) {
-        p.down = take(a.d * p.gv_ld * p.parts * 2);
+        p.down = take(a.d * p.gv_ld * factors * 2);
         p.gv = take(p.chunk * p.gv_ld * p.parts * 2);
         const int64_t tiles = p.parts <= 2 && a.d >= 512 && p.f2 >= 512 ? (p.f2 + 255) / 256 * ((a.d + 255) / 256) : a.d <= 64 ? (p.f2 + 255) / 256 : (p.f2 + 127) / 128 * ((a.d + 127) / 128);
         const int64_t blocks = p.parts <= 2 && a.d >= 512 && p.f2 >= 512 ? 256 : 512;   // one or two to a compute unit
@@ -1027,7 +1029,7 @@ template <class K, bool BACK> int launch(const GatedArgs &a, const GatedGrad *g)
     const Plan p = plan_of(a, BACK);
     char *ws = static_cast<char *>(a.workspace);
     using Tiles = InTiles<K>;
-    constexpr bool apart = !std::is_same_v<K, Tiles>;   // whether the products with G and V have x in other parts than those that make g and v
+    constexpr bool apart = !std::is_same_v<T, typename Tiles::T>;   // whether the products with G and V have x in other parts than those that make g and v
     typename Tiles::T *across = reinterpret_cast<typename Tiles::T *>(ws + p.across), *x_tiles = reinterpret_cast<typename Tiles::T *>(ws + (apart ? p.x_tiles : p.xs));
     T *down = reinterpret_cast<T *>(ws + p.down), *xs = reinterpret_cast<T *>(ws + p.xs), *gv = reinterpret_cast<T *>(ws + p.gv);
     const bool in_registers = a.d <= kNarrow, strided = a.x_cs != 1 || (BACK && g->bar_cs != 1);

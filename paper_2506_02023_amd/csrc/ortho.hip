@@ -201,7 +201,7 @@ __device__ inline void triangle(int t, int tiles, int &i, int &j)
 // Twelve matrices of 1024 x 4096: A 201 us (0.86 PF), B 63.
 template <bool SQUARE> __global__ __launch_bounds__(kThreads) void k_symmetric(List l, P *ws, int which, float b, float c)
 {
-    using M = Product<P, 2, true, true, 128, 128, 64, 64>;
+    using M = Product<P, 2, 2, true, true, 128, 128, 64, 64>;
     __shared__ typename M::Lds lds;
     uint32_t at;
     const Item &it = l.item[item_of(l, (uint32_t)xcd_order(blockIdx.x, gridDim.x), at)];
@@ -276,7 +276,7 @@ template <bool SQUARE> __global__ __launch_bounds__(kThreads) void k_symmetric(L
 template <bool LAST> __global__ __launch_bounds__(Middle::kThreads) void k_apply(List l, P *ws, int which, float a, float scale)
 {
     using B = Middle;
-    using M = typename B::template Of<P, 2, false, true>;
+    using M = typename B::template Of<P, 2, 2, false, true>;
     __shared__ typename M::Lds lds;
     uint32_t at;
     const Item &it = l.item[item_of(l, (uint32_t)xcd_order(blockIdx.x, gridDim.x), at)];

@@ -50,9 +50,10 @@ template <class T, int PARTS> __device__ inline void split(float v, T (&part)[PA
 }
 #endif
 
-// Elements of K that one step takes: 64 of one part, 32 of several (LDS), 16 of several where both panels have K in their rows, so that two blocks share a compute
-// unit (202,612 rows of 128 x 704 of three parts: 507 us in steps of 32, 312 here; panels with K in their columns would be read in quarters of lines)
-template <int PARTS, bool KC, int LEAST> constexpr int kStepK = PARTS == 1 ? 64 : KC || LEAST < 128 ? 32 : 16;
+// Elements of K that one step takes: 64 of one part, 32 of several (LDS), 16 of several where both panels have K in their rows and the tiles are of 128, so that two blocks share a
+// compute unit (202,612 rows of 128 x 704 of three parts: 507 us in steps of 32, 312 here; panels with K in their columns would be read in quarters of lines; tiles of 256 have one
+// to themselves either way: 32,768 x 1024 x 4096 bf16 2.97 ms in steps of 16, 2.74 in 32)
+template <int PARTS, bool KC, int LEAST> constexpr int kStepK = PARTS == 1 ? 64 : KC || LEAST != 128 ? 32 : 16;
 // Columns that a panel with K in its columns is filled up to: a multiple of both
 constexpr int64_t kPadK = 64;
 inline int64_t pad_to(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
@@ -108,20 +109,21 @@ template <class T, int PARTS, bool KC, int ROWS, int KT, int THREADS> struct Til
     }
 };
 
-// The pairs of parts whose products are taken, large ones last (they are added to what is there)
-template <int PARTS, class Fn> __device__ inline void for_products(Fn &&f)
+// The pairs of parts of A and B whose products are taken, large ones last (they are added to what is there)
+template <int PA, int PB, class Fn> __device__ inline void for_products(Fn &&f)
 {
-    if constexpr (PARTS == 3) { f(2, 0); f(0, 2); f(1, 1); }
-    if constexpr (PARTS >= 2) { f(1, 0); f(0, 1); }
+    if constexpr (PA == 3 && PB == 3) { f(2, 0); f(0, 2); f(1, 1); }
+    if constexpr (PA >= 2) f(1, 0);
+    if constexpr (PB >= 2) f(0, 1);
     f(0, 0);
 }
 
 // acc[i][j] += rows 32 i .. of A times rows 32 j .. of B, of a wavefront's WM x WN part of the block's BM x BN tile, summed over k in [k0, k1).
 // each(fragments of B): called in every step, for sums along K.
-template <class T, int PARTS, bool AKC, bool BKC, int BM, int BN, int WM, int WN> struct Product {
-    static constexpr int kWaves = (BM / WM) * (BN / WN), kThreads = kWaves * 64, KT = kStepK<PARTS, AKC || BKC, (BM < BN ? BM : BN)>;
-    using TA = Tile<T, PARTS, AKC, BM, KT, kThreads>;
-    using TB = Tile<T, PARTS, BKC, BN, KT, kThreads>;
+template <class T, int PA, int PB, bool AKC, bool BKC, int BM, int BN, int WM, int WN> struct Product {
+    static constexpr int kWaves = (BM / WM) * (BN / WN), kThreads = kWaves * 64, KT = kStepK<(PA > PB ? PA : PB), AKC || BKC, (BM < BN ? BM : BN)>;
+    using TA = Tile<T, PA, AKC, BM, KT, kThreads>;
+    using TB = Tile<T, PB, BKC, BN, KT, kThreads>;
     static constexpr int kStage = TA::kElems + TB::kElems;
     static constexpr int kTurned = kWaves * 64 * 64 * 2;   // what Turned takes of it afterwards
     struct alignas(16) Lds { T e[2 * kStage > kTurned ? 2 * kStage : kTurned]; };
@@ -145,15 +147,16 @@ template <class T, int PARTS, bool AKC, bool BKC, int BM, int BN, int WM, int WN
             }
 #pragma unroll
             for (int kk = 0; kk < KT / 16; ++kk) {
-                Half8<T> fa[WM / 32][PARTS], fb[WN / 32][PARTS];
+                Half8<T> fa[WM / 32][PA], fb[WN / 32][PB];
 #pragma unroll
-                for (int p = 0; p < PARTS; ++p) {
+                for (int p = 0; p < PA; ++p)
 #pragma unroll
                     for (int i = 0; i < WM / 32; ++i) fa[i][p] = TA::frag(la, p, wm + 32 * i, kk);
 #pragma unroll
+                for (int p = 0; p < PB; ++p)
+#pragma unroll
                     for (int j = 0; j < WN / 32; ++j) fb[j][p] = TB::frag(lb, p, wn + 32 * j, kk);
-                }
-                for_products<PARTS>([&](int p, int q) {
+                for_products<PA, PB>([&](int p, int q) {
 #pragma unroll
                     for (int i = 0; i < WM / 32; ++i)
 #pragma unroll
@@ -169,7 +172,7 @@ template <class T, int PARTS, bool AKC, bool BKC, int BM, int BN, int WM, int WN
 // products, the smaller one shares a compute unit with another block and leaves no one idle where there are few.
 template <int COLS, int ROWS> struct Block {   // of the first operand and of the second
     static constexpr int kCols = COLS, kRows = ROWS, kPer = COLS == 256 ? 128 : 64, kThreads = COLS / kPer * (ROWS / 64) * 64;   // kPer x 64: a wavefront's share
-    template <class T, int PARTS, bool AKC, bool BKC> using Of = Product<T, PARTS, AKC, BKC, COLS, ROWS, kPer, 64>;
+    template <class T, int PA, int PB, bool AKC, bool BKC> using Of = Product<T, PA, PB, AKC, BKC, COLS, ROWS, kPer, 64>;
     static __device__ inline int first(int wave) { return wave / (ROWS / 64) * kPer; }
     static __device__ inline int second(int wave) { return wave % (ROWS / 64) * 64; }
 };
