@@ -175,3 +175,41 @@ def test_captured():
             for a, b in zip(held, (M.mlip_gated(now, wg, wv, bg, bv), *M.mlip_gated_grad(bar, now, wg, wv, bg, bv))):
                 assert torch.equal(a, b)
             torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("n,d,f", [(300, 64, 72), (300, 128, 40)])
+def test_gradients_of_strided_rows(n, d, f):
+    """Great spread, every second column of x, a gradient that is one for all: the same bits as of copies"""
+    import torch
+    import paper_2506_02023_amd as M
+    bar, (x, wg, wv, bg, bv) = _make(n, d, f, torch.float32)
+    by = torch.exp2(torch.arange(d, device="cuda") % 2 * 40.0)
+    wide = torch.full((n, 2 * d), float("nan"), device="cuda")
+    wide[:, 1::2] = x * by
+    one = bar[:, :1].expand(n, f)
+    for a, b in zip(M.mlip_gated_grad(one, wide[:, 1::2], wg, wv / by[:, None], bg, bv), M.mlip_gated_grad(one.contiguous(), x * by, wg, wv / by[:, None], bg, bv)):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("n,d,f,dtype", [(6_000_000, 130, 32, "float32"), (12_000_000, 192, 24, "bfloat16")])
+def test_rows_of_several_chunks(n, d, f, dtype):
+    """More rows than 4 GB of scratch memory take: those around the ends of chunks and others as in a call of their own, some of great spread among them"""
+    import torch
+    import paper_2506_02023_amd as M
+    from paper_2506_02023_amd import binding as B
+    dt = getattr(torch, dtype)
+    g = torch.Generator(device="cuda").manual_seed(n)
+    x = torch.randn(n, d, generator=g, device="cuda", dtype=torch.float32).to(dt)
+    wg, wv = ((torch.randn(d, f, generator=g, device="cuda") / d ** 0.5).to(dt) for _ in range(2))
+    x[::1009, ::2] *= 2.0 ** -40
+    call, _ = B._gated_call(x, wg, wv, None, None, "silu")
+    need = B.lib().mlip_gated_workspace(call, 0)
+    assert 4e9 < need < 4.5e9 and n * d * f > 5e8       # (a chunk's rows take all but some kilobytes of it)
+    row = (d + 63) // 64 * 64
+    row = (row | 64) * (4 if dtype == "float32" else 2)
+    end = (4 << 30) // row // 1024 * 1024
+    at = torch.cat([torch.arange(0, 3000), torch.arange(end - 4000, end + 5000), torch.arange(n - 3000, n), torch.arange(0, n, 1009)[:3000]]).cuda()
+    out = M.mlip_gated(x, wg, wv)[at]
+    assert len(at) * d * f < 5e8
+    again = -(-int(5e8) // (len(at) * d * f)) + 1       # (as often as makes a call of the same way)
+    assert torch.equal(M.mlip_gated(x[at].repeat(again, 1), wg, wv)[:len(at)], out)
