@@ -1,7 +1,7 @@
 // Matrix products of 16-bit parts on the matrix units, for the operators that train node networks: a block's tile of
 // C = A B^T with A and B as panels of parts, handed to an epilogue in registers.
 //
-// An operand of a type of 16 bits is one part, itself.  fp32 operands are three bf16 parts (hi + mid + lo, exact), of whose products the six down to 2^-24 are
+// An operand of a type of 16 bits is one part, itself (or, fp16 beside bf16, two bf16 parts, exact).  fp32 operands are three bf16 parts (hi + mid + lo, exact), of whose products the six down to 2^-24 are
 // taken: 2.7 times the rate of the fp32 matrix instructions at their precision.  Values near 1 can be two fp16 parts (22 bits), three products.
 // Sums are fp32.
 #pragma once
@@ -139,6 +139,7 @@ template <class T, int PA, int PB, bool AKC, bool BKC, int BM, int BN, int WM, i
             TB::load(b, n0, k0, lds.e + TA::kElems);
         }
         for (int64_t k = k0; k < k1; k += KT, at ^= 1) {
+            __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0): loads to LDS are loads, for which a barrier by itself does not wait
             __syncthreads();   // this step's tiles are there, and all are done with the other ones
             T *la = lds.e + at * kStage, *lb = la + TA::kElems;
             if (k + KT < k1) {
